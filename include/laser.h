@@ -471,6 +471,99 @@ laser_status laser_gsta_backward(const void* seg, const void* t0, const void* wq
                                  laser_dtype dt, void* dseg_out, float* dt0_out, float* dwq_out, float* dwk_out,
                                  float* dwv_out, void* work, size_t work_bytes, void* stream);
 
+/*
+ * Attention among a history's own items: the encoder in front of STA, which the paper compares against as self-attention
+ * (Sec. 4.2) and costs as C_SA (Sec. 3.6), causal and with the sequences packed. Sequence n owns rows off[n] .. off[n+1]-1
+ * of q, k and v; query head h reads key-value head h / (H / H_kv). For item i of a sequence
+ *   s_ij = q_i . k_j / gamma (j <= i),  lse_i = log sum_j exp s_ij,  o_i = sum_j exp(s_ij - lse_i) v_j.
+ *   q [T,H,D] dt, k, v [T,H_kv,D] dt; heads of a token lie side by side, tokens q_pitch, k_pitch, v_pitch elements apart
+ *   (column blocks of one projection's output need no copy); o_out [T,H,D] dt, lse_out [T,H] fp32 (NULL: not wanted, but
+ *   the backward pass takes it). off [N+1] int32 on the device, non-decreasing; sequences may be empty. T: rows of the
+ *   buffers; L_max: at least the longest sequence, sizes the launch.
+ * Limits: D a multiple of 8, at most 128; H a multiple of H_kv, at most 1024; L_max * H < 2^30; T * H < 2^31; pitches at
+ * least heads * D, at most 2^22, and whole 16-byte pieces. Sums, the softmax's statistics and its exponents are fp32; for
+ * bf16 storage probabilities are rounded to bf16 ahead of their product with V, o is rounded once.
+ * The offsets are clamped on the device so that no access leaves the T rows (a sequence's first row into [0, T], its length
+ * into [0, min(L_max, T - first)]); offsets that break the rules give unspecified values in the rows concerned, never a
+ * fault. Rows of no sequence are neither read into a result (they may hold anything, NaN included) nor written. The items of
+ * a sequence are taken to be finite: an infinite or NaN value can reach all rows of its sequence, also earlier ones.
+ * All pointers are device pointers, caller-owned; 16-byte alignment for q, k, v, o_out, 4-byte for off and lse_out.
+ * Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on an
+ * error.
+ */
+laser_status laser_history_attention_forward(const void* q, int64_t q_pitch, const void* k, int64_t k_pitch, const void* v,
+                                             int64_t v_pitch, const int32_t* off, int N, int T, int L_max, int H, int H_kv, int D,
+                                             float gamma, laser_dtype dt, void* o_out, float* lse_out, void* stream);
+
+/*
+ * Its gradients. With p_ij = exp(s_ij - lse_i), delta_i = d_o_i . o_i, ds_ij = p_ij (d_o_i . v_j - delta_i):
+ *   dq_i = sum_j ds_ij k_j / gamma,   dk_j = sum_i ds_ij q_i / gamma,   dv_j = sum_i p_ij d_o_i
+ * (keys and values: summed over the query heads that share them, in a fixed order). o, lse as the forward pass wrote them,
+ * d_o [T,H,D] dt; dq_out [T,H,D], dk_out, dv_out [T,H_kv,D] dt with pitches of their own, summed in fp32 and rounded once (for
+ * bf16 storage p and ds are rounded to bf16 ahead of their products). Rows of no sequence are not written. work:
+ * laser_history_attention_backward_work_bytes() bytes of caller-owned scratch, contents unspecified before and after; calls
+ * that overlap need one each. The rest, limits and errors as above (work_bytes too small: LASER_ERR_SHAPE).
+ */
+size_t laser_history_attention_backward_work_bytes(int N, int T, int L_max, int H, int H_kv, int D,
+                                                   laser_dtype dt);   /* host only; 0 for invalid sizes */
+laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, const void* k, int64_t k_pitch, const void* v,
+                                              int64_t v_pitch, const void* o, const float* lse, const void* d_o,
+                                              const int32_t* off, int N, int T, int L_max, int H, int H_kv, int D, float gamma,
+                                              laser_dtype dt, void* dq_out, int64_t dq_pitch, void* dk_out, int64_t dk_pitch,
+                                              void* dv_out, int64_t dv_pitch, void* work, size_t work_bytes, void* stream);
+
+/*
+ * The same attention while it is served: keys and values of a user's items stay in a paged cache, and new items (a chunk of
+ * them, or one) or candidates attend to what is there.
+ *   k_cache, v_cache [P,H_kv,page,D] dt: P pages of `page` items (a power of two, 8 to 4096). pages [U,max_pages] int32:
+ *   item j of user u stands in page pages[u, j / page] at place j % page. Entries past a user's items are never read; an
+ *   entry outside [0, P) is a page without items: nothing reads, writes or counts its places. lens [U] int32: items of each
+ *   user, clamped to [0, min(L_max, max_pages * page)]; L_max sizes the launches.
+ * Rows beside the cache (new keys and values, queries) are packed: user u's are off[u] .. off[u+1]-1 of T, at most C_max of
+ * them, with pitches and limits as in laser_history_attention_forward (C_max * H < 2^30 too); offsets are clamped as there.
+ *
+ * laser_cache_append: user u's c new rows become the last c of its lens[u] items (lens counts them already); where
+ *   there are more rows than items the first ones have no place and are left out. weight [P,page] fp32 (NULL: none): their
+ *   places are set to 0. A page must not be listed twice, by one user or two, where new rows go.
+ * laser_cache_attention_forward: o_out [T,H,D] dt, lse_out [T,H] fp32 (NULL: not wanted). causal != 0: the rows are the last
+ *   c items of the cache (laser_cache_append has run), row i sees items 0 .. lens[u] - c + i. causal = 0: the rows are
+ *   not in the cache (a request's candidates) and see all of it. A row that sees nothing gets zeros and lse = -inf.
+ *   work: laser_cache_attention_work_bytes() bytes of caller-owned scratch, contents unspecified before and after; calls that
+ *   overlap need one each.
+ * laser_cache_weights: what each item received, weight[its place] = sum of exp(s - lse) over the rows that see it and
+ *   the H heads (add != 0: added to what stands there, atomically, so a page that several users list gets each one's part).
+ *   q, lse, causal as for laser_cache_attention_forward; places behind a user's items are left alone.
+ * laser_cache_evict: each user keeps at most `budget` items: the last `recent` ones (0 <= recent <= budget) and of
+ *   the others the heaviest by weight (of equal ones the first; NaN, and places on no page, count least). They move, in
+ *   their order, with their weights, into the pages of pages_out [U,max_pages_out], of which none may be listed twice or be one that
+ *   any user reads from in this call; a user within the budget keeps everything and moves too. lens_out [U] (may be lens
+ *   itself) receives the new lengths, kept_out [U,budget] the old places of the items that stay, -1 behind the last.
+ * Results are the same from run to run (laser_cache_weights with add: unless users share a page). Rows of no user and
+ * places behind a user's items are never written.
+ * All pointers are device pointers, caller-owned; 16-byte alignment for q, k, v, the caches, o_out and work, 4-byte for the
+ * rest. Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on
+ * an error.
+ */
+laser_status laser_cache_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,
+                                const int32_t* off, const int32_t* pages, const int32_t* lens, int U, int T, int C_max, int P,
+                                int page, int max_pages, int L_max, int H_kv, int D, laser_dtype dt, float* weight,
+                                void* stream);
+size_t laser_cache_attention_work_bytes(int U, int T, int C_max, int L_max, int H, int H_kv, int D,
+                                        laser_dtype dt);   /* host only; 0 for invalid sizes */
+laser_status laser_cache_attention_forward(const void* q, int64_t q_pitch, const void* k_cache, const void* v_cache,
+                                           const int32_t* off, const int32_t* pages, const int32_t* lens, int U, int T, int C_max,
+                                           int P, int page, int max_pages, int L_max, int H, int H_kv, int D, float gamma,
+                                           int causal, laser_dtype dt, void* o_out, float* lse_out, void* work,
+                                           size_t work_bytes, void* stream);
+laser_status laser_cache_weights(const void* q, int64_t q_pitch, const float* lse, const void* k_cache, const int32_t* off,
+                                 const int32_t* pages, const int32_t* lens, int U, int T, int C_max, int P, int page,
+                                 int max_pages, int L_max, int H, int H_kv, int D, float gamma, int causal, int add,
+                                 laser_dtype dt, float* weight, void* stream);
+laser_status laser_cache_evict(void* k_cache, void* v_cache, float* weight, const int32_t* pages, const int32_t* lens,
+                               const int32_t* pages_out, int U, int P, int page, int max_pages, int max_pages_out, int L_max,
+                               int budget, int recent, int H_kv, int D, laser_dtype dt, int32_t* lens_out, int32_t* kept_out,
+                               void* stream);
+
 /* Name of the family of STA / GSTA kernels AUTO would pick from for a shape in a batch that fills the machine (smaller ones
  * may take another form; "sta_generic" and "gsta_generic" include the matrix-core kernels that AUTO runs for fp32 at the
  * usual widths, "sta_stream_bf16" the one for a few candidates per user; static strings; host only, no GPU needed). */

@@ -31,6 +31,8 @@ EXPORTS = [
     "laser_project_kv_forward", "laser_project_kv_forward_variant", "laser_fold_query_weights",
     "laser_project_heads_forward", "laser_sta_folded_forward", "laser_sta_backward", "laser_sta_backward_bf16", "laser_sta_backward_static", "laser_sta_backward_work_bytes", "laser_gsta_backward",
     "laser_gsta_backward_work_bytes",
+    "laser_history_attention_forward", "laser_history_attention_backward", "laser_history_attention_backward_work_bytes",
+    "laser_cache_append", "laser_cache_attention_forward", "laser_cache_attention_work_bytes", "laser_cache_weights", "laser_cache_evict",
     "laser_status_string", "laser_version",
 ]
 
@@ -128,6 +130,21 @@ def load_library() -> ctypes.CDLL:
     lib.laser_gsta_backward.argtypes = [vp, vp, vp, vp, vp, ip, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp,
                                         vp, ctypes.c_size_t, vp]
     lib.laser_gsta_backward.restype = i32
+    i64, sz = ctypes.c_int64, ctypes.c_size_t
+    rows3 = [vp, i64, vp, i64, vp, i64]
+    lib.laser_history_attention_forward.argtypes = rows3 + [ip] + [i32] * 6 + [f32, i32, vp, vp, vp]
+    lib.laser_history_attention_backward.argtypes = rows3 + [vp, vp, vp, ip] + [i32] * 6 + [f32, i32] + rows3 + [vp, sz, vp]
+    lib.laser_cache_append.argtypes = [vp, i64, vp, i64, vp, vp, ip, ip, ip] + [i32] * 9 + [i32, vp, vp]
+    lib.laser_cache_attention_forward.argtypes = [vp, i64, vp, vp, ip, ip, ip] + [i32] * 10 + [f32, i32, i32, vp, vp, vp, sz, vp]
+    lib.laser_cache_weights.argtypes = [vp, i64, vp, vp, ip, ip, ip] + [i32] * 10 + [f32, i32, i32, i32, vp, vp]
+    lib.laser_cache_evict.argtypes = [vp, vp, vp, ip, ip, ip] + [i32] * 11 + [ip, ip, vp]
+    for name in ("laser_history_attention_forward", "laser_history_attention_backward", "laser_cache_append",
+                 "laser_cache_attention_forward", "laser_cache_weights", "laser_cache_evict"):
+        getattr(lib, name).restype = i32
+    lib.laser_history_attention_backward_work_bytes.argtypes = [i32] * 7
+    lib.laser_cache_attention_work_bytes.argtypes = [i32] * 8
+    for name in ("laser_history_attention_backward_work_bytes", "laser_cache_attention_work_bytes"):
+        getattr(lib, name).restype = sz
     lib.laser_sta_kernel_name.argtypes = [i32, i32, i32, i32, i32]
     lib.laser_sta_kernel_name.restype = ctypes.c_char_p
     lib.laser_gsta_kernel_name.argtypes = [i32, i32, i32, i32]
@@ -775,3 +792,249 @@ def laser_forward(q, k, v, t0, wq, wk, wv, lens, w: int, gamma: float, seg_out=N
         _ptr(seg_cnt, "seg_cnt", torch.int32), _ptr(z_out, "z_out", torch.float32), _stream(stream))
     _check(code, "laser_forward")
     return seg_out, seg_cnt, z_out
+
+
+# ----------------------------------------------------------------------------- attention among a history's items
+def _placed(tensors: dict):
+    """The one device that all of the given tensors live on, and on which the call is to be made."""
+    device = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live in device memory")
+        if device is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+        device = t.device
+    return device
+
+
+class _On:
+    """Makes a device and, where one is given, a stream current for a call: kernels run there, and what the call allocates
+    belongs there. The ordinary call (current device, no stream) costs one comparison."""
+
+    def __init__(self, device, stream):
+        torch = _torch()
+        if stream is not None and getattr(stream, "device", device) != device:
+            raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
+        self.other = stream is not None or torch._C._cuda_getDevice() != device.index
+        if self.other:
+            self.contexts = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
+
+    def __enter__(self):
+        if self.other:
+            for c in self.contexts:
+                c.__enter__()
+
+    def __exit__(self, *error):
+        if self.other:
+            for c in reversed(self.contexts):
+                c.__exit__(*error)
+
+
+def _rows(t, name: str, heads_shape=None):
+    """Pointer and pitch (elements between tokens) of [tokens, heads, D] whose heads lie side by side; tokens may be apart."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, D]")
+    if heads_shape is not None and tuple(t.shape) != tuple(heads_shape):
+        raise ValueError(f"{name} must be {list(heads_shape)}, got {list(t.shape)}")
+    n, heads, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
+        raise ValueError(f"the heads of {name} must lie side by side within a token")
+    return t.data_ptr(), (t.stride(0) if n > 1 else heads * D)
+
+
+def _given(t, name: str, shape, dtype, device):
+    """An output: the caller's, if it fits, or a new one."""
+    if t is None:
+        return _torch().empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}")
+    return t
+
+
+def _off(off, name: str = "off"):
+    if off.dim() != 1 or off.shape[0] < 2:
+        raise ValueError(f"{name} must be [N + 1]")
+    return off.shape[0] - 1
+
+
+def laser_history_attention_forward(q, k, v, off, L_max: int, gamma: float, o_out=None, lse_out=None, stream=None):
+    """Causal attention over packed sequences: q [T,H,D], k, v [T,H_kv,D] (column blocks of one tensor will do), off int32 [N+1],
+    L_max at least the longest sequence -> (o [T,H,D], lse [T,H] fp32). Rows of no sequence are not written."""
+    torch = _torch()
+    device = _placed({"q": q, "k": k, "v": v, "off": off, "o_out": o_out, "lse_out": lse_out})
+    qp, q_pitch = _rows(q, "q")
+    T, H, D = q.shape
+    kp, k_pitch = _rows(k, "k", (T, k.shape[1], D))
+    vp, v_pitch = _rows(v, "v", k.shape)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k, v must share a dtype")
+    with _On(device, stream):
+        o_out = _given(o_out, "o_out", (T, H, D), q.dtype, device)
+        lse_out = _given(lse_out, "lse_out", (T, H), torch.float32, device)
+        code = load_library().laser_history_attention_forward(
+            qp, q_pitch, kp, k_pitch, vp, v_pitch, _ptr(off, "off", torch.int32), _off(off), T, int(L_max), H, k.shape[1], D,
+            float(gamma), _dt(q), _ptr(o_out, "o_out"), _ptr(lse_out, "lse_out"), _stream(stream))
+    _check(code, "laser_history_attention_forward")
+    return o_out, lse_out
+
+
+def laser_history_attention_backward_work_bytes(N: int, T: int, L_max: int, H: int, H_kv: int, D: int, dt: int) -> int:
+    return load_library().laser_history_attention_backward_work_bytes(N, T, L_max, H, H_kv, D, dt)
+
+
+def laser_history_attention_backward(q, k, v, o, lse, d_o, off, L_max: int, gamma: float, dq_out=None, dk_out=None,
+                                     dv_out=None, work=None, stream=None):
+    """Gradients of laser_history_attention_forward: o [T,H,D], lse [T,H] as it returned them, d_o [T,H,D] ->
+    (dq [T,H,D], dk [T,H_kv,D], dv [T,H_kv,D]) in the dtype of q. The outputs may be column blocks of one tensor."""
+    torch = _torch()
+    device = _placed({"q": q, "k": k, "v": v, "o": o, "lse": lse, "d_o": d_o, "off": off, "dq_out": dq_out, "dk_out": dk_out,
+                      "dv_out": dv_out, "work": work})
+    qp, q_pitch = _rows(q, "q")
+    T, H, D = q.shape
+    kp, k_pitch = _rows(k, "k", (T, k.shape[1], D))
+    vp, v_pitch = _rows(v, "v", k.shape)
+    if any(x.dtype != q.dtype for x in (k, v, o, d_o)):
+        raise TypeError("q, k, v, o and d_o must share a dtype")
+    if tuple(o.shape) != (T, H, D) or tuple(d_o.shape) != (T, H, D) or tuple(lse.shape) != (T, H):
+        raise ValueError("o and d_o must be [T,H,D], lse [T,H]")
+    N, Hkv, lib = _off(off), k.shape[1], load_library()
+    with _On(device, stream):
+        dq_out = _given(dq_out, "dq_out", (T, H, D), q.dtype, device)
+        dk_out = _given(dk_out, "dk_out", (T, Hkv, D), q.dtype, device)
+        dv_out = _given(dv_out, "dv_out", (T, Hkv, D), q.dtype, device)
+        if work is None:
+            need = lib.laser_history_attention_backward_work_bytes(N, T, int(L_max), H, Hkv, D, _dt(q))
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        (dqp, dq_pitch), (dkp, dk_pitch), (dvp, dv_pitch) = _rows(dq_out, "dq_out"), _rows(dk_out, "dk_out"), _rows(dv_out, "dv_out")
+        code = lib.laser_history_attention_backward(
+            qp, q_pitch, kp, k_pitch, vp, v_pitch, _ptr(o, "o"), _ptr(lse, "lse", torch.float32), _ptr(d_o, "d_o"),
+            _ptr(off, "off", torch.int32), N, T, int(L_max), H, Hkv, D, float(gamma), _dt(q), dqp, dq_pitch, dkp, dk_pitch, dvp,
+            dv_pitch, _ptr(work, "work"), work.numel() * work.element_size(), _stream(stream))
+    _check(code, "laser_history_attention_backward")
+    return dq_out, dk_out, dv_out
+
+
+def _cache_shape(k_cache, v_cache, pages, lens):
+    """(P, H_kv, page, D, U, max_pages) of a paged cache and its table."""
+    torch = _torch()
+    if k_cache.dim() != 4 or tuple(v_cache.shape) != tuple(k_cache.shape):
+        raise ValueError("k_cache and v_cache must both be [P, H_kv, page, D]")
+    if v_cache.dtype != k_cache.dtype:
+        raise TypeError("k_cache and v_cache must share a dtype")
+    if pages.dim() != 2 or tuple(lens.shape) != (pages.shape[0],):
+        raise ValueError("pages must be [U, max_pages], lens [U]")
+    if pages.dtype != torch.int32 or lens.dtype != torch.int32:
+        raise TypeError("pages and lens must be int32")
+    return (*k_cache.shape, *pages.shape)
+
+
+def _of_users(off, U: int) -> None:
+    if tuple(off.shape) != (U + 1,):
+        raise ValueError("off must be [U + 1]")
+
+
+def _weight(weight, P: int, page: int):
+    if weight is not None and tuple(weight.shape) != (P, page):
+        raise ValueError("weight must be [P, page]")
+    return _ptr(weight, "weight", _torch().float32)
+
+
+def laser_cache_append(k, v, k_cache, v_cache, off, pages, lens, C_max: int, L_max: int, weight=None, stream=None):
+    """New keys and values [T,H_kv,D], packed by off int32 [U+1] (at most C_max a user), become the last items of each user's
+    lens [U] in k_cache, v_cache [P,H_kv,page,D]; pages int32 [U,max_pages]. weight [P,page]: their places are set to 0."""
+    torch = _torch()
+    device = _placed({"k": k, "v": v, "k_cache": k_cache, "v_cache": v_cache, "off": off, "pages": pages, "lens": lens,
+                      "weight": weight})
+    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
+    kp, k_pitch = _rows(k, "k", (k.shape[0], Hkv, D))
+    vp, v_pitch = _rows(v, "v", k.shape)
+    if k.dtype != k_cache.dtype or v.dtype != k_cache.dtype:
+        raise TypeError("k, v must have the dtype of the cache")
+    _of_users(off, U)
+    with _On(device, stream):
+        code = load_library().laser_cache_append(
+            kp, k_pitch, vp, v_pitch, _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(off, "off", torch.int32),
+            _ptr(pages, "pages"), _ptr(lens, "lens"), U, k.shape[0], int(C_max), P, page, max_pages, int(L_max), Hkv, D,
+            _dt(k_cache), _weight(weight, P, page), _stream(stream))
+    _check(code, "laser_cache_append")
+
+
+def laser_cache_attention_work_bytes(U: int, T: int, C_max: int, L_max: int, H: int, H_kv: int, D: int, dt: int) -> int:
+    return load_library().laser_cache_attention_work_bytes(U, T, C_max, L_max, H, H_kv, D, dt)
+
+
+def laser_cache_attention_forward(q, k_cache, v_cache, off, pages, lens, C_max: int, L_max: int, gamma: float,
+                                  causal: bool = True, o_out=None, lse_out=None, work=None, stream=None):
+    """Queries [T,H,D], packed by off int32 [U+1] (at most C_max a user), over each user's cached items -> (o [T,H,D], lse [T,H]).
+    causal: the queries are those of the cache's last items, each sees the items up to its own; otherwise (candidates) all."""
+    torch = _torch()
+    device = _placed({"q": q, "k_cache": k_cache, "v_cache": v_cache, "off": off, "pages": pages, "lens": lens,
+                      "o_out": o_out, "lse_out": lse_out, "work": work})
+    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
+    T, H = q.shape[0], q.shape[1]
+    qp, q_pitch = _rows(q, "q", (T, H, D))
+    if q.dtype != k_cache.dtype:
+        raise TypeError("q must have the dtype of the cache")
+    _of_users(off, U)
+    lib = load_library()
+    with _On(device, stream):
+        o_out = _given(o_out, "o_out", (T, H, D), q.dtype, device)
+        lse_out = _given(lse_out, "lse_out", (T, H), torch.float32, device)
+        if work is None:
+            need = lib.laser_cache_attention_work_bytes(U, T, int(C_max), int(L_max), H, Hkv, D, _dt(q))
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        code = lib.laser_cache_attention_forward(
+            qp, q_pitch, _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(off, "off", torch.int32),
+            _ptr(pages, "pages"), _ptr(lens, "lens"), U, T, int(C_max), P, page, max_pages, int(L_max), H, Hkv, D, float(gamma),
+            int(bool(causal)), _dt(q), _ptr(o_out, "o_out"), _ptr(lse_out, "lse_out"), _ptr(work, "work"),
+            work.numel() * work.element_size(), _stream(stream))
+    _check(code, "laser_cache_attention_forward")
+    return o_out, lse_out
+
+
+def laser_cache_weights(q, lse, k_cache, off, pages, lens, C_max: int, L_max: int, gamma: float, weight, causal: bool = True,
+                        add: bool = True, stream=None):
+    """What each cached item received from the queries of laser_cache_attention_forward, summed over queries and heads, into
+    weight [P,page] fp32 (add: onto what stands there). lse [T,H] as that call returned it. Returns weight."""
+    torch = _torch()
+    device = _placed({"q": q, "lse": lse, "k_cache": k_cache, "off": off, "pages": pages, "lens": lens, "weight": weight})
+    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, k_cache, pages, lens)
+    T, H = q.shape[0], q.shape[1]
+    qp, q_pitch = _rows(q, "q", (T, H, D))
+    if q.dtype != k_cache.dtype:
+        raise TypeError("q must have the dtype of the cache")
+    if tuple(lse.shape) != (T, H):
+        raise ValueError("lse must be [T,H]")
+    _of_users(off, U)
+    with _On(device, stream):
+        code = load_library().laser_cache_weights(
+            qp, q_pitch, _ptr(lse, "lse", torch.float32), _ptr(k_cache, "k_cache"), _ptr(off, "off", torch.int32),
+            _ptr(pages, "pages"), _ptr(lens, "lens"), U, T, int(C_max), P, page, max_pages, int(L_max), H, Hkv, D, float(gamma),
+            int(bool(causal)), int(bool(add)), _dt(q), _weight(weight, P, page), _stream(stream))
+    _check(code, "laser_cache_weights")
+    return weight
+
+
+def laser_cache_evict(k_cache, v_cache, weight, pages, lens, pages_out, budget: int, recent: int, L_max: int, lens_out=None,
+                      kept_out=None, stream=None):
+    """Each user keeps the `recent` last of its items and the heaviest others by weight [P,page], `budget` in all; they move, in
+    order and with their weights, into the pages of pages_out int32 [U,max_pages_out] -> (lens [U], kept [U,budget], the old
+    places, -1 behind the last)."""
+    torch = _torch()
+    device = _placed({"k_cache": k_cache, "v_cache": v_cache, "weight": weight, "pages": pages, "lens": lens,
+                      "pages_out": pages_out, "lens_out": lens_out, "kept_out": kept_out})
+    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
+    if pages_out.dim() != 2 or pages_out.shape[0] != U:
+        raise ValueError("pages_out must be [U, max_pages_out]")
+    budget = int(budget)
+    with _On(device, stream):
+        lens_out = _given(lens_out, "lens_out", (U,), torch.int32, device)
+        kept_out = _given(kept_out, "kept_out", (U, max(budget, 0)), torch.int32, device)
+        code = load_library().laser_cache_evict(
+            _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _weight(weight, P, page), _ptr(pages, "pages"),
+            _ptr(lens, "lens"), _ptr(pages_out, "pages_out", torch.int32), U, P, page, max_pages, pages_out.shape[1], int(L_max),
+            budget, int(recent), Hkv, D, _dt(k_cache), _ptr(lens_out, "lens_out"), _ptr(kept_out, "kept_out"), _stream(stream))
+    _check(code, "laser_cache_evict")
+    return lens_out, kept_out

@@ -1,0 +1,198 @@
+"""Causal attention over packed histories and its gradients against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2602_11562_amd as laser
+from history_ref import attend, close, gradients, offsets, sees
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+#        lengths                        H  Hkv  D
+SHAPES = [([1], 1, 1, 64),
+          ([5, 0, 1, 33], 2, 2, 64),
+          ([0, 64, 65, 0], 4, 2, 128),
+          ([130, 31, 127], 3, 1, 128),
+          ([300, 7], 8, 1, 64),
+          ([70, 200], 6, 3, 40),
+          ([77, 3], 5, 1, 8),
+          ([257], 4, 4, 32),
+          ([129, 100], 24, 2, 128),
+          ([520, 1, 260], 2, 1, 96),
+          ([400], 10, 1, 72)]
+
+
+def make(lens, H, Hkv, D, dtype, seed=1, packed=True, before=2, behind=3, scale=1.0):
+    """Column blocks of one projection's output; rows of no sequence hold NaN."""
+    g = torch.Generator().manual_seed(seed)
+    T = sum(lens) + before + behind
+    qkv = (torch.randn(T, H + 2 * Hkv, D, generator=g) * scale).to(DT[dtype]).cuda()
+    qkv[:before] = float("nan")
+    qkv[T - behind:] = float("nan")
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    if not packed:
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    off, host = offsets(lens, start=before)
+    return q, k, v, off, host
+
+
+def check_forward(o, lse, q, k, v, host, gamma, dtype):
+    G = q.shape[1] // k.shape[1]
+    for a, b in zip(host, host[1:]):
+        allowed = sees(b - a, b - a, True, "cuda")
+        for h in range(q.shape[1]):
+            if b > a:
+                ref = attend(q[a:b, h].double(), k[a:b, h // G].double(), v[a:b, h // G].double(), gamma, allowed, dtype == "bf16")
+                close(o[a:b, h], ref["o"], ref["o_tol"], f"o rows {a}..{b} head {h}")
+                close(lse[a:b, h], ref["lse"], ref["lse_tol"], f"lse rows {a}..{b} head {h}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,Hkv,D", SHAPES)
+def test_forward(lens, H, Hkv, D, dtype):
+    q, k, v, off, host = make(lens, H, Hkv, D, dtype)
+    gamma = math.sqrt(D)
+    o = torch.full((q.shape[0], H, D), 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full((q.shape[0], H), 7.0, device="cuda")
+    laser.laser_history_attention_forward(q, k, v, off, max(lens), gamma, o_out=o, lse_out=lse)
+    check_forward(o, lse, q, k, v, host, gamma, dtype)
+    for t in (o, lse):      # rows of no sequence are left as they were
+        assert (t[:2] == 7.0).all() and (t[host[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,gamma", [(6.0, 1.0), (1.0, 0.05), (0.0, 1.0)])
+def test_forward_of_extreme_scores(scale, gamma, dtype):
+    """Scores in the hundreds, where one item takes everything, and scores that are all equal."""
+    q, k, v, off, host = make([150, 20], 4, 2, 64, dtype, scale=scale)
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 150, gamma)
+    check_forward(o, lse, q, k, v, host, gamma, dtype)
+
+
+def test_many_short_sequences():
+    lens = [(i * 7) % 23 for i in range(700)]
+    q, k, v, off, host = make(lens, 2, 1, 64, "bf16")
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 22, 8.0)
+    check_forward(o, lse, q, k, v, host[:60], 8.0, "bf16")
+    whole, _ = laser.laser_history_attention_forward(q, k, v, off[600:], 22, 8.0)     # the same rows, fewer sequences
+    a, b = host[600], host[700]
+    assert torch.equal(whole[a:b], o[a:b])
+
+
+def test_offsets_that_break_the_rules_stay_in_bounds():
+    """A sequence longer than L_max is cut there; offsets that fall or point outside reach no other row."""
+    q, k, v, off, host = make([40, 50], 2, 2, 64, "bf16")
+    o = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    laser.laser_history_attention_forward(q, k, v, off, 30, 8.0, o_out=o)
+    short, _ = offsets([30], start=host[0])
+    want, _ = laser.laser_history_attention_forward(q, k, v, short, 30, 8.0)
+    assert torch.equal(o[host[0]:host[0] + 30], want[host[0]:host[0] + 30])
+    assert (o[host[0] + 30:host[1]] == 7.0).all() and (o[host[1] + 30:] == 7.0).all()
+    o.fill_(7.0)
+    bad = torch.tensor([-5, -9, 10 ** 9, 2 * 10 ** 9], dtype=torch.int32, device="cuda")
+    laser.laser_history_attention_forward(q, k, v, bad, 30, 8.0, o_out=o)
+    assert (o[30:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,Hkv,D", SHAPES)
+def test_backward(lens, H, Hkv, D, dtype):
+    q, k, v, off, host = make(lens, H, Hkv, D, dtype, seed=2)
+    gamma, T, G = math.sqrt(D), q.shape[0], H // Hkv
+    go = torch.randn(T, H, D, generator=torch.Generator().manual_seed(3)).to(q.dtype).cuda()
+    go[:2] = float("nan")
+    go[host[-1]:] = float("nan")
+    o = torch.full((T, H, D), float("nan"), dtype=q.dtype, device="cuda")
+    lse = torch.full((T, H), float("nan"), device="cuda")
+    laser.laser_history_attention_forward(q, k, v, off, max(lens), gamma, o_out=o, lse_out=lse)
+    d = torch.full((T, H + 2 * Hkv, D), 7.0, dtype=q.dtype, device="cuda")
+    dq, dk, dv = d[:, :H], d[:, H:H + Hkv], d[:, H + Hkv:]
+    laser.laser_history_attention_backward(q, k, v, o, lse, go, off, max(lens), gamma, dq_out=dq, dk_out=dk, dv_out=dv)
+    assert (d[:2] == 7.0).all() and (d[host[-1]:] == 7.0).all()
+    step = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    for a, b in zip(host, host[1:]):
+        if b == a:
+            continue
+        allowed = sees(b - a, b - a, True, "cuda")
+        for j in range(Hkv):
+            total = {"dk": [0.0, 0.0, 0.0], "dv": [0.0, 0.0, 0.0]}
+            for h in range(j * G, j * G + G):
+                rq, rk, rv = gradients(q[a:b, h].double(), k[a:b, j].double(), v[a:b, j].double(), go[a:b, h].double(), gamma,
+                                       allowed, dtype == "bf16")
+                close(dq[a:b, h], *rq, f"dq rows {a}..{b} head {h}")
+                for name, r in (("dk", rk), ("dv", rv)):
+                    total[name][0] = total[name][0] + r[0]
+                    total[name][1] = total[name][1] + r[1]
+            close(dk[a:b, j], total["dk"][0], total["dk"][1] + step * total["dk"][0].abs(), f"dk rows {a}..{b} head {j}")
+            close(dv[a:b, j], total["dv"][0], total["dv"][1] + step * total["dv"][0].abs(), f"dv rows {a}..{b} head {j}")
+
+
+def test_backward_against_differences():
+    """Directional differences of the forward pass itself, in single precision."""
+    q, k, v, off, host = make([37, 20], 4, 2, 32, "f32", before=0, behind=0, packed=False)
+    gamma, g = math.sqrt(32), torch.Generator().manual_seed(5)
+    go = torch.randn(q.shape, generator=g).cuda()
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 37, gamma)
+    grads = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 37, gamma)
+    for i, t in enumerate((q, k, v)):
+        d = torch.randn(t.shape, generator=g).cuda()
+        h = 2.0 ** -7
+        up, down = ([x.clone() for x in (q, k, v)] for _ in range(2))
+        up[i] += h * d
+        down[i] -= h * d
+        f = [(laser.laser_history_attention_forward(*x, off, 37, gamma)[0].double() * go.double()).sum() for x in (up, down)]
+        # the difference's own error: h^2/6 of the third derivative (a few units here) and 2^-24 of the sums over h
+        assert abs((f[0] - f[1]).item() / (2 * h) - (grads[i].double() * d.double()).sum().item()) < 2e-2
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_repeated_runs_agree_bit_for_bit(dtype):
+    q, k, v, off, host = make([300, 41, 200], 8, 2, 128, dtype, before=0, behind=0)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(5)).to(q.dtype).cuda()
+    runs = []
+    for _ in range(3):
+        o, lse = laser.laser_history_attention_forward(q, k, v, off, 300, 11.0)
+        runs.append((o, lse, *laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 300, 11.0)))
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], r))
+
+
+def test_captured_and_replayed_beside_eager_calls():
+    """Forward and backward in a graph, replayed between eager calls on other inputs that share nothing with it."""
+    q, k, v, off, host = make([150, 90], 4, 2, 64, "bf16", before=0, behind=0)
+    other = make([60, 200], 4, 2, 64, "bf16", seed=9, before=0, behind=0)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(5)).to(q.dtype).cuda()
+
+    def both(q, k, v, off, go, L):
+        o, lse = laser.laser_history_attention_forward(q, k, v, off, L, 8.0)
+        return (o, lse, *laser.laser_history_attention_backward(q, k, v, o, lse, go, off, L, 8.0))
+
+    want = [t.clone() for t in both(q, k, v, off, go, 150)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(q, k, v, off, go, 150)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(q, k, v, off, go, 150)
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        go2 = torch.ones_like(other[0])
+        both(*other[:4], go2, 200)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_on_another_stream():
+    q, k, v, off, host = make([150, 90], 4, 2, 64, "bf16", before=0, behind=0)
+    want, _ = laser.laser_history_attention_forward(q, k, v, off, 150, 8.0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got, _ = laser.laser_history_attention_forward(q, k, v, off, 150, 8.0, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
