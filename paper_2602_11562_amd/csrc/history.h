@@ -20,6 +20,7 @@ struct HistoryArgs {
   hipStream_t stream;
 };
 laser_status history_forward_launch(const HistoryArgs& a);
+laser_status history_tile_launch(const HistoryArgs& a);   // bf16, on the matrix cores
 
 struct HistoryBwdArgs {
   HistoryArgs f;           // the forward pass's arguments; o and lse are inputs here
@@ -55,6 +56,7 @@ struct CacheArgs {
 };
 size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status cache_attention_launch(const CacheArgs& a);
+laser_status cache_tile_launch(const CacheArgs& a);       // bf16, on the matrix cores
 laser_status cache_weights_launch(const CacheArgs& a);   // q, lse and k in, weight out
 
 struct CacheAppendArgs {

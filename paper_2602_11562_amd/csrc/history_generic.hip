@@ -258,7 +258,7 @@ static laser_status forward_typed(const HistoryArgs& a) {
   return launch_status();
 }
 laser_status history_forward_launch(const HistoryArgs& a) {
-  return a.dt == LASER_F32 ? forward_typed<float>(a) : forward_typed<unsigned short>(a);
+  return a.dt == LASER_F32 ? forward_typed<float>(a) : history_tile_launch(a);
 }
 
 template <typename T>
@@ -294,7 +294,7 @@ static laser_status cache_attention_typed(const CacheArgs& a) {
 }
 size_t cache_attention_work_bytes(int, int, int, int, int, int, int, laser_dtype) { return 16; }
 laser_status cache_attention_launch(const CacheArgs& a) {
-  return a.dt == LASER_F32 ? cache_attention_typed<float>(a) : cache_attention_typed<unsigned short>(a);
+  return a.dt == LASER_F32 ? cache_attention_typed<float>(a) : cache_tile_launch(a);
 }
 
 template <typename T>
