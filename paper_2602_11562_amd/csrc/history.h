@@ -33,6 +33,7 @@ struct HistoryBwdArgs {
 };
 size_t history_backward_work_bytes(int N, int T, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status history_backward_launch(const HistoryBwdArgs& a);
+laser_status history_bwd_tile_launch(const HistoryBwdArgs& a);   // bf16, on the matrix cores
 
 // A paged cache: item j of user u stands in page pages[u * max_pages + j / page], at place j % page of every key-value head.
 struct CacheArgs {

@@ -1,0 +1,325 @@
+// Gradients of attention among the items of histories on the matrix cores (bf16).
+//
+//   p = exp2(c q.k - lse), dp = d_o . v, ds = p (dp - delta), delta = d_o . o
+// Two kernels, each of which recomputes p and dp, so that every sum is one workgroup's and its order is fixed:
+//   dq: a wave owns 32 rows (token and head, packed as in the forward pass) and walks the items they see.
+//       Sc^T = K Q^T, dP^T = V dO^T (rows in lanes: lse and delta are one register each), dQ^T += K^T dS^T
+//   dk, dv: a wave owns 32 items of a key-value head and walks the rows that see them, of all its query heads.
+//       Sc = Q K^T, dP = dO V^T (items in lanes), dV^T += dO^T P, dK^T += Q^T dS
+// Seven products of two operations a multiply-add where five would do with one kernel, which would have to add one of the
+// gradients up across workgroups.
+#include <type_traits>
+
+#include "history_tile.h"
+
+namespace laser {
+
+struct BwdArgs {
+  const unsigned short* q;
+  const unsigned short* k;
+  const unsigned short* v;
+  const unsigned short* o;
+  const unsigned short* go;
+  long long qp, kp, vp;
+  const int32_t* off;
+  int N, T, L, H, Hkv, D, G, tiles;
+  MulDiv by_group;       // / G
+  float scale, inv_gamma;   // log2(e) / gamma, 1 / gamma
+  const float* lse;
+  float* delta;          // [T,H]
+  unsigned short* dq;
+  unsigned short* dk;
+  unsigned short* dv;
+  long long dqp, dkp, dvp;
+};
+
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a) {
+  using Sh = TileShape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * 32, OP = DP * 2 + 16, STAGE = 2 * Sh::BYTES, PATCH = NW * 32 * OP;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const int per = a.N * a.Hkv;
+  const int tile = a.tiles - 1 - (int)(blockIdx.x / per), nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
+  const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+
+  bf16x8 qreg[KS], greg[KS];
+  float lse2, delta;
+  int last;
+  const int first = row0 + wave * 32;
+  {
+    int r = first + l32;
+    r = r < rows ? r : rows - 1;
+    last = (int)a.by_group.div(r);
+    const int head = hk * a.G + r - last * a.G;
+    const size_t tok = (size_t)cr.first + last, at = (tok * a.H + head) * a.D;
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = s * 16 + h * 8;
+      u32x4 x = {0u, 0u, 0u, 0u}, y = x, z = x;
+      if (c < a.D) {
+        x = *reinterpret_cast<const u32x4*>(a.q + tok * a.qp + (size_t)head * a.D + c);
+        y = *reinterpret_cast<const u32x4*>(a.go + at + c);
+        z = *reinterpret_cast<const u32x4*>(a.o + at + c);
+      }
+      qreg[s] = __builtin_bit_cast(bf16x8, x);
+      greg[s] = __builtin_bit_cast(bf16x8, y);
+      const bf16x8 o = __builtin_bit_cast(bf16x8, z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)greg[s][e], (float)o[e], sum);
+    }
+    delta = half_sum(sum);
+    lse2 = a.lse[tok * a.H + head] * LOG2E;
+    if (h == 0 && first + l32 < rows) a.delta[tok * a.H + head] = delta;
+  }
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
+  const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
+
+  f32x16 acc[DB];
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero;
+
+  const TileReader<DP> read(lane);
+  auto step = [&](int t0, unsigned at, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib) {
+      f32x16 sc, dp;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, ib, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at + Sh::BYTES, ib, s), greg[s], s == 0 ? zero : dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      unsigned ds[8];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sc[r + e], a.scale, -lse2));
+          x[e] = p * (dp[r + e] - delta);
+          if (decltype(masked)::value && t0 + ib * 32 + 8 * (r >> 2) + 4 * h + (r & 3) + e > last) x[e] = 0.0f;
+        }
+        ds[r >> 1] = pack_bf16(x[0], x[1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u32x4 b = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at, ib * 2 + s, db), __builtin_bit_cast(bf16x8, b),
+                                                            acc[db], 0, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  PackedTiles<DP, NW> tiles;
+  tiles.init(a.D, a.kp, a.vp, wave, lane);
+  auto fetch = [&](int t0, unsigned at) __attribute__((always_inline)) {
+    const size_t row = (size_t)(cr.first + t0);
+    tiles.fetch(a.k + row * a.kp + (size_t)hk * a.D, a.v + row * a.vp + (size_t)hk * a.D, a.kp, a.vp, a.D, n - t0, at);
+  };
+  fetch(0, lds);
+  unsigned at = lds, other = lds + STAGE;
+  for (int t0 = 0; t0 < end; t0 += TI) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t0 + TI < end) fetch(t0 + TI, other);
+    if (t0 <= wave_last) {
+      if (t0 + TI - 1 <= wave_first) step(t0, at, std::false_type{});
+      else step(t0, at, std::true_type{});
+    }
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  barrier_lds();
+  store_block<DP>(acc, a.inv_gamma, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
+    const int i = (int)a.by_group.div(first + r), head = hk * a.G + first + r - i * a.G;
+    return a.dq + (size_t)(cr.first + i) * a.dqp + (size_t)head * a.D;
+  });
+}
+
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel(const BwdArgs a) {
+  using Sh = TileShape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32, ITEMS = NW * 32, OP = DP * 2 + 16, GPW = (Sh::GROUPS + NW - 1) / NW;
+  constexpr int STAGE = 2 * Sh::BYTES + 2 * TI * 4, PATCH = NW * 32 * OP;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const int per = a.N * a.Hkv;
+  const int tile = (int)(blockIdx.x / per), nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
+  const int n = cr.count, item0 = tile * ITEMS;
+  if (item0 >= n) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const int rows = n * a.G, first = item0 + wave * 32;
+
+  bf16x8 kreg[KS], vreg[KS];
+  int from;   // the first row that sees this lane's item
+  {
+    int j = first + l32;
+    j = j < n ? j : n - 1;
+    from = j * a.G;
+    const size_t tok = (size_t)cr.first + j;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = s * 16 + h * 8;
+      u32x4 x = {0u, 0u, 0u, 0u}, y = x;
+      if (c < a.D) {
+        x = *reinterpret_cast<const u32x4*>(a.k + tok * a.kp + (size_t)hk * a.D + c);
+        y = *reinterpret_cast<const u32x4*>(a.v + tok * a.vp + (size_t)hk * a.D + c);
+      }
+      kreg[s] = __builtin_bit_cast(bf16x8, x);
+      vreg[s] = __builtin_bit_cast(bf16x8, y);
+    }
+  }
+  const int wave_from = __builtin_amdgcn_readlane(from, 0), wave_to = __builtin_amdgcn_readlane(from, 31);
+
+  // tiles of rows: queries, behind them d_o, behind them lse and delta; rows behind the last read as zeros and add nothing
+  auto fetch = [&](int r0, unsigned at) __attribute__((always_inline)) {
+    const int i0 = (int)a.by_group.div(r0);
+    const size_t tok = (size_t)cr.first + i0, head0 = (size_t)hk * a.G;
+    const u32x4 qb = buffer_of(a.q + tok * a.qp + head0 * a.D, 0x7fffffffu);
+    const u32x4 gb = buffer_of(a.go + (tok * a.H + head0) * a.D, 0x7fffffffu);
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int g = wave + x * NW;
+      if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
+      const int in = g * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
+      const int i = (int)a.by_group.div(r), head = r - i * a.G;
+      const bool ok = r < rows && c * 8 < a.D;
+      const int tk = i - i0;
+      buffer_to_lds16(qb, ok ? (unsigned)((tk * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN, at + g * 1024);
+      buffer_to_lds16(gb, ok ? (unsigned)(((tk * a.H + head) * a.D + c * 8) * 2) : NO_COLUMN, at + Sh::BYTES + g * 1024);
+    }
+    if (wave < 2) {
+      const int r = r0 + lane, i = (int)a.by_group.div(r), head = r - i * a.G;
+      const u32x4 b = buffer_of((wave == 0 ? a.lse : a.delta) + tok * a.H + head0, 0x7fffffffu);
+      buffer_to_lds4(b, r < rows ? (unsigned)((i - i0) * a.H + head) * 4 : NO_COLUMN, at + 2 * Sh::BYTES + wave * TI * 4);
+    }
+  };
+
+  f32x16 dk[DB], dv[DB];
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dk[db] = dv[db] = zero;
+
+  const TileReader<DP> read(lane);
+  auto step = [&](int r0, unsigned at, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      f32x16 sc, dp;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, rb, s), kreg[s], s == 0 ? zero : sc, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at + Sh::BYTES, rb, s), vreg[s], s == 0 ? zero : dp, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      unsigned p[8], ds[8];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        const unsigned where = at + 2 * Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4;
+        const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
+        const f32x4 d = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + TI * 4));
+        float pv[4], dv4[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pv[e] = __builtin_amdgcn_exp2f(fmaf(sc[g * 4 + e], a.scale, -z[e] * LOG2E));
+          if (decltype(masked)::value && r0 + rb * 32 + g * 8 + h * 4 + e < from) pv[e] = 0.0f;
+          dv4[e] = pv[e] * (dp[g * 4 + e] - d[e]);
+        }
+        p[g * 2] = pack_bf16(pv[0], pv[1]);
+        p[g * 2 + 1] = pack_bf16(pv[2], pv[3]);
+        ds[g * 2] = pack_bf16(dv4[0], dv4[1]);
+        ds[g * 2 + 1] = pack_bf16(dv4[2], dv4[3]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u32x4 pb = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
+          const u32x4 sb = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
+          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at + Sh::BYTES, rb * 2 + s, db),
+                                                           __builtin_bit_cast(bf16x8, pb), dv[db], 0, 0, 0);
+          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at, rb * 2 + s, db),
+                                                           __builtin_bit_cast(bf16x8, sb), dk[db], 0, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  const int start = item0 * a.G / TI * TI;   // (rows before it see no item of this workgroup)
+  fetch(start, lds);
+  unsigned at = lds, other = lds + STAGE;
+  for (int r0 = start; r0 < rows; r0 += TI) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (r0 + TI < rows) fetch(r0 + TI, other);
+    if (first < n && r0 + TI > wave_from) {
+      if (r0 >= wave_to) step(r0, at, std::false_type{});
+      else step(r0, at, std::true_type{});
+    }
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  barrier_lds();
+  unsigned char* patch = smem + wave * 32 * OP;
+  store_block<DP>(dk, a.inv_gamma, patch, n - first, a.D, lane,
+                  [&](int r) { return a.dk + (size_t)(cr.first + first + r) * a.dkp + (size_t)hk * a.D; });
+  store_block<DP>(dv, 1.0f, patch, n - first, a.D, lane,
+                  [&](int r) { return a.dv + (size_t)(cr.first + first + r) * a.dvp + (size_t)hk * a.D; });
+}
+
+template <int DP>
+static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
+  constexpr int NW = 4;
+  const long long per = (long long)a.N * a.Hkv;
+  const long long row_tiles = ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), item_tiles = ((long long)a.L + NW * 32 - 1) / (NW * 32);
+  if (per * row_tiles > 0x7fffffffLL) return LASER_ERR_SHAPE;
+  a.tiles = (int)row_tiles;
+  history_dq_kernel<DP, NW><<<(unsigned)(per * row_tiles), 64 * NW, 0, stream>>>(a);
+  history_dkv_kernel<DP, NW><<<(unsigned)(per * item_tiles), 64 * NW, 0, stream>>>(a);
+  return launch_status();
+}
+
+laser_status history_bwd_tile_launch(const HistoryBwdArgs& b) {
+  const HistoryArgs& h = b.f;
+  BwdArgs a{};
+  a.q = static_cast<const unsigned short*>(h.q);
+  a.k = static_cast<const unsigned short*>(h.k);
+  a.v = static_cast<const unsigned short*>(h.v);
+  a.o = static_cast<const unsigned short*>(h.o);
+  a.go = static_cast<const unsigned short*>(b.go);
+  a.qp = h.qp, a.kp = h.kp, a.vp = h.vp;
+  a.off = h.off;
+  a.N = h.N, a.T = h.T, a.L = h.L, a.H = h.H, a.Hkv = h.Hkv, a.D = h.D, a.G = h.H / h.Hkv;
+  a.by_group = mul_div(a.G);
+  a.scale = LOG2E / h.gamma;
+  a.inv_gamma = 1.0f / h.gamma;
+  a.lse = h.lse;
+  a.delta = b.work;
+  a.dq = static_cast<unsigned short*>(b.dq);
+  a.dk = static_cast<unsigned short*>(b.dk);
+  a.dv = static_cast<unsigned short*>(b.dv);
+  a.dqp = b.dqp, a.dkp = b.dkp, a.dvp = b.dvp;
+  if (a.D > 64) return bwd_launch<128>(a, h.stream);
+  if (a.D > 32) return bwd_launch<64>(a, h.stream);
+  return bwd_launch<32>(a, h.stream);
+}
+
+}  // namespace laser

@@ -78,13 +78,16 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
   }
 
   // requests: wave w brings groups w, w + NW, .. of a tile, of keys and of values
-  unsigned koff[GPW], voff[GPW];
+  PackedTiles<DP, NW> packed;
+  unsigned paged_off[GPW];
+  if constexpr (PAGED) {
 #pragma unroll
-  for (int x = 0; x < GPW; ++x) {
-    const int r = (wave + x * NW) * Sh::RPI + lane / Sh::CH, in = PAGED ? lane / Sh::CH : r, pos = lane % Sh::CH;
-    const int kc = pos ^ tile_kswz<Sh::CH>(r), vc = pos ^ (4 * tile_vswz<Sh::CH>(r));
-    koff[x] = kc * 8 < a.D ? (unsigned)(in * (PAGED ? a.D : (int)a.kp) * 2 + kc * 16) : NO_COLUMN;
-    voff[x] = vc * 8 < a.D ? (unsigned)(in * (PAGED ? a.D : (int)a.vp) * 2 + vc * 16) : NO_COLUMN;
+    for (int x = 0; x < GPW; ++x) {
+      const int in = lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>((wave + x * NW) * Sh::RPI + in);
+      paged_off[x] = c * 8 < a.D ? (unsigned)(in * a.D * 2 + c * 16) : NO_COLUMN;
+    }
+  } else {
+    packed.init(a.D, a.kp, a.vp, wave, lane);
   }
   const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
   int ids[GPW][2];   // pages of the next tile's groups (a second one where a page is shorter than a group)
@@ -105,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
       for (int x = 0; x < GPW; ++x) {
         const int g = wave + x * NW;
         if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-        const int j = t0 + g * Sh::RPI, place = j & ((1 << a.log2) - 1);
+        const int j = t0 + g * Sh::RPI;
         auto half = [&](int id, int j, int rows_here, int skip) __attribute__((always_inline)) {
           const int left = n - j < rows_here ? n - j : rows_here;
           const bool ok = left > 0 && (unsigned)id < (unsigned)a.P;
@@ -113,10 +116,9 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
           // (offsets count from the group's first row: the base of a second page's rows lies `skip` rows ahead of them)
           const unsigned bytes = ok ? (unsigned)((skip + left) * a.D * 2) : 0u;
           const long long base = ((long long)row - (ok ? skip : 0)) * a.D;
-          buffer_to_lds16(buffer_of(a.k + base, bytes), koff[x], at + g * 1024);
-          buffer_to_lds16(buffer_of(a.v + base, bytes), voff[x], at + Sh::BYTES + g * 1024);
+          buffer_to_lds16(buffer_of(a.k + base, bytes), paged_off[x], at + g * 1024);
+          buffer_to_lds16(buffer_of(a.v + base, bytes), paged_off[x], at + Sh::BYTES + g * 1024);
         };
-        (void)place;
         if (Sh::RPI > 8 && a.log2 == 3) {   // two pages a group: each half of the lanes from its own
           if (lane < 32) half(ids[x][0], j, 8, 0);
           else half(ids[x][1], j + 8, 8, 8);
@@ -125,17 +127,8 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
         }
       }
     } else {
-      const int left = n - t0 < TI ? n - t0 : TI;
       const size_t row = (size_t)(cr.first + t0);
-      const u32x4 kb = buffer_of(a.k + row * a.kp + (size_t)hk * a.D, (unsigned)(((left - 1) * (int)a.kp + a.D) * 2));
-      const u32x4 vb = buffer_of(a.v + row * a.vp + (size_t)hk * a.D, (unsigned)(((left - 1) * (int)a.vp + a.D) * 2));
-#pragma unroll
-      for (int x = 0; x < GPW; ++x) {
-        const int g = wave + x * NW;
-        if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-        buffer_to_lds16(kb, koff[x], at + g * 1024);
-        buffer_to_lds16(vb, voff[x], at + Sh::BYTES + g * 1024);
-      }
+      packed.fetch(a.k + row * a.kp + (size_t)hk * a.D, a.v + row * a.vp + (size_t)hk * a.D, a.kp, a.vp, a.D, n - t0, at);
     }
   };
   // is every page of the user's items one of the pool? (then only the last tile has places without items)
@@ -166,6 +159,7 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     for (int db = 0; db < DB; ++db) acc[b][db] = zero;
   }
 
+  const TileReader<DP> read(lane);
   auto step = [&](int t0, unsigned at, unsigned long long items, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     f32x16 sc[RB][2];
@@ -173,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     for (int ib = 0; ib < 2; ++ib)
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const bf16x8 kf = tile_k<DP>(at, ib, s, l32, h);
+        const bf16x8 kf = read.rows(at, ib, s);
 #pragma unroll
         for (int b = 0; b < RB; ++b)
           sc[b][ib] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qreg[b][s], s == 0 ? zero : sc[b][ib], 0, 0, 0);
@@ -224,7 +218,7 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const bf16x8 vf = tile_vt<DP>(at + Sh::BYTES, s, db, lane);
+        const bf16x8 vf = read.cols(at + Sh::BYTES, s, db);
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
           const unsigned* w = &p[b][s >> 1][(s & 1) * 4];
@@ -263,31 +257,16 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const float sum = half_sum(l[b]), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const u32x2 o = {pack_bf16(acc[b][db][g * 4] * inv, acc[b][db][g * 4 + 1] * inv),
-                         pack_bf16(acc[b][db][g * 4 + 2] * inv, acc[b][db][g * 4 + 3] * inv)};
-        *reinterpret_cast<u32x2*>(patch + l32 * OP + (db * 32 + g * 8 + h * 4) * 2) = o;
-      }
     const int first = row0 + (wave * RB + b) * 32;
     const int r = first + l32;
     if (a.lse != nullptr && h == 0 && r < rows) {
       const int i = (int)a.by_group.div(r), g = r - i * a.G;
       a.lse[(size_t)(cr.first + i) * a.H + hk * a.G + g] = sum > 0.0f ? (m[b] + log2f(sum)) * LN2 : -INFINITY;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 2
-    for (int x = lane; x < 32 * Sh::CH; x += 64) {
-      const int pr = x / Sh::CH, c = x % Sh::CH, rr = first + pr;
-      if (rr < rows && c * 8 < a.D) {
-        const int i = (int)a.by_group.div(rr), g = rr - i * a.G;
-        *reinterpret_cast<u32x4*>(a.o + ((size_t)(cr.first + i) * a.H + hk * a.G + g) * a.D + c * 8) =
-            *reinterpret_cast<const u32x4*>(patch + pr * OP + c * 16);
-      }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    store_block<DP>(acc[b], inv, patch, rows - first, a.D, lane, [&](int r) {
+      const int i = (int)a.by_group.div(first + r), g = first + r - i * a.G;
+      return a.o + ((size_t)(cr.first + i) * a.H + hk * a.G + g) * a.D;
+    });
   }
 }
 

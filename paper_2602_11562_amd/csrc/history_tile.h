@@ -24,10 +24,12 @@ __device__ __forceinline__ void buffer_to_lds16(u32x4 buf, unsigned voff, unsign
 
 constexpr unsigned NO_COLUMN = 0x80000000u;   // an offset behind every buffer's end
 
-// A tile row of DP bf16 is CH pieces of 16 bytes, piece c of row r at place c ^ kswz(r) of a key row and c ^ 4 vswz(r) of a value
-// row: what an operand read takes at once (16 rows at one piece; four rows at four pieces) then lies in all banks.
-template <int CH> __device__ __forceinline__ int tile_kswz(int r) { return ((r * CH) >> 4) & (CH - 1); }
-template <int CH> __device__ __forceinline__ int tile_vswz(int r) { return ((r * CH) >> 4) & (CH / 4 - 1); }
+// A tile row of DP bf16 is CH pieces of 16 bytes, piece c of row r at place c ^ tile_swz(r). Both ways of reading then find all
+// banks: 16 rows at one piece (operands over the width), four rows at four pieces (the transpose load).
+template <int CH> __device__ __forceinline__ int tile_swz(int r) {
+  const int q = (r * CH) >> 4;   // 256-byte lines of all banks
+  return CH == 16 ? (q & 3) * 4 + ((q >> 2) & 3) : CH == 8 ? (q & 1) * 4 + ((q >> 1) & 3) : q & 3;
+}
 
 // Offsets of a lane's pieces: each wave-wide request brings 64 pieces, RPI rows
 template <int DP>
@@ -41,26 +43,96 @@ __device__ __forceinline__ int scalar_int(const int32_t* p, int at) {
   return ((scalar_ptr)(unsigned long long)p)[__builtin_amdgcn_readfirstlane(at)];
 }
 
-// K rows as the A operand of a product over the width: item 32 b + lane % 32, pieces 2 s + lane / 32
+// How a lane reads a tile as the A operand of its products. Tiles start at multiples of 256 bytes, so the piece's place can be
+// flipped in the sum of both.
 template <int DP>
-__device__ __forceinline__ bf16x8 tile_k(unsigned at, int b, int s, int l32, int h) {
-  constexpr int CH = DP / 8;
-  const int row = b * 32 + l32;
-  return lds_read16(lds_at(at + row * (DP * 2) + (((2 * s + h) ^ tile_kswz<CH>(row)) << 4)));
+struct TileReader {
+  static constexpr int ROW = DP * 2, CH = DP / 8;
+  unsigned row, lo, hi;
+  __device__ __forceinline__ explicit TileReader(int lane) {
+    const int l32 = lane & 31, h = lane >> 5, i16 = lane & 15, r = h * 4 + (i16 >> 2), c = 2 * (l32 >> 4) + ((i16 & 3) >> 1);
+    row = l32 * ROW + ((h ^ tile_swz<CH>(l32)) << 4);
+    lo = r * ROW + ((c ^ tile_swz<CH>(r)) << 4) + (i16 & 1) * 8;
+    hi = (r + 8) * ROW + ((c ^ tile_swz<CH>(r + 8)) << 4) + (i16 & 1) * 8;
+  }
+  // a product over the width: row 32 b + lane % 32, pieces 2 s + lane / 32
+  __device__ __forceinline__ bf16x8 rows(unsigned at, int b, int s) const {
+    return lds_read16(lds_at((at + row) ^ (s << 5)) + b * 32 * ROW);
+  }
+  // a product over the rows, of the transpose: columns 32 db .., rows 16 s + {4h .. 4h+3, 8+4h .. 8+4h+3} (the order in which a score
+  // block's accumulators hold them)
+  __device__ __forceinline__ bf16x8 cols(unsigned at, int s, int db) const {
+    auto half = [&](unsigned x) {
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_at((at + x) ^ (db << 6)) + s * 16 * ROW));
+    };
+    const s16x4 a = half(lo), b = half(hi);
+    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+  const bf16x2 c = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(unsigned, c);
 }
 
-// V^T as the A operand of a product over items: columns 32 db .., items 16 s + {4h .. 4h+3, 8+4h .. 8+4h+3} (the order in which a
-// score block's accumulators hold them)
-template <int DP>
-__device__ __forceinline__ bf16x8 tile_vt(unsigned at, int s, int db, int lane) {
-  constexpr int CH = DP / 8;
-  const int h = lane >> 5, i16 = lane & 15, vrow = h * 4 + (i16 >> 2), vlow = 2 * ((lane & 31) >> 4) + ((i16 & 3) >> 1);
-  auto half = [&](int r) {
-    const unsigned a = at + r * (DP * 2) + (((vlow + 4 * db) ^ (4 * tile_vswz<CH>(r))) << 4) + (i16 & 1) * 8;
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds_at(a));
-  };
-  const s16x4 lo = half(s * 16 + vrow), hi = half(s * 16 + 8 + vrow);
-  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+// Four bytes per lane to LDS (uniform address + 4 * lane)
+__device__ __forceinline__ void buffer_to_lds4(u32x4 buf, unsigned voff, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds\n" ::"s"(lds_addr), "v"(voff), "s"(buf)
+               : "memory");
+}
+
+// Tiles of packed keys and values: wave w of NW brings groups w, w + NW, .. (RPI rows each) of both
+template <int DP, int NW>
+struct PackedTiles {
+  using Sh = TileShape<DP>;
+  static constexpr int GPW = (Sh::GROUPS + NW - 1) / NW;
+  unsigned koff[GPW], voff[GPW];
+  int wave;
+  __device__ __forceinline__ void init(int D, long long kp, long long vp, int wave_, int lane) {
+    wave = wave_;
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int r = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
+      koff[x] = c * 8 < D ? (unsigned)(r * (int)kp * 2 + c * 16) : NO_COLUMN;
+      voff[x] = c * 8 < D ? (unsigned)(r * (int)vp * 2 + c * 16) : NO_COLUMN;
+    }
+  }
+  // rows k, v and on (`left` of them are the sequence's); keys to `at`, values behind them
+  __device__ __forceinline__ void fetch(const unsigned short* k, const unsigned short* v, long long kp, long long vp, int D, int left,
+                                        unsigned at) const {
+    left = left < TI ? left : TI;
+    const u32x4 kb = buffer_of(k, (unsigned)(((left - 1) * (int)kp + D) * 2)), vb = buffer_of(v, (unsigned)(((left - 1) * (int)vp + D) * 2));
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int g = wave + x * NW;
+      if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
+      buffer_to_lds16(kb, koff[x], at + g * 1024);
+      buffer_to_lds16(vb, voff[x], at + Sh::BYTES + g * 1024);
+    }
+  }
+};
+
+// A block of 32 rows that the accumulators hold transposed (column 32 db + 8 g + 4 h + e of row lane % 32), times `by`, through an
+// LDS patch of the wave's own so that it leaves in 16-byte pieces; to(r): where row r goes, rows from `rows` on go nowhere
+template <int DP, typename To>
+__device__ __forceinline__ void store_block(const f32x16* acc, float by, unsigned char* patch, int rows, int D, int lane, const To& to) {
+  constexpr int OP = DP * 2 + 16, CH = DP / 8;
+  const int l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32x2 o = {pack_bf16(acc[db][g * 4] * by, acc[db][g * 4 + 1] * by),
+                       pack_bf16(acc[db][g * 4 + 2] * by, acc[db][g * 4 + 3] * by)};
+      *reinterpret_cast<u32x2*>(patch + l32 * OP + (db * 32 + g * 8 + h * 4) * 2) = o;
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 2
+  for (int x = lane; x < 32 * CH; x += 64) {
+    const int r = x / CH, c = x % CH;
+    if (r < rows && c * 8 < D) *reinterpret_cast<u32x4*>(to(r) + c * 8) = *reinterpret_cast<const u32x4*>(patch + r * OP + c * 16);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
 // x of the other half of the wave: max and sum over the two lanes that share a row
@@ -71,11 +143,6 @@ __device__ __forceinline__ float half_max(float x) {
 __device__ __forceinline__ float half_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
-  const bf16x2 c = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(unsigned, c);
 }
 
 }  // namespace laser
