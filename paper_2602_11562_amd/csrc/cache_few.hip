@@ -1,0 +1,296 @@
+// A few rows per key-value head over a paged cache (bf16): one new item or a handful of candidates a user. The cache is read once
+// and everything else is small, so this is bound by memory.
+//
+// A workgroup owns (user, key-value head, run of items); its four waves take tiles of 32 items in turn, each with tiles of its own
+// in LDS and no barrier while it streams: requests run ahead of the arithmetic by as many tiles as fit. The rows (at most 32: every
+// new item's query heads of the group) are one column block of the products of history_mfma.hip. At the end the waves' maxima,
+// sums and outputs are joined in LDS. Histories longer than a run are cut into several workgroups' runs, whose results go to the work
+// buffer (outputs normalised, with log2 of their sums) and are joined by a second launch.
+#include "history_tile.h"
+
+namespace laser {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <int DP>
+struct FewShape {
+  static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, TILE = 32 * ROW, GROUPS = 32 / RPI;
+  static constexpr int REQ = 2 * GROUPS;                  // requests a tile
+  static constexpr int NST = DP == 128 ? 2 : 4;           // tiles of a wave
+  static constexpr int WAVE = NST * 2 * TILE;             // its bytes
+  static constexpr int JOIN = DP * 33 * 4;                // what it joins with: [column][33 rows] of fp32
+  static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
+};
+
+template <int DP>
+__global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, int G, MulDiv by_group, float scale, int chunk, int splits) {
+  using Sh = FewShape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * Sh::WAVE];
+  __shared__ float join_m[4][32], join_l[4][32];
+  const int per = a.U * a.Hkv;
+  const int split = blockIdx.x / per, uh = blockIdx.x % per, u = uh / a.Hkv, hk = uh % a.Hkv;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int rows = cr.count * G;
+  if (rows == 0) return;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
+  const int lo = split * chunk, hi = n < lo + chunk ? n : lo + chunk;
+  if (lo >= n && split > 0) return;   // (the first run of an empty history still writes)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem) + wave * Sh::WAVE;
+  const unsigned short* q = static_cast<const unsigned short*>(a.q);
+  const unsigned short* kc = static_cast<const unsigned short*>(a.k);
+  const unsigned short* vc = static_cast<const unsigned short*>(a.v);
+  const int32_t* table = a.pages + (size_t)u * a.max_pages;
+
+  unsigned off[Sh::GROUPS];
+#pragma unroll
+  for (int g = 0; g < Sh::GROUPS; ++g) {
+    const int in = lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(g * Sh::RPI + in);
+    off[g] = c * 8 < a.D ? (unsigned)(in * a.D * 2 + c * 16) : NO_COLUMN;
+  }
+  int ids[4];   // pages of the next tile: of its items 0, 8, 16 and 24
+  auto look_up = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) ids[x] = t0 + x * 8 < hi ? scalar_int(table, (t0 + x * 8) >> a.page_log2) : -1;
+  };
+  auto fetch = [&](int t0, unsigned at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < Sh::GROUPS; ++g) {
+      auto part = [&](int id, int j, int count, int skip) __attribute__((always_inline)) {
+        const int left = hi - j < count ? hi - j : count;
+        const bool ok = left > 0 && (unsigned)id < (unsigned)a.P;
+        const size_t row = ok ? (((size_t)id * a.Hkv + hk) << a.page_log2) + (j & ((1 << a.page_log2) - 1)) : 0;
+        const unsigned bytes = ok ? (unsigned)((skip + left) * a.D * 2) : 0u;
+        const long long base = ((long long)row - (ok ? skip : 0)) * a.D;
+        buffer_to_lds16(buffer_of(kc + base, bytes), off[g], at + g * 1024);
+        buffer_to_lds16(buffer_of(vc + base, bytes), off[g], at + Sh::TILE + g * 1024);
+      };
+      const int j = t0 + g * Sh::RPI;
+      if (Sh::RPI > 8 && a.page_log2 == 3) {   // two pages a request: each half of the lanes from its own
+        if (lane < 32) part(ids[g * 2], j, 8, 0);
+        else part(ids[g * 2 + 1], j + 8, 8, 8);
+      } else {
+        part(ids[g * Sh::RPI / 8], j, Sh::RPI, 0);
+      }
+    }
+  };
+  // (what a request brings: its own count on the page of two, twice as many)
+  const int requests = Sh::RPI > 8 && a.page_log2 == 3 ? 2 * Sh::REQ : Sh::REQ;
+
+  const int step_items = 4 * 32;
+  int ask = lo + wave * 32, mine = ask;
+  int pending = 0, slot_in = 0, slot_out = 0;
+  look_up(ask);
+  auto request = [&]() __attribute__((always_inline)) {
+    fetch(ask, lds + slot_in * 2 * Sh::TILE);
+    slot_in = slot_in + 1 == Sh::NST ? 0 : slot_in + 1;
+    ask += step_items;
+    ++pending;
+    look_up(ask);
+  };
+  for (int x = 0; x < Sh::NST && ask < hi; ++x) request();
+
+  bf16x8 qreg[KS];
+  int last;
+  {
+    const int r = l32 < rows ? l32 : rows - 1, i = (int)by_group.div(r), g = r - i * G;
+    last = a.causal ? n - cr.count + i : n - 1;
+    const unsigned short* qr = q + (size_t)(cr.first + i) * a.qp + (size_t)(hk * G + g) * a.D;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (s * 16 + h * 8 < a.D) raw = *reinterpret_cast<const u32x4*>(qr + s * 16 + h * 8);
+      qreg[s] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
+  const int first_seen = __builtin_amdgcn_readlane(last, 0);
+  bool whole_pages;
+  {
+    bool bad = false;
+    for (int x = (lo >> a.page_log2) + lane; x <= (hi - 1) >> a.page_log2 && lo < hi; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    whole_pages = __ballot(bad) == 0;
+  }
+
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero;
+  float m = -INFINITY, l = 0.0f;
+  const TileReader<DP> read(lane);
+
+  for (; mine < hi; mine += step_items) {
+    // loads return in order: with `pending` tiles asked for, the oldest is there when those of the others are all that is left
+    wait_vm((pending - 1) * requests);
+    asm volatile("" ::: "memory");
+    const unsigned at = lds + slot_out * 2 * Sh::TILE;
+    f32x16 sc;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, 0, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+    if (!whole_pages || mine + 31 > first_seen || mine + 32 > hi) {
+      const int left = hi - mine;
+      bool in = l32 < left;
+      if (!whole_pages) in = in && (unsigned)table[(mine + (in ? l32 : 0)) >> a.page_log2] < (unsigned)a.P;
+      const unsigned items = (unsigned)__ballot(in) >> (4 * h);
+      const int seen = last - mine - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i0 = 8 * (r >> 2) + (r & 3);
+        if (i0 > seen || !((items >> i0) & 1)) sc[r] = -INFINITY;
+      }
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = half_max(top) * scale;
+    if (__any(top > m)) {
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= c;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    unsigned p[8];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], scale, -base));
+      l += p0 + p1;
+      p[r >> 1] = pack_bf16(p0, p1);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 b = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at + Sh::TILE, s, db), __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again
+    --pending;
+    slot_out = slot_out + 1 == Sh::NST ? 0 : slot_out + 1;
+    if (ask < hi) request();
+  }
+
+  // the waves' results, in the place of the tiles
+  float* out = reinterpret_cast<float*>(smem + wave * Sh::WAVE);
+  l = half_sum(l);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[(db * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * 33 + l32] = acc[db][r];
+  if (h == 0) {
+    join_m[wave][l32] = m;
+    join_l[wave][l32] = l;
+  }
+  __syncthreads();
+  const bool final = n <= chunk;
+  for (int e = tid; e < rows * a.D; e += 256) {
+    const int r = e / a.D, d = e - r * a.D;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, join_m[w][r]);
+    float sum = 0.0f, x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = join_m[w][r], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
+      sum = fmaf(join_l[w][r], c, sum);
+      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 33 + r], c, x);
+    }
+    x = sum > 0.0f ? x / sum : 0.0f;
+    const float z = sum > 0.0f ? top + log2f(sum) : -INFINITY;
+    const int i = (int)by_group.div(r), g = r - i * G;
+    const size_t row = (size_t)(cr.first + i) * a.H + hk * G + g;
+    if (final) {
+      static_cast<unsigned short*>(a.o)[row * a.D + d] = f32_to_bf16_bits(x);
+      if (d == 0 && a.lse != nullptr) a.lse[row] = z * LN2;
+    } else {
+      const size_t all = (size_t)a.T * a.H;
+      a.work[(split * all + row) * a.D + d] = x;
+      if (d == 0) a.work[splits * all * a.D + split * all + row] = z;
+    }
+  }
+}
+
+// Joins the runs' results of a row: a workgroup per row, its four waves share the runs
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a, int chunk, int splits) {
+  __shared__ float part[4][128], part_s[4];
+  const int u = blockIdx.y, head = blockIdx.z;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
+  if (n <= chunk) return;   // one run: it has written the result
+  const size_t all = (size_t)a.T * a.H;
+  const float* z = a.work + splits * all * a.D;
+  for (int i = blockIdx.x; i < cr.count; i += gridDim.x) {
+    const size_t row = (size_t)(cr.first + i) * a.H + head;
+    const int seen = a.causal ? n - cr.count + i + 1 : n;
+    const int runs = seen <= 0 ? 0 : (seen + chunk - 1) / chunk;
+    float top = -INFINITY;
+    for (int s = lane; s < runs; s += 64) top = fmaxf(top, z[s * all + row]);
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    float x0 = 0.0f, x1 = 0.0f, sum = 0.0f;
+    if (top > -INFINITY) {
+#pragma unroll 4
+      for (int s = wave; s < runs; s += 4) {
+        const float c = exp2f(z[s * all + row] - top);
+        const float* o = a.work + (s * all + row) * a.D;
+        sum += c;
+        if (lane < a.D) x0 = fmaf(c, o[lane], x0);
+        if (lane + 64 < a.D) x1 = fmaf(c, o[lane + 64], x1);
+      }
+    }
+    part[wave][lane] = x0;
+    part[wave][lane + 64] = x1;
+    if (lane == 0) part_s[wave] = sum;
+    __syncthreads();
+    const float total = part_s[0] + part_s[1] + part_s[2] + part_s[3];
+    if (tid < a.D)
+      store_from_f32<T>(static_cast<T*>(a.o), row * a.D + tid,
+                        total > 0.0f ? (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / total : 0.0f);
+    if (tid == 0 && a.lse != nullptr) a.lse[row] = total > 0.0f ? (top + log2f(total)) * LN2 : -INFINITY;
+    __syncthreads();
+  }
+}
+
+laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {
+  for (int u = 0; u < a.U; u += 65535) {
+    CacheArgs part = a;
+    part.off = a.off + u;
+    part.lens = a.lens + u;
+    const dim3 grid(a.C < 1024 ? a.C : 1024, a.U - u < 65535 ? a.U - u : 65535, a.H);
+    if (a.dt == LASER_F32) cache_join_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+    else cache_join_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+  }
+  return launch_status();
+}
+
+// How the longest history is cut into runs, from what both the launch and the caller who provides the work buffer know: about two
+// workgroups a compute unit, runs of at least `least` items, whole tiles.
+CacheRuns cache_runs(int workgroups, int L, int least, int tile) {
+  const int want = workgroups > 0 && workgroups < 512 ? (512 + workgroups - 1) / workgroups : 1;
+  const int most = (L + least - 1) / least;
+  int runs = want < most ? want : most;
+  if (runs < 1) runs = 1;
+  const int chunk = ((L + runs - 1) / runs + tile - 1) / tile * tile;
+  return CacheRuns{chunk, (L + chunk - 1) / chunk};
+}
+
+template <int DP>
+static laser_status few_typed(const CacheArgs& a, const CacheRuns& r) {
+  const int G = a.H / a.Hkv;
+  const long long grid = (long long)a.U * a.Hkv * r.runs;
+  if (grid > 0x7fffffffLL) return LASER_ERR_SHAPE;
+  cache_few_kernel<DP><<<(unsigned)grid, 256, 0, a.stream>>>(a, G, mul_div(G), LOG2E / a.gamma, r.chunk, r.runs);
+  return r.runs > 1 ? cache_join_launch(a, r.chunk, r.runs) : launch_status();
+}
+laser_status cache_few_launch(const CacheArgs& a, const CacheRuns& r) {
+  if (a.D > 64) return few_typed<128>(a, r);
+  if (a.D > 32) return few_typed<64>(a, r);
+  return few_typed<32>(a, r);
+}
+
+}  // namespace laser

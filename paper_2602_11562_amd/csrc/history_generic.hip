@@ -292,9 +292,20 @@ static laser_status cache_attention_typed(const CacheArgs& a) {
   }
   return launch_status();
 }
-size_t cache_attention_work_bytes(int, int, int, int, int, int, int, laser_dtype) { return 16; }
+static bool few_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <= 32; }
+static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
+  if (dt == LASER_F32) return CacheRuns{L, 1};
+  const long long tiles = few_rows(C, H, Hkv) ? 1 : ((long long)C * (H / Hkv) + 127) / 128, all = tiles * U * Hkv;
+  return cache_runs(all < 512 ? (int)all : 512, L, few_rows(C, H, Hkv) ? 512 : 256, few_rows(C, H, Hkv) ? 128 : 64);
+}
+size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
+  const CacheRuns r = runs_of(U, C, L, H, Hkv, dt);
+  return r.runs > 1 ? (size_t)r.runs * T * H * (D + 1) * 4 : 16;
+}
 laser_status cache_attention_launch(const CacheArgs& a) {
-  return a.dt == LASER_F32 ? cache_attention_typed<float>(a) : cache_tile_launch(a);
+  if (a.dt == LASER_F32) return cache_attention_typed<float>(a);
+  const CacheRuns r = runs_of(a.U, a.C, a.L, a.H, a.Hkv, a.dt);
+  return few_rows(a.C, a.H, a.Hkv) ? cache_few_launch(a, r) : cache_tile_launch(a, r);
 }
 
 template <typename T>
@@ -308,7 +319,7 @@ static laser_status cache_weights_typed(const CacheArgs& a) {
   return launch_status();
 }
 laser_status cache_weights_launch(const CacheArgs& a) {
-  return a.dt == LASER_F32 ? cache_weights_typed<float>(a) : cache_weights_typed<unsigned short>(a);
+  return a.dt == LASER_F32 ? cache_weights_typed<float>(a) : cache_weights_tile_launch(a);
 }
 
 }  // namespace laser

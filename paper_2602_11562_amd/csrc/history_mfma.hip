@@ -29,6 +29,8 @@ struct TileArgs {
   bool causal;
   unsigned short* o;
   float* lse;
+  int chunk, runs;       // over a cache: items a workgroup walks, and into how many such runs the longest history is cut
+  float* work;           // their results where a history has several
 };
 
 // Where the maximum of a row is raised: probabilities may stand up to 2^8 above it meanwhile, sums and outputs are in its units
@@ -43,7 +45,13 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
 
   const int per = a.N * a.Hkv;
-  const int tile = a.tiles - 1 - (int)(blockIdx.x / per), nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  int tile = (int)(blockIdx.x / per), run = 0;
+  if (PAGED && a.runs > 1) {
+    run = tile / a.tiles;
+    tile -= run * a.tiles;
+  }
+  tile = a.tiles - 1 - tile;   // (the longest first)
+  const int nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.C, a.T);
   const int rows = cr.count * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
@@ -75,6 +83,13 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
   {
     const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
     end = a.causal ? n - cr.count + (int)a.by_group.div(r) + 1 : n;
+  }
+  const bool joined = PAGED && a.runs > 1 && n > a.chunk;   // others write their part of the result too
+  int begin = 0;
+  if (PAGED && a.runs > 1) {
+    begin = run * a.chunk;
+    if (run > 0 && begin >= end) return;
+    end = end < begin + a.chunk ? end : begin + a.chunk;
   }
 
   // requests: wave w brings groups w, w + NW, .. of a tile, of keys and of values
@@ -228,12 +243,12 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
       }
   };
 
-  if (end > 0) {
-    look_up(0);
-    fetch(0, lds);
-    look_up(TI);
+  if (end > begin) {
+    look_up(begin);
+    fetch(begin, lds);
+    look_up(begin + TI);
     unsigned at = lds, other = lds + STAGE;
-    for (int t0 = 0; t0 < end; t0 += TI) {
+    for (int t0 = begin; t0 < end; t0 += TI) {
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
       barrier_lds();   // the tile is there, and every wave is through with the one before
       if (t0 + TI < end) {
@@ -259,6 +274,23 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     const float sum = half_sum(l[b]), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     const int first = row0 + (wave * RB + b) * 32;
     const int r = first + l32;
+    if (joined) {
+      if (r >= rows) continue;
+      const int i = (int)a.by_group.div(r), g = r - i * a.G;
+      const size_t all = (size_t)a.T * a.H, row = (size_t)(cr.first + i) * a.H + hk * a.G + g;
+      float* to = a.work + (run * all + row) * a.D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int c = db * 32 + x * 8 + h * 4;
+          typedef float f32x4 __attribute__((ext_vector_type(4)));
+          if (c < a.D) *reinterpret_cast<f32x4*>(to + c) = f32x4{acc[b][db][x * 4] * inv, acc[b][db][x * 4 + 1] * inv,
+                                                                 acc[b][db][x * 4 + 2] * inv, acc[b][db][x * 4 + 3] * inv};
+        }
+      if (h == 0) a.work[a.runs * all * a.D + run * all + row] = sum > 0.0f ? m[b] + log2f(sum) : -INFINITY;
+      continue;
+    }
     if (a.lse != nullptr && h == 0 && r < rows) {
       const int i = (int)a.by_group.div(r), g = r - i * a.G;
       a.lse[(size_t)(cr.first + i) * a.H + hk * a.G + g] = sum > 0.0f ? (m[b] + log2f(sum)) * LN2 : -INFINITY;
@@ -274,7 +306,7 @@ template <int DP, int NW, int RB, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
   constexpr int ROWS = NW * RB * 32;
   a.tiles = (int)(((long long)a.C * a.G + ROWS - 1) / ROWS);
-  const long long grid = (long long)a.tiles * a.N * a.Hkv;
+  const long long grid = (long long)a.tiles * a.N * a.Hkv * a.runs;
   if (grid > 0x7fffffffLL) return LASER_ERR_SHAPE;
   history_tile_kernel<DP, NW, RB, PAGED><<<(unsigned)grid, 64 * NW, 0, stream>>>(a);
   return launch_status();
@@ -306,12 +338,13 @@ laser_status history_tile_launch(const HistoryArgs& h) {
   a.by_group = mul_div(a.G);
   a.scale = LOG2E / h.gamma;
   a.causal = true;
+  a.runs = 1;
   a.o = static_cast<unsigned short*>(h.o);
   a.lse = h.lse;
   return tile_launch_any<false>(a, h.stream);
 }
 
-laser_status cache_tile_launch(const CacheArgs& c) {
+laser_status cache_tile_launch(const CacheArgs& c, const CacheRuns& r) {
   TileArgs a{};
   a.q = static_cast<const unsigned short*>(c.q);
   a.k = static_cast<const unsigned short*>(c.k);
@@ -325,7 +358,10 @@ laser_status cache_tile_launch(const CacheArgs& c) {
   a.causal = c.causal;
   a.o = static_cast<unsigned short*>(c.o);
   a.lse = c.lse;
-  return tile_launch_any<true>(a, c.stream);
+  a.chunk = r.chunk, a.runs = r.runs;
+  a.work = c.work;
+  const laser_status s = tile_launch_any<true>(a, c.stream);
+  return s == LASER_OK && r.runs > 1 ? cache_join_launch(c, r.chunk, r.runs) : s;
 }
 
 }  // namespace laser
