@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const int per = a.N * a.Hkv;
-  const int tile = a.tiles - 1 - (int)(blockIdx.x / per), nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const int tile = a.tiles - 1 - (int)(blockIdx.x / per), nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const int per = a.N * a.Hkv;
-  const int tile = (int)(blockIdx.x / per), nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const int tile = (int)(blockIdx.x / per), nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, item0 = tile * ITEMS;
   if (item0 >= n) return;

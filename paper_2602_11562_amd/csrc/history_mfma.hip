@@ -36,12 +36,19 @@ struct TileArgs {
 // Where the maximum of a row is raised: probabilities may stand up to 2^8 above it meanwhile, sums and outputs are in its units
 constexpr float MAX_SLACK = 8.0f;
 
-template <int DP, int NW, int RB, bool PAGED>
-__global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_tile_kernel(const TileArgs a) {
-  using Sh = TileShape<DP>;
-  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * RB * 32, GPW = (Sh::GROUPS + NW - 1) / NW, OP = DP * 2 + 16;
-  constexpr int STAGE = 2 * Sh::BYTES, PATCH = NW * 32 * OP;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
+// Blocks of 32 items come as pairs (values of block u, keys of block u + 1), pair u to slot u % SLOTS of a ring.
+template <int DP>
+struct PairShape {
+  static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, GROUPS = 32 / RPI, KB = 32 * ROW, SLOT = 2 * KB;
+};
+
+template <int DP, int NW, int RB, int SLOTS, bool PAGED>
+__global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void history_tile_kernel(const TileArgs a) {
+  using Sh = PairShape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * RB * 32, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
+  constexpr int RPW = 2 * Sh::GROUPS / NW;   // requests of a wave for a pair
+  static_assert(2 * Sh::GROUPS % NW == 0, "every wave asks for as much");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * Sh::SLOT > PATCH ? SLOTS * Sh::SLOT : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
 
   const int per = a.N * a.Hkv;
@@ -51,12 +58,108 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     tile -= run * a.tiles;
   }
   tile = a.tiles - 1 - tile;   // (the longest first)
-  const int nh = blockIdx.x % per, n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const int nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.C, a.T);
   const int rows = cr.count * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
   const int n = PAGED ? cache_len(a.lens, n_seq, a.L, a.max_pages, a.log2) : cr.count;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+
+  int end;   // one past the last item that a row of this workgroup sees
+  {
+    const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
+    end = a.causal ? n - cr.count + (int)a.by_group.div(r) + 1 : n;
+  }
+  const bool joined = PAGED && a.runs > 1 && n > a.chunk;   // others write their part of the result too
+  int begin = 0;
+  if (PAGED && a.runs > 1) {
+    begin = run * a.chunk;
+    if (run > 0 && begin >= end) return;
+    end = end < begin + a.chunk ? end : begin + a.chunk;
+  }
+  const int blocks = end > begin ? (end - begin + 31) / 32 : 0;
+
+  // requests: numbered through, keys' groups of RPI rows first; wave w makes w, w + NW, ..
+  unsigned off[RPW];
+#pragma unroll
+  for (int x = 0; x < RPW; ++x) {
+    const int y = wave + x * NW, g = y % Sh::GROUPS, in = lane / Sh::CH, r = g * Sh::RPI + in;
+    const int c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
+    const int pitch = PAGED ? a.D : (int)(y < Sh::GROUPS ? a.kp : a.vp);
+    off[x] = c * 8 < a.D ? (unsigned)((PAGED ? in : r) * pitch * 2 + c * 16) : NO_COLUMN;
+  }
+  const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
+  const bool two_pages = PAGED && Sh::RPI > 8 && a.log2 == 3;   // a request's rows are on two pages: two requests
+  int ids[RPW][2];
+  auto item_of = [&](int u, int y) { return begin + (y < Sh::GROUPS ? u + 1 : u) * 32 + (y % Sh::GROUPS) * Sh::RPI; };
+  auto look_up = [&](int u) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int x = 0; x < RPW; ++x)
+#pragma unroll
+        for (int e = 0; e < (Sh::RPI > 8 ? 2 : 1); ++e) {
+          const int j = item_of(u, wave + x * NW) + e * 8;
+          ids[x][e] = j >= begin && j < end ? scalar_int(table, j >> a.log2) : -1;
+        }
+    }
+  };
+  auto fetch = [&](int u, unsigned at) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int x = 0; x < RPW; ++x) {
+        const int y = wave + x * NW;
+        const unsigned short* cache = y < Sh::GROUPS ? a.k : a.v;
+        const unsigned to = at + (y < Sh::GROUPS ? 0 : Sh::KB) + (y % Sh::GROUPS) * 1024;
+        auto part = [&](int id, int j, int count, int skip) __attribute__((always_inline)) {
+          const int left = n - j < count ? n - j : count;
+          const bool ok = left > 0 && (unsigned)id < (unsigned)a.P;   // (outside the run: no page)
+          const size_t row = ok ? (((size_t)id * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
+          // (offsets count from the request's first row: the base of a second page's rows lies `skip` rows ahead of them)
+          buffer_to_lds16(buffer_of(cache + ((long long)row - (ok ? skip : 0)) * a.D, ok ? (unsigned)((skip + left) * a.D * 2) : 0u),
+                          off[x], to);
+        };
+        const int j = item_of(u, y);
+        if (two_pages) {
+          if (lane < 32) part(ids[x][0], j, 8, 0);
+          else part(ids[x][1], j + 8, 8, 8);
+        } else {
+          part(ids[x][0], j, Sh::RPI, 0);
+        }
+      }
+    } else {
+      const int tk = (u + 1) * 32, tv = u * 32;
+      const size_t ik = (size_t)(cr.first + tk), iv = (size_t)(cr.first + (tv < 0 ? 0 : tv));
+      int kl = end - tk, vl = u < 0 ? 0 : end - tv;
+      kl = kl < 32 ? kl : 32;
+      vl = vl < 32 ? vl : 32;
+      const u32x4 kb = buffer_of(a.k + ik * a.kp + (size_t)hk * a.D, kl > 0 ? (unsigned)(((kl - 1) * (int)a.kp + a.D) * 2) : 0u);
+      const u32x4 vb = buffer_of(a.v + iv * a.vp + (size_t)hk * a.D, vl > 0 ? (unsigned)(((vl - 1) * (int)a.vp + a.D) * 2) : 0u);
+#pragma unroll
+      for (int x = 0; x < RPW; ++x) {
+        const int y = wave + x * NW;
+        if constexpr (Sh::GROUPS % NW == 0) {   // (a request's kind is known at compile time)
+          if (x * NW < Sh::GROUPS) buffer_to_lds16(kb, off[x], at + y * 1024);
+          else buffer_to_lds16(vb, off[x], at + y * 1024);
+        } else {
+          const u32x4 b = y < Sh::GROUPS ? kb : vb;
+          buffer_to_lds16(u32x4{(unsigned)__builtin_amdgcn_readfirstlane(b[0]), (unsigned)__builtin_amdgcn_readfirstlane(b[1]),
+                                (unsigned)__builtin_amdgcn_readfirstlane(b[2]), b[3]}, off[x], at + y * 1024);
+        }
+      }
+    }
+  };
+  int asked = -1, in = SLOTS - 1;   // pairs asked for: up to this one; the slot of the next
+  auto request = [&]() __attribute__((always_inline)) {
+    fetch(asked, lds + in * Sh::SLOT);
+    in = in + 1 == SLOTS ? 0 : in + 1;
+    ++asked;
+    look_up(asked);
+  };
+  const int requests = two_pages ? 2 * RPW : RPW;
+  if (blocks > 0) {
+    look_up(-1);
+    for (int x = 0; x < SLOTS && x <= blocks; ++x) request();   // pairs -1 .. SLOTS - 2 (asked is one past them from here on)
+  }
 
   // this lane's rows and the last item each sees
   int last[RB];
@@ -79,92 +182,19 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     wave_first = lo < wave_first ? lo : wave_first;
     wave_last = hi > wave_last ? hi : wave_last;
   }
-  int end;   // one past the last item that a row of this workgroup sees
-  {
-    const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
-    end = a.causal ? n - cr.count + (int)a.by_group.div(r) + 1 : n;
-  }
-  const bool joined = PAGED && a.runs > 1 && n > a.chunk;   // others write their part of the result too
-  int begin = 0;
-  if (PAGED && a.runs > 1) {
-    begin = run * a.chunk;
-    if (run > 0 && begin >= end) return;
-    end = end < begin + a.chunk ? end : begin + a.chunk;
-  }
-
-  // requests: wave w brings groups w, w + NW, .. of a tile, of keys and of values
-  PackedTiles<DP, NW> packed;
-  unsigned paged_off[GPW];
-  if constexpr (PAGED) {
-#pragma unroll
-    for (int x = 0; x < GPW; ++x) {
-      const int in = lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>((wave + x * NW) * Sh::RPI + in);
-      paged_off[x] = c * 8 < a.D ? (unsigned)(in * a.D * 2 + c * 16) : NO_COLUMN;
-    }
-  } else {
-    packed.init(a.D, a.kp, a.vp, wave, lane);
-  }
-  const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
-  int ids[GPW][2];   // pages of the next tile's groups (a second one where a page is shorter than a group)
-  auto look_up = [&](int t0) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
-#pragma unroll
-      for (int x = 0; x < GPW; ++x)
-#pragma unroll
-        for (int e = 0; e < (Sh::RPI > 8 ? 2 : 1); ++e) {
-          const int j = t0 + (wave + x * NW) * Sh::RPI + e * 8;
-          ids[x][e] = j < n ? scalar_int(table, j >> a.log2) : -1;
-        }
-    }
-  };
-  auto fetch = [&](int t0, unsigned at) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
-#pragma unroll
-      for (int x = 0; x < GPW; ++x) {
-        const int g = wave + x * NW;
-        if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-        const int j = t0 + g * Sh::RPI;
-        auto half = [&](int id, int j, int rows_here, int skip) __attribute__((always_inline)) {
-          const int left = n - j < rows_here ? n - j : rows_here;
-          const bool ok = left > 0 && (unsigned)id < (unsigned)a.P;
-          const size_t row = ok ? (((size_t)id * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
-          // (offsets count from the group's first row: the base of a second page's rows lies `skip` rows ahead of them)
-          const unsigned bytes = ok ? (unsigned)((skip + left) * a.D * 2) : 0u;
-          const long long base = ((long long)row - (ok ? skip : 0)) * a.D;
-          buffer_to_lds16(buffer_of(a.k + base, bytes), paged_off[x], at + g * 1024);
-          buffer_to_lds16(buffer_of(a.v + base, bytes), paged_off[x], at + Sh::BYTES + g * 1024);
-        };
-        if (Sh::RPI > 8 && a.log2 == 3) {   // two pages a group: each half of the lanes from its own
-          if (lane < 32) half(ids[x][0], j, 8, 0);
-          else half(ids[x][1], j + 8, 8, 8);
-        } else {
-          half(ids[x][0], j, Sh::RPI, 0);
-        }
-      }
-    } else {
-      const size_t row = (size_t)(cr.first + t0);
-      packed.fetch(a.k + row * a.kp + (size_t)hk * a.D, a.v + row * a.vp + (size_t)hk * a.D, a.kp, a.vp, a.D, n - t0, at);
-    }
-  };
-  // is every page of the user's items one of the pool? (then only the last tile has places without items)
+  // is every page of the user's items one of the pool? (then only the last block has places without items)
   bool whole_pages = true;
   if constexpr (PAGED) {
-    const int used = end > 0 ? ((end - 1) >> a.log2) + 1 : 0;
     bool bad = false;
-    for (int x = lane; x < used; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    if (blocks > 0)
+      for (int x = (begin >> a.log2) + lane; x <= (end - 1) >> a.log2; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
     whole_pages = __ballot(bad) == 0;
   }
-  auto items_of = [&](int t0) {   // bit i: item t0 + i is there
-    const int left = n - t0;
-    if (PAGED && !whole_pages) {
-      const bool in = lane < left && (unsigned)table[(t0 + (lane < left ? lane : 0)) >> a.log2] < (unsigned)a.P;
-      return (unsigned long long)__ballot(in);
-    }
-    return left >= TI ? ~0ull : (1ull << left) - 1;
-  };
 
-  f32x16 acc[RB][DB];
+  f32x16 acc[RB][DB], sa[RB], sb[RB];
   float m[RB], l[RB];
+  unsigned p[RB][8];
+  bf16x8 kf[KS], vf[2][DB];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -172,43 +202,73 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
     l[b] = 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[b][db] = zero;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) p[b][x] = 0;
   }
-
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) vf[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   const TileReader<DP> read(lane);
-  auto step = [&](int t0, unsigned at, unsigned long long items, auto masked) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    f32x16 sc[RB][2];
+
+  auto read_k = [&](unsigned at) __attribute__((always_inline)) {
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int s = 0; s < KS; ++s) kf[s] = read.rows(at, 0, s);
+  };
+  auto read_v = [&](unsigned at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const bf16x8 kf = read.rows(at, ib, s);
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
-          sc[b][ib] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qreg[b][s], s == 0 ? zero : sc[b][ib], 0, 0, 0);
-      }
-    unsigned p[RB][2][8];
+      for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(at + Sh::KB, s, db);
+  };
+  auto scores = [&](f32x16* sc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qreg[b][s], s == 0 ? zero : sc[b], 0, 0, 0);
+  };
+  auto values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          const u32x4 pf = {p[b][s * 4], p[b][s * 4 + 1], p[b][s * 4 + 2], p[b][s * 4 + 3]};
+          acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][db], __builtin_bit_cast(bf16x8, pf), acc[b][db], 0, 0, 0);
+        }
+  };
+  // scores of places without an item, and of items behind a row's own, become -inf
+  auto mask = [&](f32x16* sc, int t0) __attribute__((always_inline)) {
+    if (whole_pages && t0 + 31 <= wave_first && t0 + 32 <= n) return;
+    bool in = l32 < n - t0;
+    if (PAGED && !whole_pages) in = in && (unsigned)table[(t0 + (in ? l32 : 0)) >> a.log2] < (unsigned)a.P;
+    const unsigned items = (unsigned)__ballot(in) >> (4 * h);
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      if (MASKED) {
-        const int seen = last[b] - t0;
-        const unsigned long long mine = items >> (4 * h);
+      const int seen = last[b] - t0 - 4 * h;
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int i0 = ib * 32 + 8 * (r >> 2) + (r & 3);
-            if (i0 + 4 * h > seen || !((mine >> i0) & 1)) sc[b][ib][r] = -INFINITY;
-          }
+      for (int r = 0; r < 16; ++r) {
+        const int i0 = 8 * (r >> 2) + (r & 3);
+        if (i0 > seen || !((items >> i0) & 1)) sc[b][r] = -INFINITY;
       }
-      float top = sc[b][0][0];
+    }
+  };
+  auto raise = [&](const f32x16* sc) __attribute__((always_inline)) {
+    float top[RB];
+    bool over = false;
 #pragma unroll
-      for (int ib = 0; ib < 2; ++ib)
+    for (int b = 0; b < RB; ++b) {
+      top[b] = sc[b][0];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[b][ib][r]);
-      top = half_max(top) * a.scale;
-      if (__any(top > m[b] + MAX_SLACK)) {   // (the first tile: m is -inf)
-        const float next = fmaxf(m[b], top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[b] - next);
+      for (int r = 1; r < 16; ++r) top[b] = fmaxf(top[b], sc[b][r]);
+      top[b] = half_max(top[b]) * a.scale;
+      over |= top[b] > m[b] + MAX_SLACK;
+    }
+    if (__any(over)) {   // (the first block: m is -inf)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const float next = fmaxf(m[b], top[b]), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[b] - next);
         m[b] = next;
         l[b] *= c;
 #pragma unroll
@@ -216,54 +276,66 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[b][db][r] *= c;
       }
+    }
+  };
+  auto weigh = [&](const f32x16* sc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
       const float base = m[b] == -INFINITY ? 0.0f : m[b];
       float sum = 0.0f;
 #pragma unroll
-      for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[b][ib][r], a.scale, -base));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[b][ib][r + 1], a.scale, -base));
-          sum += p0 + p1;
-          p[b][ib][r >> 1] = pack_bf16(p0, p1);
-        }
-      l[b] += sum;
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const bf16x8 vf = read.cols(at + Sh::BYTES, s, db);
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          const unsigned* w = &p[b][s >> 1][(s & 1) * 4];
-          const u32x4 pf = {w[0], w[1], w[2], w[3]};
-          acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf), acc[b][db], 0, 0, 0);
-        }
+      for (int r = 0; r < 16; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.scale, -base));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[b][r + 1], a.scale, -base));
+        sum += p0 + p1;
+        p[b][r >> 1] = pack_bf16(p0, p1);
+        asm volatile("" : "+v"(p[b][r >> 1]));   // (here, not where the next turn reads it)
       }
+      l[b] += sum;
+      asm volatile("" : "+v"(l[b]));
+    }
   };
 
-  if (end > begin) {
-    look_up(begin);
-    fetch(begin, lds);
-    look_up(begin + TI);
-    unsigned at = lds, other = lds + STAGE;
-    for (int t0 = begin; t0 < end; t0 += TI) {
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      barrier_lds();   // the tile is there, and every wave is through with the one before
-      if (t0 + TI < end) {
-        fetch(t0 + TI, other);
-        look_up(t0 + 2 * TI);
+  // Block u: its scores are there, those of the next are made behind its exponentials, the last one's sum of values behind its maximum
+  int u = 0, out = 0;
+  auto turn = [&](f32x16* sc, f32x16* next) __attribute__((always_inline)) {
+    wait_vm((asked - u - 1) * requests);
+    barrier_lds();   // pair u is there, and every wave is through with the one before, whose slot is asked for again
+    if (asked < blocks) request();
+    const unsigned at = lds + out * Sh::SLOT;
+    out = out + 1 == SLOTS ? 0 : out + 1;
+    const int t0 = begin + u * 32;
+    if (t0 <= wave_last) {
+      read_k(at);
+      __builtin_amdgcn_sched_barrier(0);
+      values();
+      raise(sc);
+      __builtin_amdgcn_sched_barrier(0);
+      read_v(at);
+      scores(next);
+      weigh(sc);
+#pragma unroll
+      for (int x = 0; x < KS * RB; ++x) {   // one product, then its share of the exponentials and of the reads behind it
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / (KS * RB) > 0 ? 4 * DB / (KS * RB) : 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
       }
-      if (t0 <= wave_last) {
-        const unsigned long long items = items_of(t0);
-        if (items == ~0ull && t0 + TI - 1 <= wave_first) step(t0, at, items, std::false_type{});
-        else step(t0, at, items, std::true_type{});
-      }
-      const unsigned x = at;
-      at = other;
-      other = x;
+      __builtin_amdgcn_sched_barrier(0);
+      mask(next, t0 + 32);
     }
+    ++u;
+  };
+  if (blocks > 0) {
+    wait_vm((asked < 0 ? 0 : asked) * requests);
+    barrier_lds();
+    read_k(lds + (SLOTS - 1) * Sh::SLOT);
+    scores(sa);
+    mask(sa, begin);
+    while (u < blocks) {
+      turn(sa, sb);
+      if (u < blocks) turn(sb, sa);
+    }
+    values();
     barrier_lds();
   }
 
@@ -302,29 +374,29 @@ __global__ __launch_bounds__(64 * NW, (DP * RB <= 128 ? 2 : 1)) void history_til
   }
 }
 
-template <int DP, int NW, int RB, bool PAGED>
+template <int DP, int NW, int RB, int SLOTS, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
   constexpr int ROWS = NW * RB * 32;
   a.tiles = (int)(((long long)a.C * a.G + ROWS - 1) / ROWS);
   const long long grid = (long long)a.tiles * a.N * a.Hkv * a.runs;
   if (grid > 0x7fffffffLL) return LASER_ERR_SHAPE;
-  history_tile_kernel<DP, NW, RB, PAGED><<<(unsigned)grid, 64 * NW, 0, stream>>>(a);
+  history_tile_kernel<DP, NW, RB, SLOTS, PAGED><<<(unsigned)grid, 64 * NW, 0, stream>>>(a);
   return launch_status();
 }
 template <bool PAGED>
 static laser_status tile_launch_any(const TileArgs& a, hipStream_t stream) {
   const int form = tuning_int("LASER_HIST_FORM", 0);
   if (a.D > 64) {
-    if (form == 1) return tile_launch<128, 8, 1, PAGED>(a, stream);
-    if (form == 2) return tile_launch<128, 4, 2, PAGED>(a, stream);
-    return tile_launch<128, 4, 1, PAGED>(a, stream);
+    if (form == 1) return tile_launch<128, 8, 1, 4, PAGED>(a, stream);
+    if (form == 2) return tile_launch<128, 4, 2, 4, PAGED>(a, stream);
+    return tile_launch<128, 4, 1, 4, PAGED>(a, stream);
   }
   if (a.D > 32) {
-    if (form == 1) return tile_launch<64, 8, 1, PAGED>(a, stream);
-    if (form == 2) return tile_launch<64, 4, 2, PAGED>(a, stream);
-    return tile_launch<64, 4, 1, PAGED>(a, stream);
+    if (form == 1) return tile_launch<64, 8, 1, 4, PAGED>(a, stream);
+    if (form == 2) return tile_launch<64, 4, 2, 4, PAGED>(a, stream);
+    return tile_launch<64, 4, 1, 4, PAGED>(a, stream);
   }
-  return tile_launch<32, 4, 1, PAGED>(a, stream);
+  return tile_launch<32, 4, 1, 4, PAGED>(a, stream);
 }
 
 laser_status history_tile_launch(const HistoryArgs& h) {

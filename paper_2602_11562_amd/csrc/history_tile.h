@@ -22,6 +22,10 @@ __device__ __forceinline__ void buffer_to_lds16(u32x4 buf, unsigned voff, unsign
                : "memory");
 }
 
+// Which (sequence, head) of `per` a workgroup takes. Workgroups go to the eight dies in turn, so with a multiple of eight of them every
+// tile of a long sequence would land on the same die: the order is turned by one from row of tiles to row of tiles.
+__device__ __forceinline__ int spread(unsigned block, int per) { return (int)((block % per + block / per) % per); }
+
 constexpr unsigned NO_COLUMN = 0x80000000u;   // an offset behind every buffer's end
 
 // A tile row of DP bf16 is CH pieces of 16 bytes, piece c of row r at place c ^ tile_swz(r). Both ways of reading then find all
