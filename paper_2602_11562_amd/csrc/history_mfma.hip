@@ -36,18 +36,19 @@ struct TileArgs {
 // Where the maximum of a row is raised: probabilities may stand up to 2^8 above it meanwhile, sums and outputs are in its units
 constexpr float MAX_SLACK = 8.0f;
 
-// Blocks of 32 items come as pairs (values of block u, keys of block u + 1), pair u to slot u % SLOTS of a ring.
+// Tiles come as pairs: values of items 64 u and on, keys of 32 items later (what turn u reads), pair u to slot u % SLOTS of a ring. Pair -1
+// is the first 32 keys. A wave brings 64 / NW rows of either kind.
 template <int DP>
 struct PairShape {
-  static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, GROUPS = 32 / RPI, KB = 32 * ROW, SLOT = 2 * KB;
+  static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, KB = TI * ROW, SLOT = 2 * KB;
 };
 
 template <int DP, int NW, int RB, int SLOTS, bool PAGED>
 __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void history_tile_kernel(const TileArgs a) {
   using Sh = PairShape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * RB * 32, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
-  constexpr int RPW = 2 * Sh::GROUPS / NW;   // requests of a wave for a pair
-  static_assert(2 * Sh::GROUPS % NW == 0, "every wave asks for as much");
+  constexpr int MINE = TI / NW, RPW = MINE / Sh::RPI;   // a wave's rows of a tile, and its requests for them
+  static_assert(MINE % Sh::RPI == 0 && MINE <= 16, "whole requests, at most two pages of eight items");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * Sh::SLOT > PATCH ? SLOTS * Sh::SLOT : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
 
@@ -77,88 +78,85 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     if (run > 0 && begin >= end) return;
     end = end < begin + a.chunk ? end : begin + a.chunk;
   }
-  const int blocks = end > begin ? (end - begin + 31) / 32 : 0;
+  const int turns = end > begin ? (end - begin + TI - 1) / TI : 0;
 
-  // requests: numbered through, keys' groups of RPI rows first; wave w makes w, w + NW, ..
-  unsigned off[RPW];
+  unsigned koff[RPW], voff[RPW];
 #pragma unroll
   for (int x = 0; x < RPW; ++x) {
-    const int y = wave + x * NW, g = y % Sh::GROUPS, in = lane / Sh::CH, r = g * Sh::RPI + in;
-    const int c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
-    const int pitch = PAGED ? a.D : (int)(y < Sh::GROUPS ? a.kp : a.vp);
-    off[x] = c * 8 < a.D ? (unsigned)((PAGED ? in : r) * pitch * 2 + c * 16) : NO_COLUMN;
+    const int in = x * Sh::RPI + lane / Sh::CH, r = wave * MINE + in, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
+    koff[x] = c * 8 < a.D ? (unsigned)((PAGED ? in * a.D : r * (int)a.kp) * 2 + c * 16) : NO_COLUMN;
+    voff[x] = c * 8 < a.D ? (unsigned)((PAGED ? in * a.D : r * (int)a.vp) * 2 + c * 16) : NO_COLUMN;
   }
   const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
-  const bool two_pages = PAGED && Sh::RPI > 8 && a.log2 == 3;   // a request's rows are on two pages: two requests
-  int ids[RPW][2];
-  auto item_of = [&](int u, int y) { return begin + (y < Sh::GROUPS ? u + 1 : u) * 32 + (y % Sh::GROUPS) * Sh::RPI; };
+  const bool short_pages = PAGED && MINE > 8 && a.log2 == 3;   // a wave's rows are on two pages
+  int ids[2][2];   // of the next pair: pages of the wave's keys and values
+  auto first_of = [&](int u, int kind) { return begin + (u < 0 ? 0 : u * TI + (kind ? 0 : 32)) + wave * MINE; };
   auto look_up = [&](int u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
 #pragma unroll
-      for (int x = 0; x < RPW; ++x)
-#pragma unroll
-        for (int e = 0; e < (Sh::RPI > 8 ? 2 : 1); ++e) {
-          const int j = item_of(u, wave + x * NW) + e * 8;
-          ids[x][e] = j >= begin && j < end ? scalar_int(table, j >> a.log2) : -1;
-        }
+      for (int kind = 0; kind < 2; ++kind) {
+        const int j = first_of(u, kind);
+        ids[kind][0] = j < end ? scalar_int(table, j >> a.log2) : -1;
+        if (short_pages) ids[kind][1] = j + 8 < end ? scalar_int(table, (j + 8) >> a.log2) : -1;
+      }
     }
   };
+  const unsigned page_bytes = PAGED ? (unsigned)((a.Hkv << a.log2) * a.D * 2) : 0, head_bytes = PAGED ? (unsigned)((hk << a.log2) * a.D * 2) : 0;
   auto fetch = [&](int u, unsigned at) __attribute__((always_inline)) {
+    at += wave * MINE * Sh::ROW;
     if constexpr (PAGED) {
 #pragma unroll
-      for (int x = 0; x < RPW; ++x) {
-        const int y = wave + x * NW;
-        const unsigned short* cache = y < Sh::GROUPS ? a.k : a.v;
-        const unsigned to = at + (y < Sh::GROUPS ? 0 : Sh::KB) + (y % Sh::GROUPS) * 1024;
-        auto part = [&](int id, int j, int count, int skip) __attribute__((always_inline)) {
-          const int left = n - j < count ? n - j : count;
-          const bool ok = left > 0 && (unsigned)id < (unsigned)a.P;   // (outside the run: no page)
-          const size_t row = ok ? (((size_t)id * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
-          // (offsets count from the request's first row: the base of a second page's rows lies `skip` rows ahead of them)
-          buffer_to_lds16(buffer_of(cache + ((long long)row - (ok ? skip : 0)) * a.D, ok ? (unsigned)((skip + left) * a.D * 2) : 0u),
-                          off[x], to);
+      for (int kind = 0; kind < 2; ++kind) {
+        const int j = first_of(u, kind);
+        const char* cache = reinterpret_cast<const char*>(kind ? a.v : a.k) + head_bytes;
+        // rows j and on of a page, `skip` rows into the wave's own; places behind the last item read as zeros, like a page outside the pool
+        auto page = [&](int id, int j, int count, int skip) __attribute__((always_inline)) {
+          int left = n - j < count ? n - j : count;
+          if ((unsigned)id >= (unsigned)a.P || (kind && u < 0)) left = -skip;
+          const unsigned place = (unsigned)(j & ((1 << a.log2) - 1)) * a.D * 2;
+          return buffer_of(cache + ((unsigned long long)(id < 0 ? 0 : id) * page_bytes + place) - skip * a.D * 2,
+                           left + skip > 0 ? (unsigned)((left + skip) * a.D * 2) : 0u);
         };
-        const int j = item_of(u, y);
-        if (two_pages) {
-          if (lane < 32) part(ids[x][0], j, 8, 0);
-          else part(ids[x][1], j + 8, 8, 8);
+        const unsigned* off = kind ? voff : koff;
+        const unsigned to = at + (kind ? Sh::KB : 0);
+        if (!short_pages) {
+          const u32x4 b = page(ids[kind][0], j, MINE, 0);
+#pragma unroll
+          for (int x = 0; x < RPW; ++x) buffer_to_lds16(b, off[x], to + x * 1024);
+        } else if constexpr (Sh::RPI > 8) {   // both pages in one request: each half of the lanes from its own
+          if (lane < 32) buffer_to_lds16(page(ids[kind][0], j, 8, 0), off[0], to);
+          else buffer_to_lds16(page(ids[kind][1], j + 8, 8, 8), off[0], to);
         } else {
-          part(ids[x][0], j, Sh::RPI, 0);
+          const u32x4 b0 = page(ids[kind][0], j, 8, 0), b1 = page(ids[kind][1], j + 8, 8, 8);
+#pragma unroll
+          for (int x = 0; x < RPW; ++x) buffer_to_lds16(x * Sh::RPI < 8 ? b0 : b1, off[x], to + x * 1024);
         }
       }
     } else {
-      const int tk = (u + 1) * 32, tv = u * 32;
-      const size_t ik = (size_t)(cr.first + tk), iv = (size_t)(cr.first + (tv < 0 ? 0 : tv));
+      const int tk = u < 0 ? 0 : u * TI + 32, tv = u < 0 ? 0 : u * TI;
       int kl = end - tk, vl = u < 0 ? 0 : end - tv;
-      kl = kl < 32 ? kl : 32;
-      vl = vl < 32 ? vl : 32;
-      const u32x4 kb = buffer_of(a.k + ik * a.kp + (size_t)hk * a.D, kl > 0 ? (unsigned)(((kl - 1) * (int)a.kp + a.D) * 2) : 0u);
-      const u32x4 vb = buffer_of(a.v + iv * a.vp + (size_t)hk * a.D, vl > 0 ? (unsigned)(((vl - 1) * (int)a.vp + a.D) * 2) : 0u);
+      kl = kl < TI ? kl : TI;
+      vl = vl < TI ? vl : TI;
+      const u32x4 kb = buffer_of(a.k + (size_t)(cr.first + tk) * a.kp + (size_t)hk * a.D, kl > 0 ? (unsigned)(((kl - 1) * (int)a.kp + a.D) * 2) : 0u);
+      const u32x4 vb = buffer_of(a.v + (size_t)(cr.first + tv) * a.vp + (size_t)hk * a.D, vl > 0 ? (unsigned)(((vl - 1) * (int)a.vp + a.D) * 2) : 0u);
 #pragma unroll
       for (int x = 0; x < RPW; ++x) {
-        const int y = wave + x * NW;
-        if constexpr (Sh::GROUPS % NW == 0) {   // (a request's kind is known at compile time)
-          if (x * NW < Sh::GROUPS) buffer_to_lds16(kb, off[x], at + y * 1024);
-          else buffer_to_lds16(vb, off[x], at + y * 1024);
-        } else {
-          const u32x4 b = y < Sh::GROUPS ? kb : vb;
-          buffer_to_lds16(u32x4{(unsigned)__builtin_amdgcn_readfirstlane(b[0]), (unsigned)__builtin_amdgcn_readfirstlane(b[1]),
-                                (unsigned)__builtin_amdgcn_readfirstlane(b[2]), b[3]}, off[x], at + y * 1024);
-        }
+        buffer_to_lds16(kb, koff[x], at + x * 1024);
+        buffer_to_lds16(vb, voff[x], at + Sh::KB + x * 1024);
       }
     }
   };
-  int asked = -1, in = SLOTS - 1;   // pairs asked for: up to this one; the slot of the next
+  int asked = -1, in = SLOTS - 1;   // the next pair to ask for, and its slot
   auto request = [&]() __attribute__((always_inline)) {
     fetch(asked, lds + in * Sh::SLOT);
     in = in + 1 == SLOTS ? 0 : in + 1;
     ++asked;
     look_up(asked);
   };
-  const int requests = two_pages ? 2 * RPW : RPW;
-  if (blocks > 0) {
+  const int requests = short_pages && Sh::RPI > 8 ? 4 * RPW : 2 * RPW;
+  if (turns > 0) {
     look_up(-1);
-    for (int x = 0; x < SLOTS && x <= blocks; ++x) request();   // pairs -1 .. SLOTS - 2 (asked is one past them from here on)
+    for (int x = 0; x < SLOTS && x <= turns; ++x) request();   // pairs -1 .. SLOTS - 2
   }
 
   // this lane's rows and the last item each sees
@@ -186,7 +184,7 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
   bool whole_pages = true;
   if constexpr (PAGED) {
     bool bad = false;
-    if (blocks > 0)
+    if (turns > 0)
       for (int x = (begin >> a.log2) + lane; x <= (end - 1) >> a.log2; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
     whole_pages = __ballot(bad) == 0;
   }
@@ -211,15 +209,15 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     for (int db = 0; db < DB; ++db) vf[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   const TileReader<DP> read(lane);
 
-  auto read_k = [&](unsigned at) __attribute__((always_inline)) {
+  auto read_k = [&](unsigned at, int half) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = read.rows(at, 0, s);
+    for (int s = 0; s < KS; ++s) kf[s] = read.rows(at, half, s);
   };
-  auto read_v = [&](unsigned at) __attribute__((always_inline)) {
+  auto read_v = [&](unsigned at, int half) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(at + Sh::KB, s, db);
+      for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(at + Sh::KB, half * 2 + s, db);
   };
   auto scores = [&](f32x16* sc) __attribute__((always_inline)) {
 #pragma unroll
@@ -296,44 +294,42 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     }
   };
 
-  // Block u: its scores are there, those of the next are made behind its exponentials, the last one's sum of values behind its maximum
-  int u = 0, out = 0;
-  auto turn = [&](f32x16* sc, f32x16* next) __attribute__((always_inline)) {
-    wait_vm((asked - u - 1) * requests);
-    barrier_lds();   // pair u is there, and every wave is through with the one before, whose slot is asked for again
-    if (asked < blocks) request();
-    const unsigned at = lds + out * Sh::SLOT;
-    out = out + 1 == SLOTS ? 0 : out + 1;
-    const int t0 = begin + u * 32;
-    if (t0 <= wave_last) {
-      read_k(at);
-      __builtin_amdgcn_sched_barrier(0);
-      values();
-      raise(sc);
-      __builtin_amdgcn_sched_barrier(0);
-      read_v(at);
-      scores(next);
-      weigh(sc);
+  // A block of 32 items, half of a tile: its scores are there, those of the next block are made behind its exponentials, the last
+  // block's sum of values behind its maximum
+  auto block = [&](f32x16* sc, f32x16* next, int t0, unsigned at, int half) __attribute__((always_inline)) {
+    read_k(at, half);
+    __builtin_amdgcn_sched_barrier(0);
+    values();
+    raise(sc);
+    __builtin_amdgcn_sched_barrier(0);
+    read_v(at, half);
+    scores(next);
+    weigh(sc);
 #pragma unroll
-      for (int x = 0; x < KS * RB; ++x) {   // one product, then its share of the exponentials and of the reads behind it
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / (KS * RB) > 0 ? 4 * DB / (KS * RB) : 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      mask(next, t0 + 32);
+    for (int x = 0; x < KS * RB; ++x) {   // one product, then its share of the reads and of the exponentials
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / (KS * RB) > 0 ? 4 * DB / (KS * RB) : 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
     }
-    ++u;
+    __builtin_amdgcn_sched_barrier(0);
+    mask(next, t0 + 32);
   };
-  if (blocks > 0) {
-    wait_vm((asked < 0 ? 0 : asked) * requests);
+  if (turns > 0) {
+    wait_vm(asked * requests);
     barrier_lds();
-    read_k(lds + (SLOTS - 1) * Sh::SLOT);
+    read_k(lds + (SLOTS - 1) * Sh::SLOT, 0);
     scores(sa);
     mask(sa, begin);
-    while (u < blocks) {
-      turn(sa, sb);
-      if (u < blocks) turn(sb, sa);
+    int out = 0;
+    for (int u = 0; u < turns; ++u) {
+      wait_vm((asked - u - 1) * requests);
+      barrier_lds();   // pair u is there, and every wave is through with the one before, whose slot is asked for again
+      if (asked < turns) request();
+      const unsigned at = lds + out * Sh::SLOT;
+      out = out + 1 == SLOTS ? 0 : out + 1;
+      const int t0 = begin + u * TI;
+      if (t0 <= wave_last) block(sa, sb, t0, at, 0);
+      if (t0 + 32 <= wave_last) block(sb, sa, t0 + 32, at, 1);
     }
     values();
     barrier_lds();
@@ -387,14 +383,14 @@ template <bool PAGED>
 static laser_status tile_launch_any(const TileArgs& a, hipStream_t stream) {
   const int form = tuning_int("LASER_HIST_FORM", 0);
   if (a.D > 64) {
-    if (form == 1) return tile_launch<128, 8, 1, 4, PAGED>(a, stream);
-    if (form == 2) return tile_launch<128, 4, 2, 4, PAGED>(a, stream);
-    return tile_launch<128, 4, 1, 4, PAGED>(a, stream);
+    if (form == 1) return tile_launch<128, 8, 1, 3, PAGED>(a, stream);
+    if (form == 2) return tile_launch<128, 4, 2, 3, PAGED>(a, stream);
+    return tile_launch<128, 4, 1, 2, PAGED>(a, stream);
   }
   if (a.D > 32) {
-    if (form == 1) return tile_launch<64, 8, 1, 4, PAGED>(a, stream);
-    if (form == 2) return tile_launch<64, 4, 2, 4, PAGED>(a, stream);
-    return tile_launch<64, 4, 1, 4, PAGED>(a, stream);
+    if (form == 1) return tile_launch<64, 8, 1, 3, PAGED>(a, stream);
+    if (form == 2) return tile_launch<64, 4, 2, 3, PAGED>(a, stream);
+    return tile_launch<64, 4, 1, 3, PAGED>(a, stream);
   }
   return tile_launch<32, 4, 1, 4, PAGED>(a, stream);
 }
