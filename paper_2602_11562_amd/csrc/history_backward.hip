@@ -79,47 +79,69 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
   const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
 
-  f32x16 acc[DB];
+  f32x16 acc[DB], sc, dp;
+  unsigned ds[8];
+  bf16x8 frag[KS], kt[2][DB];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = zero;
-
+  sc = dp = zero;   // (p of the block before the first: nothing)
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) kt[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   const TileReader<DP> read(lane);
-  auto step = [&](int t0, unsigned at, auto masked) __attribute__((always_inline)) {
+
+  // ds of the block whose p and dp are there (p stands in sc's place)
+  auto form_ds = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib) {
-      f32x16 sc, dp;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, ib, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at + Sh::BYTES, ib, s), greg[s], s == 0 ? zero : dp, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      unsigned ds[8];
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        float x[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[r + e], a.scale, -lse2));
-          x[e] = p * (dp[r + e] - delta);
-          if (decltype(masked)::value && t0 + ib * 32 + 8 * (r >> 2) + 4 * h + (r & 3) + e > last) x[e] = 0.0f;
-        }
-        ds[r >> 1] = pack_bf16(x[0], x[1]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const u32x4 b = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at, ib * 2 + s, db), __builtin_bit_cast(bf16x8, b),
-                                                            acc[db], 0, 0, 0);
-        }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int r = 0; r < 16; r += 2) {
+      ds[r >> 1] = pack_bf16(sc[r] * (dp[r] - delta), sc[r + 1] * (dp[r + 1] - delta));
+      asm volatile("" : "+v"(ds[r >> 1]));
     }
+  };
+  auto add_dq = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 b = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt[s][db], __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
+      }
+  };
+  // A block of 32 items: its scores, then the last block's share of dq behind its exponentials, then its dp
+  auto block = [&](int t0, unsigned at, int ib) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) frag[s] = read.rows(at, ib, s);
+    form_ds();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s], qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) frag[s] = read.rows(at + Sh::BYTES, ib, s);
+    __builtin_amdgcn_sched_barrier(0);
+    add_dq();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -lse2));
+#pragma unroll
+    for (int x = 0; x < 2 * DB; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 16 / DB, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (t0 + 31 > wave_first) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t0 + 8 * (r >> 2) + 4 * h + (r & 3) > last) sc[r] = 0.0f;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s], greg[s], s == 0 ? zero : dp, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) kt[s][db] = read.cols(at, ib * 2 + s, db);
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   PackedTiles<DP, NW> tiles;
@@ -134,14 +156,14 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     barrier_lds();
     if (t0 + TI < end) fetch(t0 + TI, other);
-    if (t0 <= wave_last) {
-      if (t0 + TI - 1 <= wave_first) step(t0, at, std::false_type{});
-      else step(t0, at, std::true_type{});
-    }
+    if (t0 <= wave_last) block(t0, at, 0);
+    if (t0 + 32 <= wave_last) block(t0 + 32, at, 1);
     const unsigned x = at;
     at = other;
     other = x;
   }
+  form_ds();
+  add_dq();
   barrier_lds();
   store_block<DP>(acc, a.inv_gamma, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
     const int i = (int)a.by_group.div(first + r), head = hk * a.G + first + r - i * a.G;
@@ -153,8 +175,8 @@ template <int DP, int NW>
 __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel(const BwdArgs a) {
   using Sh = TileShape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32, ITEMS = NW * 32, OP = DP * 2 + 16, GPW = (Sh::GROUPS + NW - 1) / NW;
-  constexpr int STAGE = 2 * Sh::BYTES + 2 * TI * 4, PATCH = NW * 32 * OP;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
+  constexpr int STAGE = 2 * Sh::BYTES + 1024, PATCH = NW * 32 * OP, SLOTS = 3;   // (1024: lse and delta, and whole lines)
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * STAGE > PATCH ? SLOTS * STAGE : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const int per = a.N * a.Hkv;
   const int tile = (int)(blockIdx.x / per), nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
@@ -209,73 +231,147 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
     }
   };
 
-  f32x16 dk[DB], dv[DB];
+  f32x16 dk[DB], dv[DB], sa, pa, sb, pb;   // (scores and dp of a block and of the next)
+  unsigned p[8], ds[8];
+  bf16x8 qf[KS], gf[KS], cols[2][DB];
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4 z[4], d[4];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = zero;
-
   const TileReader<DP> read(lane);
-  auto step = [&](int r0, unsigned at, auto masked) __attribute__((always_inline)) {
+
+  auto read_rows = [&](unsigned at, int rb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      f32x16 sc, dp;
+    for (int s = 0; s < KS; ++s) qf[s] = read.rows(at, rb, s);
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, rb, s), kreg[s], s == 0 ? zero : sc, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int s = 0; s < KS; ++s) gf[s] = read.rows(at + Sh::BYTES, rb, s);
+  };
+  auto read_cols = [&](unsigned at, int rb) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at + Sh::BYTES, rb, s), vreg[s], s == 0 ? zero : dp, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      unsigned p[8], ds[8];
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        typedef float f32x4 __attribute__((ext_vector_type(4)));
-        const unsigned where = at + 2 * Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4;
-        const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
-        const f32x4 d = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + TI * 4));
-        float pv[4], dv4[4];
+      for (int db = 0; db < DB; ++db) cols[s][db] = read.cols(at, rb * 2 + s, db);
+  };
+  auto scores = [&](f32x16& sc) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pv[e] = __builtin_amdgcn_exp2f(fmaf(sc[g * 4 + e], a.scale, -z[e] * LOG2E));
-          if (decltype(masked)::value && r0 + rb * 32 + g * 8 + h * 4 + e < from) pv[e] = 0.0f;
-          dv4[e] = pv[e] * (dp[g * 4 + e] - d[e]);
-        }
-        p[g * 2] = pack_bf16(pv[0], pv[1]);
-        p[g * 2 + 1] = pack_bf16(pv[2], pv[3]);
-        ds[g * 2] = pack_bf16(dv4[0], dv4[1]);
-        ds[g * 2 + 1] = pack_bf16(dv4[2], dv4[3]);
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[s], kreg[s], s == 0 ? zero : sc, 0, 0, 0);
+  };
+  auto slopes = [&](f32x16& dp) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gf[s], vreg[s], s == 0 ? zero : dp, 0, 0, 0);
+  };
+  auto add = [&](f32x16* to, const unsigned* w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 b = {w[s * 4], w[s * 4 + 1], w[s * 4 + 2], w[s * 4 + 3]};
+        to[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols[s][db], __builtin_bit_cast(bf16x8, b), to[db], 0, 0, 0);
       }
-      __builtin_amdgcn_sched_barrier(0);
+  };
+  // A block of 32 rows whose scores and dp are there; those of the next block (at next_at) are made behind its exponentials and behind its
+  // ds, then it enters dv and dk
+  auto block = [&](f32x16& sc, f32x16& dp, f32x16& next_sc, f32x16& next_dp, int r0, unsigned at, int rb, unsigned next_at,
+                   int next_rb) __attribute__((always_inline)) {
+    read_rows(next_at, next_rb);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const u32x4 pb = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
-          const u32x4 sb = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
-          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at + Sh::BYTES, rb * 2 + s, db),
-                                                           __builtin_bit_cast(bf16x8, pb), dv[db], 0, 0, 0);
-          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at, rb * 2 + s, db),
-                                                           __builtin_bit_cast(bf16x8, sb), dk[db], 0, 0, 0);
-        }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int g = 0; g < 4; ++g) {
+      const unsigned where = at + 2 * Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4;
+      z[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
+      d[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + TI * 4));
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (r0 < wave_to) {   // rows that do not see all of the wave's items: -inf where they do not
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (r0 + 8 * (r >> 2) + 4 * h + (r & 3) < from) sc[r] = -INFINITY;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -LOG2E * z[r >> 2][r & 3]));
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      p[r] = pack_bf16(sc[2 * r], sc[2 * r + 1]);
+      asm volatile("" : "+v"(p[r]));
+    }
+    scores(next_sc);
+    read_cols(at + Sh::BYTES, rb);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    add(dv, p);
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      ds[r >> 1] = pack_bf16(sc[r] * (dp[r] - d[r >> 2][r & 3]), sc[r + 1] * (dp[r + 1] - d[r >> 2][(r & 3) + 1]));
+      asm volatile("" : "+v"(ds[r >> 1]));
+    }
+#pragma unroll
+    for (int x = 0; x < 2 * DB; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 24 / DB, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    slopes(next_dp);
+    read_cols(at, rb);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    add(dk, ds);
   };
 
   const int start = item0 * a.G / TI * TI;   // (rows before it see no item of this workgroup)
-  fetch(start, lds);
-  unsigned at = lds, other = lds + STAGE;
-  for (int r0 = start; r0 < rows; r0 += TI) {
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    barrier_lds();
-    if (r0 + TI < rows) fetch(r0 + TI, other);
-    if (first < n && r0 + TI > wave_from) {
-      if (r0 >= wave_to) step(r0, at, std::false_type{});
-      else step(r0, at, std::true_type{});
+  const int turns = (rows - start + TI - 1) / TI;
+  const int requests = 2 * GPW + (wave < 2 ? 1 : 0);
+  int asked = 0, slot = 0;
+  auto request = [&]() __attribute__((always_inline)) {
+    fetch(start + asked * TI, lds + slot * STAGE);
+    slot = slot + 1 == SLOTS ? 0 : slot + 1;
+    ++asked;
+  };
+  auto starts = [&](int r0) { return first < n && r0 + 32 > wave_from; };   // do the rows of a block see an item of the wave?
+  request();
+  if (turns > 1) request();
+  wait_vm((asked - 1) * requests);
+  barrier_lds();
+  if (starts(start)) {
+    read_rows(lds, 0);
+    scores(sa);
+    slopes(pa);
+  }
+  unsigned at = lds;
+  int out = 0;
+  for (int t = 0; t < turns; ++t) {
+    const int r0 = start + t * TI;
+    if (starts(r0)) {
+      block(sa, pa, sb, pb, r0, at, 0, at, 1);
+    } else if (starts(r0 + 32)) {
+      read_rows(at, 1);
+      scores(sb);
+      slopes(pb);
     }
-    const unsigned x = at;
-    at = other;
-    other = x;
+    out = out + 1 == SLOTS ? 0 : out + 1;
+    const unsigned next = lds + out * STAGE;
+    if (t + 1 < turns) {
+      wait_vm((asked - t - 2) * requests);
+      barrier_lds();   // tile t + 1 is there, and every wave is through with tile t - 1, whose slot is asked for again
+      if (asked < turns) request();
+    }
+    if (starts(r0 + 32)) {
+      block(sb, pb, sa, pa, r0 + 32, at, 1, t + 1 < turns ? next : at, 0);
+    } else if (t + 1 < turns && starts(r0 + TI)) {
+      read_rows(next, 0);
+      scores(sa);
+      slopes(pa);
+    }
+    at = next;
   }
   barrier_lds();
   unsigned char* patch = smem + wave * 32 * OP;
