@@ -117,17 +117,18 @@ __global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, in
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = zero;
   float m = -INFINITY, l = 0.0f;
-  const TileReader<DP> read(lane);
+  TileReader<DP> read(lane);
 
   for (; mine < hi; mine += step_items) {
     // loads return in order: with `pending` tiles asked for, the oldest is there when those of the others are all that is left
     wait_vm((pending - 1) * requests);
     asm volatile("" ::: "memory");
     const unsigned at = lds + slot_out * 2 * Sh::TILE;
+    read.place(at);
     f32x16 sc;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, 0, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(0, 0, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
     if (!whole_pages || mine + 31 > first_seen || mine + 32 > hi) {
       const int left = hi - mine;
       bool in = l32 < left;
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, in
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const u32x4 b = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(at + Sh::TILE, s, db), __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(Sh::TILE, s, db), __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again
     --pending;

@@ -60,17 +60,18 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
                      at + Sh::BYTES);
     }
   };
-  const TileReader<DP> read(lane);
+  TileReader<DP> read(lane);
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   bf16x8 kreg[KS];
   float sum = 0.0f;
   auto step = [&](int r0, unsigned at, auto masked) __attribute__((always_inline)) {
+    read.place_rows(at);
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       if (decltype(masked)::value && (r0 + rb * 32 >= rows || r0 + rb * 32 + 32 <= wave_from)) continue;
       f32x16 sc;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(at, rb, s), kreg[s], s == 0 ? zero : sc, 0, 0, 0);
+      for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(0, rb, s), kreg[s], s == 0 ? zero : sc, 0, 0, 0);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(at + Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4));

@@ -22,11 +22,12 @@ struct BwdArgs {
   const unsigned short* go;
   long long qp, kp, vp;
   const int32_t* off;
-  int N, T, L, H, Hkv, D, G, tiles;
+  int N, T, L, H, Hkv, D, G;
   MulDiv by_group;       // / G
+  Deal deal;
   float scale, inv_gamma;   // log2(e) / gamma, 1 / gamma
   const float* lse;
-  float* delta;          // [T,H]
+  float* rows;           // [2,T,H]: -lse log2(e) and delta, by the first kernel for the second
   unsigned short* dq;
   unsigned short* dk;
   unsigned short* dv;
@@ -39,8 +40,10 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
   constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * 32, OP = DP * 2 + 16, STAGE = 2 * Sh::BYTES, PATCH = NW * 32 * OP;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
-  const int per = a.N * a.Hkv;
-  const int tile = a.tiles - 1 - (int)(blockIdx.x / per), nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  const int tile = a.deal.tiles - 1 - place.rank;   // (the longest first)
+  const int n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
@@ -74,33 +77,57 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     }
     delta = half_sum(sum);
     lse2 = a.lse[tok * a.H + head] * LOG2E;
-    if (h == 0 && first + l32 < rows) a.delta[tok * a.H + head] = delta;
+    if (h == 0 && first + l32 < rows) {
+      a.rows[tok * a.H + head] = -lse2;
+      a.rows[((size_t)a.T + tok) * a.H + head] = delta;
+    }
   }
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
   const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
 
-  f32x16 acc[DB], sc, dp;
-  unsigned ds[8];
-  bf16x8 frag[KS], kt[2][DB];
+  f32x16 acc[DB];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = zero;
-  sc = dp = zero;   // (p of the block before the first: nothing)
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int db = 0; db < DB; ++db) kt[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-  const TileReader<DP> read(lane);
+  TileReader<DP> read(lane);
 
-  // ds of the block whose p and dp are there (p stands in sc's place)
-  auto form_ds = [&]() __attribute__((always_inline)) {
+  // A block of 32 items: scores, dp behind which the exponentials are made, then its share of dq. What is left without a product
+  // beside it is the other wave's time.
+  auto block = [&](int t0, int ib) __attribute__((always_inline)) {
+    f32x16 sc, dp;
+    unsigned ds[8];
+    bf16x8 kf[KS], vf[KS];
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      ds[r >> 1] = pack_bf16(sc[r] * (dp[r] - delta), sc[r + 1] * (dp[r + 1] - delta));
-      asm volatile("" : "+v"(ds[r >> 1]));
+    for (int s = 0; s < KS; ++s) kf[s] = read.rows(0, ib, s);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) vf[s] = read.rows(Sh::BYTES, ib, s);
+    __builtin_amdgcn_sched_barrier(0);
+    if (t0 + 31 > wave_first) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t0 + 8 * (r >> 2) + 4 * h + (r & 3) > last) sc[r] = -INFINITY;
     }
-  };
-  auto add_dq = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s], greg[s], s == 0 ? zero : dp, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -lse2));
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 32 / KS, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 kt[2][DB];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) kt[s][db] = read.cols(0, ib * 2 + s, db);
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) ds[r >> 1] = pack_bf16(sc[r] * (dp[r] - delta), sc[r + 1] * (dp[r + 1] - delta));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -108,40 +135,6 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
         const u32x4 b = {ds[s * 4], ds[s * 4 + 1], ds[s * 4 + 2], ds[s * 4 + 3]};
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt[s][db], __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
       }
-  };
-  // A block of 32 items: its scores, then the last block's share of dq behind its exponentials, then its dp
-  auto block = [&](int t0, unsigned at, int ib) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) frag[s] = read.rows(at, ib, s);
-    form_ds();
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s], qreg[s], s == 0 ? zero : sc, 0, 0, 0);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) frag[s] = read.rows(at + Sh::BYTES, ib, s);
-    __builtin_amdgcn_sched_barrier(0);
-    add_dq();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -lse2));
-#pragma unroll
-    for (int x = 0; x < 2 * DB; ++x) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 16 / DB, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (t0 + 31 > wave_first) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (t0 + 8 * (r >> 2) + 4 * h + (r & 3) > last) sc[r] = 0.0f;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s], greg[s], s == 0 ? zero : dp, 0, 0, 0);
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) kt[s][db] = read.cols(at, ib * 2 + s, db);
-    __builtin_amdgcn_sched_barrier(0);
   };
 
   PackedTiles<DP, NW> tiles;
@@ -156,14 +149,13 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     barrier_lds();
     if (t0 + TI < end) fetch(t0 + TI, other);
-    if (t0 <= wave_last) block(t0, at, 0);
-    if (t0 + 32 <= wave_last) block(t0 + 32, at, 1);
+    read.place(at);
+    if (t0 <= wave_last) block(t0, 0);
+    if (t0 + 32 <= wave_last) block(t0 + 32, 1);
     const unsigned x = at;
     at = other;
     other = x;
   }
-  form_ds();
-  add_dq();
   barrier_lds();
   store_block<DP>(acc, a.inv_gamma, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
     const int i = (int)a.by_group.div(first + r), head = hk * a.G + first + r - i * a.G;
@@ -178,8 +170,9 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
   constexpr int STAGE = 2 * Sh::BYTES + 1024, PATCH = NW * 32 * OP, SLOTS = 3;   // (1024: lse and delta, and whole lines)
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * STAGE > PATCH ? SLOTS * STAGE : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
-  const int per = a.N * a.Hkv;
-  const int tile = (int)(blockIdx.x / per), nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  const int tile = place.rank, n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;   // (the first items have the most rows)
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, item0 = tile * ITEMS;
   if (item0 >= n) return;
@@ -207,28 +200,40 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
   }
   const int wave_from = __builtin_amdgcn_readlane(from, 0), wave_to = __builtin_amdgcn_readlane(from, 31);
 
-  // tiles of rows: queries, behind them d_o, behind them lse and delta; rows behind the last read as zeros and add nothing
+  // tiles of rows: queries, behind them d_o, behind them -lse log2(e) and delta; rows behind the last read as zeros and add nothing. Where a
+  // tile is a whole number of tokens, a lane's offsets are the same in every tile.
+  const bool whole_tokens = TI % a.G == 0;
+  const int head0 = hk * a.G;
+  unsigned qoff[GPW], goff[GPW], soff;
+  auto offsets = [&](int r0, int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int in = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
+      const int i = (int)a.by_group.div(r), head = r - i * a.G, tk = i - i0;
+      qoff[x] = c * 8 < a.D ? (unsigned)((tk * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN;
+      goff[x] = c * 8 < a.D ? (unsigned)(((tk * a.H + head) * a.D + c * 8) * 2) : NO_COLUMN;
+    }
+    const int r = r0 + lane, i = (int)a.by_group.div(r);
+    soff = (unsigned)((i - i0) * a.H + r - i * a.G) * 4;
+  };
+  if (whole_tokens) offsets(0, 0);
   auto fetch = [&](int r0, unsigned at) __attribute__((always_inline)) {
     const int i0 = (int)a.by_group.div(r0);
-    const size_t tok = (size_t)cr.first + i0, head0 = (size_t)hk * a.G;
-    const u32x4 qb = buffer_of(a.q + tok * a.qp + head0 * a.D, 0x7fffffffu);
-    const u32x4 gb = buffer_of(a.go + (tok * a.H + head0) * a.D, 0x7fffffffu);
+    if (!whole_tokens) offsets(r0, i0);
+    const size_t tok = (size_t)cr.first + i0;
+    const int more = n - 1 - i0 < TI ? n - 1 - i0 : TI;   // whole tokens within reach behind the first
+    const u32x4 qb = buffer_of(a.q + tok * a.qp + (size_t)head0 * a.D, (unsigned)((more * (int)a.qp + a.G * a.D) * 2));
+    const u32x4 gb = buffer_of(a.go + (tok * a.H + head0) * a.D, (unsigned)((more * a.H + a.G) * a.D * 2));
 #pragma unroll
     for (int x = 0; x < GPW; ++x) {
       const int g = wave + x * NW;
       if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-      const int in = g * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
-      const int i = (int)a.by_group.div(r), head = r - i * a.G;
-      const bool ok = r < rows && c * 8 < a.D;
-      const int tk = i - i0;
-      buffer_to_lds16(qb, ok ? (unsigned)((tk * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN, at + g * 1024);
-      buffer_to_lds16(gb, ok ? (unsigned)(((tk * a.H + head) * a.D + c * 8) * 2) : NO_COLUMN, at + Sh::BYTES + g * 1024);
+      buffer_to_lds16(qb, qoff[x], at + g * 1024);
+      buffer_to_lds16(gb, goff[x], at + Sh::BYTES + g * 1024);
     }
-    if (wave < 2) {
-      const int r = r0 + lane, i = (int)a.by_group.div(r), head = r - i * a.G;
-      const u32x4 b = buffer_of((wave == 0 ? a.lse : a.delta) + tok * a.H + head0, 0x7fffffffu);
-      buffer_to_lds4(b, r < rows ? (unsigned)((i - i0) * a.H + head) * 4 : NO_COLUMN, at + 2 * Sh::BYTES + wave * TI * 4);
-    }
+    if (wave < 2)
+      buffer_to_lds4(buffer_of(a.rows + ((size_t)wave * a.T + tok) * a.H + head0, (unsigned)(more * a.H + a.G) * 4), soff,
+                     at + 2 * Sh::BYTES + wave * TI * 4);
   };
 
   f32x16 dk[DB], dv[DB], sa, pa, sb, pb;   // (scores and dp of a block and of the next)
@@ -239,19 +244,19 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = zero;
-  const TileReader<DP> read(lane);
+  TileReader<DP> read(lane);
 
-  auto read_rows = [&](unsigned at, int rb) __attribute__((always_inline)) {
+  auto read_rows = [&](int rb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = read.rows(at, rb, s);
+    for (int s = 0; s < KS; ++s) qf[s] = read.rows(0, rb, s);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) gf[s] = read.rows(at + Sh::BYTES, rb, s);
+    for (int s = 0; s < KS; ++s) gf[s] = read.rows(Sh::BYTES, rb, s);
   };
-  auto read_cols = [&](unsigned at, int rb) __attribute__((always_inline)) {
+  auto read_cols = [&](int more, int rb) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) cols[s][db] = read.cols(at, rb * 2 + s, db);
+      for (int db = 0; db < DB; ++db) cols[s][db] = read.cols(more, rb * 2 + s, db);
   };
   auto scores = [&](f32x16& sc) __attribute__((always_inline)) {
 #pragma unroll
@@ -270,17 +275,18 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
         to[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols[s][db], __builtin_bit_cast(bf16x8, b), to[db], 0, 0, 0);
       }
   };
-  // A block of 32 rows whose scores and dp are there; those of the next block (at next_at) are made behind its exponentials and behind its
+  // A block of 32 rows whose scores and dp are there; those of the next block (rows_at, next_rb) are made behind its exponentials and behind its
   // ds, then it enters dv and dk
-  auto block = [&](f32x16& sc, f32x16& dp, f32x16& next_sc, f32x16& next_dp, int r0, unsigned at, int rb, unsigned next_at,
+  auto block = [&](f32x16& sc, f32x16& dp, f32x16& next_sc, f32x16& next_dp, int r0, unsigned at, int rb,
                    int next_rb) __attribute__((always_inline)) {
-    read_rows(next_at, next_rb);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const unsigned where = at + 2 * Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4;
       z[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
       d[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + TI * 4));
     }
+    __builtin_amdgcn_sched_barrier(0);
+    read_rows(next_rb);
     __builtin_amdgcn_sched_barrier(0);
     if (r0 < wave_to) {   // rows that do not see all of the wave's items: -inf where they do not
 #pragma unroll
@@ -289,14 +295,14 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -LOG2E * z[r >> 2][r & 3]));
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, z[r >> 2][r & 3]));
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
       p[r] = pack_bf16(sc[2 * r], sc[2 * r + 1]);
       asm volatile("" : "+v"(p[r]));
     }
     scores(next_sc);
-    read_cols(at + Sh::BYTES, rb);
+    read_cols(Sh::BYTES, rb);
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -317,7 +323,7 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
     }
     __builtin_amdgcn_sched_barrier(0);
     slopes(next_dp);
-    read_cols(at, rb);
+    read_cols(0, rb);
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -327,50 +333,44 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
     add(dk, ds);
   };
 
+  // From the last rows to the first that see an item: what runs beside this workgroup on the die then reads the same rows at about the
+  // same time, wherever its own items begin.
   const int start = item0 * a.G / TI * TI;   // (rows before it see no item of this workgroup)
   const int turns = (rows - start + TI - 1) / TI;
   const int requests = 2 * GPW + (wave < 2 ? 1 : 0);
   int asked = 0, slot = 0;
+  auto row_of = [&](int t) { return start + (turns - 1 - t) * TI; };
   auto request = [&]() __attribute__((always_inline)) {
-    fetch(start + asked * TI, lds + slot * STAGE);
+    fetch(row_of(asked), lds + slot * STAGE);
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
     ++asked;
   };
-  auto starts = [&](int r0) { return first < n && r0 + 32 > wave_from; };   // do the rows of a block see an item of the wave?
+  const int floor = first < n ? wave_from - 32 : 0x7fffffff;   // blocks of rows from above this on see an item of the wave
   request();
   if (turns > 1) request();
   wait_vm((asked - 1) * requests);
   barrier_lds();
-  if (starts(start)) {
-    read_rows(lds, 0);
+  if (row_of(0) + 32 > floor) {
+    read.place_rows(lds);
+    read_rows(1);
     scores(sa);
     slopes(pa);
   }
   unsigned at = lds;
   int out = 0;
   for (int t = 0; t < turns; ++t) {
-    const int r0 = start + t * TI;
-    if (starts(r0)) {
-      block(sa, pa, sb, pb, r0, at, 0, at, 1);
-    } else if (starts(r0 + 32)) {
-      read_rows(at, 1);
-      scores(sb);
-      slopes(pb);
-    }
+    const int r0 = row_of(t);
+    read.place_cols(at);   // (its rows were placed by the turn before)
+    if (r0 + 32 > floor) block(sa, pa, sb, pb, r0 + 32, at, 1, 0);
     out = out + 1 == SLOTS ? 0 : out + 1;
-    const unsigned next = lds + out * STAGE;
+    const unsigned next = t + 1 < turns ? lds + out * STAGE : at;
     if (t + 1 < turns) {
       wait_vm((asked - t - 2) * requests);
       barrier_lds();   // tile t + 1 is there, and every wave is through with tile t - 1, whose slot is asked for again
       if (asked < turns) request();
     }
-    if (starts(r0 + 32)) {
-      block(sb, pb, sa, pa, r0 + 32, at, 1, t + 1 < turns ? next : at, 0);
-    } else if (t + 1 < turns && starts(r0 + TI)) {
-      read_rows(next, 0);
-      scores(sa);
-      slopes(pa);
-    }
+    read.place_rows(next);
+    if (r0 > floor) block(sb, pb, sa, pa, r0, at, 0, 1);
     at = next;
   }
   barrier_lds();
@@ -386,10 +386,10 @@ static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
   constexpr int NW = 4;
   const long long per = (long long)a.N * a.Hkv;
   const long long row_tiles = ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), item_tiles = ((long long)a.L + NW * 32 - 1) / (NW * 32);
-  if (per * row_tiles > 0x7fffffffLL) return LASER_ERR_SHAPE;
-  a.tiles = (int)row_tiles;
-  history_dq_kernel<DP, NW><<<(unsigned)(per * row_tiles), 64 * NW, 0, stream>>>(a);
-  history_dkv_kernel<DP, NW><<<(unsigned)(per * item_tiles), 64 * NW, 0, stream>>>(a);
+  BwdArgs b = a;
+  if (!deal(per, row_tiles, &a.deal) || !deal(per, item_tiles, &b.deal)) return LASER_ERR_SHAPE;
+  history_dq_kernel<DP, NW><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
+  history_dkv_kernel<DP, NW><<<b.deal.grid, 64 * NW, 0, stream>>>(b);
   return launch_status();
 }
 
@@ -408,7 +408,7 @@ laser_status history_bwd_tile_launch(const HistoryBwdArgs& b) {
   a.scale = LOG2E / h.gamma;
   a.inv_gamma = 1.0f / h.gamma;
   a.lse = h.lse;
-  a.delta = b.work;
+  a.rows = b.work;
   a.dq = static_cast<unsigned short*>(b.dq);
   a.dk = static_cast<unsigned short*>(b.dk);
   a.dv = static_cast<unsigned short*>(b.dv);

@@ -276,7 +276,7 @@ static laser_status backward_typed(const HistoryBwdArgs& b) {
   }
   return launch_status();
 }
-size_t history_backward_work_bytes(int, int T, int, int H, int, int, laser_dtype) { return (size_t)T * H * 4; }
+size_t history_backward_work_bytes(int, int T, int, int H, int, int, laser_dtype) { return (size_t)T * H * 8; }
 laser_status history_backward_launch(const HistoryBwdArgs& a) {
   return a.f.dt == LASER_F32 ? backward_typed<float>(a) : history_bwd_tile_launch(a);
 }

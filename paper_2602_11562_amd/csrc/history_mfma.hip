@@ -24,7 +24,8 @@ struct TileArgs {
   const int32_t* lens;
   int N, T, L, C, H, Hkv, D, log2, P, max_pages;
   MulDiv by_group;       // / G
-  int G, tiles;
+  int G, tiles;          // tiles of the longest sequence's rows
+  Deal deal;             // of (tile, run) to workgroups
   float scale;           // log2(e) / gamma
   bool causal;
   unsigned short* o;
@@ -52,14 +53,15 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * Sh::SLOT > PATCH ? SLOTS * Sh::SLOT : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
 
-  const int per = a.N * a.Hkv;
-  int tile = (int)(blockIdx.x / per), run = 0;
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  int tile = place.rank, run = 0;
   if (PAGED && a.runs > 1) {
     run = tile / a.tiles;
     tile -= run * a.tiles;
   }
   tile = a.tiles - 1 - tile;   // (the longest first)
-  const int nh = spread(blockIdx.x, per), n_seq = nh / a.Hkv, hk = nh % a.Hkv;
+  const int n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
   const CandRange cr = cand_range(a.off, n_seq, a.C, a.T);
   const int rows = cr.count * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
@@ -207,17 +209,17 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
   for (int s = 0; s < 2; ++s)
 #pragma unroll
     for (int db = 0; db < DB; ++db) vf[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-  const TileReader<DP> read(lane);
+  TileReader<DP> read(lane);
 
-  auto read_k = [&](unsigned at, int half) __attribute__((always_inline)) {
+  auto read_k = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = read.rows(at, half, s);
+    for (int s = 0; s < KS; ++s) kf[s] = read.rows(0, half, s);
   };
-  auto read_v = [&](unsigned at, int half) __attribute__((always_inline)) {
+  auto read_v = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(at + Sh::KB, half * 2 + s, db);
+      for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(Sh::KB, half * 2 + s, db);
   };
   auto scores = [&](f32x16* sc) __attribute__((always_inline)) {
 #pragma unroll
@@ -296,13 +298,13 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
 
   // A block of 32 items, half of a tile: its scores are there, those of the next block are made behind its exponentials, the last
   // block's sum of values behind its maximum
-  auto block = [&](f32x16* sc, f32x16* next, int t0, unsigned at, int half) __attribute__((always_inline)) {
-    read_k(at, half);
+  auto block = [&](f32x16* sc, f32x16* next, int t0, int half) __attribute__((always_inline)) {
+    read_k(half);
     __builtin_amdgcn_sched_barrier(0);
     values();
     raise(sc);
     __builtin_amdgcn_sched_barrier(0);
-    read_v(at, half);
+    read_v(half);
     scores(next);
     weigh(sc);
 #pragma unroll
@@ -317,7 +319,8 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
   if (turns > 0) {
     wait_vm(asked * requests);
     barrier_lds();
-    read_k(lds + (SLOTS - 1) * Sh::SLOT, 0);
+    read.place_rows(lds + (SLOTS - 1) * Sh::SLOT);
+    read_k(0);
     scores(sa);
     mask(sa, begin);
     int out = 0;
@@ -325,11 +328,11 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
       wait_vm((asked - u - 1) * requests);
       barrier_lds();   // pair u is there, and every wave is through with the one before, whose slot is asked for again
       if (asked < turns) request();
-      const unsigned at = lds + out * Sh::SLOT;
+      read.place(lds + out * Sh::SLOT);
       out = out + 1 == SLOTS ? 0 : out + 1;
       const int t0 = begin + u * TI;
-      if (t0 <= wave_last) block(sa, sb, t0, at, 0);
-      if (t0 + 32 <= wave_last) block(sb, sa, t0 + 32, at, 1);
+      if (t0 <= wave_last) block(sa, sb, t0, 0);
+      if (t0 + 32 <= wave_last) block(sb, sa, t0 + 32, 1);
     }
     values();
     barrier_lds();
@@ -374,9 +377,8 @@ template <int DP, int NW, int RB, int SLOTS, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
   constexpr int ROWS = NW * RB * 32;
   a.tiles = (int)(((long long)a.C * a.G + ROWS - 1) / ROWS);
-  const long long grid = (long long)a.tiles * a.N * a.Hkv * a.runs;
-  if (grid > 0x7fffffffLL) return LASER_ERR_SHAPE;
-  history_tile_kernel<DP, NW, RB, SLOTS, PAGED><<<(unsigned)grid, 64 * NW, 0, stream>>>(a);
+  if (!deal((long long)a.N * a.Hkv, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
+  history_tile_kernel<DP, NW, RB, SLOTS, PAGED><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
   return launch_status();
 }
 template <bool PAGED>

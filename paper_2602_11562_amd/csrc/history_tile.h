@@ -22,9 +22,29 @@ __device__ __forceinline__ void buffer_to_lds16(u32x4 buf, unsigned voff, unsign
                : "memory");
 }
 
-// Which (sequence, head) of `per` a workgroup takes. Workgroups go to the eight dies in turn, so with a multiple of eight of them every
-// tile of a long sequence would land on the same die: the order is turned by one from row of tiles to row of tiles.
-__device__ __forceinline__ int spread(unsigned block, int per) { return (int)((block % per + block / per) % per); }
+// Which tile of which of `per` (sequence, head) pairs a workgroup takes. Workgroups go to the eight dies in turn, and a die's 4 MB of
+// cache serve the tiles of a pair that run on it at once. So `run` tiles of a pair in a row are one die's, and the runs are dealt to the
+// dies turned by one from row of runs to row of runs (with a multiple of eight pairs, a long sequence would otherwise be one die's).
+struct Deal {
+  int per, tiles, run;
+  MulDiv by_run, by_per;
+  unsigned grid;
+};
+inline bool deal(long long per, long long tiles, Deal* d) {
+  // (16 histories of 820 to 4100 items, tiles a run 1, 2, 4, 8, 16: dq 537, 496, 481, 512, 506 us; 512 of 40 to 200, at most two tiles
+  // each, 1 and 2: dq 49 and 58 us, dk and dv 51 and 69)
+  const long long run = tiles >= 32 ? 4 : 1;
+  const long long runs = (tiles + run - 1) / run * per, grid = (runs + 7) / 8 * 8 * run;
+  if (grid > 0x7fffffffLL || per > 0x7fffffffLL) return false;
+  *d = Deal{(int)per, (int)tiles, (int)run, mul_div((unsigned)run), mul_div((unsigned)per), (unsigned)grid};
+  return true;
+}
+struct Place { int rank, pair; };   // the how manieth tile of which pair; rank >= tiles: none
+__device__ __forceinline__ Place place_of(const Deal& d, unsigned block) {
+  const unsigned at = block >> 3, row = d.by_run.div(at), chunk = row * 8 + (block & 7), turn = d.by_per.div(chunk);
+  const unsigned turned = chunk - turn * d.per + turn;
+  return Place{(int)(turn * d.run + at - row * d.run), (int)(turned - d.by_per.div(turned) * d.per)};
+}
 
 constexpr unsigned NO_COLUMN = 0x80000000u;   // an offset behind every buffer's end
 
@@ -47,29 +67,48 @@ __device__ __forceinline__ int scalar_int(const int32_t* p, int at) {
   return ((scalar_ptr)(unsigned long long)p)[__builtin_amdgcn_readfirstlane(at)];
 }
 
-// How a lane reads a tile as the A operand of its products. Tiles start at multiples of 256 bytes, so the piece's place can be
-// flipped in the sum of both.
+// How a lane reads tiles as the A operand of its products. Tiles start at multiples of 256 bytes, so a piece's place can be flipped in
+// the sum with the tile's address; place() does so once for all reads of a tile (or of several, `more` bytes behind it), whose rows are
+// then the reads' immediate offsets.
 template <int DP>
 struct TileReader {
-  static constexpr int ROW = DP * 2, CH = DP / 8;
+  static constexpr int ROW = DP * 2, CH = DP / 8, KS = DP / 16, DB = DP / 32;
   unsigned row, lo, hi;
+  unsigned rows_at[KS], lo_at[DB], hi_at[DB];
   __device__ __forceinline__ explicit TileReader(int lane) {
     const int l32 = lane & 31, h = lane >> 5, i16 = lane & 15, r = h * 4 + (i16 >> 2), c = 2 * (l32 >> 4) + ((i16 & 3) >> 1);
     row = l32 * ROW + ((h ^ tile_swz<CH>(l32)) << 4);
     lo = r * ROW + ((c ^ tile_swz<CH>(r)) << 4) + (i16 & 1) * 8;
     hi = (r + 8) * ROW + ((c ^ tile_swz<CH>(r + 8)) << 4) + (i16 & 1) * 8;
   }
-  // a product over the width: row 32 b + lane % 32, pieces 2 s + lane / 32
-  __device__ __forceinline__ bf16x8 rows(unsigned at, int b, int s) const {
-    return lds_read16(lds_at((at + row) ^ (s << 5)) + b * 32 * ROW);
+  __device__ __forceinline__ void place_rows(unsigned at) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      rows_at[s] = (at + row) ^ (s << 5);
+      asm volatile("" : "+v"(rows_at[s]));
+    }
   }
+  __device__ __forceinline__ void place_cols(unsigned at) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      lo_at[db] = (at + lo) ^ (db << 6);
+      hi_at[db] = (at + hi) ^ (db << 6);
+      asm volatile("" : "+v"(lo_at[db]), "+v"(hi_at[db]));
+    }
+  }
+  __device__ __forceinline__ void place(unsigned at) {
+    place_rows(at);
+    place_cols(at);
+  }
+  // a product over the width: row 32 b + lane % 32, pieces 2 s + lane / 32
+  __device__ __forceinline__ bf16x8 rows(int more, int b, int s) const { return lds_read16(lds_at(rows_at[s]) + more + b * 32 * ROW); }
   // a product over the rows, of the transpose: columns 32 db .., rows 16 s + {4h .. 4h+3, 8+4h .. 8+4h+3} (the order in which a score
   // block's accumulators hold them)
-  __device__ __forceinline__ bf16x8 cols(unsigned at, int s, int db) const {
+  __device__ __forceinline__ bf16x8 cols(int more, int s, int db) const {
     auto half = [&](unsigned x) {
-      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_at((at + x) ^ (db << 6)) + s * 16 * ROW));
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds_at(x) + more + s * 16 * ROW));
     };
-    const s16x4 a = half(lo), b = half(hi);
+    const s16x4 a = half(lo_at[db]), b = half(hi_at[db]);
     return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
@@ -85,33 +124,30 @@ __device__ __forceinline__ void buffer_to_lds4(u32x4 buf, unsigned voff, unsigne
                : "memory");
 }
 
-// Tiles of packed keys and values: wave w of NW brings groups w, w + NW, .. (RPI rows each) of both
+// Tiles of packed keys and values: request x of wave w brings rows (w + x NW) RPI and on, of both. These are STEP rows apart from request to
+// request, which leaves a lane's offset as it is: the buffer begins that much later.
 template <int DP, int NW>
 struct PackedTiles {
   using Sh = TileShape<DP>;
-  static constexpr int GPW = (Sh::GROUPS + NW - 1) / NW;
-  unsigned koff[GPW], voff[GPW];
-  int wave;
-  __device__ __forceinline__ void init(int D, long long kp, long long vp, int wave_, int lane) {
-    wave = wave_;
-#pragma unroll
-    for (int x = 0; x < GPW; ++x) {
-      const int r = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
-      koff[x] = c * 8 < D ? (unsigned)(r * (int)kp * 2 + c * 16) : NO_COLUMN;
-      voff[x] = c * 8 < D ? (unsigned)(r * (int)vp * 2 + c * 16) : NO_COLUMN;
-    }
+  static constexpr int RPW = Sh::GROUPS / NW, STEP = NW * Sh::RPI;
+  static_assert(Sh::GROUPS % NW == 0 && (RPW == 1 || STEP * Sh::CH % 256 == 0), "whole requests, the same places in each");
+  unsigned koff, voff, to;
+  __device__ __forceinline__ void init(int D, long long kp, long long vp, int wave, int lane) {
+    to = wave * 1024;
+    const int r = wave * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
+    koff = c * 8 < D ? (unsigned)(r * (int)kp * 2 + c * 16) : NO_COLUMN;
+    voff = c * 8 < D ? (unsigned)(r * (int)vp * 2 + c * 16) : NO_COLUMN;
   }
   // rows k, v and on (`left` of them are the sequence's); keys to `at`, values behind them
   __device__ __forceinline__ void fetch(const unsigned short* k, const unsigned short* v, long long kp, long long vp, int D, int left,
                                         unsigned at) const {
     left = left < TI ? left : TI;
-    const u32x4 kb = buffer_of(k, (unsigned)(((left - 1) * (int)kp + D) * 2)), vb = buffer_of(v, (unsigned)(((left - 1) * (int)vp + D) * 2));
 #pragma unroll
-    for (int x = 0; x < GPW; ++x) {
-      const int g = wave + x * NW;
-      if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-      buffer_to_lds16(kb, koff[x], at + g * 1024);
-      buffer_to_lds16(vb, voff[x], at + Sh::BYTES + g * 1024);
+    for (int x = 0; x < RPW; ++x) {
+      const int rest = left - x * STEP;
+      buffer_to_lds16(buffer_of(k + x * STEP * kp, rest > 0 ? (unsigned)(((rest - 1) * (int)kp + D) * 2) : 0u), koff, at + to + x * NW * 1024);
+      buffer_to_lds16(buffer_of(v + x * STEP * vp, rest > 0 ? (unsigned)(((rest - 1) * (int)vp + D) * 2) : 0u), voff,
+                      at + to + Sh::BYTES + x * NW * 1024);
     }
   }
 };
