@@ -25,9 +25,9 @@ struct BwdArgs {
   int N, T, L, H, Hkv, D, G;
   MulDiv by_group;       // / G
   Deal deal;
-  float scale, inv_gamma;   // log2(e) / gamma, 1 / gamma
+  float scale, gamma, inv_gamma;   // scale: log2(e) / gamma
   const float* lse;
-  float* rows;           // [2,T,H]: -lse log2(e) and delta, by the first kernel for the second
+  float* rows;           // [T,H,2]: -lse gamma and -delta, by the first kernel for the second
   unsigned short* dq;
   unsigned short* dk;
   unsigned short* dv;
@@ -78,8 +78,8 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     delta = half_sum(sum);
     lse2 = a.lse[tok * a.H + head] * LOG2E;
     if (h == 0 && first + l32 < rows) {
-      a.rows[tok * a.H + head] = -lse2;
-      a.rows[((size_t)a.T + tok) * a.H + head] = delta;
+      a.rows[(tok * a.H + head) * 2] = -a.lse[tok * a.H + head] * a.gamma;
+      a.rows[(tok * a.H + head) * 2 + 1] = -delta;
     }
   }
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
@@ -163,12 +163,15 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
   });
 }
 
-template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel(const BwdArgs a) {
+// RT rows a tile. The width 128 leaves no registers for the values at two waves a SIMD: they stay in LDS (V_LDS) and are read as operands.
+template <int DP, int NW, int RT>
+__global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a) {
   using Sh = TileShape<DP>;
-  constexpr int KS = DP / 16, DB = DP / 32, ITEMS = NW * 32, OP = DP * 2 + 16, GPW = (Sh::GROUPS + NW - 1) / NW;
-  constexpr int STAGE = 2 * Sh::BYTES + 1024, PATCH = NW * 32 * OP, SLOTS = 3;   // (1024: lse and delta, and whole lines)
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * STAGE > PATCH ? SLOTS * STAGE : PATCH];
+  constexpr bool V_LDS = DP > 64;
+  constexpr int KS = DP / 16, DB = DP / 32, ITEMS = NW * 32, OP = DP * 2 + 16, HALF = RT * Sh::ROW, GROUPS = RT / Sh::RPI;
+  constexpr int GPW = (GROUPS + NW - 1) / NW;
+  constexpr int STAGE = 2 * HALF + 1024, PATCH = NW * 32 * OP, VALUES = V_LDS ? ITEMS * Sh::ROW : 0;   // (1024: what a row brings, and whole lines)
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE + VALUES > PATCH ? 2 * STAGE + VALUES : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -179,7 +182,60 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
   const int rows = n * a.G, first = item0 + wave * 32;
 
-  bf16x8 kreg[KS], vreg[KS];
+  // tiles of rows: queries, behind them d_o, behind them what the first kernel left of each row; rows behind the last read as zeros and
+  // add nothing. Where a tile is a whole number of tokens, a lane's offsets are the same in every tile.
+  const bool whole_tokens = RT % a.G == 0;
+  const int head0 = hk * a.G;
+  unsigned qoff[GPW], goff[GPW], soff;
+  auto offsets = [&](int r0, int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int in = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
+      const int i = (int)a.by_group.div(r), head = r - i * a.G, tk = i - i0;
+      qoff[x] = c * 8 < a.D ? (unsigned)((tk * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN;
+      goff[x] = c * 8 < a.D ? (unsigned)(((tk * a.H + head) * a.D + c * 8) * 2) : NO_COLUMN;
+    }
+    const int r = r0 + (RT == 64 ? lane : l32), i = (int)a.by_group.div(r);
+    soff = (unsigned)((i - i0) * a.H + r - i * a.G) * 8 + (RT == 64 ? wave : h) * 4;
+  };
+  constexpr int ROW_WAVES = RT == 64 ? 2 : 1;   // waves that ask for the rows' two numbers
+  if (whole_tokens) offsets(0, 0);
+  auto fetch = [&](int r0, unsigned at) __attribute__((always_inline)) {
+    const int i0 = (int)a.by_group.div(r0);
+    if (!whole_tokens) offsets(r0, i0);
+    const size_t tok = (size_t)cr.first + i0;
+    const int more = n - 1 - i0 < RT ? n - 1 - i0 : RT;   // whole tokens within reach behind the first
+    const u32x4 qb = buffer_of(a.q + tok * a.qp + (size_t)head0 * a.D, (unsigned)((more * (int)a.qp + a.G * a.D) * 2));
+    const u32x4 gb = buffer_of(a.go + (tok * a.H + head0) * a.D, (unsigned)((more * a.H + a.G) * a.D * 2));
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int g = wave + x * NW;
+      if (GROUPS % NW != 0 && g >= GROUPS) break;
+      buffer_to_lds16(qb, qoff[x], at + g * 1024);
+      buffer_to_lds16(gb, goff[x], at + HALF + g * 1024);
+    }
+    if (wave < ROW_WAVES)
+      buffer_to_lds4(buffer_of(a.rows + (tok * a.H + head0) * 2, (unsigned)(more * a.H + a.G) * 8), soff, at + 2 * HALF + wave * 256);
+  };
+
+  // From the last rows to the first that see an item: what runs beside this workgroup on the die then reads the same rows at about the
+  // same time, wherever its own items begin.
+  const int start = item0 * a.G / RT * RT;   // (rows before it see no item of this workgroup)
+  const int turns = (rows - start + RT - 1) / RT;
+  fetch(start + (turns - 1) * RT, lds);
+  const unsigned values = lds + 2 * STAGE + wave * 32 * Sh::ROW;
+  if constexpr (V_LDS) {   // the wave's own 32
+#pragma unroll
+    for (int g = 0; g < 32 / Sh::RPI; ++g) {
+      const int in = g * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in);
+      const int left = n - first;
+      buffer_to_lds16(buffer_of(a.v + (size_t)(cr.first + (left > 0 ? first : 0)) * a.vp + (size_t)hk * a.D,
+                                left > 0 ? (unsigned)((((left < 32 ? left : 32) - 1) * (int)a.vp + a.D) * 2) : 0u),
+                      c * 8 < a.D ? (unsigned)(in * (int)a.vp * 2 + c * 16) : NO_COLUMN, values + g * 1024);
+    }
+  }
+
+  bf16x8 kreg[KS], vreg[V_LDS ? 1 : KS];
   int from;   // the first row that sees this lane's item
   {
     int j = first + l32;
@@ -192,186 +248,121 @@ __global__ __launch_bounds__(64 * NW, (DP > 64 ? 1 : 2)) void history_dkv_kernel
       u32x4 x = {0u, 0u, 0u, 0u}, y = x;
       if (c < a.D) {
         x = *reinterpret_cast<const u32x4*>(a.k + tok * a.kp + (size_t)hk * a.D + c);
-        y = *reinterpret_cast<const u32x4*>(a.v + tok * a.vp + (size_t)hk * a.D + c);
+        if constexpr (!V_LDS) y = *reinterpret_cast<const u32x4*>(a.v + tok * a.vp + (size_t)hk * a.D + c);
       }
       kreg[s] = __builtin_bit_cast(bf16x8, x);
-      vreg[s] = __builtin_bit_cast(bf16x8, y);
+      if constexpr (!V_LDS) vreg[s] = __builtin_bit_cast(bf16x8, y);
     }
   }
   const int wave_from = __builtin_amdgcn_readlane(from, 0), wave_to = __builtin_amdgcn_readlane(from, 31);
+  const int floor = first < n ? wave_from - 32 : 0x7fffffff;   // blocks of rows from above this on see an item of the wave
 
-  // tiles of rows: queries, behind them d_o, behind them -lse log2(e) and delta; rows behind the last read as zeros and add nothing. Where a
-  // tile is a whole number of tokens, a lane's offsets are the same in every tile.
-  const bool whole_tokens = TI % a.G == 0;
-  const int head0 = hk * a.G;
-  unsigned qoff[GPW], goff[GPW], soff;
-  auto offsets = [&](int r0, int i0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < GPW; ++x) {
-      const int in = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
-      const int i = (int)a.by_group.div(r), head = r - i * a.G, tk = i - i0;
-      qoff[x] = c * 8 < a.D ? (unsigned)((tk * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN;
-      goff[x] = c * 8 < a.D ? (unsigned)(((tk * a.H + head) * a.D + c * 8) * 2) : NO_COLUMN;
-    }
-    const int r = r0 + lane, i = (int)a.by_group.div(r);
-    soff = (unsigned)((i - i0) * a.H + r - i * a.G) * 4;
-  };
-  if (whole_tokens) offsets(0, 0);
-  auto fetch = [&](int r0, unsigned at) __attribute__((always_inline)) {
-    const int i0 = (int)a.by_group.div(r0);
-    if (!whole_tokens) offsets(r0, i0);
-    const size_t tok = (size_t)cr.first + i0;
-    const int more = n - 1 - i0 < TI ? n - 1 - i0 : TI;   // whole tokens within reach behind the first
-    const u32x4 qb = buffer_of(a.q + tok * a.qp + (size_t)head0 * a.D, (unsigned)((more * (int)a.qp + a.G * a.D) * 2));
-    const u32x4 gb = buffer_of(a.go + (tok * a.H + head0) * a.D, (unsigned)((more * a.H + a.G) * a.D * 2));
-#pragma unroll
-    for (int x = 0; x < GPW; ++x) {
-      const int g = wave + x * NW;
-      if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-      buffer_to_lds16(qb, qoff[x], at + g * 1024);
-      buffer_to_lds16(gb, goff[x], at + Sh::BYTES + g * 1024);
-    }
-    if (wave < 2)
-      buffer_to_lds4(buffer_of(a.rows + ((size_t)wave * a.T + tok) * a.H + head0, (unsigned)(more * a.H + a.G) * 4), soff,
-                     at + 2 * Sh::BYTES + wave * TI * 4);
-  };
-
-  f32x16 dk[DB], dv[DB], sa, pa, sb, pb;   // (scores and dp of a block and of the next)
-  unsigned p[8], ds[8];
-  bf16x8 qf[KS], gf[KS], cols[2][DB];
+  f32x16 dk[DB], dv[DB];
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  f32x4 z[4], d[4];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = zero;
   TileReader<DP> read(lane);
+  const unsigned value_row = values + read.row;
 
-  auto read_rows = [&](int rb) __attribute__((always_inline)) {
+  // A block of 32 rows. Scores start from -lse gamma and dp from -delta, so that p = exp2(scale x) and ds = p dp.
+  auto block = [&](int r0, unsigned at, int rb) __attribute__((always_inline)) {
+    f32x16 sc, dp;
+    auto of_rows = [&](f32x16& x, int kind) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = read.rows(0, rb, s);
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 y = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(
+            lds_at(at + 2 * HALF + kind * RT * 4 + (rb * 32 + g * 8 + h * 4) * 4));
 #pragma unroll
-    for (int s = 0; s < KS; ++s) gf[s] = read.rows(Sh::BYTES, rb, s);
-  };
-  auto read_cols = [&](int more, int rb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) cols[s][db] = read.cols(more, rb * 2 + s, db);
-  };
-  auto scores = [&](f32x16& sc) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[s], kreg[s], s == 0 ? zero : sc, 0, 0, 0);
-  };
-  auto slopes = [&](f32x16& dp) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gf[s], vreg[s], s == 0 ? zero : dp, 0, 0, 0);
-  };
-  auto add = [&](f32x16* to, const unsigned* w) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const u32x4 b = {w[s * 4], w[s * 4 + 1], w[s * 4 + 2], w[s * 4 + 3]};
-        to[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols[s][db], __builtin_bit_cast(bf16x8, b), to[db], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) x[g * 4 + e] = y[e];
       }
-  };
-  // A block of 32 rows whose scores and dp are there; those of the next block (rows_at, next_rb) are made behind its exponentials and behind its
-  // ds, then it enters dv and dk
-  auto block = [&](f32x16& sc, f32x16& dp, f32x16& next_sc, f32x16& next_dp, int r0, unsigned at, int rb,
-                   int next_rb) __attribute__((always_inline)) {
+    };
+    of_rows(sc, 0);
+    {
+      bf16x8 qf[KS];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const unsigned where = at + 2 * Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4;
-      z[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
-      d[g] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + TI * 4));
+      for (int s = 0; s < KS; ++s) qf[s] = read.rows(0, rb, s);
+      of_rows(dp, 1);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[s], kreg[s], sc, 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    read_rows(next_rb);
-    __builtin_amdgcn_sched_barrier(0);
-    if (r0 < wave_to) {   // rows that do not see all of the wave's items: -inf where they do not
+    if (r0 < wave_to) {   // rows that do not see all of the wave's items
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (r0 + 8 * (r >> 2) + 4 * h + (r & 3) < from) sc[r] = -INFINITY;
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, z[r >> 2][r & 3]));
+    for (int s = 0; s < KS; ++s) {
+      const bf16x8 gf = read.rows(HALF, rb, s);
+      bf16x8 vf;
+      if constexpr (V_LDS) vf = lds_read16(lds_at(value_row ^ (s << 5)));
+      else vf = vreg[s];
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gf, vf, dp, 0, 0, 0);
+    }
+    unsigned p[8], ds[8];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(sc[r] * a.scale);
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
       p[r] = pack_bf16(sc[2 * r], sc[2 * r + 1]);
       asm volatile("" : "+v"(p[r]));
     }
-    scores(next_sc);
-    read_cols(Sh::BYTES, rb);
+    __builtin_amdgcn_sched_group_barrier(0x100, V_LDS ? 4 : 2, 0);
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, V_LDS ? 2 : 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 40 / KS, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    add(dv, p);
+    auto add = [&](f32x16* to, const unsigned* w, int more) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      ds[r >> 1] = pack_bf16(sc[r] * (dp[r] - d[r >> 2][r & 3]), sc[r + 1] * (dp[r + 1] - d[r >> 2][(r & 3) + 1]));
-      asm volatile("" : "+v"(ds[r >> 1]));
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u32x4 b = {w[s * 4], w[s * 4 + 1], w[s * 4 + 2], w[s * 4 + 3]};
+          to[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.cols(more, rb * 2 + s, db), __builtin_bit_cast(bf16x8, b), to[db], 0, 0, 0);
+        }
+    };
+    add(dv, p, HALF);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      ds[r] = pack_bf16(sc[2 * r] * dp[2 * r], sc[2 * r + 1] * dp[2 * r + 1]);
+      asm volatile("" : "+v"(ds[r]));
     }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
     for (int x = 0; x < 2 * DB; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 24 / DB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 12 / DB, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    slopes(next_dp);
-    read_cols(0, rb);
+    add(dk, ds, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-    for (int x = 0; x < KS; ++x) {
+    for (int x = 0; x < 2 * DB; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    add(dk, ds);
   };
 
-  // From the last rows to the first that see an item: what runs beside this workgroup on the die then reads the same rows at about the
-  // same time, wherever its own items begin.
-  const int start = item0 * a.G / TI * TI;   // (rows before it see no item of this workgroup)
-  const int turns = (rows - start + TI - 1) / TI;
-  const int requests = 2 * GPW + (wave < 2 ? 1 : 0);
-  int asked = 0, slot = 0;
-  auto row_of = [&](int t) { return start + (turns - 1 - t) * TI; };
-  auto request = [&]() __attribute__((always_inline)) {
-    fetch(row_of(asked), lds + slot * STAGE);
-    slot = slot + 1 == SLOTS ? 0 : slot + 1;
-    ++asked;
-  };
-  const int floor = first < n ? wave_from - 32 : 0x7fffffff;   // blocks of rows from above this on see an item of the wave
-  request();
-  if (turns > 1) request();
-  wait_vm((asked - 1) * requests);
-  barrier_lds();
-  if (row_of(0) + 32 > floor) {
-    read.place_rows(lds);
-    read_rows(1);
-    scores(sa);
-    slopes(pa);
-  }
-  unsigned at = lds;
-  int out = 0;
-  for (int t = 0; t < turns; ++t) {
-    const int r0 = row_of(t);
-    read.place_cols(at);   // (its rows were placed by the turn before)
-    if (r0 + 32 > floor) block(sa, pa, sb, pb, r0 + 32, at, 1, 0);
-    out = out + 1 == SLOTS ? 0 : out + 1;
-    const unsigned next = t + 1 < turns ? lds + out * STAGE : at;
-    if (t + 1 < turns) {
-      wait_vm((asked - t - 2) * requests);
-      barrier_lds();   // tile t + 1 is there, and every wave is through with tile t - 1, whose slot is asked for again
-      if (asked < turns) request();
-    }
-    read.place_rows(next);
-    if (r0 > floor) block(sb, pb, sa, pa, r0, at, 0, 1);
-    at = next;
+  unsigned at = lds, other = lds + STAGE;
+  for (int t = turns - 1; t >= 0; --t) {
+    const int r0 = start + t * RT;
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t > 0) fetch(r0 - RT, other);
+    read.place(at);
+    if constexpr (RT == 64)
+      if (r0 + 32 > floor) block(r0 + 32, at, 1);
+    if (r0 > floor) block(r0, at, 0);
+    const unsigned x = at;
+    at = other;
+    other = x;
   }
   barrier_lds();
   unsigned char* patch = smem + wave * 32 * OP;
@@ -389,7 +380,7 @@ static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
   BwdArgs b = a;
   if (!deal(per, row_tiles, &a.deal) || !deal(per, item_tiles, &b.deal)) return LASER_ERR_SHAPE;
   history_dq_kernel<DP, NW><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
-  history_dkv_kernel<DP, NW><<<b.deal.grid, 64 * NW, 0, stream>>>(b);
+  history_dkv_kernel<DP, NW, (DP > 64 ? 32 : 64)><<<b.deal.grid, 64 * NW, 0, stream>>>(b);
   return launch_status();
 }
 
@@ -406,6 +397,7 @@ laser_status history_bwd_tile_launch(const HistoryBwdArgs& b) {
   a.N = h.N, a.T = h.T, a.L = h.L, a.H = h.H, a.Hkv = h.Hkv, a.D = h.D, a.G = h.H / h.Hkv;
   a.by_group = mul_div(a.G);
   a.scale = LOG2E / h.gamma;
+  a.gamma = h.gamma;
   a.inv_gamma = 1.0f / h.gamma;
   a.lse = h.lse;
   a.rows = b.work;
