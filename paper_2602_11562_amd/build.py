@@ -23,7 +23,7 @@ OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["laser_api.hip", "sta_generic.hip", "sta_f32.hip", "sta_mfma.hip", "sta_ring.hip", "sta_stream.hip", "sta_few.hip", "gsta_generic.hip",
            "gsta_tiled.hip", "gsta_one.hip", "gsta_project.hip", "fused_forward.hip", "multires.hip", "segment_ffn.hip", "ffn_gsta.hip", "project.hip", "sta_backward.hip", "sta_backward_mfma.hip", "gsta_backward.hip", "gsta_backward_tile.hip",
-           "history_api.hip", "history_generic.hip", "history_mfma.hip", "history_backward.hip", "cache_few.hip", "cache_weights.hip", "cache_move.hip"]
+           "history_api.hip", "history_f32.hip", "history_mfma.hip", "history_backward.hip", "cache_few.hip", "cache_weights.hip", "cache_move.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

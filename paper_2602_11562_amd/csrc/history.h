@@ -20,7 +20,8 @@ struct HistoryArgs {
   hipStream_t stream;
 };
 laser_status history_forward_launch(const HistoryArgs& a);
-laser_status history_tile_launch(const HistoryArgs& a);   // bf16, on the matrix cores
+laser_status history_tile_launch(const HistoryArgs& a);   // bf16
+laser_status history_f32_launch(const HistoryArgs& a);
 
 struct HistoryBwdArgs {
   HistoryArgs f;           // the forward pass's arguments; o and lse are inputs here
@@ -33,7 +34,8 @@ struct HistoryBwdArgs {
 };
 size_t history_backward_work_bytes(int N, int T, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status history_backward_launch(const HistoryBwdArgs& a);
-laser_status history_bwd_tile_launch(const HistoryBwdArgs& a);   // bf16, on the matrix cores
+laser_status history_bwd_tile_launch(const HistoryBwdArgs& a);   // bf16
+laser_status history_bwd_f32_launch(const HistoryBwdArgs& a);
 
 // A paged cache: item j of user u stands in page pages[u * max_pages + j / page], at place j % page of every key-value head.
 struct CacheArgs {
@@ -61,8 +63,10 @@ struct CacheRuns { int chunk, runs; };   // histories of up to L items are cut i
 CacheRuns cache_runs(int workgroups, int L, int least, int tile);
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits);
 laser_status cache_few_launch(const CacheArgs& a, const CacheRuns& r);    // bf16, at most 32 rows a key-value head
-laser_status cache_tile_launch(const CacheArgs& a, const CacheRuns& r);   // bf16, on the matrix cores
-laser_status cache_weights_tile_launch(const CacheArgs& a);               // bf16, on the matrix cores
+laser_status cache_tile_launch(const CacheArgs& a, const CacheRuns& r);   // bf16
+laser_status cache_f32_launch(const CacheArgs& a, const CacheRuns& r);
+laser_status cache_weights_tile_launch(const CacheArgs& a);               // bf16
+laser_status cache_weights_f32_launch(const CacheArgs& a);
 laser_status cache_weights_launch(const CacheArgs& a);   // q, lse and k in, weight out
 
 struct CacheAppendArgs {

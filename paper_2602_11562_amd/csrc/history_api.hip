@@ -78,6 +78,34 @@ static laser_status validate_rows(const void* rows, int64_t pitch, int heads, co
   return LASER_OK;
 }
 
+// What the backward pass keeps of every row between its two kernels
+size_t history_backward_work_bytes(int, int T, int, int H, int, int, laser_dtype) { return (size_t)T * H * 8; }
+
+laser_status history_forward_launch(const HistoryArgs& a) { return a.dt == LASER_F32 ? history_f32_launch(a) : history_tile_launch(a); }
+laser_status history_backward_launch(const HistoryBwdArgs& a) {
+  return a.f.dt == LASER_F32 ? history_bwd_f32_launch(a) : history_bwd_tile_launch(a);
+}
+laser_status cache_weights_launch(const CacheArgs& a) {
+  return a.dt == LASER_F32 ? cache_weights_f32_launch(a) : cache_weights_tile_launch(a);
+}
+
+// Rows of a key-value head that one column block holds: the streaming kernel (bf16)
+static bool few_rows(int C, int H, int Hkv, laser_dtype dt) { return dt == LASER_BF16 && (long long)C * (H / Hkv) <= 32; }
+static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
+  const bool few = few_rows(C, H, Hkv, dt);
+  const long long tiles = few ? 1 : ((long long)C * (H / Hkv) + 127) / 128, all = tiles * U * Hkv;
+  return cache_runs(all < 512 ? (int)all : 512, L, few ? 512 : 256, few ? 128 : 64);
+}
+size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
+  const CacheRuns r = runs_of(U, C, L, H, Hkv, dt);
+  return r.runs > 1 ? (size_t)r.runs * T * H * (D + 1) * 4 : 16;
+}
+laser_status cache_attention_launch(const CacheArgs& a) {
+  const CacheRuns r = runs_of(a.U, a.C, a.L, a.H, a.Hkv, a.dt);
+  if (a.dt == LASER_F32) return cache_f32_launch(a, r);
+  return few_rows(a.C, a.H, a.Hkv, a.dt) ? cache_few_launch(a, r) : cache_tile_launch(a, r);
+}
+
 }  // namespace laser
 
 using namespace laser;

@@ -1,0 +1,575 @@
+// Attention among the items of histories in single precision, on the matrix cores' fp32 products: the forms of history_mfma.hip,
+// history_backward.hip and cache_weights.hip, whose mathematics and layout of products they share.
+//
+// v_mfma_f32_32x32x2_f32 takes two steps of the contraction at a time, one from each half of the wave. Over the width a lane's 16-byte
+// piece feeds four of them; over the items register r of a score block is, as it stands, the B operand for items 8 (r / 4) + r % 4 and
+// four further, and the A operand is one float a lane, 32 columns side by side. Products take 16 times as long as bf16's, so tiles of
+// 32 rows, no second tile of registers and no ordering by hand: everything else is behind them (a large product in this
+// precision reaches 154 TFLOP/s on this card).
+#include "history_tile.h"
+
+namespace laser {
+
+constexpr int FI = 32;   // rows of a tile
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// A row of DP floats is CH pieces of 16 bytes; piece c of row r stands at place c ^ swz(r). Sixteen rows at one piece are in all banks,
+// and so are 32 columns of two rows four apart (rows of 256 bytes and more).
+template <int DP>
+struct F32Tile {
+  static constexpr int ROW = DP * 4, CH = DP / 4, RPI = 64 / CH, BYTES = FI * ROW, NW = 4, MINE = FI / NW, RPW = MINE / RPI;
+  static __device__ __forceinline__ int swz(int r) {
+    return CH >= 16 ? (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3 : (r >> 1) & 7;
+  }
+  // four steps over the width: row l32, pieces 2 a + h
+  static __device__ __forceinline__ f32x4 rows(unsigned at, int a, int lane) {
+    const int r = lane & 31;
+    return *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(at + r * ROW + (((2 * a + (lane >> 5)) ^ swz(r)) << 4)));
+  }
+  // a step over the rows: columns 32 db + l32 of rows 8 (r / 4) + r % 4 + 4 h
+  static __device__ __forceinline__ float col(unsigned at, int r, int db, int lane) {
+    const int row = 8 * (r >> 2) + (r & 3) + 4 * (lane >> 5), d = db * 32 + (lane & 31);
+    return *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at + row * ROW + (((d >> 2) ^ swz(row)) << 4) + (d & 3) * 4));
+  }
+};
+
+struct F32Args {
+  const float* q;
+  const float* k;
+  const float* v;
+  long long qp, kp, vp;
+  const int32_t* off;
+  const int32_t* pages;
+  const int32_t* lens;
+  int N, T, L, C, H, Hkv, D, log2, P, max_pages, G, tiles, chunk, runs;
+  MulDiv by_group;
+  Deal deal;
+  float scale, gamma, inv_gamma;
+  bool causal, add;
+  float* o;
+  float* lse;
+  float* work;
+  float* weight;
+  // backward
+  const float* go;
+  float* dq;
+  float* dk;
+  float* dv;
+  long long dqp, dkp, dvp;
+};
+
+// Products over the width: x[row or item in lane] += tile rows . regs, four steps a piece
+template <int DP>
+__device__ __forceinline__ f32x16 over_width(unsigned at, const f32x4* regs, f32x16 x, int lane) {
+#pragma unroll
+  for (int a = 0; a < DP / 8; ++a) {
+    const f32x4 t = F32Tile<DP>::rows(at, a, lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(t[e], regs[a][e], x, 0, 0, 0);
+  }
+  return x;
+}
+// and over the tile's rows: acc[column, lane] += tile^T . w
+template <int DP>
+__device__ __forceinline__ void over_rows(unsigned at, const f32x16& w, f32x16* acc, int lane) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(F32Tile<DP>::col(at, r, db, lane), w[r], acc[db], 0, 0, 0);
+}
+// 16-byte pieces 2 a + h of a row of D floats, zeros behind its end
+template <int DP>
+__device__ __forceinline__ void load_row(f32x4* regs, const float* row, int D, int h) {
+#pragma unroll
+  for (int a = 0; a < DP / 8; ++a) regs[a] = a * 8 < D ? *reinterpret_cast<const f32x4*>(row + a * 8 + h * 4) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+// A lane's row of the transposed accumulators: columns 32 db + 8 x + 4 h and on, times `by`
+template <int DP>
+__device__ __forceinline__ void store_row(float* row, const f32x16* acc, float by, int D, int h) {
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int c = db * 32 + x * 8 + h * 4;
+      if (c < D) *reinterpret_cast<f32x4*>(row + c) = f32x4{acc[db][x * 4] * by, acc[db][x * 4 + 1] * by, acc[db][x * 4 + 2] * by, acc[db][x * 4 + 3] * by};
+    }
+}
+
+__device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
+
+// Requests for tiles of items: wave w brings eight rows of keys and of values, which a page of eight or more holds together
+template <int DP, bool PAGED>
+struct F32Items {
+  using Sh = F32Tile<DP>;
+  unsigned koff[Sh::RPW], voff[Sh::RPW];
+  int wave, id;
+  __device__ __forceinline__ void init(const F32Args& a, int wave_, int lane) {
+    wave = wave_;
+    id = -1;
+#pragma unroll
+    for (int x = 0; x < Sh::RPW; ++x) {
+      const int in = x * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(wave * Sh::MINE + in);
+      koff[x] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.kp) + c * 4) * 4) : NO_COLUMN;
+      voff[x] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.vp) + c * 4) * 4) : NO_COLUMN;
+    }
+  }
+  __device__ __forceinline__ void look_up(const F32Args& a, const int32_t* table, int t0, int n) {
+    const int j = t0 + wave * Sh::MINE;
+    if (PAGED) id = j < n ? scalar_int(table, j >> a.log2) : -1;
+  }
+  // items t0 and on of n
+  __device__ __forceinline__ void fetch(const F32Args& a, size_t first, int hk, int t0, int n, unsigned at) const {
+    const int j = t0 + wave * Sh::MINE;
+    int left = n - j < Sh::MINE ? n - j : Sh::MINE;
+    const float *k, *v;
+    if constexpr (PAGED) {
+      if ((unsigned)id >= (unsigned)a.P) left = 0;
+      const size_t row = left > 0 ? (((size_t)id * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
+      k = a.k + row * a.D;
+      v = a.v + row * a.D;
+    } else {
+      const size_t row = left > 0 ? first + j : first;
+      k = a.k + row * a.kp + (size_t)hk * a.D;
+      v = a.v + row * a.vp + (size_t)hk * a.D;
+    }
+    const int kp = PAGED ? a.D : (int)a.kp, vp = PAGED ? a.D : (int)a.vp;
+    const u32x4 kb = buffer_of(k, left > 0 ? (unsigned)(((left - 1) * kp + a.D) * 4) : 0u);
+    const u32x4 vb = buffer_of(v, left > 0 ? (unsigned)(((left - 1) * vp + a.D) * 4) : 0u);
+    const unsigned to = at + wave * Sh::MINE * Sh::ROW;
+#pragma unroll
+    for (int x = 0; x < Sh::RPW; ++x) {
+      buffer_to_lds16(kb, koff[x], to + x * 1024);
+      buffer_to_lds16(vb, voff[x], to + Sh::BYTES + x * 1024);
+    }
+  }
+};
+
+template <int DP, bool PAGED>
+__global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
+  using Sh = F32Tile<DP>;
+  constexpr int DB = DP / 32, ROWS = 128, STAGE = 2 * Sh::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  int tile = place.rank, run = 0;
+  if (PAGED && a.runs > 1) {
+    run = tile / a.tiles;
+    tile -= run * a.tiles;
+  }
+  tile = a.tiles - 1 - tile;   // (the longest first)
+  const int n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.C, a.T);
+  const int rows = cr.count * a.G, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const int n = PAGED ? cache_len(a.lens, n_seq, a.L, a.max_pages, a.log2) : cr.count;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  int end;   // one past the last item that a row of this workgroup sees
+  {
+    const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
+    end = a.causal ? n - cr.count + (int)a.by_group.div(r) + 1 : n;
+  }
+  const bool joined = PAGED && a.runs > 1 && n > a.chunk;   // others write their part of the result too
+  int begin = 0;
+  if (PAGED && a.runs > 1) {
+    begin = run * a.chunk;
+    if (run > 0 && begin >= end) return;
+    end = end < begin + a.chunk ? end : begin + a.chunk;
+  }
+  const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
+  F32Items<DP, PAGED> items;
+  items.init(a, wave, lane);
+  if (end > begin) {
+    items.look_up(a, table, begin, n);
+    items.fetch(a, (size_t)cr.first, hk, begin, n, lds);
+    items.look_up(a, table, begin + FI, n);
+  }
+
+  const int mine = row0 + wave * 32 + l32, r = mine < rows ? mine : rows - 1, i = (int)a.by_group.div(r), head = hk * a.G + r - i * a.G;
+  const size_t tok = (size_t)cr.first + i;
+  const bool busy = row0 + wave * 32 < rows;
+  const int last = a.causal ? n - cr.count + i : n - 1;
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = busy ? __builtin_amdgcn_readlane(last, 31) : -1;
+  f32x4 q[DP / 8];
+  load_row<DP>(q, a.q + tok * a.qp + (size_t)head * a.D, a.D, h);
+  bool whole_pages = true;
+  if constexpr (PAGED) {
+    bool bad = false;
+    if (end > begin)
+      for (int x = (begin >> a.log2) + lane; x <= (end - 1) >> a.log2; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    whole_pages = __ballot(bad) == 0;
+  }
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = splat(0.0f);
+  float m = -INFINITY, l = 0.0f;
+  unsigned at = lds, other = lds + STAGE;
+  for (int t0 = begin; t0 < end; t0 += FI) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t0 + FI < end) {
+      items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
+      items.look_up(a, table, t0 + 2 * FI, n);
+    }
+    if (t0 <= wave_last) {
+      f32x16 sc = over_width<DP>(at, q, splat(0.0f), lane);
+      if (!whole_pages || t0 + FI - 1 > wave_first || t0 + FI > n) {
+        bool in = l32 < n - t0;
+        if (PAGED && !whole_pages) in = in && (unsigned)table[(t0 + (in ? l32 : 0)) >> a.log2] < (unsigned)a.P;
+        const unsigned there = (unsigned)__ballot(in) >> (4 * h);
+        const int seen = last - t0 - 4 * h;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int i0 = 8 * (x >> 2) + (x & 3);
+          if (i0 > seen || !((there >> i0) & 1)) sc[x] = -INFINITY;
+        }
+      }
+      float top = sc[0];
+#pragma unroll
+      for (int x = 1; x < 16; ++x) top = fmaxf(top, sc[x]);
+      top = half_max(top) * a.scale;
+      if (__any(top > m)) {
+        const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= c;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) acc[db][x] *= c;
+      }
+      const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], a.scale, -base));
+        l += sc[x];
+      }
+      over_rows<DP>(at + Sh::BYTES, sc, acc, lane);
+    }
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  if (mine >= rows) return;
+  const float sum = half_sum(l), inv = sum > 0.0f ? 1.0f / sum : 0.0f, z = sum > 0.0f ? m + log2f(sum) : -INFINITY;
+  const size_t row = tok * a.H + head;
+  if (joined) {
+    const size_t all = (size_t)a.T * a.H;
+    store_row<DP>(a.work + (run * all + row) * a.D, acc, inv, a.D, h);
+    if (h == 0) a.work[a.runs * all * a.D + run * all + row] = z;
+  } else {
+    store_row<DP>(a.o + row * a.D, acc, inv, a.D, h);
+    if (h == 0 && a.lse != nullptr) a.lse[row] = z * LN2;
+  }
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a) {
+  using Sh = F32Tile<DP>;
+  constexpr int DB = DP / 32, ROWS = 128, STAGE = 2 * Sh::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  const int tile = a.deal.tiles - 1 - place.rank, n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
+  const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
+  F32Items<DP, false> items;
+  items.init(a, wave, lane);
+  items.fetch(a, (size_t)cr.first, hk, 0, n, lds);
+
+  const int mine = row0 + wave * 32 + l32, r = mine < rows ? mine : rows - 1, last = (int)a.by_group.div(r), head = hk * a.G + r - last * a.G;
+  const size_t tok = (size_t)cr.first + last, row = tok * a.H + head;
+  const int wave_first = __builtin_amdgcn_readlane(last, 0);
+  const int wave_last = row0 + wave * 32 < rows ? __builtin_amdgcn_readlane(last, 31) : -1;
+  f32x4 q[DP / 8], go[DP / 8], o[DP / 8];
+  load_row<DP>(q, a.q + tok * a.qp + (size_t)head * a.D, a.D, h);
+  load_row<DP>(go, a.go + row * a.D, a.D, h);
+  load_row<DP>(o, a.o + row * a.D, a.D, h);
+  float delta = 0.0f;
+#pragma unroll
+  for (int x = 0; x < DP / 8; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) delta = fmaf(go[x][e], o[x][e], delta);
+  delta = half_sum(delta);
+  const float lse2 = a.lse[row] * LOG2E;
+  if (h == 0 && mine < rows) {
+    a.work[row * 2] = -a.lse[row] * a.gamma;
+    a.work[row * 2 + 1] = -delta;
+  }
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = splat(0.0f);
+  unsigned at = lds, other = lds + STAGE;
+  for (int t0 = 0; t0 < end; t0 += FI) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t0 + FI < end) items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
+    if (t0 <= wave_last) {
+      f32x16 sc = over_width<DP>(at, q, splat(0.0f), lane);
+      const f32x16 dp = over_width<DP>(at + Sh::BYTES, go, splat(-delta), lane);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], a.scale, -lse2)) * dp[x];
+        if (t0 + FI - 1 > wave_first && t0 + 8 * (x >> 2) + 4 * h + (x & 3) > last) sc[x] = 0.0f;
+      }
+      over_rows<DP>(at, sc, acc, lane);
+    }
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  if (mine < rows) store_row<DP>(a.dq + tok * a.dqp + (size_t)head * a.D, acc, a.inv_gamma, a.D, h);
+}
+
+// Requests for tiles of a group's rows: one tensor's rows of 32, offsets from the first token's
+template <int DP>
+struct F32Rows {
+  using Sh = F32Tile<DP>;
+  // `pitch` between tokens of p (at the tile's first token and the group's first head), n - i0 tokens left
+  static __device__ __forceinline__ void fetch(const F32Args& a, const float* p, int pitch, int r0, int i0, int more, unsigned at, int wave, int lane) {
+    const u32x4 b = buffer_of(p, (unsigned)((more * pitch + a.G * a.D) * 4));
+#pragma unroll
+    for (int x = 0; x < Sh::RPW; ++x) {
+      const int in = wave * Sh::MINE + x * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(in), r = r0 + in;
+      const int i = (int)a.by_group.div(r), head = r - i * a.G;
+      buffer_to_lds16(b, c * 4 < a.D ? (unsigned)(((i - i0) * pitch + head * a.D + c * 4) * 4) : NO_COLUMN,
+                      at + wave * Sh::MINE * Sh::ROW + x * 1024);
+    }
+  }
+};
+
+template <int DP>
+__global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a) {
+  using Sh = F32Tile<DP>;
+  constexpr int DB = DP / 32, ITEMS = 128, STAGE = 2 * Sh::BYTES + 1024;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  const int tile = place.rank, n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
+  const int n = cr.count, item0 = tile * ITEMS;
+  if (item0 >= n) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  const int rows = n * a.G, first = item0 + wave * 32, head0 = hk * a.G;
+  auto fetch = [&](int r0, unsigned at) {
+    const int i0 = (int)a.by_group.div(r0), more = n - 1 - i0 < FI ? n - 1 - i0 : FI;
+    const size_t tok = (size_t)cr.first + i0;
+    F32Rows<DP>::fetch(a, a.q + tok * a.qp + (size_t)head0 * a.D, (int)a.qp, r0, i0, more, at, wave, lane);
+    F32Rows<DP>::fetch(a, a.go + (tok * a.H + head0) * a.D, a.H * a.D, r0, i0, more, at + Sh::BYTES, wave, lane);
+    if (wave == 0) {
+      const int r = r0 + l32, i = (int)a.by_group.div(r);
+      buffer_to_lds4(buffer_of(a.work + (tok * a.H + head0) * 2, (unsigned)(more * a.H + a.G) * 8),
+                     (unsigned)((i - i0) * a.H + r - i * a.G) * 8 + h * 4, at + 2 * Sh::BYTES);
+    }
+  };
+  const int start = item0 * a.G / FI * FI, turns = (rows - start + FI - 1) / FI;
+  fetch(start + (turns - 1) * FI, lds);
+  const int mine = first + l32, j = mine < n ? mine : n - 1, from = j * a.G;
+  const size_t item = (size_t)cr.first + j;
+  const int wave_from = __builtin_amdgcn_readlane(from, 0);
+  const int floor = first < n ? wave_from - 32 : 0x7fffffff;
+  f32x4 k[DP / 8], v[DP / 8];
+  load_row<DP>(k, a.k + item * a.kp + (size_t)hk * a.D, a.D, h);
+  load_row<DP>(v, a.v + item * a.vp + (size_t)hk * a.D, a.D, h);
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dk[db] = dv[db] = splat(0.0f);
+  unsigned at = lds, other = lds + STAGE;
+  for (int t = turns - 1; t >= 0; --t) {
+    const int r0 = start + t * FI;
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t > 0) fetch(r0 - FI, other);
+    if (r0 > floor) {
+      f32x16 sc, dp;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const unsigned where = at + 2 * Sh::BYTES + (g * 8 + h * 4) * 4;
+        const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
+        const f32x4 d = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + FI * 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[g * 4 + e] = z[e], dp[g * 4 + e] = d[e];
+      }
+      sc = over_width<DP>(at, k, sc, lane);
+      dp = over_width<DP>(at + Sh::BYTES, v, dp, lane);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        sc[x] = __builtin_amdgcn_exp2f(sc[x] * a.scale);
+        if (r0 + 8 * (x >> 2) + 4 * h + (x & 3) < from) sc[x] = 0.0f;
+        dp[x] *= sc[x];
+      }
+      over_rows<DP>(at + Sh::BYTES, sc, dv, lane);
+      over_rows<DP>(at, dp, dk, lane);
+    }
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  if (mine >= n) return;
+  store_row<DP>(a.dk + item * a.dkp + (size_t)hk * a.D, dk, a.inv_gamma, a.D, h);
+  store_row<DP>(a.dv + item * a.dvp + (size_t)hk * a.D, dv, 1.0f, a.D, h);
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void cache_weights_f32_kernel(const F32Args a) {
+  using Sh = F32Tile<DP>;
+  constexpr int STAGE = Sh::BYTES + 1024;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const int u = blockIdx.y;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.log2), item0 = (int)blockIdx.x * 128;
+  if (item0 >= n) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  const int rows = cr.count * a.G, first = item0 + wave * 32, mine = first + l32, j = mine < n ? mine : n - 1;
+  const int page = a.pages[(size_t)u * a.max_pages + (j >> a.log2)], place = j & ((1 << a.log2) - 1);
+  const bool there = (unsigned)page < (unsigned)a.P;
+  const size_t slot = there ? (size_t)page : 0;
+  int from = a.causal ? (j - (n - cr.count)) * a.G : 0, start = a.causal ? (item0 - (n - cr.count)) * a.G : 0;
+  from = from < 0 ? 0 : from;
+  start = start < 0 ? 0 : start / FI * FI;
+  const int wave_from = __builtin_amdgcn_readlane(from, 0);
+  auto fetch = [&](int hk, int r0, unsigned at) {
+    const int i0 = (int)a.by_group.div(r0), more = cr.count - 1 - i0 < FI ? cr.count - 1 - i0 : FI;
+    const size_t tok = (size_t)cr.first + i0, head0 = (size_t)hk * a.G;
+    F32Rows<DP>::fetch(a, a.q + tok * a.qp + head0 * a.D, (int)a.qp, r0, i0, more, at, wave, lane);
+    if (wave == 0) {
+      const int r = r0 + l32, i = (int)a.by_group.div(r);
+      buffer_to_lds4(buffer_of(a.lse + tok * a.H + head0, (unsigned)(more * a.H + a.G) * 4), (unsigned)((i - i0) * a.H + r - i * a.G) * 4,
+                     at + Sh::BYTES);
+    }
+  };
+  float sum = 0.0f;
+  f32x4 k[DP / 8];
+  if (rows > start) {
+    fetch(0, start, lds);
+    unsigned at = lds, other = lds + STAGE;
+    for (int hk = 0; hk < a.Hkv; ++hk) {
+      load_row<DP>(k, a.k + (((slot * a.Hkv + hk) << a.log2) + place) * (size_t)a.D, a.D, h);
+      for (int r0 = start; r0 < rows; r0 += FI) {
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        barrier_lds();
+        if (r0 + FI < rows) fetch(hk, r0 + FI, other);
+        else if (hk + 1 < a.Hkv) fetch(hk + 1, start, other);
+        if (first < n && r0 + FI > wave_from) {
+          const f32x16 sc = over_width<DP>(at, k, splat(0.0f), lane);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(at + Sh::BYTES + (g * 8 + h * 4) * 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = r0 + g * 8 + h * 4 + e;
+              const float p = __builtin_amdgcn_exp2f(fmaf(sc[g * 4 + e], a.scale, -z[e] * LOG2E));
+              sum += r < from || r >= rows ? 0.0f : p;
+            }
+          }
+        }
+        const unsigned x = at;
+        at = other;
+        other = x;
+      }
+    }
+  }
+  sum = half_sum(sum);
+  if (h == 0 && mine < n && there) {
+    float* w = a.weight + (slot << a.log2) + place;
+    if (a.add) unsafeAtomicAdd(w, sum);
+    else *w = sum;
+  }
+}
+
+static F32Args of_history(const HistoryArgs& h) {
+  F32Args a{};
+  a.q = static_cast<const float*>(h.q);
+  a.k = static_cast<const float*>(h.k);
+  a.v = static_cast<const float*>(h.v);
+  a.qp = h.qp, a.kp = h.kp, a.vp = h.vp;
+  a.off = h.off;
+  a.N = h.N, a.T = h.T, a.L = a.C = h.L, a.H = h.H, a.Hkv = h.Hkv, a.D = h.D, a.G = h.H / h.Hkv;
+  a.by_group = mul_div(a.G);
+  a.scale = LOG2E / h.gamma, a.gamma = h.gamma, a.inv_gamma = 1.0f / h.gamma;
+  a.causal = true;
+  a.runs = 1;
+  a.o = static_cast<float*>(h.o);
+  a.lse = h.lse;
+  a.tiles = (int)(((long long)a.L * a.G + 127) / 128);
+  return a;
+}
+static F32Args of_cache(const CacheArgs& c) {
+  F32Args a{};
+  a.q = static_cast<const float*>(c.q);
+  a.k = static_cast<const float*>(c.k);
+  a.v = static_cast<const float*>(c.v);
+  a.qp = c.qp;
+  a.off = c.off, a.pages = c.pages, a.lens = c.lens;
+  a.N = c.U, a.T = c.T, a.L = c.L, a.C = c.C, a.H = c.H, a.Hkv = c.Hkv, a.D = c.D, a.G = c.H / c.Hkv;
+  a.log2 = c.page_log2, a.P = c.P, a.max_pages = c.max_pages;
+  a.by_group = mul_div(a.G);
+  a.scale = LOG2E / c.gamma;
+  a.causal = c.causal, a.add = c.add;
+  a.o = static_cast<float*>(c.o);
+  a.lse = c.lse;
+  a.weight = c.weight;
+  a.tiles = (int)(((long long)a.C * a.G + 127) / 128);
+  return a;
+}
+
+template <int DP, bool PAGED>
+static laser_status forward_typed(F32Args a, hipStream_t stream) {
+  if (!deal((long long)a.N * a.Hkv, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
+  history_f32_kernel<DP, PAGED><<<a.deal.grid, 256, 0, stream>>>(a);
+  return launch_status();
+}
+laser_status history_f32_launch(const HistoryArgs& h) {
+  const F32Args a = of_history(h);
+  return a.D > 64 ? forward_typed<128, false>(a, h.stream) : a.D > 32 ? forward_typed<64, false>(a, h.stream) : forward_typed<32, false>(a, h.stream);
+}
+laser_status cache_f32_launch(const CacheArgs& c, const CacheRuns& r) {
+  F32Args a = of_cache(c);
+  a.chunk = r.chunk, a.runs = r.runs, a.work = c.work;
+  const laser_status s = a.D > 64 ? forward_typed<128, true>(a, c.stream) : a.D > 32 ? forward_typed<64, true>(a, c.stream) : forward_typed<32, true>(a, c.stream);
+  return s == LASER_OK && r.runs > 1 ? cache_join_launch(c, r.chunk, r.runs) : s;
+}
+
+template <int DP>
+static laser_status backward_typed(F32Args a, hipStream_t stream) {
+  F32Args b = a;
+  const long long per = (long long)a.N * a.Hkv;
+  if (!deal(per, a.tiles, &a.deal) || !deal(per, ((long long)a.L + 127) / 128, &b.deal)) return LASER_ERR_SHAPE;
+  history_dq_f32_kernel<DP><<<a.deal.grid, 256, 0, stream>>>(a);
+  history_dkv_f32_kernel<DP><<<b.deal.grid, 256, 0, stream>>>(b);
+  return launch_status();
+}
+laser_status history_bwd_f32_launch(const HistoryBwdArgs& b) {
+  F32Args a = of_history(b.f);
+  a.go = static_cast<const float*>(b.go);
+  a.dq = static_cast<float*>(b.dq);
+  a.dk = static_cast<float*>(b.dk);
+  a.dv = static_cast<float*>(b.dv);
+  a.dqp = b.dqp, a.dkp = b.dkp, a.dvp = b.dvp;
+  a.work = b.work;
+  return a.D > 64 ? backward_typed<128>(a, b.f.stream) : a.D > 32 ? backward_typed<64>(a, b.f.stream) : backward_typed<32>(a, b.f.stream);
+}
+
+template <int DP>
+static laser_status weights_typed(const F32Args& a, hipStream_t stream) {
+  for (int u = 0; u < a.N; u += 65535) {
+    F32Args part = a;
+    part.off = a.off + u;
+    part.lens = a.lens + u;
+    part.pages = a.pages + (size_t)u * a.max_pages;
+    cache_weights_f32_kernel<DP><<<dim3((a.L + 127) / 128, a.N - u < 65535 ? a.N - u : 65535), 256, 0, stream>>>(part);
+  }
+  return launch_status();
+}
+laser_status cache_weights_f32_launch(const CacheArgs& c) {
+  const F32Args a = of_cache(c);
+  return a.D > 64 ? weights_typed<128>(a, c.stream) : a.D > 32 ? weights_typed<64>(a, c.stream) : weights_typed<32>(a, c.stream);
+}
+
+}  // namespace laser
