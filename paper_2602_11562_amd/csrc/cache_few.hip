@@ -16,20 +16,21 @@ template <int DP>
 struct FewShape {
   static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, TILE = 32 * ROW, GROUPS = 32 / RPI;
   static constexpr int REQ = 2 * GROUPS;                  // requests a tile
-  static constexpr int NST = DP == 128 ? 2 : 4;           // tiles of a wave
+  static constexpr int NST = DP == 128 ? 1 : 2;           // tiles of a wave
   static constexpr int WAVE = NST * 2 * TILE;             // its bytes
-  static constexpr int JOIN = DP * 33 * 4;                // what it joins with: [column][33 rows] of fp32
+  static constexpr int JOIN = DP * 32 * 4;                // what it joins with: [column][32 rows] of fp32, row r at r ^ column % 32
   static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
 };
 
 template <int DP>
-__global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, int G, MulDiv by_group, float scale, int chunk, int splits) {
+__global__ __launch_bounds__(256, 2) void cache_few_kernel(const CacheArgs a, int G, MulDiv by_group, float scale, int chunk, int splits) {
   using Sh = FewShape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * Sh::WAVE];
   __shared__ float join_m[4][32], join_l[4][32];
   const int per = a.U * a.Hkv;
-  const int split = blockIdx.x / per, uh = blockIdx.x % per, u = uh / a.Hkv, hk = uh % a.Hkv;
+  // (turned by one from run to run: a user's runs are not all one die's)
+  const int split = blockIdx.x / per, uh = (blockIdx.x + split) % per, u = uh / a.Hkv, hk = uh % a.Hkv;
   const CandRange cr = cand_range(a.off, u, a.C, a.T);
   const int rows = cr.count * G;
   if (rows == 0) return;
@@ -181,7 +182,10 @@ __global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, in
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) out[(db * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * 33 + l32] = acc[db][r];
+    for (int r = 0; r < 16; ++r) {
+      const int d = 8 * (r >> 2) + 4 * h + (r & 3);
+      out[(db * 32 + d) * 32 + (l32 ^ d)] = acc[db][r];
+    }
   if (h == 0) {
     join_m[wave][l32] = m;
     join_l[wave][l32] = l;
@@ -198,7 +202,7 @@ __global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, in
     for (int w = 0; w < 4; ++w) {
       const float mw = join_m[w][r], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
       sum = fmaf(join_l[w][r], c, sum);
-      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 33 + r], c, x);
+      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 32 + (r ^ (d & 31))], c, x);
     }
     x = sum > 0.0f ? x / sum : 0.0f;
     const float z = sum > 0.0f ? top + log2f(sum) : -INFINITY;
@@ -215,67 +219,110 @@ __global__ __launch_bounds__(256, 1) void cache_few_kernel(const CacheArgs a, in
   }
 }
 
-// Joins the runs' results of a row: a workgroup per row, its four waves share the runs
-template <typename T>
-__global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a, int chunk, int splits) {
-  __shared__ float part[4][128], part_s[4];
-  const int u = blockIdx.y, head = blockIdx.z;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+// Joins the runs' results of a row, a workgroup of NT threads each (a wave where rows are many): the runs' shares first, then their
+// outputs, 16 bytes a lane and as many runs at a time as there are lanes for.
+constexpr int MOST_RUNS = 1024;
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void cache_join_kernel(const CacheArgs a, int chunk, int splits) {
+  __shared__ float share[MOST_RUNS];
+  __shared__ __attribute__((aligned(16))) float part[NT * 4];
+  __shared__ float wave_top[NT / 64], wave_sum[NT / 64];
+  const int u = blockIdx.y, tid = threadIdx.x;
   const CandRange cr = cand_range(a.off, u, a.C, a.T);
   const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
   if (n <= chunk) return;   // one run: it has written the result
   const size_t all = (size_t)a.T * a.H;
   const float* z = a.work + splits * all * a.D;
-  for (int i = blockIdx.x; i < cr.count; i += gridDim.x) {
-    const size_t row = (size_t)(cr.first + i) * a.H + head;
+  const int pieces = a.D / 4, groups = NT / pieces, group = tid / pieces, piece = tid - group * pieces;
+  for (long long x = blockIdx.x; x < (long long)cr.count * a.H; x += gridDim.x) {
+    const int i = (int)(x / a.H);
+    const size_t row = (size_t)cr.first * a.H + x;
     const int seen = a.causal ? n - cr.count + i + 1 : n;
     const int runs = seen <= 0 ? 0 : (seen + chunk - 1) / chunk;
-    float top = -INFINITY;
-    for (int s = lane; s < runs; s += 64) top = fmaxf(top, z[s * all + row]);
-    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    float x0 = 0.0f, x1 = 0.0f, sum = 0.0f;
-    if (top > -INFINITY) {
-#pragma unroll 4
-      for (int s = wave; s < runs; s += 4) {
-        const float c = exp2f(z[s * all + row] - top);
-        const float* o = a.work + (s * all + row) * a.D;
-        sum += c;
-        if (lane < a.D) x0 = fmaf(c, o[lane], x0);
-        if (lane + 64 < a.D) x1 = fmaf(c, o[lane + 64], x1);
-      }
+    float mine[MOST_RUNS / NT], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < MOST_RUNS / NT; ++s) {
+      mine[s] = s * NT + tid < runs ? z[(s * NT + tid) * all + row] : -INFINITY;
+      top = fmaxf(top, mine[s]);
     }
-    part[wave][lane] = x0;
-    part[wave][lane + 64] = x1;
-    if (lane == 0) part_s[wave] = sum;
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if constexpr (NT > 64) {
+      if ((tid & 63) == 0) wave_top[tid >> 6] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, wave_top[w]);
+    }
+#pragma unroll
+    for (int s = 0; s < MOST_RUNS / NT; ++s)
+      if (s * NT + tid < runs) {
+        const float c = mine[s] == -INFINITY ? 0.0f : exp2f(mine[s] - top);
+        share[s * NT + tid] = c;
+        sum += c;
+      }
+    for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+    if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
     __syncthreads();
-    const float total = part_s[0] + part_s[1] + part_s[2] + part_s[3];
-    if (tid < a.D)
-      store_from_f32<T>(static_cast<T*>(a.o), row * a.D + tid,
-                        total > 0.0f ? (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / total : 0.0f);
-    if (tid == 0 && a.lse != nullptr) a.lse[row] = total > 0.0f ? (top + log2f(total)) * LN2 : -INFINITY;
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) sum += wave_sum[w];
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (group < groups) {
+      const float* at = a.work + row * a.D + piece * 4;
+      for (int s0 = group; s0 < runs; s0 += 4 * groups) {
+        f32x4 y[4];
+        float c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {   // (behind the last run: the last one again, with no share)
+          const int s = s0 + e * groups, k = s < runs ? s : runs - 1;
+          c[e] = s < runs ? share[k] : 0.0f;
+          y[e] = *reinterpret_cast<const f32x4*>(at + k * all * a.D);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[d] = fmaf(c[e], y[e][d], o[d]);
+      }
+      *reinterpret_cast<f32x4*>(part + (group * pieces + piece) * 4) = o;
+    }
+    __syncthreads();
+    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+    for (int d = tid; d < a.D; d += NT) {
+      float y = 0.0f;
+      for (int g = 0; g < groups; ++g) y += part[g * a.D + d];
+      store_from_f32<T>(static_cast<T*>(a.o), row * a.D + d, y * by);
+    }
+    if (tid == 0 && a.lse != nullptr) a.lse[row] = sum > 0.0f ? (top + log2f(sum)) * LN2 : -INFINITY;
     __syncthreads();
   }
 }
 
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {
+  const long long rows = (long long)a.C * a.H;
   for (int u = 0; u < a.U; u += 65535) {
     CacheArgs part = a;
     part.off = a.off + u;
     part.lens = a.lens + u;
-    const dim3 grid(a.C < 1024 ? a.C : 1024, a.U - u < 65535 ? a.U - u : 65535, a.H);
-    if (a.dt == LASER_F32) cache_join_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
-    else cache_join_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+    const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), a.U - u < 65535 ? a.U - u : 65535);
+    const bool wide = splits > 16;   // (254 runs of 128 columns: a wave takes ___ us for 16 rows, four waves ___)
+    if (wide) {
+      if (a.dt == LASER_F32) cache_join_kernel<float, 256><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+      else cache_join_kernel<unsigned short, 256><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+    } else {
+      if (a.dt == LASER_F32) cache_join_kernel<float, 64><<<grid, 64, 0, a.stream>>>(part, chunk, splits);
+      else cache_join_kernel<unsigned short, 64><<<grid, 64, 0, a.stream>>>(part, chunk, splits);
+    }
   }
   return launch_status();
 }
 
-// How the longest history is cut into runs, from what both the launch and the caller who provides the work buffer know: about two
-// workgroups a compute unit, runs of at least `least` items, whole tiles.
-CacheRuns cache_runs(int workgroups, int L, int least, int tile) {
-  const int want = workgroups > 0 && workgroups < 512 ? (512 + workgroups - 1) / workgroups : 1;
+// How the longest history is cut into runs of whole tiles, of `least` items or more: into as many as make `want` workgroups of all
+// users' histories together. Sizes alone decide, which the caller who provides the work buffer knows too.
+CacheRuns cache_runs(long long workgroups, int L, int want, int least, int tile) {
+  const long long wanted = (want + workgroups - 1) / workgroups;
   const int most = (L + least - 1) / least;
-  int runs = want < most ? want : most;
-  if (runs < 1) runs = 1;
+  int runs = wanted < most ? (int)wanted : most;
+  runs = runs < MOST_RUNS ? runs : MOST_RUNS;
   const int chunk = ((L + runs - 1) / runs + tile - 1) / tile * tile;
   return CacheRuns{chunk, (L + chunk - 1) / chunk};
 }

@@ -1,9 +1,8 @@
 // What the items of a cache receive from rows that attended to them (bf16, on the matrix cores): weight_j = sum over rows r and heads
 // of exp2(c q_r . k_j - lse_r).
 //
-// A wave owns 32 items; for each key-value head their keys are loaded once, straight into registers as the B operand (item in
-// lane), and the rows of the head's group pass through LDS in tiles of 64 that the workgroup's four waves share:
-//   Sc[row, item] = Q K^T,  then exp2 and a sum over the accumulators, which are rows: one number a lane at the end.
+// A wave owns 32 items; for each key-value head their keys are loaded once, straight into registers as the A operand, and the rows of the head's group pass through LDS in tiles of 64 that the workgroup's four waves share:
+//   Sc^T[item, row] = K Q^T,  then exp2 and a sum for every accumulator (an item), over the lanes only at the end.
 // For few rows this reads the keys and little else; for a chunk it costs half of the attention's products and its exponentials.
 #include <type_traits>
 
@@ -18,9 +17,9 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
   typedef float f32x4 __attribute__((ext_vector_type(4)));
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
-  const int u = blockIdx.y;
+  const int u = blockIdx.y;   // (users are turned against each other: their first items are not all one die's)
   const CandRange cr = cand_range(a.off, u, a.C, a.T);
-  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2), item0 = (int)blockIdx.x * NW * 32;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2), item0 = (int)((blockIdx.x + u) % gridDim.x) * NW * 32;
   if (item0 >= n) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
   const int rows = cr.count * G, first = item0 + wave * 32;
@@ -63,24 +62,24 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
   TileReader<DP> read(lane);
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   bf16x8 kreg[KS];
-  float sum = 0.0f;
+  // Sc^T[item, row] = K Q^T: rows in lanes, so a row's lse is one register and the items' sums stay apart until the end
+  f32x16 sums = zero;
+  const int wave_item = first - (n - cr.count);   // (causal: row r sees item j of the wave if r / G >= wave_item + j)
   auto step = [&](int r0, unsigned at, auto masked) __attribute__((always_inline)) {
     read.place_rows(at);
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       if (decltype(masked)::value && (r0 + rb * 32 >= rows || r0 + rb * 32 + 32 <= wave_from)) continue;
+      const float z = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at + Sh::BYTES + (rb * 32 + l32) * 4)) * LOG2E;
       f32x16 sc;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(0, rb, s), kreg[s], s == 0 ? zero : sc, 0, 0, 0);
+      for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[s], read.rows(0, rb, s), s == 0 ? zero : sc, 0, 0, 0);
+      const int r = r0 + rb * 32 + l32, seen = a.causal ? (int)by_group.div(r) - wave_item - 4 * h : 32;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(at + Sh::BYTES + (rb * 32 + g * 8 + h * 4) * 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[g * 4 + e], scale, -z[e] * LOG2E));
-          const int r = r0 + rb * 32 + g * 8 + h * 4 + e;
-          sum += decltype(masked)::value && (r < from || r >= rows) ? 0.0f : p;
-        }
+      for (int x = 0; x < 16; ++x) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[x], scale, -z));
+        if (decltype(masked)::value && (r >= rows || 8 * (x >> 2) + (x & 3) > seen)) continue;
+        sums[x] += p;
       }
     }
   };
@@ -111,7 +110,17 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
       }
     }
   }
-  sum = half_sum(sum);
+  // over the 32 lanes of a half: with every step a lane keeps half of its items, at last lane l the sum of accumulator l / 2
+#pragma unroll
+  for (int step = 16, left = 8; step > 1; step >>= 1, left >>= 1)
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      if (x < left) {
+        const float keep = l32 & step ? sums[x + left] : sums[x], give = l32 & step ? sums[x] : sums[x + left];
+        sums[x] = keep + __shfl_xor(give, step);
+      }
+  sums[0] += __shfl_xor(sums[0], 1);
+  const float sum = __shfl(sums[0], ((l32 >> 2) & 1) * 32 + 2 * ((l32 >> 3) * 4 + (l32 & 3)));   // to the lane that has the item
   if (h == 0 && inside && there) {
     float* w = a.weight + (slot << a.page_log2) + place;
     if (a.add) unsafeAtomicAdd(w, sum);

@@ -60,7 +60,7 @@ struct CacheArgs {
 size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status cache_attention_launch(const CacheArgs& a);
 struct CacheRuns { int chunk, runs; };   // histories of up to L items are cut into runs of `chunk`
-CacheRuns cache_runs(int workgroups, int L, int least, int tile);
+CacheRuns cache_runs(long long workgroups, int L, int want, int least, int tile);
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits);
 laser_status cache_few_launch(const CacheArgs& a, const CacheRuns& r);    // bf16, at most 32 rows a key-value head
 laser_status cache_tile_launch(const CacheArgs& a, const CacheRuns& r);   // bf16

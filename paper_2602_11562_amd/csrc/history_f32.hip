@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_f32_kernel(const F32Args
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const int u = blockIdx.y;
   const CandRange cr = cand_range(a.off, u, a.C, a.T);
-  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.log2), item0 = (int)blockIdx.x * 128;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.log2), item0 = (int)((blockIdx.x + u) % gridDim.x) * 128;   // (see cache_weights.hip)
   if (item0 >= n) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
   const int rows = cr.count * a.G, first = item0 + wave * 32, mine = first + l32, j = mine < n ? mine : n - 1;
