@@ -219,12 +219,13 @@ __global__ __launch_bounds__(256, 2) void cache_few_kernel(const CacheArgs a, in
   }
 }
 
-// Joins the runs' results of a row, a workgroup of NT threads each (a wave where rows are many): the runs' shares first, then their
+// Joins the runs' results of a row, a workgroup each: the runs' shares first, then their
 // outputs, 16 bytes a lane and as many runs at a time as there are lanes for.
 constexpr int MOST_RUNS = 1024;
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void cache_join_kernel(const CacheArgs a, int chunk, int splits) {
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a, int chunk, int splits) {
+  constexpr int NT = 256;
   __shared__ float share[MOST_RUNS];
   __shared__ __attribute__((aligned(16))) float part[NT * 4];
   __shared__ float wave_top[NT / 64], wave_sum[NT / 64];
@@ -247,12 +248,10 @@ __global__ __launch_bounds__(NT) void cache_join_kernel(const CacheArgs a, int c
       top = fmaxf(top, mine[s]);
     }
     for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if constexpr (NT > 64) {
-      if ((tid & 63) == 0) wave_top[tid >> 6] = top;
-      __syncthreads();
+    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
+    __syncthreads();
 #pragma unroll
-      for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, wave_top[w]);
-    }
+    for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, wave_top[w]);
 #pragma unroll
     for (int s = 0; s < MOST_RUNS / NT; ++s)
       if (s * NT + tid < runs) {
@@ -297,20 +296,77 @@ __global__ __launch_bounds__(NT) void cache_join_kernel(const CacheArgs a, int c
   }
 }
 
+// The same for few runs: a thread per row and 16 bytes
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_few_kernel(const CacheArgs a, int chunk, int splits, MulDiv by_pieces, MulDiv by_heads) {
+  const int u = blockIdx.y;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
+  if (n <= chunk) return;
+  const size_t all = (size_t)a.T * a.H;
+  const float* z = a.work + splits * all * a.D;
+  const unsigned pieces = a.D / 4, e = blockIdx.x * 256 + threadIdx.x, x = by_pieces.div(e), piece = e - x * pieces;
+  if (x >= (unsigned)(cr.count * a.H)) return;
+  const int i = (int)by_heads.div(x);
+  const size_t row = (size_t)cr.first * a.H + x;
+  const int seen = a.causal ? n - cr.count + i + 1 : n;
+  const int runs = seen <= 0 ? 0 : (seen + chunk - 1) / chunk;
+  const float* at = a.work + row * a.D + piece * 4;
+  float top = -INFINITY, sum = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < runs; s0 += 4) {
+    float zs[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {   // (behind the last run: the last one again, with no share)
+      const int k = s0 + s < runs ? s0 + s : runs - 1;
+      zs[s] = z[k * all + row];
+      y[s] = *reinterpret_cast<const f32x4*>(at + k * all * a.D);
+    }
+    float next = top;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) next = fmaxf(next, zs[s]);
+    if (next == -INFINITY) continue;
+    const float old = exp2f(top - next);
+    top = next;
+    sum *= old;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] *= old;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const float c = s0 + s < runs ? exp2f(zs[s] - top) : 0.0f;
+      sum += c;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) o[d] = fmaf(c, y[s][d], o[d]);
+    }
+  }
+  const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + row * a.D + piece * 4) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+  } else {
+    *reinterpret_cast<u32x2*>(static_cast<unsigned short*>(a.o) + row * a.D + piece * 4) = u32x2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
+  }
+  if (piece == 0 && a.lse != nullptr) a.lse[row] = sum > 0.0f ? (top + log2f(sum)) * LN2 : -INFINITY;
+}
+
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {
   const long long rows = (long long)a.C * a.H;
   for (int u = 0; u < a.U; u += 65535) {
     CacheArgs part = a;
     part.off = a.off + u;
     part.lens = a.lens + u;
-    const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), a.U - u < 65535 ? a.U - u : 65535);
-    const bool wide = splits > 16;   // (254 runs of 128 columns: a wave takes ___ us for 16 rows, four waves ___)
-    if (wide) {
-      if (a.dt == LASER_F32) cache_join_kernel<float, 256><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
-      else cache_join_kernel<unsigned short, 256><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+    const unsigned users = a.U - u < 65535 ? a.U - u : 65535;
+    if (splits > 16) {   // (16 rows of 128 columns in 127 runs: 5.3 us; 40000 rows in four runs: 18 us by the other, 31 by this one)
+      const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), users);
+      if (a.dt == LASER_F32) cache_join_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
+      else cache_join_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
     } else {
-      if (a.dt == LASER_F32) cache_join_kernel<float, 64><<<grid, 64, 0, a.stream>>>(part, chunk, splits);
-      else cache_join_kernel<unsigned short, 64><<<grid, 64, 0, a.stream>>>(part, chunk, splits);
+      const long long threads = rows * (a.D / 4);
+      if (threads > 0x7fffff00LL) return LASER_ERR_SHAPE;
+      const dim3 grid((unsigned)((threads + 255) / 256), users);
+      const MulDiv pieces = mul_div(a.D / 4), heads = mul_div(a.H);
+      if (a.dt == LASER_F32) cache_join_few_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits, pieces, heads);
+      else cache_join_few_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits, pieces, heads);
     }
   }
   return launch_status();

@@ -91,15 +91,23 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
   }
   const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
   const bool short_pages = PAGED && MINE > 8 && a.log2 == 3;   // a wave's rows are on two pages
-  int ids[2][2];   // of the next pair: pages of the wave's keys and values
+  // The table's next 64 entries wait in the lanes of a register, and those of the next pair are read from there: a scalar load under way
+  // would make every wait for LDS in between a wait for all of them (chunks of 512 over 10000 items: ___ us so, ___ by scalar loads).
+  int ids[2][2], window = 0, window_at = -64;
   auto first_of = [&](int u, int kind) { return begin + (u < 0 ? 0 : u * TI + (kind ? 0 : 32)) + wave * MINE; };
   auto look_up = [&](int u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
+      const int lowest = first_of(u, 1) >> a.log2, highest = (first_of(u, 0) + 8) >> a.log2;
+      if (highest >= window_at + 64) {
+        window_at = lowest;
+        const int x = window_at + lane, most = (end - 1) >> a.log2;
+        window = table[x < most ? x : most];
+      }
 #pragma unroll
       for (int kind = 0; kind < 2; ++kind) {
         const int j = first_of(u, kind);
-        ids[kind][0] = j < end ? scalar_int(table, j >> a.log2) : -1;
-        if (short_pages) ids[kind][1] = j + 8 < end ? scalar_int(table, (j + 8) >> a.log2) : -1;
+        ids[kind][0] = j < end ? __builtin_amdgcn_readlane(window, (j >> a.log2) - window_at) : -1;
+        if (short_pages) ids[kind][1] = j + 8 < end ? __builtin_amdgcn_readlane(window, ((j + 8) >> a.log2) - window_at) : -1;
       }
     }
   };
