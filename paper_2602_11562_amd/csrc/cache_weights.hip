@@ -41,23 +41,33 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
   start = start < 0 ? 0 : start / TI * TI;
   const int tiles = rows > start ? (rows - start + TI - 1) / TI : 0;   // of each key-value head
 
+  // (offsets as in history_backward.hip: the same in every tile of whole tokens)
+  const bool whole_tokens = TI % G == 0;
+  unsigned qoff[GPW], zoff;
+  auto offsets = [&](int r0, int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < GPW; ++x) {
+      const int in = (wave + x * NW) * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
+      const int i = (int)by_group.div(r), head = r - i * G;
+      qoff[x] = c * 8 < a.D ? (unsigned)(((i - i0) * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN;
+    }
+    const int r = r0 + lane, i = (int)by_group.div(r);
+    zoff = (unsigned)((i - i0) * a.H + r - i * G) * 4;
+  };
+  if (whole_tokens) offsets(0, 0);
   auto fetch = [&](int hk, int r0, unsigned at) __attribute__((always_inline)) {
     const int i0 = (int)by_group.div(r0);
+    if (!whole_tokens) offsets(r0, i0);
     const size_t tok = (size_t)cr.first + i0, head0 = (size_t)hk * G;
-    const u32x4 qb = buffer_of(q + tok * a.qp + head0 * a.D, 0x7fffffffu);
+    const int more = cr.count - 1 - i0 < TI ? cr.count - 1 - i0 : TI;   // whole tokens within reach behind the first
+    const u32x4 qb = buffer_of(q + tok * a.qp + head0 * a.D, (unsigned)((more * (int)a.qp + G * a.D) * 2));
 #pragma unroll
     for (int x = 0; x < GPW; ++x) {
       const int g = wave + x * NW;
       if (Sh::GROUPS % NW != 0 && g >= Sh::GROUPS) break;
-      const int in = g * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in), r = r0 + in;
-      const int i = (int)by_group.div(r), head = r - i * G;
-      buffer_to_lds16(qb, r < rows && c * 8 < a.D ? (unsigned)(((i - i0) * (int)a.qp + head * a.D + c * 8) * 2) : NO_COLUMN, at + g * 1024);
+      buffer_to_lds16(qb, qoff[x], at + g * 1024);
     }
-    if (wave == 0) {
-      const int r = r0 + lane, i = (int)by_group.div(r), head = r - i * G;
-      buffer_to_lds4(buffer_of(a.lse + tok * a.H + head0, 0x7fffffffu), r < rows ? (unsigned)((i - i0) * a.H + head) * 4 : NO_COLUMN,
-                     at + Sh::BYTES);
-    }
+    if (wave == 0) buffer_to_lds4(buffer_of(a.lse + tok * a.H + head0, (unsigned)(more * a.H + G) * 4), zoff, at + Sh::BYTES);
   };
   TileReader<DP> read(lane);
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};

@@ -94,7 +94,7 @@ static bool few_rows(int C, int H, int Hkv, laser_dtype dt) { return dt == LASER
 static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
   const bool few = few_rows(C, H, Hkv, dt);
   const long long tiles = few ? 1 : ((long long)C * (H / Hkv) + 127) / 128;
-  const int want = tuning_int("LASER_CACHE_WANT", few ? 1024 : 1024), least = tuning_int("LASER_CACHE_LEAST", few ? 512 : 256);
+  const int want = tuning_int("LASER_CACHE_WANT", few ? 1024 : 2048), least = tuning_int("LASER_CACHE_LEAST", few ? 512 : 256);
   return cache_runs(tiles * U * Hkv, L, want, least, few ? 128 : 64);
 }
 size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
