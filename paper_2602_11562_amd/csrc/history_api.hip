@@ -93,9 +93,10 @@ laser_status cache_weights_launch(const CacheArgs& a) {
 static bool few_rows(int C, int H, int Hkv, laser_dtype dt) { return dt == LASER_BF16 && (long long)C * (H / Hkv) <= 32; }
 static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
   const bool few = few_rows(C, H, Hkv, dt);
-  const long long tiles = few ? 1 : ((long long)C * (H / Hkv) + 127) / 128;
-  const int want = tuning_int("LASER_CACHE_WANT", few ? 1024 : 2048), least = tuning_int("LASER_CACHE_LEAST", few ? 512 : 256);
-  return cache_runs(tiles * U * Hkv, L, want, least, few ? 128 : 64);
+  const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
+  // (a single-precision tile takes its waves 1.7 us for 64 columns, so its runs may be short: one tile for each of four waves)
+  if (dt == LASER_F32) return cache_runs((rows + 127) / 128 * pairs, L, 1024, 128, 128);
+  return few ? cache_runs(pairs, L, 1024, 512, 128) : cache_runs((rows + 127) / 128 * pairs, L, 2048, 256, 64);
 }
 size_t cache_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const CacheRuns r = runs_of(U, C, L, H, Hkv, dt);

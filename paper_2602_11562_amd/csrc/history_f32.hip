@@ -6,6 +6,10 @@
 // four further, and the A operand is one float a lane, 32 columns side by side. Products take 16 times as long as bf16's, so tiles of
 // 32 rows, no second tile of registers and no ordering by hand: everything else is behind them (a large product in this
 // precision reaches 154 TFLOP/s on this card).
+//
+// Every kernel but the weights' has two forms. Wide: the four waves of a workgroup own 32 rows (items) each and share the tiles they walk.
+// SPLIT: the workgroup owns 32, its waves take the tiles in turn, each through a place of its own, and are summed up at the end; four
+// times the workgroups with a quarter of the way, for calls whose wide workgroups would not fill the machine.
 #include "history_tile.h"
 
 namespace laser {
@@ -18,7 +22,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // and so are 32 columns of two rows four apart (rows of 256 bytes and more).
 template <int DP>
 struct F32Tile {
-  static constexpr int ROW = DP * 4, CH = DP / 4, RPI = 64 / CH, BYTES = FI * ROW, NW = 4, MINE = FI / NW, RPW = MINE / RPI;
+  static constexpr int ROW = DP * 4, CH = DP / 4, RPI = 64 / CH, BYTES = FI * ROW;
   static __device__ __forceinline__ int swz(int r) {
     return CH >= 16 ? (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3 : (r >> 1) & 7;
   }
@@ -98,58 +102,86 @@ __device__ __forceinline__ void store_row(float* row, const f32x16* acc, float b
 
 __device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
-// Requests for tiles of items: wave w brings eight rows of keys and of values, which a page of eight or more holds together
-template <int DP, bool PAGED>
+// Requests for tiles of items, in eights of rows, which a page of eight or more holds together: of a shared tile wave w brings the
+// eight w, of a tile of its own all four
+template <int DP, bool PAGED, bool SPLIT>
 struct F32Items {
   using Sh = F32Tile<DP>;
-  unsigned koff[Sh::RPW], voff[Sh::RPW];
-  int wave, id;
+  static constexpr int EIGHTS = SPLIT ? 4 : 1, PER = 8 / Sh::RPI;
+  unsigned koff[EIGHTS][PER], voff[EIGHTS][PER];
+  int wave, ids[EIGHTS];
+  __device__ __forceinline__ int row_of(int x) const { return SPLIT ? x * 8 : wave * 8; }
   __device__ __forceinline__ void init(const F32Args& a, int wave_, int lane) {
     wave = wave_;
-    id = -1;
 #pragma unroll
-    for (int x = 0; x < Sh::RPW; ++x) {
-      const int in = x * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(wave * Sh::MINE + in);
-      koff[x] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.kp) + c * 4) * 4) : NO_COLUMN;
-      voff[x] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.vp) + c * 4) * 4) : NO_COLUMN;
-    }
+    for (int x = 0; x < EIGHTS; ++x)
+#pragma unroll
+      for (int y = 0; y < PER; ++y) {
+        const int in = y * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(row_of(x) + in);
+        koff[x][y] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.kp) + c * 4) * 4) : NO_COLUMN;
+        voff[x][y] = c * 4 < a.D ? (unsigned)((in * (PAGED ? a.D : (int)a.vp) + c * 4) * 4) : NO_COLUMN;
+      }
   }
   __device__ __forceinline__ void look_up(const F32Args& a, const int32_t* table, int t0, int n) {
-    const int j = t0 + wave * Sh::MINE;
-    if (PAGED) id = j < n ? scalar_int(table, j >> a.log2) : -1;
+    if (PAGED)
+#pragma unroll
+      for (int x = 0; x < EIGHTS; ++x) {
+        const int j = t0 + row_of(x);
+        ids[x] = j < n ? scalar_int(table, j >> a.log2) : -1;
+      }
   }
   // items t0 and on of n
   __device__ __forceinline__ void fetch(const F32Args& a, size_t first, int hk, int t0, int n, unsigned at) const {
-    const int j = t0 + wave * Sh::MINE;
-    int left = n - j < Sh::MINE ? n - j : Sh::MINE;
-    const float *k, *v;
-    if constexpr (PAGED) {
-      if ((unsigned)id >= (unsigned)a.P) left = 0;
-      const size_t row = left > 0 ? (((size_t)id * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
-      k = a.k + row * a.D;
-      v = a.v + row * a.D;
-    } else {
-      const size_t row = left > 0 ? first + j : first;
-      k = a.k + row * a.kp + (size_t)hk * a.D;
-      v = a.v + row * a.vp + (size_t)hk * a.D;
-    }
-    const int kp = PAGED ? a.D : (int)a.kp, vp = PAGED ? a.D : (int)a.vp;
-    const u32x4 kb = buffer_of(k, left > 0 ? (unsigned)(((left - 1) * kp + a.D) * 4) : 0u);
-    const u32x4 vb = buffer_of(v, left > 0 ? (unsigned)(((left - 1) * vp + a.D) * 4) : 0u);
-    const unsigned to = at + wave * Sh::MINE * Sh::ROW;
 #pragma unroll
-    for (int x = 0; x < Sh::RPW; ++x) {
-      buffer_to_lds16(kb, koff[x], to + x * 1024);
-      buffer_to_lds16(vb, voff[x], to + Sh::BYTES + x * 1024);
+    for (int x = 0; x < EIGHTS; ++x) {
+      const int j = t0 + row_of(x);
+      int left = n - j < 8 ? n - j : 8;
+      const float *k, *v;
+      if constexpr (PAGED) {
+        if ((unsigned)ids[x] >= (unsigned)a.P) left = 0;
+        const size_t row = left > 0 ? (((size_t)ids[x] * a.Hkv + hk) << a.log2) + (j & ((1 << a.log2) - 1)) : 0;
+        k = a.k + row * a.D;
+        v = a.v + row * a.D;
+      } else {
+        const size_t row = left > 0 ? first + j : first;
+        k = a.k + row * a.kp + (size_t)hk * a.D;
+        v = a.v + row * a.vp + (size_t)hk * a.D;
+      }
+      const int kp = PAGED ? a.D : (int)a.kp, vp = PAGED ? a.D : (int)a.vp;
+      const u32x4 kb = buffer_of(k, left > 0 ? (unsigned)(((left - 1) * kp + a.D) * 4) : 0u);
+      const u32x4 vb = buffer_of(v, left > 0 ? (unsigned)(((left - 1) * vp + a.D) * 4) : 0u);
+      const unsigned to = at + row_of(x) * Sh::ROW;
+#pragma unroll
+      for (int y = 0; y < PER; ++y) {
+        buffer_to_lds16(kb, koff[x][y], to + y * 1024);
+        buffer_to_lds16(vb, voff[x][y], to + Sh::BYTES + y * 1024);
+      }
     }
   }
 };
 
-template <int DP, bool PAGED>
-__global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
+// SPLIT: the waves' accumulators in LDS, [column][32 rows], row r of column d at r ^ d % 32, in the place of each wave's tile
+template <int DP>
+__device__ __forceinline__ void leave(unsigned char* place, const f32x16* acc, int lane) {
+  float* out = reinterpret_cast<float*>(place);
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int d = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+      out[(db * 32 + d) * 32 + ((lane & 31) ^ d)] = acc[db][r];
+    }
+}
+__device__ __forceinline__ float left_by(const unsigned char* place, int r, int d) {
+  return reinterpret_cast<const float*>(place)[d * 32 + (r ^ (d & 31))];
+}
+
+template <int DP, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT && DP > 64 ? 1 : 2) void history_f32_kernel(const F32Args a) {
   using Sh = F32Tile<DP>;
-  constexpr int DB = DP / 32, ROWS = 128, STAGE = 2 * Sh::BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  constexpr int DB = DP / 32, ROWS = SPLIT ? 32 : 128, STAGE = 2 * Sh::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[(SPLIT ? 4 : 2) * STAGE];
+  __shared__ float join_m[SPLIT ? 4 : 1][32], join_l[SPLIT ? 4 : 1][32];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -178,17 +210,19 @@ __global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
     end = end < begin + a.chunk ? end : begin + a.chunk;
   }
   const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
-  F32Items<DP, PAGED> items;
+  F32Items<DP, PAGED, SPLIT> items;
   items.init(a, wave, lane);
-  if (end > begin) {
-    items.look_up(a, table, begin, n);
-    items.fetch(a, (size_t)cr.first, hk, begin, n, lds);
-    items.look_up(a, table, begin + FI, n);
+  const int first_tile = begin + (SPLIT ? wave * FI : 0), stride = SPLIT ? 4 * FI : FI;
+  unsigned at = lds + (SPLIT ? wave * STAGE : 0), other = at + STAGE;
+  if (end > first_tile) {
+    items.look_up(a, table, first_tile, n);
+    items.fetch(a, (size_t)cr.first, hk, first_tile, n, at);
+    items.look_up(a, table, first_tile + stride, n);
   }
 
-  const int mine = row0 + wave * 32 + l32, r = mine < rows ? mine : rows - 1, i = (int)a.by_group.div(r), head = hk * a.G + r - i * a.G;
+  const int mine = row0 + (SPLIT ? 0 : wave * 32) + l32, r = mine < rows ? mine : rows - 1, i = (int)a.by_group.div(r), head = hk * a.G + r - i * a.G;
   const size_t tok = (size_t)cr.first + i;
-  const bool busy = row0 + wave * 32 < rows;
+  const bool busy = SPLIT || row0 + wave * 32 < rows;
   const int last = a.causal ? n - cr.count + i : n - 1;
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = busy ? __builtin_amdgcn_readlane(last, 31) : -1;
   f32x4 q[DP / 8];
@@ -204,13 +238,16 @@ __global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = splat(0.0f);
   float m = -INFINITY, l = 0.0f;
-  unsigned at = lds, other = lds + STAGE;
-  for (int t0 = begin; t0 < end; t0 += FI) {
+  for (int t0 = first_tile; t0 < end; t0 += stride) {
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    barrier_lds();
-    if (t0 + FI < end) {
-      items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
-      items.look_up(a, table, t0 + 2 * FI, n);
+    if constexpr (!SPLIT) {
+      barrier_lds();
+      if (t0 + FI < end) {
+        items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
+        items.look_up(a, table, t0 + 2 * FI, n);
+      }
+    } else {
+      asm volatile("" ::: "memory");
     }
     if (t0 <= wave_last) {
       f32x16 sc = over_width<DP>(at, q, splat(0.0f), lane);
@@ -246,9 +283,51 @@ __global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
       }
       over_rows<DP>(at + Sh::BYTES, sc, acc, lane);
     }
-    const unsigned x = at;
-    at = other;
-    other = x;
+    if constexpr (SPLIT) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again
+      if (t0 + stride < end) {
+        items.fetch(a, (size_t)cr.first, hk, t0 + stride, n, at);
+        items.look_up(a, table, t0 + 2 * stride, n);
+      }
+    } else {
+      const unsigned x = at;
+      at = other;
+      other = x;
+    }
+  }
+  if constexpr (SPLIT) {
+    l = half_sum(l);
+    leave<DP>(smem + wave * STAGE, acc, lane);
+    if (h == 0) {
+      join_m[wave][l32] = m;
+      join_l[wave][l32] = l;
+    }
+    __syncthreads();
+    const int here = rows - row0 < 32 ? rows - row0 : 32;
+    for (int e = threadIdx.x; e < here * a.D; e += 256) {
+      const int x = e / a.D, d = e - x * a.D;
+      float top = -INFINITY, sum = 0.0f, o = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, join_m[w][x]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float mw = join_m[w][x], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
+        sum = fmaf(join_l[w][x], c, sum);
+        o = fmaf(left_by(smem + w * STAGE, x, d), c, o);
+      }
+      const float by = sum > 0.0f ? 1.0f / sum : 0.0f, z = sum > 0.0f ? top + log2f(sum) : -INFINITY;
+      const int tk = (int)a.by_group.div(row0 + x);
+      const size_t to = (size_t)(cr.first + tk) * a.H + hk * a.G + row0 + x - tk * a.G;
+      if (joined) {
+        const size_t all = (size_t)a.T * a.H;
+        a.work[(run * all + to) * a.D + d] = o * by;
+        if (d == 0) a.work[a.runs * all * a.D + run * all + to] = z;
+      } else {
+        a.o[to * a.D + d] = o * by;
+        if (d == 0 && a.lse != nullptr) a.lse[to] = z * LN2;
+      }
+    }
+    return;
   }
   if (mine >= rows) return;
   const float sum = half_sum(l), inv = sum > 0.0f ? 1.0f / sum : 0.0f, z = sum > 0.0f ? m + log2f(sum) : -INFINITY;
@@ -263,11 +342,11 @@ __global__ __launch_bounds__(256, 2) void history_f32_kernel(const F32Args a) {
   }
 }
 
-template <int DP>
+template <int DP, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a) {
   using Sh = F32Tile<DP>;
-  constexpr int DB = DP / 32, ROWS = 128, STAGE = 2 * Sh::BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  constexpr int DB = DP / 32, ROWS = SPLIT ? 32 : 128, STAGE = 2 * Sh::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[(SPLIT ? 4 : 2) * STAGE];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -277,14 +356,16 @@ __global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a)
   if (row0 >= rows) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
   const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
-  F32Items<DP, false> items;
+  F32Items<DP, false, SPLIT> items;
   items.init(a, wave, lane);
-  items.fetch(a, (size_t)cr.first, hk, 0, n, lds);
+  const int first_tile = SPLIT ? wave * FI : 0, stride = SPLIT ? 4 * FI : FI;
+  unsigned at = lds + (SPLIT ? wave * STAGE : 0), other = at + STAGE;
+  if (end > first_tile) items.fetch(a, (size_t)cr.first, hk, first_tile, n, at);
 
-  const int mine = row0 + wave * 32 + l32, r = mine < rows ? mine : rows - 1, last = (int)a.by_group.div(r), head = hk * a.G + r - last * a.G;
+  const int mine = row0 + (SPLIT ? 0 : wave * 32) + l32, r = mine < rows ? mine : rows - 1, last = (int)a.by_group.div(r), head = hk * a.G + r - last * a.G;
   const size_t tok = (size_t)cr.first + last, row = tok * a.H + head;
   const int wave_first = __builtin_amdgcn_readlane(last, 0);
-  const int wave_last = row0 + wave * 32 < rows ? __builtin_amdgcn_readlane(last, 31) : -1;
+  const int wave_last = SPLIT || row0 + wave * 32 < rows ? __builtin_amdgcn_readlane(last, 31) : -1;
   f32x4 q[DP / 8], go[DP / 8], o[DP / 8];
   load_row<DP>(q, a.q + tok * a.qp + (size_t)head * a.D, a.D, h);
   load_row<DP>(go, a.go + row * a.D, a.D, h);
@@ -296,18 +377,21 @@ __global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a)
     for (int e = 0; e < 4; ++e) delta = fmaf(go[x][e], o[x][e], delta);
   delta = half_sum(delta);
   const float lse2 = a.lse[row] * LOG2E;
-  if (h == 0 && mine < rows) {
+  if (h == 0 && mine < rows && (!SPLIT || wave == 0)) {
     a.work[row * 2] = -a.lse[row] * a.gamma;
     a.work[row * 2 + 1] = -delta;
   }
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = splat(0.0f);
-  unsigned at = lds, other = lds + STAGE;
-  for (int t0 = 0; t0 < end; t0 += FI) {
+  for (int t0 = first_tile; t0 < end; t0 += stride) {
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    barrier_lds();
-    if (t0 + FI < end) items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
+    if constexpr (!SPLIT) {
+      barrier_lds();
+      if (t0 + FI < end) items.fetch(a, (size_t)cr.first, hk, t0 + FI, n, other);
+    } else {
+      asm volatile("" ::: "memory");
+    }
     if (t0 <= wave_last) {
       f32x16 sc = over_width<DP>(at, q, splat(0.0f), lane);
       const f32x16 dp = over_width<DP>(at + Sh::BYTES, go, splat(-delta), lane);
@@ -318,35 +402,50 @@ __global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a)
       }
       over_rows<DP>(at, sc, acc, lane);
     }
-    const unsigned x = at;
-    at = other;
-    other = x;
+    if constexpr (SPLIT) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (t0 + stride < end) items.fetch(a, (size_t)cr.first, hk, t0 + stride, n, at);
+    } else {
+      const unsigned x = at;
+      at = other;
+      other = x;
+    }
+  }
+  if constexpr (SPLIT) {
+    leave<DP>(smem + wave * STAGE, acc, lane);
+    __syncthreads();
+    const int here = rows - row0 < 32 ? rows - row0 : 32;
+    for (int e = threadIdx.x; e < here * a.D; e += 256) {
+      const int x = e / a.D, d = e - x * a.D, tk = (int)a.by_group.div(row0 + x);
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) sum += left_by(smem + w * STAGE, x, d);
+      a.dq[(size_t)(cr.first + tk) * a.dqp + (size_t)(hk * a.G + row0 + x - tk * a.G) * a.D + d] = sum * a.inv_gamma;
+    }
+    return;
   }
   if (mine < rows) store_row<DP>(a.dq + tok * a.dqp + (size_t)head * a.D, acc, a.inv_gamma, a.D, h);
 }
 
-// Requests for tiles of a group's rows: one tensor's rows of 32, offsets from the first token's
+// Requests for tiles of a group's rows, of one tensor: `pitch` between tokens of p (at the tile's first token i0 and the group's first
+// head), `more` tokens within reach behind the first; the eight `eight` of the tile
 template <int DP>
-struct F32Rows {
+__device__ __forceinline__ void fetch_rows(const F32Args& a, const float* p, int pitch, int r0, int i0, int more, unsigned at, int eight, int lane) {
   using Sh = F32Tile<DP>;
-  // `pitch` between tokens of p (at the tile's first token and the group's first head), n - i0 tokens left
-  static __device__ __forceinline__ void fetch(const F32Args& a, const float* p, int pitch, int r0, int i0, int more, unsigned at, int wave, int lane) {
-    const u32x4 b = buffer_of(p, (unsigned)((more * pitch + a.G * a.D) * 4));
+  const u32x4 b = buffer_of(p, (unsigned)((more * pitch + a.G * a.D) * 4));
 #pragma unroll
-    for (int x = 0; x < Sh::RPW; ++x) {
-      const int in = wave * Sh::MINE + x * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(in), r = r0 + in;
-      const int i = (int)a.by_group.div(r), head = r - i * a.G;
-      buffer_to_lds16(b, c * 4 < a.D ? (unsigned)(((i - i0) * pitch + head * a.D + c * 4) * 4) : NO_COLUMN,
-                      at + wave * Sh::MINE * Sh::ROW + x * 1024);
-    }
+  for (int x = 0; x < 8 / Sh::RPI; ++x) {
+    const int in = eight * 8 + x * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ Sh::swz(in), r = r0 + in;
+    const int i = (int)a.by_group.div(r), head = r - i * a.G;
+    buffer_to_lds16(b, c * 4 < a.D ? (unsigned)(((i - i0) * pitch + head * a.D + c * 4) * 4) : NO_COLUMN, at + eight * 8 * Sh::ROW + x * 1024);
   }
-};
+}
 
-template <int DP>
+template <int DP, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a) {
   using Sh = F32Tile<DP>;
-  constexpr int DB = DP / 32, ITEMS = 128, STAGE = 2 * Sh::BYTES + 1024;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  constexpr int DB = DP / 32, ITEMS = SPLIT ? 32 : 128, STAGE = 2 * Sh::BYTES + 1024;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[(SPLIT ? 4 : 2) * STAGE];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -355,20 +454,26 @@ __global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a
   const int n = cr.count, item0 = tile * ITEMS;
   if (item0 >= n) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
-  const int rows = n * a.G, first = item0 + wave * 32, head0 = hk * a.G;
+  const int rows = n * a.G, first = item0 + (SPLIT ? 0 : wave * 32), head0 = hk * a.G;
   auto fetch = [&](int r0, unsigned at) {
     const int i0 = (int)a.by_group.div(r0), more = n - 1 - i0 < FI ? n - 1 - i0 : FI;
     const size_t tok = (size_t)cr.first + i0;
-    F32Rows<DP>::fetch(a, a.q + tok * a.qp + (size_t)head0 * a.D, (int)a.qp, r0, i0, more, at, wave, lane);
-    F32Rows<DP>::fetch(a, a.go + (tok * a.H + head0) * a.D, a.H * a.D, r0, i0, more, at + Sh::BYTES, wave, lane);
-    if (wave == 0) {
+#pragma unroll
+    for (int x = 0; x < (SPLIT ? 4 : 1); ++x) {
+      const int eight = SPLIT ? x : wave;
+      fetch_rows<DP>(a, a.q + tok * a.qp + (size_t)head0 * a.D, (int)a.qp, r0, i0, more, at, eight, lane);
+      fetch_rows<DP>(a, a.go + (tok * a.H + head0) * a.D, a.H * a.D, r0, i0, more, at + Sh::BYTES, eight, lane);
+    }
+    if (SPLIT || wave == 0) {
       const int r = r0 + l32, i = (int)a.by_group.div(r);
       buffer_to_lds4(buffer_of(a.work + (tok * a.H + head0) * 2, (unsigned)(more * a.H + a.G) * 8),
                      (unsigned)((i - i0) * a.H + r - i * a.G) * 8 + h * 4, at + 2 * Sh::BYTES);
     }
   };
   const int start = item0 * a.G / FI * FI, turns = (rows - start + FI - 1) / FI;
-  fetch(start + (turns - 1) * FI, lds);
+  const int first_turn = turns - 1 - (SPLIT ? wave : 0), stride = SPLIT ? 4 : 1;
+  unsigned at = lds + (SPLIT ? wave * STAGE : 0), other = at + STAGE;
+  if (first_turn >= 0) fetch(start + first_turn * FI, at);
   const int mine = first + l32, j = mine < n ? mine : n - 1, from = j * a.G;
   const size_t item = (size_t)cr.first + j;
   const int wave_from = __builtin_amdgcn_readlane(from, 0);
@@ -379,12 +484,15 @@ __global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = splat(0.0f);
-  unsigned at = lds, other = lds + STAGE;
-  for (int t = turns - 1; t >= 0; --t) {
+  for (int t = first_turn; t >= 0; t -= stride) {
     const int r0 = start + t * FI;
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    barrier_lds();
-    if (t > 0) fetch(r0 - FI, other);
+    if constexpr (!SPLIT) {
+      barrier_lds();
+      if (t > 0) fetch(r0 - FI, other);
+    } else {
+      asm volatile("" ::: "memory");
+    }
     if (r0 > floor) {
       f32x16 sc, dp;
 #pragma unroll
@@ -406,9 +514,33 @@ __global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a
       over_rows<DP>(at + Sh::BYTES, sc, dv, lane);
       over_rows<DP>(at, dp, dk, lane);
     }
-    const unsigned x = at;
-    at = other;
-    other = x;
+    if constexpr (SPLIT) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (t >= stride) fetch(r0 - stride * FI, at);
+    } else {
+      const unsigned x = at;
+      at = other;
+      other = x;
+    }
+  }
+  if constexpr (SPLIT) {
+    leave<DP>(smem + wave * STAGE, dk, lane);
+    leave<DP>(smem + wave * STAGE + Sh::BYTES, dv, lane);
+    __syncthreads();
+    const int here = n - item0 < 32 ? n - item0 : 32;
+    for (int e = threadIdx.x; e < here * a.D; e += 256) {
+      const int x = e / a.D, d = e - x * a.D;
+      float k_sum = 0.0f, v_sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        k_sum += left_by(smem + w * STAGE, x, d);
+        v_sum += left_by(smem + w * STAGE + Sh::BYTES, x, d);
+      }
+      const size_t to = (size_t)(cr.first + item0 + x);
+      a.dk[to * a.dkp + (size_t)hk * a.D + d] = k_sum * a.inv_gamma;
+      a.dv[to * a.dvp + (size_t)hk * a.D + d] = v_sum;
+    }
+    return;
   }
   if (mine >= n) return;
   store_row<DP>(a.dk + item * a.dkp + (size_t)hk * a.D, dk, a.inv_gamma, a.D, h);
@@ -437,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_f32_kernel(const F32Args
   auto fetch = [&](int hk, int r0, unsigned at) {
     const int i0 = (int)a.by_group.div(r0), more = cr.count - 1 - i0 < FI ? cr.count - 1 - i0 : FI;
     const size_t tok = (size_t)cr.first + i0, head0 = (size_t)hk * a.G;
-    F32Rows<DP>::fetch(a, a.q + tok * a.qp + head0 * a.D, (int)a.qp, r0, i0, more, at, wave, lane);
+    fetch_rows<DP>(a, a.q + tok * a.qp + head0 * a.D, (int)a.qp, r0, i0, more, at, wave, lane);
     if (wave == 0) {
       const int r = r0 + l32, i = (int)a.by_group.div(r);
       buffer_to_lds4(buffer_of(a.lse + tok * a.H + head0, (unsigned)(more * a.H + a.G) * 4), (unsigned)((i - i0) * a.H + r - i * a.G) * 4,
@@ -497,7 +629,6 @@ static F32Args of_history(const HistoryArgs& h) {
   a.runs = 1;
   a.o = static_cast<float*>(h.o);
   a.lse = h.lse;
-  a.tiles = (int)(((long long)a.L * a.G + 127) / 128);
   return a;
 }
 static F32Args of_cache(const CacheArgs& c) {
@@ -515,14 +646,20 @@ static F32Args of_cache(const CacheArgs& c) {
   a.o = static_cast<float*>(c.o);
   a.lse = c.lse;
   a.weight = c.weight;
-  a.tiles = (int)(((long long)a.C * a.G + 127) / 128);
   return a;
 }
 
+// The split form where the wide one's workgroups are fewer than two a compute unit, or hold rows for one or two of their waves only
+static bool splits(long long workgroups, long long rows_of_a_pair) { return workgroups < 512 || rows_of_a_pair <= 64; }
+
 template <int DP, bool PAGED>
 static laser_status forward_typed(F32Args a, hipStream_t stream) {
-  if (!deal((long long)a.N * a.Hkv, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
-  history_f32_kernel<DP, PAGED><<<a.deal.grid, 256, 0, stream>>>(a);
+  const long long rows = (long long)a.C * a.G, per = (long long)a.N * a.Hkv;
+  const bool split = splits((rows + 127) / 128 * a.runs * per, rows);
+  a.tiles = (int)((rows + (split ? 31 : 127)) / (split ? 32 : 128));
+  if (!deal(per, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
+  if (split) history_f32_kernel<DP, PAGED, true><<<a.deal.grid, 256, 0, stream>>>(a);
+  else history_f32_kernel<DP, PAGED, false><<<a.deal.grid, 256, 0, stream>>>(a);
   return launch_status();
 }
 laser_status history_f32_launch(const HistoryArgs& h) {
@@ -539,10 +676,15 @@ laser_status cache_f32_launch(const CacheArgs& c, const CacheRuns& r) {
 template <int DP>
 static laser_status backward_typed(F32Args a, hipStream_t stream) {
   F32Args b = a;
-  const long long per = (long long)a.N * a.Hkv;
-  if (!deal(per, a.tiles, &a.deal) || !deal(per, ((long long)a.L + 127) / 128, &b.deal)) return LASER_ERR_SHAPE;
-  history_dq_f32_kernel<DP><<<a.deal.grid, 256, 0, stream>>>(a);
-  history_dkv_f32_kernel<DP><<<b.deal.grid, 256, 0, stream>>>(b);
+  const long long per = (long long)a.N * a.Hkv, rows = (long long)a.L * a.G;
+  const bool split_rows = splits((rows + 127) / 128 * per, rows), split_items = splits(((long long)a.L + 127) / 128 * per, a.L);
+  if (!deal(per, (rows + (split_rows ? 31 : 127)) / (split_rows ? 32 : 128), &a.deal) ||
+      !deal(per, ((long long)a.L + (split_items ? 31 : 127)) / (split_items ? 32 : 128), &b.deal))
+    return LASER_ERR_SHAPE;
+  if (split_rows) history_dq_f32_kernel<DP, true><<<a.deal.grid, 256, 0, stream>>>(a);
+  else history_dq_f32_kernel<DP, false><<<a.deal.grid, 256, 0, stream>>>(a);
+  if (split_items) history_dkv_f32_kernel<DP, true><<<b.deal.grid, 256, 0, stream>>>(b);
+  else history_dkv_f32_kernel<DP, false><<<b.deal.grid, 256, 0, stream>>>(b);
   return launch_status();
 }
 laser_status history_bwd_f32_launch(const HistoryBwdArgs& b) {
