@@ -795,67 +795,65 @@ def laser_forward(q, k, v, t0, wq, wk, wv, lens, w: int, gamma: float, seg_out=N
 
 
 # ----------------------------------------------------------------------------- attention among a history's items
-def _placed(tensors: dict):
-    """The one device that all of the given tensors live on, and on which the call is to be made."""
-    device = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{name} must live in device memory")
-        if device is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
-        device = t.device
-    return device
+# (A small call is a few microseconds of kernels: each attribute of a tensor is read once here, and names are only put together for
+# errors. Four heads over 60 items: 13.3 us a call through the general helpers, 7 so, on a slow core.)
+def _one_device(names: str, *tensors) -> int:
+    """The index of the device that all of the given tensors live on."""
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != index or index < 0):
+            for name, x in zip(names.split(), tensors):
+                if x is not None and x.get_device() < 0:
+                    raise ValueError(f"{name} must live in device memory")
+            raise ValueError(f"{names} must live on one device")
+    return index
 
 
-class _On:
-    """Makes a device and, where one is given, a stream current for a call: kernels run there, and what the call allocates
-    belongs there. The ordinary call (current device, no stream) costs one comparison."""
-
-    def __init__(self, device, stream):
-        torch = _torch()
-        if stream is not None and getattr(stream, "device", device) != device:
-            raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
-        self.other = stream is not None or torch._C._cuda_getDevice() != device.index
-        if self.other:
-            self.contexts = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
-
-    def __enter__(self):
-        if self.other:
-            for c in self.contexts:
-                c.__enter__()
-
-    def __exit__(self, *error):
-        if self.other:
-            for c in reversed(self.contexts):
-                c.__exit__(*error)
+def _there(index: int, stream, call):
+    """call() with the device, and the stream where one is given, current: kernels run there, and what is allocated belongs there."""
+    torch = _torch()
+    if stream is None and torch._C._cuda_getDevice() == index:
+        return call()
+    if stream is not None and stream.device_index != index:
+        raise ValueError(f"the stream is of device {stream.device_index}, the tensors are on {index}")
+    with torch.cuda.device(index):
+        if stream is None:
+            return call()
+        with torch.cuda.stream(stream):
+            return call()
 
 
-def _rows(t, name: str, heads_shape=None):
-    """Pointer and pitch (elements between tokens) of [tokens, heads, D] whose heads lie side by side; tokens may be apart."""
+def _pitch(t, name: str, shape) -> int:
+    """Elements between the tokens of a [tokens, heads, D] tensor of this shape whose heads lie side by side; tokens may be apart."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    n, heads, D = shape
+    tokens, head, column = t.stride()
+    if (column != 1 and D > 1) or (head != D and heads > 1):
+        raise ValueError(f"the heads of {name} must lie side by side within a token")
+    return tokens if n > 1 else heads * D
+
+
+def _flat(t, name: str, shape, dtype) -> int:
+    """Pointer of a contiguous tensor of this shape and type."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _heads_of(t, name: str):
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, D]")
-    if heads_shape is not None and tuple(t.shape) != tuple(heads_shape):
-        raise ValueError(f"{name} must be {list(heads_shape)}, got {list(t.shape)}")
-    n, heads, D = t.shape
-    if (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
-        raise ValueError(f"the heads of {name} must lie side by side within a token")
-    return t.data_ptr(), (t.stride(0) if n > 1 else heads * D)
+    return t.shape
 
 
-def _given(t, name: str, shape, dtype, device):
-    """An output: the caller's, if it fits, or a new one."""
-    if t is None:
-        return _torch().empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name} must be {list(shape)} of {dtype}")
-    return t
-
-
-def _off(off, name: str = "off"):
+def _parts_of(off) -> int:
     if off.dim() != 1 or off.shape[0] < 2:
-        raise ValueError(f"{name} must be [N + 1]")
+        raise ValueError("off must be [N + 1]")
     return off.shape[0] - 1
 
 
@@ -863,21 +861,25 @@ def laser_history_attention_forward(q, k, v, off, L_max: int, gamma: float, o_ou
     """Causal attention over packed sequences: q [T,H,D], k, v [T,H_kv,D] (column blocks of one tensor will do), off int32 [N+1],
     L_max at least the longest sequence -> (o [T,H,D], lse [T,H] fp32). Rows of no sequence are not written."""
     torch = _torch()
-    device = _placed({"q": q, "k": k, "v": v, "off": off, "o_out": o_out, "lse_out": lse_out})
-    qp, q_pitch = _rows(q, "q")
-    T, H, D = q.shape
-    kp, k_pitch = _rows(k, "k", (T, k.shape[1], D))
-    vp, v_pitch = _rows(v, "v", k.shape)
-    if k.dtype != q.dtype or v.dtype != q.dtype:
+    index = _one_device("q k v off o_out lse_out", q, k, v, off, o_out, lse_out)
+    shape, dtype = _heads_of(q, "q"), q.dtype
+    T, H, D = shape
+    kv = (T, _heads_of(k, "k")[1], D)
+    if k.dtype != dtype or v.dtype != dtype:
         raise TypeError("q, k, v must share a dtype")
-    with _On(device, stream):
-        o_out = _given(o_out, "o_out", (T, H, D), q.dtype, device)
-        lse_out = _given(lse_out, "lse_out", (T, H), torch.float32, device)
-        code = load_library().laser_history_attention_forward(
-            qp, q_pitch, kp, k_pitch, vp, v_pitch, _ptr(off, "off", torch.int32), _off(off), T, int(L_max), H, k.shape[1], D,
-            float(gamma), _dt(q), _ptr(o_out, "o_out"), _ptr(lse_out, "lse_out"), _stream(stream))
-    _check(code, "laser_history_attention_forward")
-    return o_out, lse_out
+
+    def call():
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if o_out is None else o_out
+        lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if lse_out is None else lse_out
+        N = _parts_of(off)
+        _check(load_library().laser_history_attention_forward(
+            q.data_ptr(), _pitch(q, "q", shape), k.data_ptr(), _pitch(k, "k", kv), v.data_ptr(), _pitch(v, "v", kv),
+            _flat(off, "off", (N + 1,), torch.int32), N, T, int(L_max), H, kv[1], D, float(gamma), _dt(q),
+            _flat(o, "o_out", shape, dtype), _flat(lse, "lse_out", (T, H), torch.float32), _stream(stream)),
+            "laser_history_attention_forward")
+        return o, lse
+
+    return _there(index, stream, call)
 
 
 def laser_history_attention_backward_work_bytes(N: int, T: int, L_max: int, H: int, H_kv: int, D: int, dt: int) -> int:
@@ -889,76 +891,63 @@ def laser_history_attention_backward(q, k, v, o, lse, d_o, off, L_max: int, gamm
     """Gradients of laser_history_attention_forward: o [T,H,D], lse [T,H] as it returned them, d_o [T,H,D] ->
     (dq [T,H,D], dk [T,H_kv,D], dv [T,H_kv,D]) in the dtype of q. The outputs may be column blocks of one tensor."""
     torch = _torch()
-    device = _placed({"q": q, "k": k, "v": v, "o": o, "lse": lse, "d_o": d_o, "off": off, "dq_out": dq_out, "dk_out": dk_out,
-                      "dv_out": dv_out, "work": work})
-    qp, q_pitch = _rows(q, "q")
-    T, H, D = q.shape
-    kp, k_pitch = _rows(k, "k", (T, k.shape[1], D))
-    vp, v_pitch = _rows(v, "v", k.shape)
-    if any(x.dtype != q.dtype for x in (k, v, o, d_o)):
-        raise TypeError("q, k, v, o and d_o must share a dtype")
-    if tuple(o.shape) != (T, H, D) or tuple(d_o.shape) != (T, H, D) or tuple(lse.shape) != (T, H):
-        raise ValueError("o and d_o must be [T,H,D], lse [T,H]")
-    N, Hkv, lib = _off(off), k.shape[1], load_library()
-    with _On(device, stream):
-        dq_out = _given(dq_out, "dq_out", (T, H, D), q.dtype, device)
-        dk_out = _given(dk_out, "dk_out", (T, Hkv, D), q.dtype, device)
-        dv_out = _given(dv_out, "dv_out", (T, Hkv, D), q.dtype, device)
-        if work is None:
-            need = lib.laser_history_attention_backward_work_bytes(N, T, int(L_max), H, Hkv, D, _dt(q))
-            work = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-        (dqp, dq_pitch), (dkp, dk_pitch), (dvp, dv_pitch) = _rows(dq_out, "dq_out"), _rows(dk_out, "dk_out"), _rows(dv_out, "dv_out")
-        code = lib.laser_history_attention_backward(
-            qp, q_pitch, kp, k_pitch, vp, v_pitch, _ptr(o, "o"), _ptr(lse, "lse", torch.float32), _ptr(d_o, "d_o"),
-            _ptr(off, "off", torch.int32), N, T, int(L_max), H, Hkv, D, float(gamma), _dt(q), dqp, dq_pitch, dkp, dk_pitch, dvp,
-            dv_pitch, _ptr(work, "work"), work.numel() * work.element_size(), _stream(stream))
-    _check(code, "laser_history_attention_backward")
-    return dq_out, dk_out, dv_out
+    index = _one_device("q k v o lse d_o off dq_out dk_out dv_out work", q, k, v, o, lse, d_o, off, dq_out, dk_out, dv_out, work)
+    shape, dtype = _heads_of(q, "q"), q.dtype
+    T, H, D = shape
+    kv = (T, _heads_of(k, "k")[1], D)
+    if k.dtype != dtype or v.dtype != dtype or any(x is not None and x.dtype != dtype for x in (dq_out, dk_out, dv_out)):
+        raise TypeError("q, k, v and the gradients must share a dtype")
+
+    def call():
+        N, lib = _parts_of(off), load_library()
+        dq = torch.empty(shape, dtype=dtype, device=q.device) if dq_out is None else dq_out
+        dk = torch.empty(kv, dtype=dtype, device=q.device) if dk_out is None else dk_out
+        dv = torch.empty(kv, dtype=dtype, device=q.device) if dv_out is None else dv_out
+        room = work
+        if room is None:
+            need = lib.laser_history_attention_backward_work_bytes(N, T, int(L_max), H, kv[1], D, _dt(q))
+            room = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        _check(lib.laser_history_attention_backward(
+            q.data_ptr(), _pitch(q, "q", shape), k.data_ptr(), _pitch(k, "k", kv), v.data_ptr(), _pitch(v, "v", kv),
+            _flat(o, "o", shape, dtype), _flat(lse, "lse", (T, H), torch.float32), _flat(d_o, "d_o", shape, dtype),
+            _flat(off, "off", (N + 1,), torch.int32), N, T, int(L_max), H, kv[1], D, float(gamma), _dt(q),
+            dq.data_ptr(), _pitch(dq, "dq_out", shape), dk.data_ptr(), _pitch(dk, "dk_out", kv), dv.data_ptr(),
+            _pitch(dv, "dv_out", kv), _ptr(room, "work"), room.numel() * room.element_size(), _stream(stream)),
+            "laser_history_attention_backward")
+        return dq, dk, dv
+
+    return _there(index, stream, call)
 
 
-def _cache_shape(k_cache, v_cache, pages, lens):
-    """(P, H_kv, page, D, U, max_pages) of a paged cache and its table."""
-    torch = _torch()
-    if k_cache.dim() != 4 or tuple(v_cache.shape) != tuple(k_cache.shape):
-        raise ValueError("k_cache and v_cache must both be [P, H_kv, page, D]")
-    if v_cache.dtype != k_cache.dtype:
-        raise TypeError("k_cache and v_cache must share a dtype")
-    if pages.dim() != 2 or tuple(lens.shape) != (pages.shape[0],):
-        raise ValueError("pages must be [U, max_pages], lens [U]")
-    if pages.dtype != torch.int32 or lens.dtype != torch.int32:
-        raise TypeError("pages and lens must be int32")
-    return (*k_cache.shape, *pages.shape)
-
-
-def _of_users(off, U: int) -> None:
-    if tuple(off.shape) != (U + 1,):
-        raise ValueError("off must be [U + 1]")
-
-
-def _weight(weight, P: int, page: int):
-    if weight is not None and tuple(weight.shape) != (P, page):
-        raise ValueError("weight must be [P, page]")
-    return _ptr(weight, "weight", _torch().float32)
+def _cache_of(k_cache, v_cache, pages, lens):
+    """(P, H_kv, page, D, U, max_pages) of a paged cache and its table, and the pointers of all four."""
+    i32 = _torch().int32
+    if k_cache.dim() != 4 or pages.dim() != 2:
+        raise ValueError("k_cache and v_cache must be [P, H_kv, page, D], pages [U, max_pages]")
+    shape, table = k_cache.shape, pages.shape
+    k = _flat(k_cache, "k_cache", shape, k_cache.dtype)
+    v = k if v_cache is k_cache else _flat(v_cache, "v_cache", shape, k_cache.dtype)
+    return (*shape, *table), k, v, _flat(pages, "pages", table, i32), _flat(lens, "lens", (table[0],), i32)
 
 
 def laser_cache_append(k, v, k_cache, v_cache, off, pages, lens, C_max: int, L_max: int, weight=None, stream=None):
     """New keys and values [T,H_kv,D], packed by off int32 [U+1] (at most C_max a user), become the last items of each user's
     lens [U] in k_cache, v_cache [P,H_kv,page,D]; pages int32 [U,max_pages]. weight [P,page]: their places are set to 0."""
     torch = _torch()
-    device = _placed({"k": k, "v": v, "k_cache": k_cache, "v_cache": v_cache, "off": off, "pages": pages, "lens": lens,
-                      "weight": weight})
-    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
-    kp, k_pitch = _rows(k, "k", (k.shape[0], Hkv, D))
-    vp, v_pitch = _rows(v, "v", k.shape)
+    index = _one_device("k v k_cache v_cache off pages lens weight", k, v, k_cache, v_cache, off, pages, lens, weight)
+    (P, Hkv, page, D, U, max_pages), kc, vc, table, held = _cache_of(k_cache, v_cache, pages, lens)
+    shape = (_heads_of(k, "k")[0], Hkv, D)
     if k.dtype != k_cache.dtype or v.dtype != k_cache.dtype:
         raise TypeError("k, v must have the dtype of the cache")
-    _of_users(off, U)
-    with _On(device, stream):
-        code = load_library().laser_cache_append(
-            kp, k_pitch, vp, v_pitch, _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(off, "off", torch.int32),
-            _ptr(pages, "pages"), _ptr(lens, "lens"), U, k.shape[0], int(C_max), P, page, max_pages, int(L_max), Hkv, D,
-            _dt(k_cache), _weight(weight, P, page), _stream(stream))
-    _check(code, "laser_cache_append")
+
+    def call():
+        _check(load_library().laser_cache_append(
+            k.data_ptr(), _pitch(k, "k", shape), v.data_ptr(), _pitch(v, "v", shape), kc, vc,
+            _flat(off, "off", (U + 1,), torch.int32), table, held, U, shape[0], int(C_max), P, page, max_pages, int(L_max), Hkv, D,
+            _dt(k_cache), None if weight is None else _flat(weight, "weight", (P, page), torch.float32), _stream(stream)),
+            "laser_cache_append")
+
+    _there(index, stream, call)
 
 
 def laser_cache_attention_work_bytes(U: int, T: int, C_max: int, L_max: int, H: int, H_kv: int, D: int, dt: int) -> int:
@@ -970,28 +959,30 @@ def laser_cache_attention_forward(q, k_cache, v_cache, off, pages, lens, C_max: 
     """Queries [T,H,D], packed by off int32 [U+1] (at most C_max a user), over each user's cached items -> (o [T,H,D], lse [T,H]).
     causal: the queries are those of the cache's last items, each sees the items up to its own; otherwise (candidates) all."""
     torch = _torch()
-    device = _placed({"q": q, "k_cache": k_cache, "v_cache": v_cache, "off": off, "pages": pages, "lens": lens,
-                      "o_out": o_out, "lse_out": lse_out, "work": work})
-    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
-    T, H = q.shape[0], q.shape[1]
-    qp, q_pitch = _rows(q, "q", (T, H, D))
-    if q.dtype != k_cache.dtype:
+    index = _one_device("q k_cache v_cache off pages lens o_out lse_out work", q, k_cache, v_cache, off, pages, lens, o_out, lse_out,
+                        work)
+    (P, Hkv, page, D, U, max_pages), kc, vc, table, held = _cache_of(k_cache, v_cache, pages, lens)
+    T, H, _ = _heads_of(q, "q")
+    shape, dtype = (T, H, D), q.dtype
+    if dtype != k_cache.dtype:
         raise TypeError("q must have the dtype of the cache")
-    _of_users(off, U)
-    lib = load_library()
-    with _On(device, stream):
-        o_out = _given(o_out, "o_out", (T, H, D), q.dtype, device)
-        lse_out = _given(lse_out, "lse_out", (T, H), torch.float32, device)
-        if work is None:
+
+    def call():
+        lib = load_library()
+        o = torch.empty(shape, dtype=dtype, device=q.device) if o_out is None else o_out
+        lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if lse_out is None else lse_out
+        room = work
+        if room is None:
             need = lib.laser_cache_attention_work_bytes(U, T, int(C_max), int(L_max), H, Hkv, D, _dt(q))
-            work = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-        code = lib.laser_cache_attention_forward(
-            qp, q_pitch, _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(off, "off", torch.int32),
-            _ptr(pages, "pages"), _ptr(lens, "lens"), U, T, int(C_max), P, page, max_pages, int(L_max), H, Hkv, D, float(gamma),
-            int(bool(causal)), _dt(q), _ptr(o_out, "o_out"), _ptr(lse_out, "lse_out"), _ptr(work, "work"),
-            work.numel() * work.element_size(), _stream(stream))
-    _check(code, "laser_cache_attention_forward")
-    return o_out, lse_out
+            room = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        _check(lib.laser_cache_attention_forward(
+            q.data_ptr(), _pitch(q, "q", shape), kc, vc, _flat(off, "off", (U + 1,), torch.int32), table, held, U, T, int(C_max), P,
+            page, max_pages, int(L_max), H, Hkv, D, float(gamma), 1 if causal else 0, _dt(q), _flat(o, "o_out", shape, dtype),
+            _flat(lse, "lse_out", (T, H), torch.float32), _ptr(room, "work"), room.numel() * room.element_size(), _stream(stream)),
+            "laser_cache_attention_forward")
+        return o, lse
+
+    return _there(index, stream, call)
 
 
 def laser_cache_weights(q, lse, k_cache, off, pages, lens, C_max: int, L_max: int, gamma: float, weight, causal: bool = True,
@@ -999,22 +990,21 @@ def laser_cache_weights(q, lse, k_cache, off, pages, lens, C_max: int, L_max: in
     """What each cached item received from the queries of laser_cache_attention_forward, summed over queries and heads, into
     weight [P,page] fp32 (add: onto what stands there). lse [T,H] as that call returned it. Returns weight."""
     torch = _torch()
-    device = _placed({"q": q, "lse": lse, "k_cache": k_cache, "off": off, "pages": pages, "lens": lens, "weight": weight})
-    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, k_cache, pages, lens)
-    T, H = q.shape[0], q.shape[1]
-    qp, q_pitch = _rows(q, "q", (T, H, D))
+    index = _one_device("q lse k_cache off pages lens weight", q, lse, k_cache, off, pages, lens, weight)
+    (P, Hkv, page, D, U, max_pages), kc, _, table, held = _cache_of(k_cache, k_cache, pages, lens)
+    T, H, _ = _heads_of(q, "q")
     if q.dtype != k_cache.dtype:
         raise TypeError("q must have the dtype of the cache")
-    if tuple(lse.shape) != (T, H):
-        raise ValueError("lse must be [T,H]")
-    _of_users(off, U)
-    with _On(device, stream):
-        code = load_library().laser_cache_weights(
-            qp, q_pitch, _ptr(lse, "lse", torch.float32), _ptr(k_cache, "k_cache"), _ptr(off, "off", torch.int32),
-            _ptr(pages, "pages"), _ptr(lens, "lens"), U, T, int(C_max), P, page, max_pages, int(L_max), H, Hkv, D, float(gamma),
-            int(bool(causal)), int(bool(add)), _dt(q), _weight(weight, P, page), _stream(stream))
-    _check(code, "laser_cache_weights")
-    return weight
+
+    def call():
+        _check(load_library().laser_cache_weights(
+            q.data_ptr(), _pitch(q, "q", (T, H, D)), _flat(lse, "lse", (T, H), torch.float32), kc,
+            _flat(off, "off", (U + 1,), torch.int32), table, held, U, T, int(C_max), P, page, max_pages, int(L_max), H, Hkv, D,
+            float(gamma), 1 if causal else 0, 1 if add else 0, _dt(q), _flat(weight, "weight", (P, page), torch.float32),
+            _stream(stream)), "laser_cache_weights")
+        return weight
+
+    return _there(index, stream, call)
 
 
 def laser_cache_evict(k_cache, v_cache, weight, pages, lens, pages_out, budget: int, recent: int, L_max: int, lens_out=None,
@@ -1023,18 +1013,21 @@ def laser_cache_evict(k_cache, v_cache, weight, pages, lens, pages_out, budget: 
     order and with their weights, into the pages of pages_out int32 [U,max_pages_out] -> (lens [U], kept [U,budget], the old
     places, -1 behind the last)."""
     torch = _torch()
-    device = _placed({"k_cache": k_cache, "v_cache": v_cache, "weight": weight, "pages": pages, "lens": lens,
-                      "pages_out": pages_out, "lens_out": lens_out, "kept_out": kept_out})
-    P, Hkv, page, D, U, max_pages = _cache_shape(k_cache, v_cache, pages, lens)
+    index = _one_device("k_cache v_cache weight pages lens pages_out lens_out kept_out", k_cache, v_cache, weight, pages, lens,
+                        pages_out, lens_out, kept_out)
+    (P, Hkv, page, D, U, max_pages), kc, vc, table, held = _cache_of(k_cache, v_cache, pages, lens)
+    budget, i32 = int(budget), torch.int32
     if pages_out.dim() != 2 or pages_out.shape[0] != U:
         raise ValueError("pages_out must be [U, max_pages_out]")
-    budget = int(budget)
-    with _On(device, stream):
-        lens_out = _given(lens_out, "lens_out", (U,), torch.int32, device)
-        kept_out = _given(kept_out, "kept_out", (U, max(budget, 0)), torch.int32, device)
-        code = load_library().laser_cache_evict(
-            _ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _weight(weight, P, page), _ptr(pages, "pages"),
-            _ptr(lens, "lens"), _ptr(pages_out, "pages_out", torch.int32), U, P, page, max_pages, pages_out.shape[1], int(L_max),
-            budget, int(recent), Hkv, D, _dt(k_cache), _ptr(lens_out, "lens_out"), _ptr(kept_out, "kept_out"), _stream(stream))
-    _check(code, "laser_cache_evict")
-    return lens_out, kept_out
+
+    def call():
+        left = torch.empty((U,), dtype=i32, device=lens.device) if lens_out is None else lens_out
+        kept = torch.empty((U, max(budget, 0)), dtype=i32, device=lens.device) if kept_out is None else kept_out
+        _check(load_library().laser_cache_evict(
+            kc, vc, _flat(weight, "weight", (P, page), torch.float32), table, held, _flat(pages_out, "pages_out", pages_out.shape, i32),
+            U, P, page, max_pages, pages_out.shape[1], int(L_max), budget, int(recent), Hkv, D, _dt(k_cache),
+            _flat(left, "lens_out", (U,), i32), _flat(kept, "kept_out", (U, max(budget, 0)), i32), _stream(stream)),
+            "laser_cache_evict")
+        return left, kept
+
+    return _there(index, stream, call)

@@ -361,9 +361,7 @@ laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {
       if (a.dt == LASER_F32) cache_join_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
       else cache_join_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits);
     } else {
-      const long long threads = rows * (a.D / 4);
-      if (threads > 0x7fffff00LL) return LASER_ERR_SHAPE;
-      const dim3 grid((unsigned)((threads + 255) / 256), users);
+      const dim3 grid((unsigned)((rows * (a.D / 4) + 255) / 256), users);   // (rows are few enough to be cut into runs)
       const MulDiv pieces = mul_div(a.D / 4), heads = mul_div(a.H);
       if (a.dt == LASER_F32) cache_join_few_kernel<float><<<grid, 256, 0, a.stream>>>(part, chunk, splits, pieces, heads);
       else cache_join_few_kernel<unsigned short><<<grid, 256, 0, a.stream>>>(part, chunk, splits, pieces, heads);
