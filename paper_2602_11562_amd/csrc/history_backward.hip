@@ -77,12 +77,11 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     }
     delta = half_sum(sum);
     lse2 = a.lse[tok * a.H + head] * LOG2E;
-    if (h == 0 && first + l32 < rows) {
-      a.rows[(tok * a.H + head) * 2] = -a.lse[tok * a.H + head] * a.gamma;
-      a.rows[(tok * a.H + head) * 2 + 1] = -delta;
-    }
   }
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
+  // o is as stored, in bf16, and what that costs delta weighs most where a row sees few items (against dq, 2^-9 / sqrt of their number).
+  // Rows that see one block have their delta from that block instead, as the sum of p dp.
+  const bool one_block = wave_last < 32;
   const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;
 
   f32x16 acc[DB];
@@ -120,6 +119,12 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
       __builtin_amdgcn_sched_group_barrier(0x402, 32 / KS, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (one_block) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum = fmaf(sc[r], dp[r], sum);
+      delta = half_sum(sum);
+    }
     bf16x8 kt[2][DB];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -155,6 +160,12 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     const unsigned x = at;
     at = other;
     other = x;
+  }
+  if (h == 0 && first + l32 < rows) {
+    const int head = hk * a.G + first + l32 - last * a.G;
+    float* row = a.rows + ((size_t)(cr.first + last) * a.H + head) * 2;
+    row[0] = -lse2 * LN2 * a.gamma;
+    row[1] = -delta;
   }
   barrier_lds();
   store_block<DP>(acc, a.inv_gamma, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
