@@ -51,7 +51,7 @@ laser_status cache_append_launch(const CacheAppendArgs& a) {
 // Which items stay: the `recent` last ones and, of the others, the budget - recent heaviest (of equal ones the first). A
 // workgroup per user finds the weight of the last one that stays by four passes over the weights, eight bits of the key a pass
 // (a key orders as its float does, NaN below everything), then lists the items that stay in order by counting them.
-constexpr int SEL = 1024;
+constexpr int SEL = 1024, HELD = 8;
 
 __device__ __forceinline__ unsigned weight_key(float w) {
   if (w != w) return 0u;
@@ -84,6 +84,16 @@ __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restri
     const int page = table[j >> log2];
     return (unsigned)page < (unsigned)P ? weight_key(weight[((size_t)page << log2) + (j & ((1 << log2) - 1))]) : 0u;
   };
+  // a thread's first keys wait in registers; a longer history's others are read again in every pass
+  unsigned keys[HELD];
+#pragma unroll
+  for (int x = 0; x < HELD; ++x) keys[x] = x * SEL + tid < old ? key_of(x * SEL + tid) : 0u;
+  auto each = [&](auto&& use) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < HELD; ++x)
+      if (x * SEL + tid < old) use(keys[x]);
+    for (int j = HELD * SEL + tid; j < old; j += SEL) use(key_of(j));
+  };
   unsigned limit = 0xffffffffu;            // the smallest key that stays
   int ties = 0;                            // how many of the items with that key stay
   if (want > 0) {
@@ -92,10 +102,9 @@ __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restri
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int b = tid; b < 256; b += SEL) hist[b] = 0;
       __syncthreads();
-      for (int j = tid; j < old; j += SEL) {
-        const unsigned key = key_of(j);
+      each([&](unsigned key) {
         if (shift == 24 || (key >> (shift + 8)) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1);
-      }
+      });
       __syncthreads();
       if (tid < 64) {   // the digit in which the items counted from the heaviest reach `left`
         int mine[4], sum = 0;
@@ -123,9 +132,9 @@ __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restri
     ties = left;
   }
   int at = 0, tied = 0;                    // items listed so far, and those of them with the limit's key
-  for (int base = 0; base < n; base += SEL) {
+  auto list = [&](int base, unsigned held, bool is_held) __attribute__((always_inline)) {
     const int j = base + tid;
-    const unsigned key = j < old ? key_of(j) : 0u;
+    const unsigned key = is_held ? held : j < old ? key_of(j) : 0u;
     const bool tie = want > 0 && j < old && key == limit;
     const unsigned long long ties_here = __ballot(tie), under = (1ull << lane) - 1;
     if (lane == 0) wave_tie[wave] = __popcll(ties_here);
@@ -147,7 +156,11 @@ __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restri
     if (keep) out[before + __popcll(keeps & under)] = j;
     at += all;
     tied += tie_all;
-  }
+  };
+#pragma unroll
+  for (int x = 0; x < HELD; ++x)
+    if (x * SEL < n) list(x * SEL, keys[x], true);
+  for (int base = HELD * SEL; base < n; base += SEL) list(base, 0u, false);
 }
 
 // The items that stay into their new pages, with their weights: a thread per 16 bytes of a key row and of a value row. Bound by

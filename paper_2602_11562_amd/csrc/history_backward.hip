@@ -175,14 +175,17 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
 }
 
 // RT rows a tile. The width 128 leaves no registers for the values at two waves a SIMD: they stay in LDS (V_LDS) and are read as operands.
-template <int DP, int NW, int RT>
-__global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a) {
+// The first items of a long history have all its rows to walk, and such a workgroup would still run when the others are done: its waves
+// are NG groups of NW, which own the same items, take the tiles in turn and are summed up at the end.
+template <int DP, int NW, int NG, int RT>
+__global__ __launch_bounds__(64 * NW * NG, 2) void history_dkv_kernel(const BwdArgs a) {
   using Sh = TileShape<DP>;
   constexpr bool V_LDS = DP > 64;
   constexpr int KS = DP / 16, DB = DP / 32, ITEMS = NW * 32, OP = DP * 2 + 16, HALF = RT * Sh::ROW, GROUPS = RT / Sh::RPI;
   constexpr int GPW = (GROUPS + NW - 1) / NW;
-  constexpr int STAGE = 2 * HALF + 1024, PATCH = NW * 32 * OP, VALUES = V_LDS ? ITEMS * Sh::ROW : 0;   // (1024: what a row brings, and whole lines)
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE + VALUES > PATCH ? 2 * STAGE + VALUES : PATCH];
+  constexpr int STAGE = 2 * HALF + 1024, VALUES = V_LDS ? ITEMS * Sh::ROW : 0;   // (1024: what a row brings, and whole lines)
+  constexpr int PATCH = NW * 32 * OP, JOIN = NG > 1 ? ITEMS * DP * 4 : 0, LAST = PATCH > JOIN ? PATCH : JOIN, TILES = 2 * NG * STAGE + VALUES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[TILES > LAST ? TILES : LAST];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -190,7 +193,8 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, item0 = tile * ITEMS;
   if (item0 >= n) return;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_all / NW, wave = wave_all % NW;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
   const int rows = n * a.G, first = item0 + wave * 32;
 
   // tiles of rows: queries, behind them d_o, behind them what the first kernel left of each row; rows behind the last read as zeros and
@@ -233,9 +237,10 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a
   // same time, wherever its own items begin.
   const int start = item0 * a.G / RT * RT;   // (rows before it see no item of this workgroup)
   const int turns = (rows - start + RT - 1) / RT;
-  fetch(start + (turns - 1) * RT, lds);
-  const unsigned values = lds + 2 * STAGE + wave * 32 * Sh::ROW;
-  if constexpr (V_LDS) {   // the wave's own 32
+  unsigned at = lds + group * 2 * STAGE, other = at + STAGE;
+  if (turns - 1 - group >= 0) fetch(start + (turns - 1 - group) * RT, at);
+  const unsigned values = lds + 2 * NG * STAGE + wave * 32 * Sh::ROW;
+  if (V_LDS && group == 0) {   // 32 for each wave of a group
 #pragma unroll
     for (int g = 0; g < 32 / Sh::RPI; ++g) {
       const int in = g * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(in);
@@ -361,21 +366,46 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  unsigned at = lds, other = lds + STAGE;
-  for (int t = turns - 1; t >= 0; --t) {
+  for (int t = turns - 1 - group, left = (turns + NG - 1) / NG; left > 0; --left, t -= NG) {
     const int r0 = start + t * RT;
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     barrier_lds();
-    if (t > 0) fetch(r0 - RT, other);
+    if (t >= NG) fetch(r0 - NG * RT, other);
     read.place(at);
-    if constexpr (RT == 64)
-      if (r0 + 32 > floor) block(r0 + 32, at, 1);
-    if (r0 > floor) block(r0, at, 0);
+    if (t >= 0) {
+      if constexpr (RT == 64)
+        if (r0 + 32 > floor) block(r0 + 32, at, 1);
+      if (r0 > floor) block(r0, at, 0);
+    }
     const unsigned x = at;
     at = other;
     other = x;
   }
   barrier_lds();
+  if constexpr (NG > 1) {   // the other groups' sums to the first, lane by lane, in their order
+    float* mine = reinterpret_cast<float*>(smem) + (size_t)wave * 32 * DP + lane;
+#pragma unroll 1
+    for (int g = 1; g < NG; ++g)
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        f32x16* acc = which == 0 ? dk : dv;
+        if (group == g) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mine[(db * 16 + r) * 64] = acc[db][r];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[db][r] += mine[(db * 16 + r) * 64];
+        }
+        __syncthreads();
+      }
+    if (group > 0) return;
+  }
   unsigned char* patch = smem + wave * 32 * OP;
   store_block<DP>(dk, a.inv_gamma, patch, n - first, a.D, lane,
                   [&](int r) { return a.dk + (size_t)(cr.first + first + r) * a.dkp + (size_t)hk * a.D; });
@@ -383,16 +413,29 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dkv_kernel(const BwdArgs a
                   [&](int r) { return a.dv + (size_t)(cr.first + first + r) * a.dvp + (size_t)hk * a.D; });
 }
 
+template <int DP, int NW, int NG>
+static laser_status dkv_launch(BwdArgs a, hipStream_t stream) {
+  if (!deal((long long)a.N * a.Hkv, ((long long)a.L + NW * 32 - 1) / (NW * 32), &a.deal)) return LASER_ERR_SHAPE;
+  history_dkv_kernel<DP, NW, NG, (DP > 64 ? 32 : 64)><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
+  return launch_status();
+}
+
 template <int DP>
 static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
   constexpr int NW = 4;
   const long long per = (long long)a.N * a.Hkv;
-  const long long row_tiles = ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), item_tiles = ((long long)a.L + NW * 32 - 1) / (NW * 32);
-  BwdArgs b = a;
-  if (!deal(per, row_tiles, &a.deal) || !deal(per, item_tiles, &b.deal)) return LASER_ERR_SHAPE;
+  Deal items;
+  if (!deal(per, ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), &a.deal) || !deal(per, ((long long)a.L + 31) / 32, &items)) return LASER_ERR_SHAPE;
   history_dq_kernel<DP, NW><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
-  history_dkv_kernel<DP, NW, (DP > 64 ? 32 : 64)><<<b.deal.grid, 64 * NW, 0, stream>>>(b);
-  return launch_status();
+  // How many groups of waves share the items of a workgroup, by how many workgroups of 128 items there are and how many rows the first
+  // has to walk. Forward and backward, one, two (of four waves) and four groups (of two): 16 histories up to 4096 of 8 heads of 128 over 2
+  // (1024 workgroups) 1209, 1130, 1168 us; two of 4096 (128) 740, 585, 451; 64 up to 1024 of 4 heads over 4 (2048) 250, 277, 345; 256 up to
+  // 200 of 4 over 2 (1024) 112, 126, 151.
+  const long long workgroups = per * ((a.L + 127) / 128), rows = (long long)a.L * a.G;
+  if (workgroups <= 256 && rows >= 1024) return dkv_launch<DP, 2, 4>(a, stream);
+  if constexpr (DP > 64)
+    if (workgroups < 1536 && rows >= 4096) return dkv_launch<DP, 4, 2>(a, stream);
+  return dkv_launch<DP, 4, 1>(a, stream);
 }
 
 laser_status history_bwd_tile_launch(const HistoryBwdArgs& b) {
