@@ -1,15 +1,19 @@
 // Attention among the items of histories on the matrix cores (bf16): packed sequences, and rows over a paged cache.
 //
 // The rows of a key-value head are its G = H / H_kv query heads of every token, row r = token r / G, head r % G: shared keys and
-// values are then read once for all of them. A workgroup owns NW * RB * 32 consecutive rows of one head of one sequence and
-// walks the items that the last of them sees in tiles of 64; a wave owns RB blocks of 32 rows, whose queries stay in registers.
+// values are then read once for all of them. A workgroup of four waves owns 128 consecutive rows of one head of one sequence and
+// walks the items that the last of them sees in tiles of 64; a wave owns 32 rows, whose queries stay in registers.
 //   Sc^T[item, row] = K . Q^T             A = K from LDS, B = Q^T
 //   P^T = exp2(Sc^T c - m)                the running maximum m and sum l of a row are one lane's (and its other half's) registers
 //   acc^T[column, row] += V^T . P^T       A = V^T by the LDS transpose load, B = P^T as the accumulators hold it
-// Tiles come by direct loads to LDS, the next one behind the current one's arithmetic, one barrier a tile. Rows behind the valid
+// Tiles come by direct loads to LDS, the next ones behind the current one's arithmetic, one barrier a tile. Rows behind the valid
 // ones read as zeros (the buffer's end), so padding that holds NaN never enters; their scores are masked.
-#include <type_traits>
-
+//
+// Bound: products and exponentials together. A block of 32 items costs a wave of width 128 512 cycles of products and about 360 of vector
+// arithmetic beside them, two waves share a SIMD, and the matrix cores are busy 40 % of the time (a library's large product: 52 %).
+// Histories of 2000 to 9200 items, 16 heads of 128 over 4: 700 us, 960 TFLOP/s (1250 us without the pipeline of block(); 1100 with it
+// and every long sequence on one or two dies; 745 before a tile's read addresses were made once). Workgroups of eight waves 700 us
+// and 64 rows a wave 760; over caches both are 10 to 35 % slower.
 #include "history_tile.h"
 
 namespace laser {
@@ -38,18 +42,19 @@ struct TileArgs {
 constexpr float MAX_SLACK = 8.0f;
 
 // Tiles come as pairs: values of items 64 u and on, keys of 32 items later (what turn u reads), pair u to slot u % SLOTS of a ring. Pair -1
-// is the first 32 keys. A wave brings 64 / NW rows of either kind.
+// is the first 32 keys. A wave brings 16 rows of either kind.
+constexpr int NW = 4;
 template <int DP>
 struct PairShape {
   static constexpr int ROW = DP * 2, CH = DP / 8, RPI = 64 / CH, KB = TI * ROW, SLOT = 2 * KB;
 };
 
-template <int DP, int NW, int RB, int SLOTS, bool PAGED>
-__global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void history_tile_kernel(const TileArgs a) {
+template <int DP, int SLOTS, bool PAGED>
+__global__ __launch_bounds__(64 * NW, 2) void history_tile_kernel(const TileArgs a) {
   using Sh = PairShape<DP>;
-  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * RB * 32, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
+  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * 32, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
   constexpr int MINE = TI / NW, RPW = MINE / Sh::RPI;   // a wave's rows of a tile, and its requests for them
-  static_assert(MINE % Sh::RPI == 0 && MINE <= 16, "whole requests, at most two pages of eight items");
+  static_assert(MINE % Sh::RPI == 0 && MINE == 16, "whole requests, at most two pages of eight items");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * Sh::SLOT > PATCH ? SLOTS * Sh::SLOT : PATCH];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
 
@@ -90,9 +95,9 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     voff[x] = c * 8 < a.D ? (unsigned)((PAGED ? in * a.D : r * (int)a.vp) * 2 + c * 16) : NO_COLUMN;
   }
   const int32_t* table = PAGED ? a.pages + (size_t)n_seq * a.max_pages : nullptr;
-  const bool short_pages = PAGED && MINE > 8 && a.log2 == 3;   // a wave's rows are on two pages
+  const bool short_pages = PAGED && a.log2 == 3;   // a wave's rows are on two pages
   // The table's next 64 entries wait in the lanes of a register, and those of the next pair are read from there: a scalar load under way
-  // would make every wait for LDS in between a wait for all of them (chunks of 512 over 10000 items: ___ us so, ___ by scalar loads).
+  // would make every wait for LDS in between a wait for it and for all of them.
   int ids[2][2], window = 0, window_at = -64;
   auto first_of = [&](int u, int kind) { return begin + (u < 0 ? 0 : u * TI + (kind ? 0 : 32)) + wave * MINE; };
   auto look_up = [&](int u) __attribute__((always_inline)) {
@@ -169,27 +174,24 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     for (int x = 0; x < SLOTS && x <= turns; ++x) request();   // pairs -1 .. SLOTS - 2
   }
 
-  // this lane's rows and the last item each sees
-  int last[RB];
-  bf16x8 qreg[RB][KS];
-  int wave_last = -1, wave_first = 0x7fffffff;
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    int r = row0 + (wave * RB + b) * 32 + l32;
+  // this lane's row and the last item it sees
+  const int first = row0 + wave * 32;
+  int last;
+  bf16x8 qreg[KS];
+  {
+    int r = first + l32;
     r = r < rows ? r : rows - 1;
     const int i = (int)a.by_group.div(r), g = r - i * a.G;
-    last[b] = a.causal ? n - cr.count + i : n - 1;
+    last = a.causal ? n - cr.count + i : n - 1;
     const unsigned short* qr = a.q + (size_t)(cr.first + i) * a.qp + (size_t)(hk * a.G + g) * a.D;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       u32x4 raw = {0u, 0u, 0u, 0u};
       if (s * 16 + h * 8 < a.D) raw = *reinterpret_cast<const u32x4*>(qr + s * 16 + h * 8);
-      qreg[b][s] = __builtin_bit_cast(bf16x8, raw);
+      qreg[s] = __builtin_bit_cast(bf16x8, raw);
     }
-    const int lo = __builtin_amdgcn_readlane(last[b], 0), hi = __builtin_amdgcn_readlane(last[b], 31);
-    wave_first = lo < wave_first ? lo : wave_first;
-    wave_last = hi > wave_last ? hi : wave_last;
   }
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
   // is every page of the user's items one of the pool? (then only the last block has places without items)
   bool whole_pages = true;
   if constexpr (PAGED) {
@@ -199,24 +201,16 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     whole_pages = __ballot(bad) == 0;
   }
 
-  f32x16 acc[RB][DB], sa[RB], sb[RB];
-  float m[RB], l[RB];
-  unsigned p[RB][8];
+  f32x16 acc[DB], sa, sb;   // (scores of a block and of the next)
+  float m = -INFINITY, l = 0.0f;
+  unsigned p[8] = {};
   bf16x8 kf[KS], vf[2][DB];
   const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    m[b] = -INFINITY;
-    l[b] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) acc[b][db] = zero;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) p[b][x] = 0;
+  for (int db = 0; db < DB; ++db) {
+    acc[db] = zero;
+    vf[0][db] = vf[1][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   }
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int db = 0; db < DB; ++db) vf[s][db] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   TileReader<DP> read(lane);
 
   auto read_k = [&](int half) __attribute__((always_inline)) {
@@ -229,84 +223,65 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
 #pragma unroll
       for (int db = 0; db < DB; ++db) vf[s][db] = read.cols(Sh::KB, half * 2 + s, db);
   };
-  auto scores = [&](f32x16* sc) __attribute__((always_inline)) {
+  auto scores = [&](f32x16& sc) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int b = 0; b < RB; ++b) sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qreg[b][s], s == 0 ? zero : sc[b], 0, 0, 0);
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qreg[s], s == 0 ? zero : sc, 0, 0, 0);
   };
   auto values = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          const u32x4 pf = {p[b][s * 4], p[b][s * 4 + 1], p[b][s * 4 + 2], p[b][s * 4 + 3]};
-          acc[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][db], __builtin_bit_cast(bf16x8, pf), acc[b][db], 0, 0, 0);
-        }
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 pf = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][db], __builtin_bit_cast(bf16x8, pf), acc[db], 0, 0, 0);
+      }
   };
   // scores of places without an item, and of items behind a row's own, become -inf
-  auto mask = [&](f32x16* sc, int t0) __attribute__((always_inline)) {
+  auto mask = [&](f32x16& sc, int t0) __attribute__((always_inline)) {
     if (whole_pages && t0 + 31 <= wave_first && t0 + 32 <= n) return;
     bool in = l32 < n - t0;
     if (PAGED && !whole_pages) in = in && (unsigned)table[(t0 + (in ? l32 : 0)) >> a.log2] < (unsigned)a.P;
     const unsigned items = (unsigned)__ballot(in) >> (4 * h);
+    const int seen = last - t0 - 4 * h;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const int seen = last[b] - t0 - 4 * h;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i0 = 8 * (r >> 2) + (r & 3);
-        if (i0 > seen || !((items >> i0) & 1)) sc[b][r] = -INFINITY;
-      }
+    for (int r = 0; r < 16; ++r) {
+      const int i0 = 8 * (r >> 2) + (r & 3);
+      if (i0 > seen || !((items >> i0) & 1)) sc[r] = -INFINITY;
     }
   };
-  auto raise = [&](const f32x16* sc) __attribute__((always_inline)) {
-    float top[RB];
-    bool over = false;
+  auto raise = [&](const f32x16& sc) __attribute__((always_inline)) {
+    float top = sc[0];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      top[b] = sc[b][0];
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = half_max(top) * a.scale;
+    if (__any(top > m + MAX_SLACK)) {   // (the first block: m is -inf)
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
 #pragma unroll
-      for (int r = 1; r < 16; ++r) top[b] = fmaxf(top[b], sc[b][r]);
-      top[b] = half_max(top[b]) * a.scale;
-      over |= top[b] > m[b] + MAX_SLACK;
-    }
-    if (__any(over)) {   // (the first block: m is -inf)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        const float next = fmaxf(m[b], top[b]), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[b] - next);
-        m[b] = next;
-        l[b] *= c;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[b][db][r] *= c;
-      }
+        for (int r = 0; r < 16; ++r) acc[db][r] *= c;
     }
   };
-  auto weigh = [&](const f32x16* sc) __attribute__((always_inline)) {
+  auto weigh = [&](const f32x16& sc) __attribute__((always_inline)) {
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const float base = m[b] == -INFINITY ? 0.0f : m[b];
-      float sum = 0.0f;
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.scale, -base));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[b][r + 1], a.scale, -base));
-        sum += p0 + p1;
-        p[b][r >> 1] = pack_bf16(p0, p1);
-        asm volatile("" : "+v"(p[b][r >> 1]));   // (here, not where the next turn reads it)
-      }
-      l[b] += sum;
-      asm volatile("" : "+v"(l[b]));
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -base));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], a.scale, -base));
+      sum += p0 + p1;
+      p[r >> 1] = pack_bf16(p0, p1);
+      asm volatile("" : "+v"(p[r >> 1]));   // (here, not where the next turn reads it)
     }
+    l += sum;
+    asm volatile("" : "+v"(l));
   };
 
   // A block of 32 items, half of a tile: its scores are there, those of the next block are made behind its exponentials, the last
   // block's sum of values behind its maximum
-  auto block = [&](f32x16* sc, f32x16* next, int t0, int half) __attribute__((always_inline)) {
+  auto block = [&](f32x16& sc, f32x16& next, int t0, int half) __attribute__((always_inline)) {
     read_k(half);
     __builtin_amdgcn_sched_barrier(0);
     values();
@@ -316,9 +291,9 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     scores(next);
     weigh(sc);
 #pragma unroll
-    for (int x = 0; x < KS * RB; ++x) {   // one product, then its share of the reads and of the exponentials
+    for (int x = 0; x < KS; ++x) {   // one product, then its share of the reads and of the exponentials
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / (KS * RB) > 0 ? 4 * DB / (KS * RB) : 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * DB / KS, 0);
       __builtin_amdgcn_sched_group_barrier(0x402, 64 / KS, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -346,63 +321,49 @@ __global__ __launch_bounds__(64 * NW, (DP * RB * NW <= 512 ? 2 : 1)) void histor
     barrier_lds();
   }
 
-  // out: a block's rows through a patch of the wave's own, so that they leave in whole 16-byte pieces
-  unsigned char* patch = smem + wave * 32 * OP;
+  // out: through a patch of the wave's own, so that the rows leave in whole 16-byte pieces
+  const float sum = half_sum(l), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const int r = first + l32;
+  if (joined) {
+    if (r >= rows) return;
+    const int i = (int)a.by_group.div(r), g = r - i * a.G;
+    const size_t all = (size_t)a.T * a.H, row = (size_t)(cr.first + i) * a.H + hk * a.G + g;
+    float* to = a.work + (run * all + row) * a.D;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const float sum = half_sum(l[b]), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    const int first = row0 + (wave * RB + b) * 32;
-    const int r = first + l32;
-    if (joined) {
-      if (r >= rows) continue;
-      const int i = (int)a.by_group.div(r), g = r - i * a.G;
-      const size_t all = (size_t)a.T * a.H, row = (size_t)(cr.first + i) * a.H + hk * a.G + g;
-      float* to = a.work + (run * all + row) * a.D;
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int c = db * 32 + x * 8 + h * 4;
-          typedef float f32x4 __attribute__((ext_vector_type(4)));
-          if (c < a.D) *reinterpret_cast<f32x4*>(to + c) = f32x4{acc[b][db][x * 4] * inv, acc[b][db][x * 4 + 1] * inv,
-                                                                 acc[b][db][x * 4 + 2] * inv, acc[b][db][x * 4 + 3] * inv};
-        }
-      if (h == 0) a.work[a.runs * all * a.D + run * all + row] = sum > 0.0f ? m[b] + log2f(sum) : -INFINITY;
-      continue;
-    }
-    if (a.lse != nullptr && h == 0 && r < rows) {
-      const int i = (int)a.by_group.div(r), g = r - i * a.G;
-      a.lse[(size_t)(cr.first + i) * a.H + hk * a.G + g] = sum > 0.0f ? (m[b] + log2f(sum)) * LN2 : -INFINITY;
-    }
-    store_block<DP>(acc[b], inv, patch, rows - first, a.D, lane, [&](int r) {
-      const int i = (int)a.by_group.div(first + r), g = first + r - i * a.G;
-      return a.o + ((size_t)(cr.first + i) * a.H + hk * a.G + g) * a.D;
-    });
+      for (int x = 0; x < 4; ++x) {
+        const int c = db * 32 + x * 8 + h * 4;
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        if (c < a.D) *reinterpret_cast<f32x4*>(to + c) = f32x4{acc[db][x * 4] * inv, acc[db][x * 4 + 1] * inv, acc[db][x * 4 + 2] * inv,
+                                                               acc[db][x * 4 + 3] * inv};
+      }
+    if (h == 0) a.work[a.runs * all * a.D + run * all + row] = sum > 0.0f ? m + log2f(sum) : -INFINITY;
+    return;
   }
+  if (a.lse != nullptr && h == 0 && r < rows) {
+    const int i = (int)a.by_group.div(r), g = r - i * a.G;
+    a.lse[(size_t)(cr.first + i) * a.H + hk * a.G + g] = sum > 0.0f ? (m + log2f(sum)) * LN2 : -INFINITY;
+  }
+  store_block<DP>(acc, inv, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
+    const int i = (int)a.by_group.div(first + r), g = first + r - i * a.G;
+    return a.o + ((size_t)(cr.first + i) * a.H + hk * a.G + g) * a.D;
+  });
 }
 
-template <int DP, int NW, int RB, int SLOTS, bool PAGED>
+template <int DP, int SLOTS, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
-  constexpr int ROWS = NW * RB * 32;
-  a.tiles = (int)(((long long)a.C * a.G + ROWS - 1) / ROWS);
+  a.tiles = (int)(((long long)a.C * a.G + NW * 32 - 1) / (NW * 32));
   if (!deal((long long)a.N * a.Hkv, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
-  history_tile_kernel<DP, NW, RB, SLOTS, PAGED><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
+  history_tile_kernel<DP, SLOTS, PAGED><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
   return launch_status();
 }
 template <bool PAGED>
 static laser_status tile_launch_any(const TileArgs& a, hipStream_t stream) {
-  const int form = tuning_int("LASER_HIST_FORM", 0);
-  if (a.D > 64) {
-    if (form == 1) return tile_launch<128, 8, 1, 3, PAGED>(a, stream);
-    if (form == 2) return tile_launch<128, 4, 2, 3, PAGED>(a, stream);
-    return tile_launch<128, 4, 1, 2, PAGED>(a, stream);
-  }
-  if (a.D > 32) {
-    if (form == 1) return tile_launch<64, 8, 1, 3, PAGED>(a, stream);
-    if (form == 2) return tile_launch<64, 4, 2, 3, PAGED>(a, stream);
-    return tile_launch<64, 4, 1, 3, PAGED>(a, stream);
-  }
-  return tile_launch<32, 4, 1, 4, PAGED>(a, stream);
+  // (as many pairs on the way as leave LDS for the two or three workgroups that the registers allow)
+  if (a.D > 64) return tile_launch<128, 2, PAGED>(a, stream);
+  if (a.D > 32) return tile_launch<64, 3, PAGED>(a, stream);
+  return tile_launch<32, 4, PAGED>(a, stream);
 }
 
 laser_status history_tile_launch(const HistoryArgs& h) {

@@ -196,3 +196,103 @@ def test_on_another_stream():
     got, _ = laser.laser_history_attention_forward(q, k, v, off, 150, 8.0, stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,Hkv,D,L", [([140, 3, 70], 4, 2, 128, 16384),     # (what the launch is sized for, far above the lengths)
+                                            ([140, 3, 70], 4, 2, 64, 16384), ([33, 0, 150], 2, 2, 32, 40000),
+                                            ([200, 20], 6, 3, 96, 30000), ([66] * 9, 3, 1, 24, 20000)])
+def test_launches_sized_for_longer_sequences(lens, H, Hkv, D, L, dtype):
+    """The forms that long or many sequences run in, on short ones."""
+    q, k, v, off, host = make(lens, H, Hkv, D, dtype, seed=12)
+    gamma = math.sqrt(D)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(3)).to(q.dtype).cuda()
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, L, gamma)
+    check_forward(o, lse, q, k, v, host, gamma, dtype)
+    grads = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, L, gamma)
+    check_backward(grads, q, k, v, go, host, gamma, dtype)
+
+
+def check_backward(grads, q, k, v, go, host, gamma, dtype):
+    G, step = q.shape[1] // k.shape[1], (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+    for a, b in zip(host, host[1:]):
+        if b == a:
+            continue
+        allowed = sees(b - a, b - a, True, "cuda")
+        for j in range(k.shape[1]):
+            total = [[0.0, 0.0], [0.0, 0.0]]
+            for h in range(j * G, j * G + G):
+                refs = gradients(q[a:b, h].double(), k[a:b, j].double(), v[a:b, j].double(), go[a:b, h].double(), gamma, allowed,
+                                 dtype == "bf16")
+                close(grads[0][a:b, h], *refs[0], f"dq rows {a}..{b} head {h}")
+                for t, r in zip(total, refs[1:]):
+                    t[0], t[1] = t[0] + r[0], t[1] + r[1]
+            for name, got, t in zip(("dk", "dv"), grads[1:], total):
+                close(got[a:b, j], t[0], t[1] + step * t[0].abs(), f"{name} rows {a}..{b} head {j}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sequences(dtype):
+    """Thousands of items: gradients of every kind of workgroup, checked whole."""
+    q, k, v, off, host = make([2300, 700], 4, 2, 128 if dtype == "bf16" else 64, dtype, seed=13, before=0, behind=0)
+    gamma = 11.0
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(3)).to(q.dtype).cuda()
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 2300, gamma)
+    check_forward(o, lse, q, k, v, host, gamma, dtype)
+    check_backward(laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 2300, gamma), q, k, v, go, host, gamma, dtype)
+
+
+def test_a_row_that_sees_itself_alone():
+    """One item: p = 1 whatever the score, so o = v, dv = d_o, and dq = dk = 0."""
+    q, k, v, off, host = make([1] * 40, 4, 2, 64, "bf16", before=0, behind=0)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(3)).to(q.dtype).cuda()
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 1, 8.0)
+    assert torch.equal(o, v.repeat_interleave(2, 1))
+    dq, dk, dv = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 1, 8.0)
+    # p is made again from the score and the stored lse, each an fp32 number below 8, so it is off from 1 by at most 2^-19 (four
+    # roundings of 2^-24, times 8); dp = d_o . v is below 64, so ds = p (dp - p dp) is below 2^-13; q and k are below 6, gamma is 8, and
+    # dk adds up two heads
+    assert dq.float().abs().max() < 2.0 ** -13 and dk.float().abs().max() < 2.0 ** -12
+    assert torch.allclose(dv.float(), go.float().view(40, 2, 2, 64).sum(2), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+def test_gradients_of_a_leaf_beside_a_captured_backward():
+    """An eager graph of the same leaves lives while the explicit gradients are captured and replayed."""
+    q, k, v, off, host = make([50, 31], 2, 1, 64, "f32", before=0, behind=0, packed=False)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(3)).cuda()
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    eager = sum((t * t).sum() for t in leaves)
+
+    def both():
+        with torch.no_grad():
+            o, lse = laser.laser_history_attention_forward(*leaves, off, 50, 8.0)
+            return laser.laser_history_attention_backward(*leaves, o, lse, go, off, 50, 8.0)
+
+    want = [t.clone() for t in both()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    eager.backward()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(t.grad, 2 * t.detach()) for t in leaves)
+
+
+def test_example_of_training_a_step_through_the_gradients():
+    """The derivative of a loss along the gradients is their squared length: one small step changes the loss by it."""
+    q, k, v, off, host = make([60, 45], 4, 2, 32, "f32", before=0, behind=0, packed=False)
+    target = torch.randn(q.shape, generator=torch.Generator().manual_seed(4)).cuda()
+
+    def loss(q, k, v):
+        o, lse = laser.laser_history_attention_forward(q, k, v, off, 60, 5.0)
+        return 0.5 * ((o - target).double() ** 2).sum(), o, lse
+
+    base, o, lse = loss(q, k, v)
+    grads = laser.laser_history_attention_backward(q, k, v, o, lse, o - target, off, 60, 5.0)
+    length = sum((g.double() ** 2).sum() for g in grads).item()
+    h = 2.0 ** -9
+    up, down = (loss(*(t + s * h * g for t, g in zip((q, k, v), grads)))[0].item() for s in (1, -1))
+    assert abs((up - down) / (2 * h) / length - 1.0) < 1e-2

@@ -58,7 +58,10 @@ SHAPES = [([1], [1], 1, 1, 64, 8),
           ([1500], [1], 16, 2, 128, 16),
           ([3000, 2900], [3, 2], 4, 4, 64, 128),
           ([2000], [200], 2, 1, 128, 64),
-          ([40], [6], 24, 1, 8, 4096)]
+          ([40], [6], 24, 1, 8, 4096),
+          ([20001], [1], 8, 1, 64, 32),               # many runs of one history
+          ([9000, 12], [50, 2], 4, 1, 128, 8),
+          ([2500], [70], 8, 2, 32, 8)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -340,3 +343,46 @@ def test_a_cache_past_32_bits():
             ref = attend(q[:, h].double(), rows[0][:, h // 2].double(), rows[1][:, h // 2].double(), 11.0,
                          sees(C, n, True, "cuda"), True)
             close(o[:, h], ref["o"], ref["o_tol"], f"{C} rows, head {h}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_launches_sized_for_more(causal, dtype):
+    """C_max and L_max far above what the users have: the forms of large calls, and workgroups with nothing to do."""
+    lens, new = [130, 0, 300, 64], [40, 2, 1, 64]
+    cache = Cache(lens, 2, 64, 16, DT[dtype])
+    wide = torch.full((4, 4096), -1, dtype=torch.int32, device="cuda")
+    wide[:, :cache.pages.shape[1]] = cache.pages
+    q, off, host = queries(new, 8, 64, dtype)
+    for C, L in ((3000, 300), (64, 60000), (5000, 65536)):
+        o, lse = laser.laser_cache_attention_forward(q, cache.k, cache.v, off, wide, cache.lens, C, L, 8.0, causal=causal)
+        weight = laser.laser_cache_weights(q, lse, cache.k, off, wide, cache.lens, C, L, 8.0, torch.zeros(cache.P, 16, device="cuda"),
+                                           causal=causal)
+        check(o, lse, weight, q, cache, host, 8.0, causal, dtype)
+
+
+def test_two_graphs_with_workspaces_of_their_own():
+    """Long caches in runs: two captured calls, each with its work buffer, replayed in turn and at once on two streams."""
+    cache = Cache([4000, 900], 2, 64, 32, torch.bfloat16)
+    calls = []
+    for seed in (1, 2):
+        q, off, host = queries([1, 1], 8, 64, "bf16", seed=seed, before=0, behind=0)
+        work = torch.empty(laser.laser_cache_attention_work_bytes(2, 2, 1, 4000, 8, 2, 64, laser.LASER_BF16), dtype=torch.uint8, device="cuda")
+        o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        args = (q, cache.k, cache.v, off, cache.pages, cache.lens, 1, 4000, 8.0)
+        laser.laser_cache_attention_forward(*args, o_out=o, lse_out=lse, work=work)
+        want = o.clone(), lse.clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            laser.laser_cache_attention_forward(*args, o_out=o, lse_out=lse, work=work)
+        calls.append((graph, o, lse, want))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for (graph, o, lse, _), s in zip(calls, streams):
+            o.zero_()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[0]) and torch.equal(lse, want[1]) for _, o, lse, want in calls)
