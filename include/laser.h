@@ -487,7 +487,8 @@ laser_status laser_gsta_backward(const void* seg, const void* t0, const void* wq
  * into [0, min(L_max, T - first)]); offsets that break the rules give unspecified values in the rows concerned, never a
  * fault. Rows of no sequence are neither read into a result (they may hold anything, NaN included) nor written. The items of
  * a sequence are taken to be finite: an infinite or NaN value can reach all rows of its sequence, also earlier ones.
- * All pointers are device pointers, caller-owned; 16-byte alignment for q, k, v, o_out, 4-byte for off and lse_out.
+ * All pointers are device pointers, caller-owned, outputs apart from inputs; 16-byte alignment for q, k, v, o_out, 4-byte for off
+ * and lse_out.
  * Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on an
  * error.
  */
@@ -540,8 +541,8 @@ laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, co
  *   itself) receives the new lengths, kept_out [U,budget] the old places of the items that stay, -1 behind the last.
  * Results are the same from run to run (laser_cache_weights with add: unless users share a page). Rows of no user and
  * places behind a user's items are never written.
- * All pointers are device pointers, caller-owned; 16-byte alignment for q, k, v, the caches, o_out and work, 4-byte for the
- * rest. Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on
+ * All pointers are device pointers, caller-owned, outputs apart from inputs (but for lens_out); 16-byte alignment for q, k, v, the
+ * caches, o_out and work, 4-byte for the rest. Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on
  * an error.
  */
 laser_status laser_cache_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,
