@@ -170,3 +170,29 @@ def test_row_pitches_as_the_binding_reads_them():
         _flat(qkv[:, :4], "o", (7, 4, 16), torch.float32)
     with pytest.raises(TypeError):
         _flat(qkv, "o", (7, 8, 16), torch.bfloat16)
+
+
+def test_the_native_marshalling_leaves_every_other_form_alone():
+    """Host tensors, subclasses, no tensors, numbers of other types and other numbers of arguments: None, whatever the address."""
+    class Sub(torch.Tensor):
+        pass
+    fast = laser.binding._fast()
+    x, c, w = torch.zeros(3, 2, 8), torch.zeros(4, 2, 8, 8), torch.zeros(4, 8)
+    off, lens, pages = torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 4, dtype=torch.int32)
+    lse, room = torch.zeros(3, 2), torch.zeros(16, dtype=torch.uint8)
+    good = {"history_forward": [x, x, x, off, 3, 1.0, x, lse, None],
+            "history_backward": [x, x, x, x, lse, x, off, 3, 1.0, x, x, x, room, None],
+            "cache_append": [x, x, c, c, off, pages, lens, 1, 3, None, None],
+            "cache_attention": [x, c, c, off, pages, lens, 1, 3, 1.0, True, x, lse, room, None],
+            "cache_weights": [x, lse, c, off, pages, lens, 1, 3, 1.0, w, True, True, None],
+            "cache_evict": [c, c, w, pages, lens, pages, 2, 1, 3, lens, torch.zeros(1, 2, dtype=torch.int32), None]}
+    for name, args in good.items():
+        f = getattr(fast, name)
+        for device in (0, -1, 1 << 40, "0"):
+            assert f(1, device, *args) is None, name          # (host tensors)
+        for address in (0, 1 << 70, -(1 << 70), 1.0, None):
+            assert f(address, 0, *args) is None, name
+        for at in range(len(args)):
+            for other in (None, "k", 1 << 40, 2.0, -1, x.as_subclass(Sub), torch.zeros(2, 2)):
+                assert f(1, 0, *args[:at], other, *args[at + 1:]) is None, (name, at)
+        assert f(1, 0, *args[:-1]) is None and f(1, 0, *args, None) is None and f() is None, name

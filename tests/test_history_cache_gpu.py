@@ -386,3 +386,69 @@ def test_two_graphs_with_workspaces_of_their_own():
                 graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, want[0]) and torch.equal(lse, want[1]) for _, o, lse, want in calls)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_native_and_python_marshalling_agree(dtype, monkeypatch):
+    """The same calls by both ways, bit for bit, with columns of one tensor, rows apart and every optional output given; the native
+    part takes each of them, and leaves what it does not know to the checks in Python."""
+    binding, taken = laser.binding, []
+    native = binding._native
+
+    def spy(name, *args):
+        code = native(name, *args)
+        taken.append((name, code))
+        return code
+    H, Hkv, D, page, gamma = 4, 2, 40, 8, 3.0
+    lens, counts = [70, 9], [5, 1]
+    g = torch.Generator().manual_seed(5)
+    off, _ = offsets(counts)
+    T, P = sum(counts), 30
+    x = torch.randn(T, H + 2 * Hkv, D, generator=g).to(DT[dtype]).cuda()
+    go = torch.randn(T, H, D, generator=g).to(DT[dtype]).cuda()
+    start = torch.randn(P, Hkv, page, D, generator=g).to(DT[dtype]).cuda()
+    pages = torch.arange(20, dtype=torch.int32, device="cuda").reshape(2, 10)
+    held = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    fresh = torch.arange(20, 30, dtype=torch.int32, device="cuda").reshape(2, 5)
+
+    def run(fast):
+        monkeypatch.setattr(binding, "_native", spy if fast else (lambda *args: None))
+        out, bf = [], DT[dtype]
+        e = lambda *s, d=bf: torch.zeros(s, dtype=d, device="cuda")
+        q, k, v = x.split([H, Hkv, Hkv], dim=1)
+        o, lse = laser.laser_history_attention_forward(q, k, v, off, 5, gamma, e(T, H, D), e(T, H, d=torch.float32))
+        grads = e(T, H + 2 * Hkv, D)
+        parts = grads.split([H, Hkv, Hkv], dim=1)
+        room = e(laser.laser_history_attention_backward_work_bytes(2, T, 5, H, Hkv, D, 0 if dtype == "f32" else 1), d=torch.uint8)
+        laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 5, gamma, *parts, room)
+        out += [o, lse, grads]
+        kc, vc, w = start.clone(), start.clone(), torch.ones(P, page, device="cuda")
+        laser.laser_cache_append(k, v, kc, vc, off, pages, held, 5, 70, w)
+        laser.laser_cache_append(k, v, kc, vc, off, pages, held, 5, 70)
+        room = e(laser.laser_cache_attention_work_bytes(2, T, 5, 70, H, Hkv, D, 0 if dtype == "f32" else 1), d=torch.uint8)
+        for causal in (True, 0):
+            o, lse = laser.laser_cache_attention_forward(q, kc, vc, off, pages, held, 5, 70, gamma, causal, e(T, H, D),
+                                                         e(T, H, d=torch.float32), room)
+            w2 = laser.laser_cache_weights(q, lse, kc, off, pages, held, 5, 70, gamma, w.clone(), causal, 2 if causal else False)
+            out += [o, lse, w2]
+        left, kept = laser.laser_cache_evict(kc, vc, w2, pages, held, fresh, 12, 3, 70, e(2, d=torch.int32), e(2, 12, d=torch.int32))
+        torch.cuda.synchronize()
+        return out + [kc, vc, left, kept]
+    for a, b in zip(run(True), run(False)):
+        assert torch.equal(a, b)
+    assert {name for name, _ in taken} == {"history_forward", "history_backward", "cache_append", "cache_attention", "cache_weights",
+                                           "cache_evict"} and all(code == 0 for _, code in taken)
+    monkeypatch.setattr(binding, "_native", spy)
+    o, lse, q, k, v = (torch.empty_like(go), torch.empty(T, H, device="cuda"), *x.split([H, Hkv, Hkv], dim=1))
+    with pytest.raises(TypeError):
+        laser.laser_history_attention_forward(q, k, v, off.long(), 5, gamma, o, lse)
+    with pytest.raises(ValueError):
+        laser.laser_history_attention_forward(q, k, v, off, 5, gamma, o.transpose(0, 1).contiguous().transpose(0, 1), lse)
+    with pytest.raises(ValueError):
+        laser.laser_history_attention_forward(q.transpose(1, 2).contiguous().transpose(1, 2), k, v, off, 5, gamma, o, lse)
+    with pytest.raises(ValueError):
+        laser.laser_history_attention_forward(q, k.cpu(), v, off, 5, gamma, o, lse)
+    with pytest.raises(ValueError):
+        laser.laser_cache_weights(q, lse, start, off, pages, held[:1], 5, 70, gamma, torch.zeros(P, page, device="cuda"))
+    laser.laser_history_attention_forward(q, k, v, off, 5, 3, o, lse)      # (an integer: by Python)
+    assert taken[-1] == ("history_forward", None) and all(code is None for _, code in taken[-6:])
