@@ -1,9 +1,12 @@
 // What the items of a cache receive from rows that attended to them (bf16, on the matrix cores): weight_j = sum over rows r and heads
 // of exp2(c q_r . k_j - lse_r).
 //
-// A wave owns 32 items; for each key-value head their keys are loaded once, straight into registers as the A operand, and the rows of the head's group pass through LDS in tiles of 64 that the workgroup's four waves share:
+// A wave owns 32 items; for each key-value head their keys are loaded once, straight into registers as the A operand, and the rows of the
+// head's group pass through LDS in tiles of 64 that the workgroup's four waves share:
 //   Sc^T[item, row] = K Q^T,  then exp2 and a sum for every accumulator (an item), over the lanes only at the end.
-// For few rows this reads the keys and little else; for a chunk it costs half of the attention's products and its exponentials.
+// For few rows this reads the keys and little else: 128 users of up to 4096 items, 8 heads of 128 over 2, one row each 22 us for 65 MB
+// (2.9 TB/s; a wave's keys of one head wait for each other). For a chunk it costs half of the attention's products and its exponentials:
+// 512 rows for 16 users of up to 10000 items 130 us, where the attention takes 240; the matrix cores are busy 30 % of the time.
 #include <type_traits>
 
 #include "history_tile.h"

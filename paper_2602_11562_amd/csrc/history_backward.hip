@@ -8,8 +8,8 @@
 //       Sc = Q K^T, dP = dO V^T (items in lanes), dV^T += dO^T P, dK^T += Q^T dS
 // Seven products where five would do with one kernel, which would have to add one of the gradients up across workgroups.
 //
-// Bound: as the forward pass, by products with their exponentials. Width 128: dq 350 us for 16 histories of 820 to 4100 items, 8 heads over
-// 2 (970 TFLOP/s of its three products), dk and dv 560 (810 of their four), whose first items' workgroups run longest. Widths to 64
+// Bound: as the forward pass, by products with their exponentials. Width 128: dq 380 us for 16 histories of 820 to 4100 items, 8 heads over
+// 2 (900 TFLOP/s of its three products), dk and dv 560 (810 of their four), whose first items' workgroups run longest. Widths to 64
 // over histories of 40 to 200 items are bound by memory: 47 and 50 us where their bytes take 40 each at a copy's rate.
 #include "history_tile.h"
 
