@@ -533,17 +533,19 @@ laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, co
  *   overlap need one each.
  * laser_cache_weights: what each item received, weight[its place] = sum of exp(s - lse) over the rows that see it and
  *   the H heads (add != 0: added to what stands there, atomically, so a page that several users list gets each one's part).
- *   q, lse, causal as for laser_cache_attention_forward; places behind a user's items are left alone.
+ *   q, lse, causal as for laser_cache_attention_forward; places behind a user's items are left alone. add = 0: a page that
+ *   several users list ends up with one of their parts.
  * laser_cache_evict: each user keeps at most `budget` items: the last `recent` ones (0 <= recent <= budget) and of
  *   the others the heaviest by weight (of equal ones the first; NaN, and places on no page, count least). They move, in
  *   their order, with their weights, into the pages of pages_out [U,max_pages_out], of which none may be listed twice or be one that
- *   any user reads from in this call; a user within the budget keeps everything and moves too. lens_out [U] (may be lens
+ *   any user reads from in this call; a user within the budget keeps everything and moves too (an item on no page that stays
+ *   all the same leaves its new place as it was: what stands there counts as an item from then on). lens_out [U] (may be lens
  *   itself) receives the new lengths, kept_out [U,budget] the old places of the items that stay, -1 behind the last.
  * Results are the same from run to run (laser_cache_weights with add: unless users share a page). Rows of no user and
  * places behind a user's items are never written.
  * All pointers are device pointers, caller-owned, outputs apart from inputs (but for lens_out); 16-byte alignment for q, k, v, the
- * caches, o_out and work, 4-byte for the rest. Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on
- * an error.
+ * caches, o_out and work, 4-byte for the rest. Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_ALIGN,
+ * LASER_ERR_LAUNCH. Nothing is launched on an error.
  */
 laser_status laser_cache_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,
                                 const int32_t* off, const int32_t* pages, const int32_t* lens, int U, int T, int C_max, int P,

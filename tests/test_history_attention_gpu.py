@@ -296,3 +296,30 @@ def test_example_of_training_a_step_through_the_gradients():
     h = 2.0 ** -9
     up, down = (loss(*(t + s * h * g for t, g in zip((q, k, v), grads)))[0].item() for s in (1, -1))
     assert abs((up - down) / (2 * h) / length - 1.0) < 1e-2
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hkv,D", [(2, 1, 128), (3, 3, 40)])
+def test_rows_far_apart(H, Hkv, D, dtype):
+    """Tokens 2^22 elements apart, the farthest that is allowed: rows past 2^31 elements, the same bits as from rows side by side."""
+    T, wide, lens, gamma = 560, 1 << 22, [300, 0, 257], 6.0
+    g = torch.Generator().manual_seed(8)
+    x = torch.randn(T, H + 2 * Hkv, D, generator=g).to(DT[dtype]).cuda()
+    go = torch.randn(T, H, D, generator=g).to(DT[dtype]).cuda()
+    off, _ = offsets(lens)
+    far, grads = torch.empty(T, wide, dtype=DT[dtype], device="cuda"), torch.empty(T, wide, dtype=DT[dtype], device="cuda")
+    W = (H + 2 * Hkv) * D
+    at = wide - W                       # (the last columns of a row, up to the very end of the allocation)
+    far[:, at:] = x.reshape(T, W)
+    grads[:, at:] = 0
+    q, k, v = x.split([H, Hkv, Hkv], 1)
+    fq, fk, fv = far[:, at:].unflatten(1, (H + 2 * Hkv, D)).split([H, Hkv, Hkv], 1)
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, 300, gamma)
+    fo, flse = laser.laser_history_attention_forward(fq, fk, fv, off, 300, gamma)
+    n = sum(lens)
+    assert torch.equal(o[:n], fo[:n]) and torch.equal(lse[:n], flse[:n])
+    near = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, 300, gamma)
+    parts = grads[:, at:].unflatten(1, (H + 2 * Hkv, D)).split([H, Hkv, Hkv], 1)
+    laser.laser_history_attention_backward(fq, fk, fv, o, lse, go, off, 300, gamma, *parts)
+    for a, b in zip(near, parts):
+        assert torch.equal(a[:n], b[:n]) and (b[n:] == 0).all()
