@@ -35,11 +35,14 @@ struct BwdArgs {
   long long dqp, dkp, dvp;
 };
 
-template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a) {
+// The waves are NG groups of NW, which own the same rows, take the tiles in turn and are summed up at the end: where workgroups are few,
+// the longest walk is what counts.
+template <int DP, int NW, int NG>
+__global__ __launch_bounds__(64 * NW * NG, 2) void history_dq_kernel(const BwdArgs a) {
   using Sh = TileShape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * 32, OP = DP * 2 + 16, STAGE = 2 * Sh::BYTES, PATCH = NW * 32 * OP;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE > PATCH ? 2 * STAGE : PATCH];
+  constexpr int JOIN = NG > 1 ? ROWS * DP * 4 : 0, LAST = PATCH > JOIN ? PATCH : JOIN, TILES = 2 * NG * STAGE;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[TILES > LAST ? TILES : LAST];
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const Place place = place_of(a.deal, blockIdx.x);
   if (place.rank >= a.deal.tiles) return;
@@ -48,7 +51,8 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
   const CandRange cr = cand_range(a.off, n_seq, a.L, a.T);
   const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
   if (row0 >= rows) return;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_all / NW, wave = wave_all % NW;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
 
   bf16x8 qreg[KS], greg[KS];
   float lse2, delta;
@@ -149,12 +153,12 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     const size_t row = (size_t)(cr.first + t0);
     tiles.fetch(a.k + row * a.kp + (size_t)hk * a.D, a.v + row * a.vp + (size_t)hk * a.D, a.kp, a.vp, a.D, n - t0, at);
   };
-  fetch(0, lds);
-  unsigned at = lds, other = lds + STAGE;
-  for (int t0 = 0; t0 < end; t0 += TI) {
+  unsigned at = lds + group * 2 * STAGE, other = at + STAGE;
+  if (group * TI < end) fetch(group * TI, at);
+  for (int t0 = group * TI, turn = 0; turn < end; t0 += NG * TI, turn += NG * TI) {   // (every group the same number of turns)
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     barrier_lds();
-    if (t0 + TI < end) fetch(t0 + TI, other);
+    if (t0 + NG * TI < end) fetch(t0 + NG * TI, other);
     read.place(at);
     if (t0 <= wave_last) block(t0, 0);
     if (t0 + 32 <= wave_last) block(t0 + 32, 1);
@@ -162,13 +166,34 @@ __global__ __launch_bounds__(64 * NW, 2) void history_dq_kernel(const BwdArgs a)
     at = other;
     other = x;
   }
-  if (h == 0 && first + l32 < rows) {
+  if (group == 0 && h == 0 && first + l32 < rows) {   // (a row that sees one block saw it in the first tile)
     const int head = hk * a.G + first + l32 - last * a.G;
     float* row = a.rows + ((size_t)(cr.first + last) * a.H + head) * 2;
     row[0] = -lse2 * LN2 * a.gamma;
     row[1] = -delta;
   }
   barrier_lds();
+  if constexpr (NG > 1) {   // the other groups' sums to the first, lane by lane, in their order
+    float* mine = reinterpret_cast<float*>(smem) + (size_t)wave * 32 * DP + lane;
+#pragma unroll 1
+    for (int g = 1; g < NG; ++g) {
+      if (group == g) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mine[(db * 16 + r) * 64] = acc[db][r];
+      }
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[db][r] += mine[(db * 16 + r) * 64];
+      }
+      __syncthreads();
+    }
+    if (group > 0) return;
+  }
   store_block<DP>(acc, a.inv_gamma, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
     const int i = (int)a.by_group.div(first + r), head = hk * a.G + first + r - i * a.G;
     return a.dq + (size_t)(cr.first + i) * a.dqp + (size_t)head * a.D;
@@ -414,26 +439,46 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void history_dkv_kernel(const BwdA
                   [&](int r) { return a.dv + (size_t)(cr.first + first + r) * a.dvp + (size_t)hk * a.D; });
 }
 
-template <int DP, int NW, int NG>
+template <int DP, int NW, int NG, int RT = (DP > 64 ? 32 : 64)>
 static laser_status dkv_launch(BwdArgs a, hipStream_t stream) {
   if (!deal((long long)a.N * a.Hkv, ((long long)a.L + NW * 32 - 1) / (NW * 32), &a.deal)) return LASER_ERR_SHAPE;
-  history_dkv_kernel<DP, NW, NG, (DP > 64 ? 32 : 64)><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
+  history_dkv_kernel<DP, NW, NG, RT><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
+  return launch_status();
+}
+
+template <int DP, int NW, int NG>
+static laser_status dq_launch(BwdArgs a, hipStream_t stream) {
+  if (!deal((long long)a.N * a.Hkv, ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), &a.deal)) return LASER_ERR_SHAPE;
+  history_dq_kernel<DP, NW, NG><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
   return launch_status();
 }
 
 template <int DP>
 static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
-  constexpr int NW = 4;
   const long long per = (long long)a.N * a.Hkv;
-  Deal items;
-  if (!deal(per, ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), &a.deal) || !deal(per, ((long long)a.L + 31) / 32, &items)) return LASER_ERR_SHAPE;
-  history_dq_kernel<DP, NW><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
+  Deal items;   // (before anything is launched)
+  if (!deal(per, ((long long)a.L + 31) / 32, &items) || !deal(per, ((long long)a.L * a.G + 31) / 32, &items)) return LASER_ERR_SHAPE;
+  // dq has two groups (of four waves, width 128) or four (of two) where its workgroups of 128 rows would leave much of the machine idle,
+  // and at width 128 also where there are a few more, but long. Forward and backward without and with: one history of 2894 items, 4 heads
+  // of 32 over 2 (92 workgroups) 74 and 54 us; of 64 104 and 78; four of 300, 4 of 64 over 2 (40) 27.0 and 26.4; two of 2635, 4 of 128 over
+  // one (166) 218 and 204; two of 4096, 8 of 128 over 2 (512) 359 and 334; but eight of 1000 (512, of 4000 rows) 107 and 110.
+  const long long rows = (long long)a.L * a.G, row_workgroups = per * ((rows + 127) / 128);
+  const bool few = row_workgroups <= 256 && rows >= 256;
+  laser_status s;
+  if constexpr (DP > 64) s = few || (row_workgroups <= 512 && rows >= 8192) ? dq_launch<DP, 4, 2>(a, stream) : dq_launch<DP, 4, 1>(a, stream);
+  else s = few ? dq_launch<DP, 2, 4>(a, stream) : dq_launch<DP, 4, 1>(a, stream);
+  if (s != LASER_OK) return s;
   // How many groups of waves share the items of a workgroup, by how many workgroups of 128 items there are and how many rows the first
   // has to walk. Forward and backward, one, two (of four waves) and four groups (of two): 16 histories up to 4096 of 8 heads of 128 over 2
   // (1024 workgroups) 1209, 1130, 1168 us; two of 4096 (128) 740, 585, 451; 64 up to 1024 of 4 heads over 4 (2048) 250, 277, 345; 256 up to
   // 200 of 4 over 2 (1024) 112, 126, 151.
-  const long long workgroups = per * ((a.L + 127) / 128), rows = (long long)a.L * a.G;
-  if (workgroups <= 256 && rows >= 1024) return dkv_launch<DP, 2, 4>(a, stream);
+  // Few workgroups, four groups of two and one of four: 16 histories of 500, 2 of 64 over 2 (128) 24 and 26 us; four of 300, 4 over 2 (24)
+  // 21.6 and 26.5; 64 of 200, 4 over 2 (256, of 400 rows) 34 and 28. Eight groups of one wave, where even those of 32 items are few: one of
+  // 2894, 4 of 32 over 2 (182 of them) 44 us, with four groups of two 54; eight of 1000, 8 of 64 over 2 (512) 70 and 67.
+  const long long workgroups = per * ((a.L + 127) / 128);
+  if constexpr (DP <= 64)
+    if (per * ((a.L + 31) / 32) <= 256 && rows >= 1024) return dkv_launch<DP, 1, 8, 32>(a, stream);
+  if ((workgroups <= 256 && rows >= 1024) || (workgroups <= 128 && rows >= 384)) return dkv_launch<DP, 2, 4>(a, stream);
   if constexpr (DP > 64)
     if (workgroups < 1536 && rows >= 4096) return dkv_launch<DP, 4, 2>(a, stream);
   return dkv_launch<DP, 4, 1>(a, stream);

@@ -125,18 +125,23 @@ __device__ __forceinline__ void buffer_to_lds4(u32x4 buf, unsigned voff, unsigne
 }
 
 // Tiles of packed keys and values: request x of wave w brings rows (w + x NW) RPI and on, of both. These are STEP rows apart from request to
-// request, which leaves a lane's offset as it is: the buffer begins that much later.
+// request, which leaves a lane's offset as it is where STEP rows are whole turns of tile_swz: the buffer begins that much later.
 template <int DP, int NW>
 struct PackedTiles {
   using Sh = TileShape<DP>;
   static constexpr int RPW = Sh::GROUPS / NW, STEP = NW * Sh::RPI;
-  static_assert(Sh::GROUPS % NW == 0 && (RPW == 1 || STEP * Sh::CH % 256 == 0), "whole requests, the same places in each");
-  unsigned koff, voff, to;
+  static constexpr int OFFS = STEP * Sh::CH % 256 == 0 ? 1 : RPW;   // offsets that differ
+  static_assert(Sh::GROUPS % NW == 0, "whole requests");
+  unsigned koff[OFFS], voff[OFFS], to;
   __device__ __forceinline__ void init(int D, long long kp, long long vp, int wave, int lane) {
     to = wave * 1024;
-    const int r = wave * Sh::RPI + lane / Sh::CH, c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r);
-    koff = c * 8 < D ? (unsigned)(r * (int)kp * 2 + c * 16) : NO_COLUMN;
-    voff = c * 8 < D ? (unsigned)(r * (int)vp * 2 + c * 16) : NO_COLUMN;
+    const int r = wave * Sh::RPI + lane / Sh::CH;
+#pragma unroll
+    for (int x = 0; x < OFFS; ++x) {
+      const int c = (lane % Sh::CH) ^ tile_swz<Sh::CH>(r + x * STEP);
+      koff[x] = c * 8 < D ? (unsigned)(r * (int)kp * 2 + c * 16) : NO_COLUMN;
+      voff[x] = c * 8 < D ? (unsigned)(r * (int)vp * 2 + c * 16) : NO_COLUMN;
+    }
   }
   // rows k, v and on (`left` of them are the sequence's); keys to `at`, values behind them
   __device__ __forceinline__ void fetch(const unsigned short* k, const unsigned short* v, long long kp, long long vp, int D, int left,
@@ -145,8 +150,8 @@ struct PackedTiles {
 #pragma unroll
     for (int x = 0; x < RPW; ++x) {
       const int rest = left - x * STEP;
-      buffer_to_lds16(buffer_of(k + x * STEP * kp, rest > 0 ? (unsigned)(((rest - 1) * (int)kp + D) * 2) : 0u), koff, at + to + x * NW * 1024);
-      buffer_to_lds16(buffer_of(v + x * STEP * vp, rest > 0 ? (unsigned)(((rest - 1) * (int)vp + D) * 2) : 0u), voff,
+      buffer_to_lds16(buffer_of(k + x * STEP * kp, rest > 0 ? (unsigned)(((rest - 1) * (int)kp + D) * 2) : 0u), koff[x % OFFS], at + to + x * NW * 1024);
+      buffer_to_lds16(buffer_of(v + x * STEP * vp, rest > 0 ? (unsigned)(((rest - 1) * (int)vp + D) * 2) : 0u), voff[x % OFFS],
                       at + to + Sh::BYTES + x * NW * 1024);
     }
   }

@@ -323,3 +323,22 @@ def test_rows_far_apart(H, Hkv, D, dtype):
     laser.laser_history_attention_backward(fq, fk, fv, o, lse, go, off, 300, gamma, *parts)
     for a, b in zip(near, parts):
         assert torch.equal(a[:n], b[:n]) and (b[n:] == 0).all()
+
+
+@pytest.mark.parametrize("lens,H,Hkv,D", [([1100], 1, 1, 64), ([600, 40], 4, 2, 40), ([300, 1, 0], 2, 2, 32), ([2100, 30], 2, 1, 128),
+                                          ([33, 520], 3, 1, 96), ([400] * 3, 5, 1, 16), ([129, 257], 3, 1, 64), ([2731], 3, 1, 128)])
+def test_few_and_long(lens, H, Hkv, D):
+    """So few workgroups that their waves share one's way: forward, gradients, and the same bits again."""
+    gamma = math.sqrt(D)
+    q, k, v, off, host = make(lens, H, Hkv, D, "bf16", seed=11)
+    L = max(lens)
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, L, gamma)
+    check_forward(o, lse, q, k, v, host, gamma, "bf16")
+    go = torch.randn(o.shape, generator=torch.Generator().manual_seed(12)).to(torch.bfloat16).cuda()
+    grads = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, L, gamma)
+    check_backward(grads, q, k, v, go, host, gamma, "bf16")
+    again = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, L, gamma)
+    o2, lse2 = laser.laser_history_attention_forward(q, k, v, off, L, gamma)
+    for a, b in ((o, o2), (lse, lse2), *zip(grads, again)):
+        n, start = host[-1] - host[0], host[0]
+        assert torch.equal(a[start:start + n], b[start:start + n])
