@@ -353,6 +353,160 @@ __global__ __launch_bounds__(64 * NW, 2) void history_tile_kernel(const TileArgs
   });
 }
 
+// The same over packed sequences where workgroups are few and the longest one's way is what counts: the waves are NG groups of NW, which own
+// the same rows, take the tiles in turn, each with its own maximum and sum, and are joined at the end in their order.
+template <int DP, int NW, int NG>
+__global__ __launch_bounds__(64 * NW * NG, 2) void history_groups_kernel(const TileArgs a) {
+  using Sh = TileShape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32, ROWS = NW * 32, OP = DP * 2 + 16, STAGE = 2 * Sh::BYTES, TILES = 2 * NG * STAGE;
+  static_assert(ROWS * DP * 4 <= TILES && NW * 32 * OP <= TILES, "what is joined, and the patches, take the tiles' place");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[TILES];
+  __shared__ float join_m[ROWS], join_l[ROWS];
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const Place place = place_of(a.deal, blockIdx.x);
+  if (place.rank >= a.deal.tiles) return;
+  const int tile = a.tiles - 1 - place.rank;   // (the longest first)
+  const int n_seq = place.pair / a.Hkv, hk = place.pair - n_seq * a.Hkv;
+  const CandRange cr = cand_range(a.off, n_seq, a.C, a.T);
+  const int n = cr.count, rows = n * a.G, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_all / NW, wave = wave_all % NW;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  const int end = (int)a.by_group.div(row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1) + 1;   // behind the last item that is seen
+
+  PackedTiles<DP, NW> tiles;
+  tiles.init(a.D, a.kp, a.vp, wave, lane);
+  auto fetch = [&](int t0, unsigned at) __attribute__((always_inline)) {
+    const size_t row = (size_t)(cr.first + t0);
+    tiles.fetch(a.k + row * a.kp + (size_t)hk * a.D, a.v + row * a.vp + (size_t)hk * a.D, a.kp, a.vp, a.D, n - t0, at);
+  };
+  unsigned at = lds + group * 2 * STAGE, other = at + STAGE;
+  if (group * TI < end) fetch(group * TI, at);
+
+  const int first = row0 + wave * 32;
+  int last;
+  bf16x8 qreg[KS];
+  {
+    int r = first + l32;
+    r = r < rows ? r : rows - 1;
+    last = (int)a.by_group.div(r);
+    const unsigned short* qr = a.q + (size_t)(cr.first + last) * a.qp + (size_t)(hk * a.G + r - last * a.G) * a.D;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (s * 16 + h * 8 < a.D) raw = *reinterpret_cast<const u32x4*>(qr + s * 16 + h * 8);
+      qreg[s] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
+
+  f32x16 acc[DB];
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero;
+  float m = -INFINITY, l = 0.0f;
+  TileReader<DP> read(lane);
+  auto block = [&](int t0, int ib) __attribute__((always_inline)) {
+    f32x16 sc;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read.rows(0, ib, s), qreg[s], s == 0 ? zero : sc, 0, 0, 0);
+    bf16x8 vt[2][DB];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vt[s][db] = read.cols(Sh::BYTES, ib * 2 + s, db);
+    if (t0 + 31 > wave_first) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t0 + 8 * (r >> 2) + 4 * h + (r & 3) > last) sc[r] = -INFINITY;
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = half_max(top) * a.scale;
+    if (__any(top > m + MAX_SLACK)) {   // (the first block: m is -inf)
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= c;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    unsigned p[8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], a.scale, -base));
+      sum += p0 + p1;
+      p[r >> 1] = pack_bf16(p0, p1);
+    }
+    l += sum;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 b = {p[s * 4], p[s * 4 + 1], p[s * 4 + 2], p[s * 4 + 3]};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[s][db], __builtin_bit_cast(bf16x8, b), acc[db], 0, 0, 0);
+      }
+  };
+  for (int t0 = group * TI, turn = 0; turn < end; t0 += NG * TI, turn += NG * TI) {   // (every group the same number of turns)
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    barrier_lds();
+    if (t0 + NG * TI < end) fetch(t0 + NG * TI, other);
+    read.place(at);
+    if (t0 <= wave_last) block(t0, 0);
+    if (t0 + 32 <= wave_last) block(t0 + 32, 1);
+    const unsigned x = at;
+    at = other;
+    other = x;
+  }
+  barrier_lds();
+  l = half_sum(l);
+  float* mine = reinterpret_cast<float*>(smem) + (size_t)wave * 32 * DP + lane;
+#pragma unroll 1
+  for (int g = 1; g < NG; ++g) {
+    if (group == g) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mine[(db * 16 + r) * 64] = acc[db][r];
+      if (h == 0) {
+        join_m[wave * 32 + l32] = m;
+        join_l[wave * 32 + l32] = l;
+      }
+    }
+    __syncthreads();
+    if (group == 0) {   // (it has the first tile, of which every row sees an item: its maximum is finite)
+      const float m2 = join_m[wave * 32 + l32], top = fmaxf(m, m2), c = __builtin_amdgcn_exp2f(m - top), c2 = __builtin_amdgcn_exp2f(m2 - top);
+      m = top;
+      l = fmaf(join_l[wave * 32 + l32], c2, l * c);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = fmaf(mine[(db * 16 + r) * 64], c2, acc[db][r] * c);
+    }
+    __syncthreads();
+  }
+  if (group > 0) return;
+  const int r = first + l32;
+  if (a.lse != nullptr && h == 0 && r < rows)
+    a.lse[(size_t)(cr.first + last) * a.H + hk * a.G + r - last * a.G] = (m + log2f(l)) * LN2;
+  store_block<DP>(acc, 1.0f / l, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
+    const int i = (int)a.by_group.div(first + r), g = first + r - i * a.G;
+    return a.o + ((size_t)(cr.first + i) * a.H + hk * a.G + g) * a.D;
+  });
+}
+
+template <int DP, int NW, int NG>
+static laser_status groups_launch(TileArgs a, hipStream_t stream) {
+  a.tiles = (int)(((long long)a.C * a.G + NW * 32 - 1) / (NW * 32));
+  if (!deal((long long)a.N * a.Hkv, a.tiles, &a.deal)) return LASER_ERR_SHAPE;
+  history_groups_kernel<DP, NW, NG><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
+  return launch_status();
+}
+
 template <int DP, int SLOTS, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
   a.tiles = (int)(((long long)a.C * a.G + NW * 32 - 1) / (NW * 32));
@@ -382,6 +536,18 @@ laser_status history_tile_launch(const HistoryArgs& h) {
   a.runs = 1;
   a.o = static_cast<unsigned short*>(h.o);
   a.lse = h.lse;
+  // Groups of waves where workgroups of 128 rows would leave much of the machine idle; four of two waves down to 256 rows, or two of four,
+  // at width 128 only these, and there also where there are a few more, but long (us by the ring, four groups, two groups): one history of
+  // 2894 items, 4 heads of 64 over 2 (92 workgroups) 46, 23, 34; 30 of 200, 4 of 64 over 4 (240, of 200 rows) 9.0, 12.2, 7.4; eight of 1000,
+  // 8 of 64 over 2 (512) 22, 33, 19; width 128: two of 2635, 4 over one (166) 57, two groups 44; two of 4096, 8 over 2 (512) 102 and 85;
+  // eight of 1000, 8 over 2 (512, of 4000 rows) 31.3 and 31.4.
+  const long long rows = (long long)h.L * a.G, workgroups = (rows + 127) / 128 * h.N * h.Hkv;
+  if (a.D > 64) {
+    if (workgroups <= 256 || (workgroups <= 512 && rows >= 8192)) return groups_launch<128, 4, 2>(a, h.stream);
+  } else if (workgroups <= 512) {
+    if (workgroups <= 256 && rows >= 256) return a.D > 32 ? groups_launch<64, 2, 4>(a, h.stream) : groups_launch<32, 2, 4>(a, h.stream);
+    return a.D > 32 ? groups_launch<64, 4, 2>(a, h.stream) : groups_launch<32, 4, 2>(a, h.stream);
+  }
   return tile_launch_any<false>(a, h.stream);
 }
 

@@ -326,7 +326,8 @@ def test_rows_far_apart(H, Hkv, D, dtype):
 
 
 @pytest.mark.parametrize("lens,H,Hkv,D", [([1100], 1, 1, 64), ([600, 40], 4, 2, 40), ([300, 1, 0], 2, 2, 32), ([2100, 30], 2, 1, 128),
-                                          ([33, 520], 3, 1, 96), ([400] * 3, 5, 1, 16), ([129, 257], 3, 1, 64), ([2731], 3, 1, 128)])
+                                          ([33, 520], 3, 1, 96), ([400] * 3, 5, 1, 16), ([129, 257], 3, 1, 64), ([2731], 3, 1, 128),
+                                          ([200] * 30, 4, 4, 64), ([31, 1, 65, 0, 64], 2, 2, 24), ([4100, 4000], 8, 2, 72)])
 def test_few_and_long(lens, H, Hkv, D):
     """So few workgroups that their waves share one's way: forward, gradients, and the same bits again."""
     gamma = math.sqrt(D)
