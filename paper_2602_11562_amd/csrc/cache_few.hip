@@ -386,10 +386,20 @@ CacheRuns cache_runs(long long workgroups, int L, int want, int least, int tile)
 template <int DP>
 static laser_status few_typed(const CacheArgs& a, const CacheRuns& r) {
   const int G = a.H / a.Hkv;
-  const long long grid = (long long)a.U * a.Hkv * r.runs;
-  if (grid > 0x7fffffffLL) return LASER_ERR_SHAPE;
-  cache_few_kernel<DP><<<(unsigned)grid, 256, 0, a.stream>>>(a, G, mul_div(G), LOG2E / a.gamma, r.chunk, r.runs);
-  return r.runs > 1 ? cache_join_launch(a, r.chunk, r.runs) : launch_status();
+  const long long each = (long long)a.Hkv * r.runs;   // workgroups of a user
+  if (a.U * each > 0x7fffffffLL) return LASER_ERR_SHAPE;
+  const long long most = 0xffffffffLL / 256 / each;   // (a launch has fewer than 2^32 threads; a user has Hkv * runs <= 2^20 workgroups)
+  for (long long u = 0; u < a.U; u += most) {
+    CacheArgs part = a;
+    part.U = a.U - u < most ? (int)(a.U - u) : (int)most;
+    part.off = a.off + u;
+    part.pages = a.pages + u * a.max_pages;
+    part.lens = a.lens + u;
+    cache_few_kernel<DP><<<(unsigned)(part.U * each), 256, 0, a.stream>>>(part, G, mul_div(G), LOG2E / a.gamma, r.chunk, r.runs);
+    const laser_status s = launch_status();
+    if (s != LASER_OK) return s;
+  }
+  return r.runs > 1 ? cache_join_launch(a, r.chunk, r.runs) : LASER_OK;
 }
 laser_status cache_few_launch(const CacheArgs& a, const CacheRuns& r) {
   if (a.D > 64) return few_typed<128>(a, r);

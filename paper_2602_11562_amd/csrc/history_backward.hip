@@ -440,24 +440,26 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void history_dkv_kernel(const BwdA
 }
 
 template <int DP, int NW, int NG, int RT = (DP > 64 ? 32 : 64)>
-static laser_status dkv_launch(BwdArgs a, hipStream_t stream) {
-  if (!deal((long long)a.N * a.Hkv, ((long long)a.L + NW * 32 - 1) / (NW * 32), &a.deal)) return LASER_ERR_SHAPE;
-  history_dkv_kernel<DP, NW, NG, RT><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
-  return launch_status();
+static laser_status dkv_launch(const BwdArgs& a, hipStream_t stream) {
+  return launch_dealt(a, ((long long)a.L + NW * 32 - 1) / (NW * 32), 64 * NW * NG, [&](const BwdArgs& part, long long) {
+    history_dkv_kernel<DP, NW, NG, RT><<<part.deal.grid, 64 * NW * NG, 0, stream>>>(part);
+  });
 }
 
 template <int DP, int NW, int NG>
-static laser_status dq_launch(BwdArgs a, hipStream_t stream) {
-  if (!deal((long long)a.N * a.Hkv, ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), &a.deal)) return LASER_ERR_SHAPE;
-  history_dq_kernel<DP, NW, NG><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
-  return launch_status();
+static laser_status dq_launch(const BwdArgs& a, hipStream_t stream) {
+  return launch_dealt(a, ((long long)a.L * a.G + NW * 32 - 1) / (NW * 32), 64 * NW * NG, [&](const BwdArgs& part, long long) {
+    history_dq_kernel<DP, NW, NG><<<part.deal.grid, 64 * NW * NG, 0, stream>>>(part);
+  });
 }
 
 template <int DP>
-static laser_status bwd_launch(BwdArgs a, hipStream_t stream) {
+static laser_status bwd_launch(const BwdArgs& a, hipStream_t stream) {
   const long long per = (long long)a.N * a.Hkv;
-  Deal items;   // (before anything is launched)
-  if (!deal(per, ((long long)a.L + 31) / 32, &items) || !deal(per, ((long long)a.L * a.G + 31) / 32, &items)) return LASER_ERR_SHAPE;
+  // (before anything is launched; the forms with smaller tiles or more threads are those of few workgroups)
+  if (sequences_a_launch(a.N, a.Hkv, ((long long)a.L * a.G + 127) / 128, 256) <= 0 ||
+      sequences_a_launch(a.N, a.Hkv, ((long long)a.L + 127) / 128, 256) <= 0)
+    return LASER_ERR_SHAPE;
   // dq has two groups (of four waves, width 128) or four (of two) where its workgroups of 128 rows would leave much of the machine idle,
   // and at width 128 also where there are a few more, but long. Forward and backward without and with: one history of 2894 items, 4 heads
   // of 32 over 2 (92 workgroups) 74 and 54 us; of 64 104 and 78; four of 300, 4 of 64 over 2 (40) 27.0 and 26.4; two of 2635, 4 of 128 over

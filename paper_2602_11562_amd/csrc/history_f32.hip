@@ -657,10 +657,14 @@ static laser_status forward_typed(F32Args a, hipStream_t stream) {
   const long long rows = (long long)a.C * a.G, per = (long long)a.N * a.Hkv;
   const bool split = splits((rows + 127) / 128 * a.runs * per, rows);
   a.tiles = (int)((rows + (split ? 31 : 127)) / (split ? 32 : 128));
-  if (!deal(per, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
-  if (split) history_f32_kernel<DP, PAGED, true><<<a.deal.grid, 256, 0, stream>>>(a);
-  else history_f32_kernel<DP, PAGED, false><<<a.deal.grid, 256, 0, stream>>>(a);
-  return launch_status();
+  return launch_dealt(a, (long long)a.tiles * a.runs, 256, [&](F32Args& part, long long n) {
+    if constexpr (PAGED) {
+      part.pages += n * a.max_pages;
+      part.lens += n;
+    }
+    if (split) history_f32_kernel<DP, PAGED, true><<<part.deal.grid, 256, 0, stream>>>(part);
+    else history_f32_kernel<DP, PAGED, false><<<part.deal.grid, 256, 0, stream>>>(part);
+  });
 }
 laser_status history_f32_launch(const HistoryArgs& h) {
   const F32Args a = of_history(h);
@@ -674,18 +678,22 @@ laser_status cache_f32_launch(const CacheArgs& c, const CacheRuns& r) {
 }
 
 template <int DP>
-static laser_status backward_typed(F32Args a, hipStream_t stream) {
-  F32Args b = a;
+static laser_status backward_typed(const F32Args& a, hipStream_t stream) {
   const long long per = (long long)a.N * a.Hkv, rows = (long long)a.L * a.G;
   const bool split_rows = splits((rows + 127) / 128 * per, rows), split_items = splits(((long long)a.L + 127) / 128 * per, a.L);
-  if (!deal(per, (rows + (split_rows ? 31 : 127)) / (split_rows ? 32 : 128), &a.deal) ||
-      !deal(per, ((long long)a.L + (split_items ? 31 : 127)) / (split_items ? 32 : 128), &b.deal))
-    return LASER_ERR_SHAPE;
-  if (split_rows) history_dq_f32_kernel<DP, true><<<a.deal.grid, 256, 0, stream>>>(a);
-  else history_dq_f32_kernel<DP, false><<<a.deal.grid, 256, 0, stream>>>(a);
-  if (split_items) history_dkv_f32_kernel<DP, true><<<b.deal.grid, 256, 0, stream>>>(b);
-  else history_dkv_f32_kernel<DP, false><<<b.deal.grid, 256, 0, stream>>>(b);
-  return launch_status();
+  const long long row_tiles = (rows + (split_rows ? 31 : 127)) / (split_rows ? 32 : 128);
+  const long long item_tiles = ((long long)a.L + (split_items ? 31 : 127)) / (split_items ? 32 : 128);
+  // (both before anything is launched)
+  if (sequences_a_launch(a.N, a.Hkv, row_tiles, 256) <= 0 || sequences_a_launch(a.N, a.Hkv, item_tiles, 256) <= 0) return LASER_ERR_SHAPE;
+  const laser_status s = launch_dealt(a, row_tiles, 256, [&](const F32Args& part, long long) {
+    if (split_rows) history_dq_f32_kernel<DP, true><<<part.deal.grid, 256, 0, stream>>>(part);
+    else history_dq_f32_kernel<DP, false><<<part.deal.grid, 256, 0, stream>>>(part);
+  });
+  if (s != LASER_OK) return s;
+  return launch_dealt(a, item_tiles, 256, [&](const F32Args& part, long long) {
+    if (split_items) history_dkv_f32_kernel<DP, true><<<part.deal.grid, 256, 0, stream>>>(part);
+    else history_dkv_f32_kernel<DP, false><<<part.deal.grid, 256, 0, stream>>>(part);
+  });
 }
 laser_status history_bwd_f32_launch(const HistoryBwdArgs& b) {
   F32Args a = of_history(b.f);

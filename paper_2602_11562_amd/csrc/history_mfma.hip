@@ -502,17 +502,21 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void history_groups_kernel(const T
 template <int DP, int NW, int NG>
 static laser_status groups_launch(TileArgs a, hipStream_t stream) {
   a.tiles = (int)(((long long)a.C * a.G + NW * 32 - 1) / (NW * 32));
-  if (!deal((long long)a.N * a.Hkv, a.tiles, &a.deal)) return LASER_ERR_SHAPE;
-  history_groups_kernel<DP, NW, NG><<<a.deal.grid, 64 * NW * NG, 0, stream>>>(a);
-  return launch_status();
+  return launch_dealt(a, a.tiles, 64 * NW * NG, [&](const TileArgs& part, long long) {
+    history_groups_kernel<DP, NW, NG><<<part.deal.grid, 64 * NW * NG, 0, stream>>>(part);
+  });
 }
 
 template <int DP, int SLOTS, bool PAGED>
 static laser_status tile_launch(TileArgs a, hipStream_t stream) {
   a.tiles = (int)(((long long)a.C * a.G + NW * 32 - 1) / (NW * 32));
-  if (!deal((long long)a.N * a.Hkv, (long long)a.tiles * a.runs, &a.deal)) return LASER_ERR_SHAPE;
-  history_tile_kernel<DP, SLOTS, PAGED><<<a.deal.grid, 64 * NW, 0, stream>>>(a);
-  return launch_status();
+  return launch_dealt(a, (long long)a.tiles * a.runs, 64 * NW, [&](TileArgs& part, long long n) {
+    if constexpr (PAGED) {
+      part.pages += n * a.max_pages;
+      part.lens += n;
+    }
+    history_tile_kernel<DP, SLOTS, PAGED><<<part.deal.grid, 64 * NW, 0, stream>>>(part);
+  });
 }
 template <bool PAGED>
 static laser_status tile_launch_any(const TileArgs& a, hipStream_t stream) {

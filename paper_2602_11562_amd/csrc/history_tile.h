@@ -39,6 +39,30 @@ inline bool deal(long long per, long long tiles, Deal* d) {
   *d = Deal{(int)per, (int)tiles, (int)run, mul_div((unsigned)run), mul_div((unsigned)per), (unsigned)grid};
   return true;
 }
+// How many sequences of `tiles` tiles for each of Hkv heads one launch holds, which has fewer than 2^32 threads (the grid grows with the
+// longest sequence, whatever the rows are in all). 0: the N of the call have more than 2^31 - 1 workgroups, or one has too many.
+inline int sequences_a_launch(int N, int Hkv, long long tiles, int threads) {
+  Deal all;
+  if (!deal((long long)N * Hkv, tiles, &all)) return 0;
+  const long long runs = (tiles + all.run - 1) / all.run, most = 0xffffffffLL / threads / (8 * all.run) * 8 / (runs * Hkv);
+  return most < N ? (int)most : N;
+}
+// The call in as many launches as that takes, mostly one. go(part, n): a launch for sequences n and on, part.N of them
+template <typename Args, typename Go>
+laser_status launch_dealt(const Args& a, long long tiles, int threads, Go&& go) {
+  const int most = sequences_a_launch(a.N, a.Hkv, tiles, threads);
+  if (most <= 0) return LASER_ERR_SHAPE;
+  for (long long n = 0; n < a.N; n += most) {
+    Args part = a;
+    part.N = a.N - n < most ? (int)(a.N - n) : most;
+    part.off = a.off + n;
+    deal((long long)part.N * a.Hkv, tiles, &part.deal);
+    go(part, n);
+    const laser_status s = launch_status();
+    if (s != LASER_OK) return s;
+  }
+  return LASER_OK;
+}
 struct Place { int rank, pair; };   // the how manieth tile of which pair; rank >= tiles: none
 __device__ __forceinline__ Place place_of(const Deal& d, unsigned block) {
   const unsigned at = block >> 3, row = d.by_run.div(at), chunk = row * 8 + (block & 7), turn = d.by_per.div(chunk);

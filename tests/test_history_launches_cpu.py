@@ -1,0 +1,73 @@
+"""What attention among a history's items launches, without a GPU: calls of more threads than one launch holds, their slices."""
+import ctypes
+
+import pytest
+
+from test_launches_cpu import A, BF16, F32, launches, recorder   # noqa: F401 (a fixture)
+
+SHAPE = 2
+THREADS = 1 << 32     # a launch holds fewer
+
+
+def forward(N, T, L, H, Hkv, D, dt):
+    return lambda lib: lib.laser_history_attention_forward(A, H * D, A, Hkv * D, A, Hkv * D, A, N, T, L, H, Hkv, D, 1.0, dt, A, A, None)
+
+
+def backward(N, T, L, H, Hkv, D, dt):
+    return lambda lib: lib.laser_history_attention_backward(A, H * D, A, Hkv * D, A, Hkv * D, A, A, A, A, N, T, L, H, Hkv, D, 1.0, dt, A, H * D,
+                                                            A, Hkv * D, A, Hkv * D, A, 1 << 50, None)
+
+
+def attend(U, T, C, L, H, Hkv, D, dt):
+    return lambda lib: lib.laser_cache_attention_forward(A, H * D, A, A, A, A, A, U, T, C, 1 << 20, 16, 1 << 20, L, H, Hkv, D, 1.0, 1, dt, A, A, A,
+                                                         1 << 50, None)
+
+
+def sums(records):
+    """{kernel: workgroups of all its launches}; every launch holds fewer than 2^32 threads."""
+    out = {}
+    for r in records:
+        assert r.grid > 0 and r.grid * r.block < THREADS, (r.kernel, r.grid, r.block)
+        out.setdefault(r.kernel.decode(), []).append(r.grid)
+    return out
+
+
+#              N        T          L      H Hkv  D
+PACKED = [(100_000, 10_000_000, 8000, 4, 4, 32), (100_000, 10_000_000, 8000, 4, 4, 128), (3_000_000, 4_000_000, 700, 4, 2, 64),
+          (9_000_000, 9_000_000, 20, 2, 2, 64), (2, 100, 50, 4, 2, 64), (300, 100_000, 5000, 8, 2, 128)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("N,T,L,H,Hkv,D", PACKED)
+def test_packed_batches_with_a_long_outlier(recorder, N, T, L, H, Hkv, D, dt):
+    """Grids grow with N * L_max, whatever T is: they go out in slices that hold whole sequences, and cover all of them."""
+    for call, kernels in ((forward, 1), (backward, 2)):
+        seen = sums(launches(recorder, call(N, T, L, H, Hkv, D, dt)))
+        print(call.__name__, {k[-60:]: v for k, v in seen.items()})
+        assert len(seen) == kernels
+        for grids in seen.values():
+            # tiles of 32 to 128 rows or items, whole eights of workgroups (of runs of four tiles) in each launch
+            least, most = N * Hkv * -(-L // 128), N * Hkv * (-(-L * H // Hkv // 32) + 3)
+            assert least <= sum(grids) <= most + 32 * len(grids)
+            assert all(g % 8 == 0 for g in grids) and max(grids) == grids[0]
+
+
+def test_a_call_of_too_many_workgroups_launches_nothing(recorder):
+    """More than 2^31 - 1 workgroups, counted in the tiles of the form that the call has: refused as a whole, both ways."""
+    for call in (forward, backward):
+        for dt in (F32, BF16):
+            recorder.launch_clear()
+            assert call(1 << 30, 1 << 20, 1 << 20, 64, 64, 64, dt)(recorder) == SHAPE and recorder.launch_count() == 0
+    # what the forward pass takes the backward pass takes: 2^29 workgroups of 128 rows, 2^31 of 32
+    for call in (forward, backward):
+        recorder.launch_clear()
+        assert call(1 << 20, 1 << 20, 1 << 16, 1, 1, 64, BF16)(recorder) == 0, call.__name__
+
+
+@pytest.mark.parametrize("dt,D,U,C,L,H,Hkv", [(BF16, 64, 9_000_000, 1, 500, 2, 2), (BF16, 128, 20_000_000, 1, 40, 1, 1), (F32, 64, 6_000_000, 3, 90, 6, 3),
+                                             (BF16, 32, 5_000_000, 40, 90, 8, 4), (BF16, 64, 70_000, 1, 5000, 4, 2)])
+def test_caches_of_many_users(recorder, dt, D, U, C, L, H, Hkv):
+    seen = sums(launches(recorder, attend(U, U, C, L, H, Hkv, D, dt)))
+    print({k[-60:]: v for k, v in seen.items()})
+    (grids,) = seen.values()
+    assert U * Hkv <= sum(grids) <= U * Hkv * (-(-C * H // Hkv // 32) + 3) + 32 * len(grids)
