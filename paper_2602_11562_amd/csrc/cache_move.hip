@@ -172,7 +172,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(unsigned char* k, unsig
                                                          int Hkv, int head_bytes, int log2, int P, int max_pages,
                                                          int max_pages_out, int budget) {
   const int u = blockIdx.y;
-  const int n = lens_out[u];
+  int n = lens_out[u];   // (the selection's; whatever stands there, no more than kept has room for)
+  n = n < 0 ? 0 : (n > budget ? budget : n);
   const int pieces = head_bytes >> 4, per_row = pieces * Hkv, mask = (1 << log2) - 1;
   const long long all = (long long)n * per_row;
   for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < all; e += (long long)gridDim.x * 256) {
@@ -191,8 +192,15 @@ __global__ __launch_bounds__(256) void cache_move_kernel(unsigned char* k, unsig
 laser_status cache_evict_launch(const CacheEvictArgs& a) {
   const CacheArgs& c = a.c;
   const int head_bytes = c.D * (c.dt == LASER_F32 ? 4 : 2);
-  cache_select_kernel<<<c.U, SEL, 0, c.stream>>>(c.weight, c.pages, c.lens, c.L, c.page_log2, c.P, c.max_pages, a.budget,
-                                                 a.recent, a.lens_out, a.kept);
+  // (a launch holds fewer than 2^32 threads; rows are moved only once every list of them is under way)
+  constexpr int USERS = 1 << 21;
+  for (long long u = 0; u < c.U; u += USERS) {
+    const int users = c.U - u < USERS ? (int)(c.U - u) : USERS;
+    cache_select_kernel<<<users, SEL, 0, c.stream>>>(c.weight, c.pages + u * c.max_pages, c.lens + u, c.L, c.page_log2, c.P, c.max_pages, a.budget,
+                                                     a.recent, a.lens_out + u, a.kept + u * a.budget);
+    const laser_status s = launch_status();
+    if (s != LASER_OK) return s;
+  }
   const int rows = a.budget < c.L ? a.budget : c.L;
   const long long most = ((long long)rows * c.Hkv * head_bytes / 16 + 255) / 256;
   for (int u = 0; u < c.U; u += 65535) {

@@ -71,3 +71,14 @@ def test_caches_of_many_users(recorder, dt, D, U, C, L, H, Hkv):
     print({k[-60:]: v for k, v in seen.items()})
     (grids,) = seen.values()
     assert U * Hkv <= sum(grids) <= U * Hkv * (-(-C * H // Hkv // 32) + 3) + 32 * len(grids)
+
+
+@pytest.mark.parametrize("U,budget", [(4_300_000, 1), (1 << 22, 500), ((1 << 22) - 1, 3), (70_000, 20), (3, 1000)])
+def test_eviction_of_many_users(recorder, U, budget):
+    """The selection, a workgroup of 1024 threads a user, covers every user in launches that hold it, all of them ahead of the moves."""
+    records = launches(recorder, lambda lib: lib.laser_cache_evict(A, A, A, A, A, A, U, 1 << 20, 16, 64, 64, 1000, budget, 0, 2, 64, BF16, A, A, None))
+    names = [r.kernel.decode() for r in records]
+    seen = sums(records)
+    select, = (grids for name, grids in seen.items() if "cache_select_kernel" in name)
+    assert sum(select) == U and all("cache_select_kernel" in n for n in names[:len(select)])
+    assert all("cache_move_kernel" in n for n in names[len(select):]) and len(names) - len(select) == -(-U // 65535)

@@ -80,3 +80,34 @@ def test_cache(C, dtype):
     laser.laser_cache_weights(q, lse, kc, off, pages, held, C, L, 8.0, weight, add=False)
     host = sorted(set(off.tolist()))
     check(o, lse, weight, q, cache, host, 8.0, True, dtype)
+
+
+def test_evict():
+    """Past 2^22 users, with lens_out the lengths themselves."""
+    U, Hkv, D, page, budget = 4_300_000, 2, 40, 8, 3
+    lens, places = spread(U, 1 << 21, [7, 2, 3, 4, 8, 1, 5, 6])
+    users = len(places)
+    g = torch.Generator().manual_seed(7)
+    table = torch.randperm(2 * users + 2, generator=g)
+    pages, pages_out = (torch.full((U, 1), -1, dtype=torch.int32) for _ in range(2))
+    pages[places, 0], pages_out[places, 0] = table[:users].int(), table[users:2 * users].int()
+    pages, pages_out, held = pages.cuda(), pages_out.cuda(), lens.int().cuda()
+    k = torch.randn(2 * users + 2, Hkv, page, D, generator=g).cuda()
+    v, weight = k + 1.0, torch.rand(2 * users + 2, page, generator=g).cuda()
+    want_k, want_v, want_w = k.clone(), v.clone(), weight.clone()
+    want = {}
+    for i, u in enumerate(places):
+        n, src, dst = int(lens[u]), int(table[i]), int(table[users + i])
+        w = weight[src].tolist()
+        stay = list(range(n))
+        if n > budget:      # the last one, and the heaviest two of the others
+            stay = sorted(sorted(range(n - 1), key=lambda j: (-w[j], j))[:budget - 1]) + [n - 1]
+        want[u] = stay + [-1] * (budget - len(stay))
+        for to, j in enumerate(stay):
+            want_k[dst, :, to], want_v[dst, :, to], want_w[dst, to] = k[src, :, j], v[src, :, j], weight[src, j]
+    left, kept = laser.laser_cache_evict(k, v, weight, pages, held, pages_out, budget, 1, 8, lens_out=held)
+    assert torch.equal(left.cpu().long(), lens.clamp(max=budget))
+    assert {u: kept[u].tolist() for u in places} == want
+    kept[places] = -1
+    assert (kept == -1).all()
+    assert torch.equal(k, want_k) and torch.equal(v, want_v) and torch.equal(weight, want_w)
