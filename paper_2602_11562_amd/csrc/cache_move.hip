@@ -59,9 +59,10 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// (lens and lens_out may be one array)
 __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restrict__ weight, const int32_t* __restrict__ pages,
-                                                           const int32_t* __restrict__ lens, int L, int log2, int P,
-                                                           int max_pages, int budget, int recent, int32_t* __restrict__ lens_out,
+                                                           const int32_t* lens, int L, int log2, int P,
+                                                           int max_pages, int budget, int recent, int32_t* lens_out,
                                                            int32_t* __restrict__ kept) {
   __shared__ int hist[256];
   __shared__ int wave_keep[SEL / 64], wave_tie[SEL / 64];
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(SEL) void cache_select_kernel(const float* __restri
   const int stay = n < budget ? n : budget;
   int32_t* out = kept + (size_t)u * budget;
   const int32_t* table = pages + (size_t)u * max_pages;
-  __syncthreads();   // (lens_out may be lens itself)
+  __syncthreads();   // (every wave has its length before it is overwritten)
   if (tid == 0) lens_out[u] = stay;
   for (int i = stay + tid; i < budget; i += SEL) out[i] = -1;
   if (n <= budget) {
