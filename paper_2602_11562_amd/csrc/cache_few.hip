@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(const CacheArgs a, 
 
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {
   const long long rows = (long long)a.C * a.H;
-  for (int u = 0; u < a.U; u += 65535) {
+  for (long long u = 0; u < a.U; u += 65535) {
     CacheArgs part = a;
     part.off = a.off + u;
     part.lens = a.lens + u;

@@ -38,7 +38,7 @@ laser_status cache_append_launch(const CacheAppendArgs& a) {
   const int e = c.dt == LASER_F32 ? 4 : 2;
   const long long most = (long long)c.C * c.Hkv * c.D * e / 16;   // pieces of a user with C rows
   const int gx = (int)((most + 255) / 256 < 256 ? (most + 255) / 256 : 256);
-  for (int u = 0; u < c.U; u += 65535) {
+  for (long long u = 0; u < c.U; u += 65535) {
     const int users = c.U - u < 65535 ? c.U - u : 65535;
     cache_append_kernel<<<dim3(gx, users), 256, 0, c.stream>>>(
         static_cast<const unsigned char*>(a.k), static_cast<const unsigned char*>(a.v), a.kp * e, a.vp * e,
@@ -204,7 +204,7 @@ laser_status cache_evict_launch(const CacheEvictArgs& a) {
   }
   const int rows = a.budget < c.L ? a.budget : c.L;
   const long long most = ((long long)rows * c.Hkv * head_bytes / 16 + 255) / 256;
-  for (int u = 0; u < c.U; u += 65535) {
+  for (long long u = 0; u < c.U; u += 65535) {
     const int users = c.U - u < 65535 ? c.U - u : 65535;
     cache_move_kernel<<<dim3((unsigned)(most < 1024 ? most : 1024), users), 256, 0, c.stream>>>(
         static_cast<unsigned char*>(c.k), static_cast<unsigned char*>(c.v), c.weight, c.pages + (size_t)u * c.max_pages,

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_kernel(const CacheArgs a
 template <int DP>
 static laser_status weights_typed(const CacheArgs& a) {
   const int G = a.H / a.Hkv;
-  for (int u = 0; u < a.U; u += 65535) {
+  for (long long u = 0; u < a.U; u += 65535) {
     CacheArgs part = a;
     part.off = a.off + u;
     part.lens = a.lens + u;

@@ -708,7 +708,7 @@ laser_status history_bwd_f32_launch(const HistoryBwdArgs& b) {
 
 template <int DP>
 static laser_status weights_typed(const F32Args& a, hipStream_t stream) {
-  for (int u = 0; u < a.N; u += 65535) {
+  for (long long u = 0; u < a.N; u += 65535) {
     F32Args part = a;
     part.off = a.off + u;
     part.lens = a.lens + u;

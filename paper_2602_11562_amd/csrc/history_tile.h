@@ -30,21 +30,20 @@ struct Deal {
   MulDiv by_run, by_per;
   unsigned grid;
 };
-inline bool deal(long long per, long long tiles, Deal* d) {
+inline long long tiles_a_run(long long tiles) {
   // (16 histories of 820 to 4100 items, tiles a run 1, 2, 4, 8, 16: dq 537, 496, 481, 512, 506 us; 512 of 40 to 200, at most two tiles
   // each, 1 and 2: dq 49 and 58 us, dk and dv 51 and 69)
-  const long long run = tiles >= 32 ? 4 : 1;
-  const long long runs = (tiles + run - 1) / run * per, grid = (runs + 7) / 8 * 8 * run;
-  if (grid > 0x7fffffffLL || per > 0x7fffffffLL) return false;
-  *d = Deal{(int)per, (int)tiles, (int)run, mul_div((unsigned)run), mul_div((unsigned)per), (unsigned)grid};
-  return true;
+  return tiles >= 32 ? 4 : 1;
+}
+inline Deal deal(long long per, long long tiles) {
+  const long long run = tiles_a_run(tiles), runs = (tiles + run - 1) / run * per, grid = (runs + 7) / 8 * 8 * run;
+  return Deal{(int)per, (int)tiles, (int)run, mul_div((unsigned)run), mul_div((unsigned)per), (unsigned)grid};
 }
 // How many sequences of `tiles` tiles for each of Hkv heads one launch holds, which has fewer than 2^32 threads (the grid grows with the
 // longest sequence, whatever the rows are in all). 0: the N of the call have more than 2^31 - 1 workgroups, or one has too many.
 inline int sequences_a_launch(int N, int Hkv, long long tiles, int threads) {
-  Deal all;
-  if (!deal((long long)N * Hkv, tiles, &all)) return 0;
-  const long long runs = (tiles + all.run - 1) / all.run, most = 0xffffffffLL / threads / (8 * all.run) * 8 / (runs * Hkv);
+  if ((long long)N * Hkv > 0x7fffffffLL / tiles) return 0;
+  const long long run = tiles_a_run(tiles), runs = (tiles + run - 1) / run, most = 0xffffffffLL / threads / (8 * run) * 8 / (runs * Hkv);
   return most < N ? (int)most : N;
 }
 // The call in as many launches as that takes, mostly one. go(part, n): a launch for sequences n and on, part.N of them
@@ -56,7 +55,7 @@ laser_status launch_dealt(const Args& a, long long tiles, int threads, Go&& go) 
     Args part = a;
     part.N = a.N - n < most ? (int)(a.N - n) : most;
     part.off = a.off + n;
-    deal((long long)part.N * a.Hkv, tiles, &part.deal);
+    part.deal = deal((long long)part.N * a.Hkv, tiles);
     go(part, n);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;

@@ -82,3 +82,21 @@ def test_eviction_of_many_users(recorder, U, budget):
     select, = (grids for name, grids in seen.items() if "cache_select_kernel" in name)
     assert sum(select) == U and all("cache_select_kernel" in n for n in names[:len(select)])
     assert all("cache_move_kernel" in n for n in names[len(select):]) and len(names) - len(select) == -(-U // 65535)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_as_many_users_as_an_int_counts(recorder, dt):
+    """Slices of 65535 users up to the last user that there can be."""
+    U, D = (1 << 31) - 1, 8
+    slices = -(-U // 65535)
+    append = lambda lib: lib.laser_cache_append(A, D, A, D, A, A, A, A, A, U, 5, 1, 9, 16, 1, 16, 1, D, dt, A, None)
+    weights = lambda lib: lib.laser_cache_weights(A, D, A, A, A, A, A, U, 5, 1, 9, 16, 1, 16, 1, 1, D, 1.0, 1, 1, dt, A, None)
+    evict = lambda lib: lib.laser_cache_evict(A, A, A, A, A, A, U, 9, 16, 1, 1, 16, 1, 0, 1, D, dt, A, A, None)
+    assert len(launches(recorder, append)) == slices and len(launches(recorder, weights)) == slices
+    grids = sums(launches(recorder, evict))
+    assert {k for k, v in grids.items() if len(v) == slices and "cache_move_kernel" in k} and U in [sum(v) for v in grids.values()]
+    grids, = sums(launches(recorder, attend(U, 5, 1, 16, 1, 1, D, dt))).values()
+    assert U <= sum(grids) <= U + 8 * len(grids)
+    for call in (forward, backward):
+        for grids in sums(launches(recorder, call(U - 7, 5, 16, 1, 1, D, dt))).values():
+            assert U - 7 <= sum(grids) <= U - 7 + 8 * len(grids)
