@@ -481,9 +481,11 @@ laser_status laser_gsta_backward(const void* seg, const void* t0, const void* wq
  *   the backward pass takes it). off [N+1] int32 on the device, non-decreasing; sequences may be empty. T: rows of the
  *   buffers; L_max: at least the longest sequence, sizes the launch.
  * Limits: D a multiple of 8, at most 128; H a multiple of H_kv, at most 1024; L_max * H < 2^30; T * H < 2^31; pitches at
- * least heads * D, at most 2^22, and whole 16-byte pieces; N * H_kv times the tiles of L_max * H / H_kv rows (of 128 rows, fp32 up to
- * 64 of 32) at most 2^31 - 1 (where they are more than 2^23 a kernel may go out in several launches, each of whole sequences). Sums, the softmax's statistics and its exponents are fp32; for
- * bf16 storage probabilities are rounded to bf16 ahead of their product with V, o is rounded once.
+ * least heads * D, at most 2^22, and whole 16-byte pieces; N * H_kv times the tiles of L_max * H / H_kv rows (of 128 rows, fp32 up
+ * to 64 of 32) at most 2^31 - 1 (where they are more than 2^23 a kernel may go out in several launches, each of whole sequences);
+ * gamma finite, at least 2^-126 (backward: and at most 2^120), and scores log2(e) q_i . k_j / gamma within fp32. Sums, the
+ * softmax's statistics and its exponents are fp32; for bf16 storage probabilities are rounded to bf16 ahead of their product
+ * with V, o is rounded once.
  * The offsets are clamped on the device so that no access leaves the T rows (a sequence's first row into [0, T], its length
  * into [0, min(L_max, T - first)]); offsets that break the rules give unspecified values in the rows concerned, never a
  * fault. Rows of no sequence are neither read into a result (they may hold anything, NaN included) nor written. The items of

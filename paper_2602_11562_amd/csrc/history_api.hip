@@ -22,12 +22,15 @@ static bool pitch_fits(long long pitch, int heads, int D, laser_dtype dt) {
   return pitch >= (long long)heads * D && pitch <= (1 << 22) && pitch * element_bytes(dt) % 16 == 0;
 }
 
+// log2(e) / gamma, and 1 / gamma of the gradients, are fp32 numbers
+static bool gamma_fits(float gamma) { return gamma >= 0x1p-126f && gamma < INFINITY; }
+
 static laser_status validate_history(const void* q, int64_t qp, const void* k, int64_t kp, const void* v, int64_t vp,
                                      const int32_t* off, int N, int T, int L, int H, int Hkv, int D, float gamma, laser_dtype dt,
                                      const void* o, const float* lse, void* stream, HistoryArgs* out) {
   if (!q || !k || !v || !off || !o) return LASER_ERR_NULL;
   if (dt != LASER_F32 && dt != LASER_BF16) return LASER_ERR_DTYPE;
-  if (!sizes_fit(N, T, L, H, Hkv, D) || !(gamma > 0.0f) || !(gamma < INFINITY)) return LASER_ERR_SHAPE;
+  if (!sizes_fit(N, T, L, H, Hkv, D) || !gamma_fits(gamma)) return LASER_ERR_SHAPE;
   if (!pitch_fits(qp, H, D, dt) || !pitch_fits(kp, Hkv, D, dt) || !pitch_fits(vp, Hkv, D, dt)) return LASER_ERR_SHAPE;
   for (const void* p : {q, k, v, o})
     if (!aligned(p, 16)) return LASER_ERR_ALIGN;
@@ -138,6 +141,7 @@ laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, co
   const laser_status s = validate_history(q, q_pitch, k, k_pitch, v, v_pitch, off, N, T, L_max, H, H_kv, D, gamma, dt, o, lse,
                                           stream, &a.f);
   if (s != LASER_OK) return s;
+  if (gamma > 0x1p120f) return LASER_ERR_SHAPE;   // (scores start at -gamma lse, with lse up to log(L_max) < 21 past the largest score)
   if (!pitch_fits(dq_pitch, H, D, dt) || !pitch_fits(dk_pitch, H_kv, D, dt) || !pitch_fits(dv_pitch, H_kv, D, dt))
     return LASER_ERR_SHAPE;
   for (const void* p : {d_o, (const void*)dq_out, (const void*)dk_out, (const void*)dv_out, (const void*)work})
@@ -188,7 +192,7 @@ laser_status laser_cache_attention_forward(const void* q, int64_t q_pitch, const
   laser_status s = validate_cache(k_cache, v_cache, pages, lens, U, P, page, max_pages, L_max, H_kv, D, dt, stream, &a);
   if (s == LASER_OK) s = validate_rows(q, q_pitch, H, off, T, C_max, &a);
   if (s != LASER_OK) return s;
-  if (!(gamma > 0.0f) || !(gamma < INFINITY)) return LASER_ERR_SHAPE;
+  if (!gamma_fits(gamma)) return LASER_ERR_SHAPE;
   if (!aligned(o_out, 16) || !aligned(lse_out, 4) || !aligned(work, 16)) return LASER_ERR_ALIGN;
   if (work_bytes < cache_attention_work_bytes(U, T, C_max, L_max, H, H_kv, D, dt)) return LASER_ERR_SHAPE;
   a.q = q;
@@ -210,7 +214,7 @@ laser_status laser_cache_weights(const void* q, int64_t q_pitch, const float* ls
   laser_status s = validate_cache(k_cache, k_cache, pages, lens, U, P, page, max_pages, L_max, H_kv, D, dt, stream, &a);
   if (s == LASER_OK) s = validate_rows(q, q_pitch, H, off, T, C_max, &a);
   if (s != LASER_OK) return s;
-  if (!(gamma > 0.0f) || !(gamma < INFINITY)) return LASER_ERR_SHAPE;
+  if (!gamma_fits(gamma)) return LASER_ERR_SHAPE;
   if (!aligned(lse, 4) || !aligned(weight, 4)) return LASER_ERR_ALIGN;
   a.q = q;
   a.qp = q_pitch;
