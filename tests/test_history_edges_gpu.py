@@ -1,4 +1,4 @@
-"""Attention among a history's items at the edges of what it takes: gamma far from one."""
+"""Attention among a history's items at the edges of what it takes: gamma far from one, extreme scores, offsets that break the rules."""
 import pytest
 import torch
 
@@ -22,3 +22,45 @@ def test_gamma_far_from_one(gamma, scale, dtype):
     q, k, v, off, host = make([150, 20, 1, 70], 4, 2, 64, dtype, packed=False)
     q, k = q * scale, k * scale
     both(q, k, v, off, host, 150, gamma, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,gamma", [(6.0, 1.0), (1.0, 0.05), (0.0, 1.0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_gradients_of_extreme_scores(scale, gamma, D, dtype):
+    """Scores in the hundreds, where one item takes everything, and scores that are all equal; rows that see one block and more."""
+    q, k, v, off, host = make([150, 20, 33, 260], 4, 2, D, dtype, scale=scale)
+    both(q, k, v, off, host, 260, gamma, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("off,L,clamped,touched", [
+    ([0, 40, 90], 30, [0, 30], None),                                    # a sequence longer than L_max is cut there
+    ([0, 90], 30, [0, 30], range(30)),
+    ([-5, -9, 10 ** 9, 2 * 10 ** 9], 30, [0, 30], range(30)),            # below, falling, behind the end
+    ([-2 ** 31, 2 ** 31 - 1, 7, 50, 20, 85], 25, None, range(0, 45)),    # a difference past an int; two that overlap
+    ([80, 2 ** 31 - 1, -2 ** 31, 100], 40, None, [*range(0, 40), *range(80, 90)])])
+def test_offsets_that_break_the_rules(off, L, clamped, touched, dtype):
+    """No row outside the clamped sequences is written, by the forward pass or by the gradients; where one sequence is left alone its
+    results are those of the call that names it so."""
+    q, k, v, _, _ = make([90], 4, 2, 64, dtype, before=0, behind=0)
+    go = torch.randn(q.shape, generator=torch.Generator().manual_seed(3)).to(q.dtype).cuda()
+
+    def run(off):
+        off = torch.tensor(off, dtype=torch.int32, device="cuda")
+        out = [torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:2], 7.0, device="cuda")]
+        grads = [torch.full(t.shape, 7.0, dtype=q.dtype, device="cuda") for t in (q, k, v)]
+        laser.laser_history_attention_forward(q, k, v, off, L, 8.0, *out)
+        laser.laser_history_attention_backward(q, k, v, *out, go, off, L, 8.0, *grads)
+        return out + grads
+
+    got = run(off)
+    if touched is None:
+        touched = [*range(30), *range(40, 70)]
+    rest = torch.ones(90, dtype=torch.bool)
+    rest[list(touched)] = False
+    for t in got:
+        assert (t[rest.cuda()] == 7.0).all()
+    if clamped is not None:
+        for t, want in zip(got, run(clamped)):
+            assert torch.equal(t[clamped[0]:clamped[1]], want[clamped[0]:clamped[1]])
