@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2602_11562_amd as laser
+from history_ref import gradients, sees
 from test_history_attention_gpu import check_backward, check_forward, make
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +65,47 @@ def test_offsets_that_break_the_rules(off, L, clamped, touched, dtype):
     if clamped is not None:
         for t, want in zip(got, run(clamped)):
             assert torch.equal(t[clamped[0]:clamped[1]], want[clamped[0]:clamped[1]])
+
+
+class Attention(torch.autograd.Function):
+    """The entry points as a training program wraps them."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, off, L, gamma):
+        o, lse = laser.laser_history_attention_forward(q, k, v, off, L, gamma)
+        ctx.save_for_backward(q, k, v, o, lse, off)
+        ctx.sizes = L, gamma
+        return o
+
+    @staticmethod
+    def backward(ctx, d_o):
+        q, k, v, o, lse, off = ctx.saved_tensors
+        return (*laser.laser_history_attention_backward(q, k, v, o, lse, d_o.contiguous(), off, *ctx.sizes), None, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_through_an_autograd_function(dtype):
+    """A loss of the outputs, differentiated by autograd here and, from the definition in 64 bits, there."""
+    q, k, v, off, host = make([70, 1, 33], 4, 2, 40, dtype, before=0, behind=0, packed=False)
+    gamma, aim = 6.0, torch.randn(q.shape, generator=torch.Generator().manual_seed(9)).to(q.dtype).cuda()
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    (Attention.apply(*leaves, off, 70, gamma) * aim).sum().backward()
+    check_backward([t.grad for t in leaves], q, k, v, aim, host, gamma, dtype)
+    whole = [t.double().requires_grad_() for t in (q, k, v)]
+    loss = 0.0
+    for a, b in zip(host, host[1:]):
+        allowed = torch.ones(b - a, b - a, dtype=torch.bool, device="cuda").tril()
+        for h in range(4):
+            s = torch.where(allowed, whole[0][a:b, h] @ whole[1][a:b, h // 2].t() / gamma, -float("inf"))
+            loss = loss + ((torch.softmax(s, 1) @ whole[2][a:b, h // 2]) * aim[a:b, h].double()).sum()
+    loss.backward()
+    exact = [t.grad for t in whole]
+    # (the definition's derivative and the formulas that the bounds above stand on agree to 64 bits)
+    for a, b in zip(host, host[1:]):
+        allowed = sees(b - a, b - a, True, "cuda")
+        for j in range(2):
+            parts = [gradients(*(t.double() for t in (q[a:b, h], k[a:b, j], v[a:b, j], aim[a:b, h])), gamma, allowed, False) for h in (2 * j, 2 * j + 1)]
+            for h, part in zip((2 * j, 2 * j + 1), parts):
+                assert torch.allclose(exact[0][a:b, h], part[0][0], rtol=1e-10, atol=1e-12)
+            for got, i in ((exact[1], 1), (exact[2], 2)):
+                assert torch.allclose(got[a:b, j], parts[0][i][0] + parts[1][i][0], rtol=1e-10, atol=1e-12)
