@@ -649,13 +649,43 @@ static F32Args of_cache(const CacheArgs& c) {
   return a;
 }
 
-// The split form where the wide one's workgroups are fewer than two a compute unit, or hold rows for one or two of their waves only
-static bool splits(long long workgroups, long long rows_of_a_pair) { return workgroups < 512 || rows_of_a_pair <= 64; }
+// Workgroups of 128 rows, or items, that have any: `longest` of them in each of `per` pairs, `all` in the whole batch
+static long long in_128(long long longest, long long per, long long all) {
+  const long long a = (longest + 127) / 128 * per, b = (all + 127) / 128;
+  return a < b ? a : b;
+}
+// When the split form: the wide form's workgroups against the items that one walks, whose tiles its four waves share; two split
+// workgroups of width 128 do not fit a compute unit. us wide and split, full histories, 4 heads over 4:
+//   items, workgroups        30, 15       60, 60       120, 60      120, 240     500, 125     500, 688     3000, 658    3000, 2344
+//   width 64, forward        6.8, 9.6     9.6, 9.5     15.7, 9.4    17, 24       45, 21       80, 106      387, 303     1002, 1058
+//   width 128, forward       10.5, 15.8   16.5, 16.3   28, 16       32, 65       97, 53       151, 264     709, 758     2139, 2752
+//   width 128, gradients with dq wide and split: 33, 37; 53, 49; 92, 71; 100, 133; 326, 255; 670, 715; 2804, 2655; 9088, 8988
+static bool splits(long long workgroups, long long walk, int D) { return walk > FI && workgroups * (D > 64 ? 2 : 1) <= walk; }
+// dk, dv: the rows of all heads of the group are walked; the split form of width 128 spills. Gradients with dk, dv wide and split: width
+// 64, 1000 items, 4 heads over 2: 782 workgroups (of 128 items) 1030 and 997 us, 195 of 250 items 212 and 176; width 128: 1000 items, 187
+// workgroups 989 and 740, 344 of them 1177 and 1288; 500 items, 4 over 4, 125 326 and 264, 250 328 and 387; 3000 items, 281 1817 and
+// 1713, 375 1820 and 2061. Also where items keep one or two waves of the wide form busy and many rows see them: 1000 histories, widths 64 and
+// 128: 20 items, 4 over 2, 156, 331 and 112, 290; 45 items, 8 over 2, 433, 968 and 331, 929; 2250 of 64, 4 over 2, 686, 1471 and 568, 1597;
+// 1125 of 60, 4 over 4, 436, 962 and 485, 1221.
+static bool splits_items(long long workgroups, long long items, long long walk, int D) {
+  if (items <= 64 && walk > FI && walk >= (D > 64 && items > FI ? 4 : 2) * items) return true;
+  return D > 64 ? workgroups * 3 <= walk && workgroups < 320 : walk > FI && workgroups <= walk;
+}
+// Over a cache histories are cut into runs, of 128 items or more, until workgroups are enough; of lengths below the longest the runs at the
+// end are empty. Split also where the rows of a head keep one or two waves of the wide form busy and the runs are longer than two tiles.
+// us wide and split, 2 heads of widths 32, 64, 128: 2 rows over 2000 items, 256 users: 62, 161, 369 and 45, 84, 190; 32 rows over 2000, 100
+// users: 32, 72, 156 and 29, 49, 110; 64 over 2000, 60 users: 33, 54, 136 and 31, 55, 129; 64 over 64, 500 users: 14, 26, 53 and 21, 48, 130;
+// 400 over 1000, 1 user (64 workgroups): 15, 21, 35 and 12, 15, 23; 800 over 1000, 2 users (200): 16, 23, 40 and 19, 30, 70.
+static bool splits_over_cache(long long workgroups, long long rows, long long walk, int D) {
+  return walk > FI && ((D > 64 ? workgroups * 4 <= walk * 3 : workgroups <= walk) || (rows <= 64 && walk > 2 * FI));
+}
 
 template <int DP, bool PAGED>
 static laser_status forward_typed(F32Args a, hipStream_t stream) {
-  const long long rows = (long long)a.C * a.G, per = (long long)a.N * a.Hkv;
-  const bool split = splits((rows + 127) / 128 * a.runs * per, rows);
+  const long long rows = (long long)a.C * a.G, per = (long long)a.N * a.Hkv, walk = a.runs > 1 ? a.chunk : a.L;
+  long long workgroups = in_128(rows, per, (long long)a.T * a.H) * a.runs;
+  if (PAGED && a.causal) workgroups -= workgroups * (a.C < a.L ? a.C : a.L) / (2LL * a.L);   // (of the runs behind a row's own item)
+  const bool split = PAGED ? splits_over_cache(workgroups, rows, walk, a.D) : splits(workgroups, walk, a.D);
   a.tiles = (int)((rows + (split ? 31 : 127)) / (split ? 32 : 128));
   return launch_dealt(a, (long long)a.tiles * a.runs, 256, [&](F32Args& part, long long n) {
     if constexpr (PAGED) {
@@ -680,7 +710,8 @@ laser_status cache_f32_launch(const CacheArgs& c, const CacheRuns& r) {
 template <int DP>
 static laser_status backward_typed(const F32Args& a, hipStream_t stream) {
   const long long per = (long long)a.N * a.Hkv, rows = (long long)a.L * a.G;
-  const bool split_rows = splits((rows + 127) / 128 * per, rows), split_items = splits(((long long)a.L + 127) / 128 * per, a.L);
+  const bool split_rows = splits(in_128(rows, per, (long long)a.T * a.H), a.L, a.D);
+  const bool split_items = splits_items(in_128(a.L, per, (long long)a.T * a.Hkv), a.L, rows, a.D);
   const long long row_tiles = (rows + (split_rows ? 31 : 127)) / (split_rows ? 32 : 128);
   const long long item_tiles = ((long long)a.L + (split_items ? 31 : 127)) / (split_items ? 32 : 128);
   // (both before anything is launched)

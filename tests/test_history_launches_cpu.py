@@ -1,8 +1,7 @@
-"""What attention among a history's items launches, without a GPU: calls of more threads than one launch holds, their slices."""
-import ctypes
-
+"""What attention among a history's items launches, without a GPU: calls of more threads than one launch holds, their slices, and forms."""
 import pytest
 
+from test_history_f32_forms_gpu import CACHED, PACKED as F32_PACKED, lengths
 from test_launches_cpu import A, BF16, F32, launches, recorder   # noqa: F401 (a fixture)
 
 SHAPE = 2
@@ -100,3 +99,22 @@ def test_as_many_users_as_an_int_counts(recorder, dt):
     for call in (forward, backward):
         for grids in sums(launches(recorder, call(U - 7, 5, 16, 1, 1, D, dt))).values():
             assert U - 7 <= sum(grids) <= U - 7 + 8 * len(grids)
+
+
+@pytest.mark.parametrize("N,L,H,Hkv,D,split,items", F32_PACKED)
+def test_forms_of_packed_calls_in_single_precision(recorder, N, L, H, Hkv, D, split, items):
+    T = sum(lengths(N, L)) + 5
+    first, dq, dkv = (r.kernel.decode() for call in (forward, backward) for r in launches(recorder, call(N, T, L, H, Hkv, D, F32)))
+    print(first, dq, dkv)
+    assert "history_f32_kernelILi" in first and f"Lb0ELb{int(split)}EE" in first
+    assert "history_dq_f32" in dq and f"ELb{int(split)}EE" in dq and "history_dkv_f32" in dkv and f"ELb{int(items)}EE" in dkv
+
+
+@pytest.mark.parametrize("U,C,L,H,Hkv,D,page,split", CACHED)
+def test_forms_of_cached_calls_in_single_precision(recorder, U, C, L, H, Hkv, D, page, split):
+    T = sum(C if i % 3 else (i * 11) % (C + 1) for i in range(U)) + 3
+    for causal in (0, 1):
+        first = launches(recorder, lambda lib: lib.laser_cache_attention_forward(A, H * D, A, A, A, A, A, U, T, C, 1 << 20, page, 1 << 20, L, H, Hkv, D, 1.0,
+                                                                                causal, F32, A, A, A, 1 << 50, None))[0]
+        print(first.kernel)
+        assert f"Lb1ELb{int(split)}EE" in first.kernel.decode()
