@@ -130,6 +130,37 @@ def build_host_check(out: str) -> str:
     return out
 
 
+def build_history_host_check(out: str) -> str:
+    """Build tests/history_host_check.cpp with the host halves of the sources for attention among a history's items, validation and
+    launchers, instrumented with AddressSanitizer and UndefinedBehaviorSanitizer; launches are recorded (tests/launch_recorder.cpp), no
+    device code is there. No GPU needed to build or run it."""
+    os.makedirs(OBJDIR, exist_ok=True)
+    no_kernels = os.path.join(OBJDIR, "no_kernels_host_check.bin")
+    with open(no_kernels, "wb") as f:
+        f.write(b"none")
+    san = ["-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined"]
+    arch_host = [x for f in san for x in ("-Xarch_host", f)]
+    flags = [f for f in HIPCC_FLAGS if not f.startswith("--offload-arch") and f != "-O3"] + [
+        "-O1", "-g", "-Xclang", "-fcuda-include-gpubinary", "-Xclang", no_kernels]
+
+    def compile_one(src: str) -> str:
+        obj = os.path.join(OBJDIR, "san_" + os.path.basename(src).rsplit(".", 1)[0] + ".o")
+        cmd = [_hipcc(), "-x", "hip", "--offload-host-only", *flags, *arch_host, "-c", src, "-o", obj]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"host half of {src}:\n" + r.stderr[-4000:])
+        return obj
+
+    srcs = [os.path.join(CSRC, s) for s in SOURCES if s.startswith(("history_", "cache_"))]
+    srcs += [os.path.join(ROOT, "tests", s) for s in ("launch_recorder.cpp", "history_host_check.cpp")]
+    with ThreadPoolExecutor(max_workers=6) as ex:
+        objs = list(ex.map(compile_one, srcs))
+    r = subprocess.run(["/opt/rocm/lib/llvm/bin/clang++", *san, "-o", out, *objs, "-ldl"], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("history host check link failed:\n" + r.stderr[-4000:])
+    return out
+
+
 def build_launch_recorder(out: str) -> str:
     """Build a library of the same entry points whose launches are recorded instead of made (tests/launch_recorder.cpp): the
     host halves of the sources, with the overrides of a tuning build. No GPU needed to build or use it."""

@@ -92,12 +92,22 @@ laser_status cache_weights_launch(const CacheArgs& a) {
   return a.dt == LASER_F32 ? cache_weights_f32_launch(a) : cache_weights_tile_launch(a);
 }
 
-// Rows of a key-value head that one column block holds: the streaming kernel (bf16)
+// Rows of a key-value head that one column block holds: the streaming kernel (bf16). us by it and by the kernel of tiles: 64 users of up to
+// 4000 items, 8 heads of 128 over 2, 4 rows 46 and 57, 8 rows 50 and 58 (of 64 28 and 34); 300 of 1000, 8 rows of 64 31 and 39; two of
+// 30000, 8 rows of 128 22.5 and 20.9.
 static bool few_rows(int C, int H, int Hkv, laser_dtype dt) { return dt == LASER_BF16 && (long long)C * (H / Hkv) <= 32; }
+// Into how many runs: workgroups wanted, the fewest items of a run and the items that it is a whole number of. us, 8 heads over 2, rows x
+// items, users:
+//   single rows, 512 / 1024 / 2048 wanted: 1 x 20000, 8 of 128: 24.0, 23.8, 24.1; 1 x 5000, 64 of 64: 23.0, 26.8, 25.8, of 128 63, 66, 69;
+//     2 x 3000, 200 of 128: 41.6, 40.0, 41.6; 256 / 512 / 1024 items: 1 x 30000, 1 of 128: 16.4, 16.9, 21.4; 1 x 20000, 8: 28.4, 24.1, 27.1
+//   tiles of rows, 1024 / 2048 wanted: 200 x 20000, 8 of 128: 138, 132; 300 x 3000, 24 of 64: 57.2, 55.1; 400 new items x 9000, 12 of 128: 151, 146;
+//     256 / 512 / 1024 items: 100 x 1000, 1 of 64: 13.9, 18.0, 23.0; 100 x 3000, 1 of 128: 19, 24, 36; 100 x 30000 (118 runs, joined by
+//     the form for many): 45, 35, 40
+//   fp32, 512 / 1024 / 2048 wanted: 1 x 20000, 4 of 128: 54, 44, 46; 1 x 3000, 32 of 64: 25, 31, 32; 2 x 3000, 100 of 128: 81, 72, 79; 128 / 256 /
+//     512 items (its tiles are 32 items, one for each of four waves): 1 x 700, 5 of 64: 11.5, 13.2, 15.2; 1 x 20000, 1 of 64: 17.3, 16.1, 20.6
 static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
   const bool few = few_rows(C, H, Hkv, dt);
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
-  // (a single-precision tile takes its waves 1.7 us for 64 columns, so its runs may be short: one tile for each of four waves)
   if (dt == LASER_F32) return cache_runs((rows + 127) / 128 * pairs, L, 1024, 128, 128);
   return few ? cache_runs(pairs, L, 1024, 512, 128) : cache_runs((rows + 127) / 128 * pairs, L, 2048, 256, 64);
 }
