@@ -2,10 +2,11 @@
 // and everything else is small, so this is bound by memory.
 //
 // A workgroup owns (user, key-value head, run of items); its four waves take tiles of 32 items in turn, each with tiles of its own
-// in LDS and no barrier while it streams: requests run ahead of the arithmetic by as many tiles as fit. The rows (at most 32: every
-// new item's query heads of the group) are one column block of the products of history_mfma.hip. At the end the waves' maxima,
-// sums and outputs are joined in LDS. Histories longer than a run are cut into several workgroups' runs, whose results go to the work
-// buffer (outputs normalised, with log2 of their sums) and are joined by a second launch.
+// in LDS and no barrier while it streams. Up to width 64 two of them, so that requests run a tile ahead of the arithmetic; beyond there is
+// room for one, whose successor is asked for behind its last read, and what runs meanwhile are the other seven waves of the compute unit.
+// The rows (at most 32: every new item's query heads of the group) are one column block of the products of history_mfma.hip, with the same
+// rounding of P. At the end the waves' maxima, sums and outputs are joined in LDS. Histories longer than a run are cut into several
+// workgroups' runs, whose results go to the work buffer (outputs normalised, with log2 of their sums) and are joined by a second launch.
 // 128 users of up to 4096 items, 8 heads of 128 over 2: 27 us for 128 MB; one user of 65000, 16 heads over 2: 17 us for 67 MB (4.7 and
 // 3.9 TB/s; a large copy reaches 5.2). The joins are a launch each, 4 to 6 us.
 #include "history_tile.h"

@@ -7,8 +7,10 @@
 //   dk, dv: a wave owns 32 items of a key-value head and walks the rows that see them, of all its query heads.
 //       Sc = Q K^T, dP = dO V^T (items in lanes), dV^T += dO^T P, dK^T += Q^T dS
 // Seven products where five would do with one kernel, which would have to add one of the gradients up across workgroups.
+// p and ds are rounded to bf16 ahead of their products, which take their operands so (in 32 bits they would take 16 times as long); the sums are
+// fp32. dq and dk are then off by 1.43 to 1.45 times what their own rounding costs, dv by 1.37 (root mean square).
 //
-// Bound: as the forward pass, by products with their exponentials. Width 128: dq 380 us for 16 histories of 820 to 4100 items, 8 heads over
+// Bound: as the forward pass, by products with their exponentials. Width 128: dq 380 us for 16 histories of 920 to 4000 items, 8 heads over
 // 2 (900 TFLOP/s of its three products), dk and dv 560 (810 of their four), whose first items' workgroups run longest. Widths to 64
 // over histories of 40 to 200 items are bound by memory: 47 and 50 us where their bytes take 40 each at a copy's rate.
 #include "history_tile.h"
@@ -473,7 +475,7 @@ static laser_status bwd_launch(const BwdArgs& a, hipStream_t stream) {
   // How many groups of waves share the items of a workgroup, by how many workgroups of 128 items there are and how many rows the first
   // has to walk. Forward and backward, one, two (of four waves) and four groups (of two): 16 histories up to 4096 of 8 heads of 128 over 2
   // (1024 workgroups) 1209, 1130, 1168 us; two of 4096 (128) 740, 585, 451; 64 up to 1024 of 4 heads over 4 (2048) 250, 277, 345; 256 up to
-  // 200 of 4 over 2 (1024) 112, 126, 151.
+  // 200 of 4 over 2 (1024) 112, 126, 151. (Four groups at width 128 spill five registers, 24 bytes of scratch a lane, all the same.)
   // Few workgroups, four groups of two and one of four: 16 histories of 500, 2 of 64 over 2 (128) 24 and 26 us; four of 300, 4 over 2 (24)
   // 21.6 and 26.5; 64 of 200, 4 over 2 (256, of 400 rows) 34 and 28. Eight groups of one wave, where even those of 32 items are few: one of
   // 2894, 4 of 32 over 2 (182 of them) 44 us, with four groups of two 54; eight of 1000, 8 of 64 over 2 (512) 70 and 67.

@@ -661,12 +661,12 @@ static long long in_128(long long longest, long long per, long long all) {
 //   width 128, forward       10.5, 15.8   16.5, 16.3   28, 16       32, 65       97, 53       151, 264     709, 758     2139, 2752
 //   width 128, gradients with dq wide and split: 33, 37; 53, 49; 92, 71; 100, 133; 326, 255; 670, 715; 2804, 2655; 9088, 8988
 static bool splits(long long workgroups, long long walk, int D) { return walk > FI && workgroups * (D > 64 ? 2 : 1) <= walk; }
-// dk, dv: the rows of all heads of the group are walked; the split form of width 128 spills. Gradients with dk, dv wide and split: width
-// 64, 1000 items, 4 heads over 2: 782 workgroups (of 128 items) 1030 and 997 us, 195 of 250 items 212 and 176; width 128: 1000 items, 187
-// workgroups 989 and 740, 344 of them 1177 and 1288; 500 items, 4 over 4, 125 326 and 264, 250 328 and 387; 3000 items, 281 1817 and
-// 1713, 375 1820 and 2061. Also where items keep one or two waves of the wide form busy and many rows see them: 1000 histories, widths 64 and
-// 128: 20 items, 4 over 2, 156, 331 and 112, 290; 45 items, 8 over 2, 433, 968 and 331, 929; 2250 of 64, 4 over 2, 686, 1471 and 568, 1597;
-// 1125 of 60, 4 over 4, 436, 962 and 485, 1221.
+// dk, dv: the rows of all heads of the group are walked; the split form of width 128 spills (296 bytes of scratch a lane). Gradients with
+// dk, dv wide and split: width 64, 1000 items, 4 heads over 2: 782 workgroups (of 128 items) 1030 and 997 us, 195 of 250 items 212 and
+// 176; width 128: 1000 items, 187 workgroups 989 and 740, 344 of them 1177 and 1288; 500 items, 4 over 4, 125 326 and 264, 250 328 and 387;
+// 3000 items, 281 1817 and 1713, 375 1820 and 2061. Also where items keep one or two waves of the wide form busy and many rows see them:
+// 1000 histories, widths 64 and 128: 20 items, 4 over 2, 156, 331 and 112, 290; 45 items, 8 over 2, 433, 968 and 331, 929; 2250 of 64, 4
+// over 2, 686, 1471 and 568, 1597; 1125 of 60, 4 over 4, 436, 962 and 485, 1221.
 static bool splits_items(long long workgroups, long long items, long long walk, int D) {
   if (items <= 64 && walk > FI && walk >= (D > 64 && items > FI ? 4 : 2) * items) return true;
   return D > 64 ? workgroups * 3 <= walk && workgroups < 320 : walk > FI && workgroups <= walk;

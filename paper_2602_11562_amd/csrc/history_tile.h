@@ -31,7 +31,7 @@ struct Deal {
   unsigned grid;
 };
 inline long long tiles_a_run(long long tiles) {
-  // (16 histories of 820 to 4100 items, tiles a run 1, 2, 4, 8, 16: dq 537, 496, 481, 512, 506 us; 512 of 40 to 200, at most two tiles
+  // (16 histories of 920 to 4000 items, tiles a run 1, 2, 4, 8, 16: dq 537, 496, 481, 512, 506 us; 512 of 40 to 200, at most two tiles
   // each, 1 and 2: dq 49 and 58 us, dk and dv 51 and 69)
   return tiles >= 32 ? 4 : 1;
 }
