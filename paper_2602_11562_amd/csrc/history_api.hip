@@ -104,7 +104,7 @@ static bool few_rows(int C, int H, int Hkv, laser_dtype dt) { return dt == LASER
 //     256 / 512 / 1024 items: 100 x 1000, 1 of 64: 13.9, 18.0, 23.0; 100 x 3000, 1 of 128: 19, 24, 36; 100 x 30000 (118 runs, joined by
 //     the form for many): 45, 35, 40
 //   fp32, 512 / 1024 / 2048 wanted: 1 x 20000, 4 of 128: 54, 44, 46; 1 x 3000, 32 of 64: 25, 31, 32; 2 x 3000, 100 of 128: 81, 72, 79; 128 / 256 /
-//     512 items (its tiles are 32 items, one for each of four waves): 1 x 700, 5 of 64: 11.5, 13.2, 15.2; 1 x 20000, 1 of 64: 17.3, 16.1, 20.6
+//     512 items (its tiles are 32 items, one for each of four waves): 1 x 700, 5 of 64 (4 heads): 11.5, 13.2, 15.2; 1 x 20000, 1 of 64: 17.3, 16.1, 20.6
 static CacheRuns runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt) {
   const bool few = few_rows(C, H, Hkv, dt);
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);

@@ -656,13 +656,13 @@ static long long in_128(long long longest, long long per, long long all) {
 }
 // When the split form: the wide form's workgroups against the items that one walks, whose tiles its four waves share; two split
 // workgroups of width 128 do not fit a compute unit. us wide and split, full histories, 4 heads over 4:
-//   items, workgroups        30, 15       60, 60       120, 60      120, 240     500, 125     500, 688     3000, 658    3000, 2344
-//   width 64, forward        6.8, 9.6     9.6, 9.5     15.7, 9.4    17, 24       45, 21       80, 106      387, 303     1002, 1058
+//   items, workgroups        30, 60       60, 60       120, 56      120, 240     500, 125     500, 688     3000, 656    3000, 2344
+//   width 64, forward        6.8, 9.6     9.6, 9.5     15.9, 9.6    17, 26       49, 24       80, 106      387, 303     1002, 1058
 //   width 128, forward       10.5, 15.8   16.5, 16.3   28, 16       32, 65       97, 53       151, 264     709, 758     2139, 2752
-//   width 128, gradients with dq wide and split: 33, 37; 53, 49; 92, 71; 100, 133; 326, 255; 670, 715; 2804, 2655; 9088, 8988
+//   width 128, gradients with dq wide and split: 33, 37; 53, 49; 94, 74; 100, 133; 326, 255; 670, 715; 2804, 2655; 9088, 8989
 static bool splits(long long workgroups, long long walk, int D) { return walk > FI && workgroups * (D > 64 ? 2 : 1) <= walk; }
 // dk, dv: the rows of all heads of the group are walked; the split form of width 128 spills (296 bytes of scratch a lane). Gradients with
-// dk, dv wide and split: width 64, 1000 items, 4 heads over 2: 782 workgroups (of 128 items) 1030 and 997 us, 195 of 250 items 212 and
+// dk, dv wide and split: width 64, 1000 items, 4 heads over 2: 782 workgroups (of 128 items) 1030 and 997 us, 344 of 250 items 212 and
 // 176; width 128: 1000 items, 187 workgroups 989 and 740, 344 of them 1177 and 1288; 500 items, 4 over 4, 125 326 and 264, 250 328 and 387;
 // 3000 items, 281 1817 and 1713, 375 1820 and 2061. Also where items keep one or two waves of the wide form busy and many rows see them:
 // 1000 histories, widths 64 and 128: 20 items, 4 over 2, 156, 331 and 112, 290; 45 items, 8 over 2, 433, 968 and 331, 929; 2250 of 64, 4
@@ -674,7 +674,7 @@ static bool splits_items(long long workgroups, long long items, long long walk, 
 // Over a cache histories are cut into runs, of 128 items or more, until workgroups are enough; of lengths below the longest the runs at the
 // end are empty. Split also where the rows of a head keep one or two waves of the wide form busy and the runs are longer than two tiles.
 // us wide and split, 2 heads of widths 32, 64, 128: 2 rows over 2000 items, 256 users: 62, 161, 369 and 45, 84, 190; 32 rows over 2000, 100
-// users: 32, 72, 156 and 29, 49, 110; 64 over 2000, 60 users: 33, 54, 136 and 31, 55, 129; 64 over 64, 500 users: 14, 26, 53 and 21, 48, 130;
+// users: 32, 72, 156 and 29, 49, 110; 64 over 2000, 60 users: 33, 54, 136 and 31, 55, 129; 64 over 64, 500 users: 14, 27, 53 and 21, 48, 130;
 // 400 over 1000, 1 user (64 workgroups): 15, 21, 35 and 12, 15, 23; 800 over 1000, 2 users (200): 16, 23, 40 and 19, 30, 70.
 static bool splits_over_cache(long long workgroups, long long rows, long long walk, int D) {
   return walk > FI && ((D > 64 ? workgroups * 4 <= walk * 3 : workgroups <= walk) || (rows <= 64 && walk > 2 * FI));
