@@ -151,7 +151,7 @@ laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, co
   const laser_status s = validate_history(q, q_pitch, k, k_pitch, v, v_pitch, off, N, T, L_max, H, H_kv, D, gamma, dt, o, lse,
                                           stream, &a.f);
   if (s != LASER_OK) return s;
-  if (gamma > 0x1p120f) return LASER_ERR_SHAPE;   // (scores start at -gamma lse, with lse up to log(L_max) < 21 past the largest score)
+  if (gamma > 0x1p120f) return LASER_ERR_SHAPE;   // (bf16 scores start at -gamma lse, lse up to log(L_max) < 21 past the largest)
   if (!pitch_fits(dq_pitch, H, D, dt) || !pitch_fits(dk_pitch, H_kv, D, dt) || !pitch_fits(dv_pitch, H_kv, D, dt))
     return LASER_ERR_SHAPE;
   for (const void* p : {d_o, (const void*)dq_out, (const void*)dk_out, (const void*)dv_out, (const void*)work})

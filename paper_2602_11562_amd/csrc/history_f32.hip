@@ -49,7 +49,7 @@ struct F32Args {
   int N, T, L, C, H, Hkv, D, log2, P, max_pages, G, tiles, chunk, runs;
   MulDiv by_group;
   Deal deal;
-  float scale, gamma, inv_gamma;
+  float scale, inv_gamma;
   bool causal, add;
   float* o;
   float* lse;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(256, 1) void history_dq_f32_kernel(const F32Args a)
   delta = half_sum(delta);
   const float lse2 = a.lse[row] * LOG2E;
   if (h == 0 && mine < rows && (!SPLIT || wave == 0)) {
-    a.work[row * 2] = -a.lse[row] * a.gamma;
+    a.work[row * 2] = -lse2;
     a.work[row * 2 + 1] = -delta;
   }
   f32x16 acc[DB];
@@ -494,22 +494,28 @@ __global__ __launch_bounds__(256, 1) void history_dkv_f32_kernel(const F32Args a
       asm volatile("" ::: "memory");
     }
     if (r0 > floor) {
-      f32x16 sc, dp;
+      auto of_rows = [&](int g, int kind) {   // -lse log2(e), and -delta, of rows 8 g + 4 h and on
+        return *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(at + 2 * Sh::BYTES + kind * FI * 4 + (g * 8 + h * 4) * 4));
+      };
+      // (scores begin at zero: begun at the row's log-sum, their sum would lose what is below its half step, up to 2^-17 of p at width 128)
+      f32x16 sc = over_width<DP>(at, k, splat(0.0f), lane), dp;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const unsigned where = at + 2 * Sh::BYTES + (g * 8 + h * 4) * 4;
-        const f32x4 z = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where));
-        const f32x4 d = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(lds_at(where + FI * 4));
+        const f32x4 d = of_rows(g, 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[g * 4 + e] = z[e], dp[g * 4 + e] = d[e];
+        for (int e = 0; e < 4; ++e) dp[g * 4 + e] = d[e];
       }
-      sc = over_width<DP>(at, k, sc, lane);
       dp = over_width<DP>(at + Sh::BYTES, v, dp, lane);
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        sc[x] = __builtin_amdgcn_exp2f(sc[x] * a.scale);
-        if (r0 + 8 * (x >> 2) + 4 * h + (x & 3) < from) sc[x] = 0.0f;
-        dp[x] *= sc[x];
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 z = of_rows(g, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int x = g * 4 + e;
+          sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], a.scale, z[e]));
+          if (r0 + 8 * g + 4 * h + e < from) sc[x] = 0.0f;
+          dp[x] *= sc[x];
+        }
       }
       over_rows<DP>(at + Sh::BYTES, sc, dv, lane);
       over_rows<DP>(at, dp, dk, lane);
@@ -624,7 +630,7 @@ static F32Args of_history(const HistoryArgs& h) {
   a.off = h.off;
   a.N = h.N, a.T = h.T, a.L = a.C = h.L, a.H = h.H, a.Hkv = h.Hkv, a.D = h.D, a.G = h.H / h.Hkv;
   a.by_group = mul_div(a.G);
-  a.scale = LOG2E / h.gamma, a.gamma = h.gamma, a.inv_gamma = 1.0f / h.gamma;
+  a.scale = LOG2E / h.gamma, a.inv_gamma = 1.0f / h.gamma;
   a.causal = true;
   a.runs = 1;
   a.o = static_cast<float*>(h.o);

@@ -109,3 +109,19 @@ def test_through_an_autograd_function(dtype):
                 assert torch.allclose(exact[0][a:b, h], part[0][0], rtol=1e-10, atol=1e-12)
             for got, i in ((exact[1], 1), (exact[2], 2)):
                 assert torch.allclose(got[a:b, j], parts[0][i][0] + parts[1][i][0], rtol=1e-10, atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,D", [(1, 128), (1, 64), (2000, 128), (2000, 32)])
+def test_scores_far_below_their_log_sum(N, D, dtype):
+    """Scores of products so small that a sum which begins at the row's log-sum, between 2 and 4, would lose every one of them: 0.45 of its
+    half step each, two at a time. They are what the gradients' probabilities have to see."""
+    n = 20
+    q, k, v, off, host = make([n] * N, 1, 1, D, dtype, before=0, behind=0, packed=False)
+    q.fill_(0.45 * 2.0 ** -11)
+    k.copy_((2.0 ** -12 * torch.ones(n, device="cuda")).repeat(N)[:, None, None])
+    go = torch.ones_like(q)
+    o, lse = laser.laser_history_attention_forward(q, k, v, off, n, 1.0)
+    grads = laser.laser_history_attention_backward(q, k, v, o, lse, go, off, n, 1.0)
+    check_forward(o, lse, q, k, v, host[:3], 1.0, dtype)
+    check_backward(grads, q, k, v, go, host[:3], 1.0, dtype)
