@@ -570,6 +570,117 @@ laser_status laser_cache_evict(void* k_cache, void* v_cache, float* weight, cons
                                int budget, int recent, int H_kv, int D, laser_dtype dt, int32_t* lens_out, int32_t* kept_out,
                                void* stream);
 
+/*
+ * Rotary positions for the encoder above: pair i < R / 2 of the first R columns of every head of token t is turned by the angle
+ * pos[t] * freq[i] and scaled, the columns from R on are passed on. With c, s = cos, sin of the angle and pairs (a, b) of columns
+ *   LASER_ROTARY_HALF          (i, i + R / 2)
+ *   LASER_ROTARY_INTERLEAVED   (2 i, 2 i + 1)
+ * laser_rotary_forward:  (a, b) -> scale (a c - b s, a s + b c);   laser_rotary_backward, its transpose: gradients
+ * (a, b) -> scale (a c + b s, b c - a s). Queries and keys are turned by one launch.
+ *   q [T,H,D] dt, k [T,H_kv,D] dt (NULL exactly when H_kv = 0, k_out too), heads of a token side by side, tokens at pitches of
+ *   their own, as in laser_history_attention_forward; q_out, k_out likewise. An output may be its input (with its pitch: turned in
+ *   place), and lies apart from all others. pos [T] int32: a token whose position is negative is left out, neither read nor written
+ *   (rows of no sequence in a padded batch). freq [R/2] fp64, radians a position. Angles are formed and reduced in fp64, the rest is
+ *   fp32, results are rounded once. R even, 2 to D; T, heads, D and pitches within the limits above; scale finite.
+ * laser_rotary_frequencies: freq_out[i] = f_i = base^(-2i/R) for 2 <= R <= 128, for contexts `factor` times as long as those of training by
+ *   LASER_ROTARY_LINEAR   f_i / factor
+ *   LASER_ROTARY_BASE     base replaced by base * factor^(R / (R - 2)): the slowest pair is stretched by factor, the fastest is not
+ *   LASER_ROTARY_PARTS    f_i (g + (1 - g) / factor), g = (length f_i / (2 pi) - low) / (high - low) within [0, 1]: pairs that make `high`
+ *                         turns and more within the training's `length` stay, those of `low` and fewer are stretched
+ *   (arguments that the way does not name are not looked at).
+ * All pointers are device pointers, 16-byte alignment for q, k and the outputs, 8 for freq, 4 for pos. Errors: LASER_ERR_NULL,
+ * LASER_ERR_SHAPE, LASER_ERR_DTYPE, LASER_ERR_UNSUPPORTED (no such layout or way), LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is
+ * launched on an error.
+ */
+typedef enum { LASER_ROTARY_HALF = 0, LASER_ROTARY_INTERLEAVED = 1, LASER_ROTARY_LAYOUT_ANY_INT = 0x7fffffff } laser_rotary_layout;
+typedef enum {
+  LASER_ROTARY_NONE = 0,
+  LASER_ROTARY_LINEAR = 1,
+  LASER_ROTARY_BASE = 2,
+  LASER_ROTARY_PARTS = 3,
+  LASER_ROTARY_SCALING_ANY_INT = 0x7fffffff
+} laser_rotary_scaling;
+laser_status laser_rotary_frequencies(int R, double base, laser_rotary_scaling scaling, double factor, double length, double low,
+                                      double high, double* freq_out, void* stream);
+laser_status laser_rotary_forward(const void* q, int64_t q_pitch, const void* k, int64_t k_pitch, const int32_t* pos,
+                                  const double* freq, int T, int H, int H_kv, int D, int R, laser_rotary_layout layout, float scale,
+                                  laser_dtype dt, void* q_out, int64_t q_out_pitch, void* k_out, int64_t k_out_pitch, void* stream);
+laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const void* d_k, int64_t d_k_pitch, const int32_t* pos,
+                                   const double* freq, int T, int H, int H_kv, int D, int R, laser_rotary_layout layout, float scale,
+                                   laser_dtype dt, void* dq_out, int64_t dq_pitch, void* dk_out, int64_t dk_pitch, void* stream);
+
+/*
+ * The paged cache with its items in 8 bits, half the bytes of the bf16 one and what bounds few rows over long histories.
+ *   k_cache, v_cache [P,H_kv,page,D] e4m3 (4 bits of exponent, 3 of mantissa, largest 448, no infinities); D a multiple of 16, at most 128.
+ *   k_scale, v_scale [P,H_kv,page/block] fp32: what the numbers of each block of `block` items (a power of two, 8 to page) of a head are
+ *   times; a power of two from 2^-100 to 2^119 (of any other value, what comes of the block's items is unspecified).
+ *   Pages, tables, lengths, rows, offsets and their limits are those of the cache above; dt is the type of the rows (fp32 or bf16).
+ *
+ * laser_cache8_append: user u's c new rows become the last c of its lens[u] items, as in laser_cache_append. For every head's keys and
+ *   values, a block that rows come into has the scale max(the one it had, where it held items of the user before them; the
+ *   smallest power of two 2^x, -100 <= x <= 119, with |y| <= 448 2^x for all finite elements y of the new ones); each new element becomes
+ *   the e4m3 number nearest to y / scale (of two equally near the even one), at most 448 in magnitude, infinities too; NaN stays
+ *   NaN. Where the scale grows, the older items' numbers are rounded again to the new one. Places behind a user's items are not
+ *   written. A page must not be listed twice, by one user or two, where new rows go.
+ * laser_cache8_attention_forward: as laser_cache_attention_forward over the items' values (number times scale). bf16 rows:
+ *   probabilities are rounded to bf16 ahead of their product with the values, o is rounded once; fp32 rows: every product and sum is of
+ *   fp32's precision. work: laser_cache8_attention_work_bytes() bytes.
+ * Results are the same from run to run. Everything else, alignment (4 bytes for scales) and errors as for the cache above.
+ */
+laser_status laser_cache8_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,
+                                 float* k_scale, float* v_scale, const int32_t* off, const int32_t* pages, const int32_t* lens, int U,
+                                 int T, int C_max, int P, int page, int block, int max_pages, int L_max, int H_kv, int D,
+                                 laser_dtype dt, void* stream);
+size_t laser_cache8_attention_work_bytes(int U, int T, int C_max, int L_max, int H, int H_kv, int D,
+                                         laser_dtype dt);   /* host only; 0 for invalid sizes */
+laser_status laser_cache8_attention_forward(const void* q, int64_t q_pitch, const void* k_cache, const void* v_cache,
+                                            const float* k_scale, const float* v_scale, const int32_t* off, const int32_t* pages,
+                                            const int32_t* lens, int U, int T, int C_max, int P, int page, int block, int max_pages,
+                                            int L_max, int H, int H_kv, int D, float gamma, int causal, laser_dtype dt, void* o_out,
+                                            float* lse_out, void* work, size_t work_bytes, void* stream);
+
+/*
+ * Who holds the pages of a cache, of whatever type. refs [P] int32 counts, for every page, the places of tables that name it
+ * (pages [U,max_pages], the first ceil(lens[u] / page) of user u); a page with count 0 or less is free. Free pages are taken from the
+ * lowest number up, users in order, so results are the same from run to run. A page's contents are its parts: n_parts arrays
+ * (at most 1024) [P, part_bytes[i] bytes], parts and part_bytes being arrays in HOST memory (read before the call returns) of device
+ * pointers and of sizes (at most 2^27; copies are by 16 bytes where pointer and size are multiples of 16, by 4, or by 1).
+ * Entries outside [0, P) are pages without items: they pass on as they are, are counted and copied nowhere. lens are clamped to
+ * [0, max_pages * page].
+ * laser_pages_grow: lens[u] += off[u+1] - off[u] (nothing where that is negative; to max_pages * page at most), and the table gets
+ *   fresh pages, counts 1, for the entries that the new length asks for. Ahead of an append of the rows that off packs.
+ * laser_pages_fork: history v of the new tables pages_out [V,max_pages_out], lens_out [V] is the one of user source[v] (int32; outside
+ *   [0, U): an empty one; a longer one than max_pages_out pages hold is cut there). Whole pages are shared, their counts go up; a partly filled last
+ *   one is copied into a fresh page, all of it, so that either history can be appended to. Entries behind a history's pages become -1. The old tables
+ *   stay valid and hold what they held.
+ * missing_out [1] int32: fresh pages that there were none for; their entries are -1, the last ones in order.
+ * laser_pages_free: of the users with gone[u] != 0 (NULL: all) every page's count goes down (never below 0), and lens[u] becomes 0;
+ *   entries are left alone.
+ * laser_pages_compact: the M pages in use move so that they are pages 0 .. M-1: those numbered M and more, in order, into the free ones
+ *   below M, in order. pages_out [U,max_pages]: the tables with the new numbers (-1 behind a user's pages), refs_out [P] the counts,
+ *   in_use_out [1] M. Tables must name no page whose count is 0.
+ * laser_pages_copy: page to[i] becomes a copy of page from[i] (int32 [n]; a pair with one outside [0, P) is left out). No page may be
+ *   in `to` twice or in both.
+ * page: items of one, a power of two, 8 to 4096. P <= 2^26; U * max_pages, V * max_pages_out, and items of a table below 2^31. work:
+ * laser_pages_work_bytes(max(U, V), P) bytes of caller-owned scratch, contents unspecified before and after; calls that overlap need one
+ * each. All other pointers are device pointers, 4-byte aligned, outputs apart from inputs (lens, refs, and grow's pages: in place).
+ * Errors: LASER_ERR_NULL, LASER_ERR_SHAPE, LASER_ERR_ALIGN, LASER_ERR_LAUNCH. Nothing is launched on an error.
+ */
+size_t laser_pages_work_bytes(int U, int P);   /* host only; 0 for invalid sizes */
+laser_status laser_pages_grow(int32_t* pages, int32_t* lens, const int32_t* off, int32_t* refs, int U, int P, int page, int max_pages,
+                              int32_t* missing_out, void* work, size_t work_bytes, void* stream);
+laser_status laser_pages_fork(void* const* parts, const int64_t* part_bytes, int n_parts, const int32_t* pages, const int32_t* lens,
+                              const int32_t* source, int32_t* refs, int U, int V, int P, int page, int max_pages, int max_pages_out,
+                              int32_t* pages_out, int32_t* lens_out, int32_t* missing_out, void* work, size_t work_bytes,
+                              void* stream);
+laser_status laser_pages_free(const int32_t* pages, int32_t* lens, const int32_t* gone, int32_t* refs, int U, int P, int page,
+                              int max_pages, void* stream);
+laser_status laser_pages_compact(void* const* parts, const int64_t* part_bytes, int n_parts, const int32_t* pages, const int32_t* lens,
+                                 const int32_t* refs, int U, int P, int page, int max_pages, int32_t* pages_out, int32_t* refs_out,
+                                 int32_t* in_use_out, void* work, size_t work_bytes, void* stream);
+laser_status laser_pages_copy(void* const* parts, const int64_t* part_bytes, int n_parts, const int32_t* from, const int32_t* to,
+                              int n, int P, void* stream);
+
 /* Name of the family of STA / GSTA kernels AUTO would pick from for a shape in a batch that fills the machine (smaller ones
  * may take another form; "sta_generic" and "gsta_generic" include the matrix-core kernels that AUTO runs for fp32 at the
  * usual widths, "sta_stream_bf16" the one for a few candidates per user; static strings; host only, no GPU needed). */

@@ -12,6 +12,10 @@ from .binding import (LaserError, laser_forward, laser_forward_fused, laser_mult
                       laser_gsta_kernel_name, laser_version, load_library, status_string,
                       laser_history_attention_forward, laser_history_attention_backward, laser_history_attention_backward_work_bytes,
                       laser_cache_append, laser_cache_attention_forward, laser_cache_attention_work_bytes, laser_cache_weights, laser_cache_evict,
+                      laser_rotary_frequencies, laser_rotary_forward, laser_rotary_backward, laser_cache8_append,
+                      laser_cache8_attention_forward, laser_cache8_attention_work_bytes, laser_pages_work_bytes,
+                      laser_pages_grow, laser_pages_fork, laser_pages_free, laser_pages_compact, laser_pages_copy, ROTARY_HALF,
+                      ROTARY_INTERLEAVED, ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS,
                       LASER_F32, LASER_BF16, STA_AUTO, STA_GENERIC, STA_MFMA, STA_STREAM,
                       GSTA_AUTO, GSTA_GENERIC, GSTA_TILED, GSTA_SPLIT)
 
@@ -23,5 +27,9 @@ __all__ = ["LaserError", "laser_forward", "laser_forward_fused", "laser_multires
            "laser_gsta_kernel_name", "laser_version", "load_library", "status_string",
            "laser_history_attention_forward", "laser_history_attention_backward", "laser_history_attention_backward_work_bytes",
            "laser_cache_append", "laser_cache_attention_forward", "laser_cache_attention_work_bytes", "laser_cache_weights", "laser_cache_evict",
+           "laser_rotary_frequencies", "laser_rotary_forward", "laser_rotary_backward", "laser_cache8_append",
+           "laser_cache8_attention_forward", "laser_cache8_attention_work_bytes", "laser_pages_work_bytes", "laser_pages_grow",
+           "laser_pages_fork", "laser_pages_free", "laser_pages_compact", "laser_pages_copy", "ROTARY_HALF",
+           "ROTARY_INTERLEAVED", "ROTARY_NONE", "ROTARY_LINEAR", "ROTARY_BASE", "ROTARY_PARTS",
            "LASER_F32", "LASER_BF16", "STA_AUTO", "STA_GENERIC", "STA_MFMA", "STA_STREAM",
            "GSTA_AUTO", "GSTA_GENERIC", "GSTA_TILED", "GSTA_SPLIT"]

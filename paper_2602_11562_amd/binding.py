@@ -19,6 +19,8 @@ STA_AUTO, STA_GENERIC, STA_MFMA, STA_STREAM, STA_MFMA_CACHED = 0, 1, 2, 3, 4
 GSTA_AUTO, GSTA_GENERIC, GSTA_TILED, GSTA_SPLIT, GSTA_ONE = 0, 1, 2, 3, 4
 FFN_AUTO, FFN_GENERIC, FFN_MFMA = 0, 1, 2
 PROJECT_AUTO, PROJECT_GENERIC, PROJECT_MFMA = 0, 1, 2
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 
 EXPORTS = [
     "laser_sta_forward", "laser_sta_forward_variant", "laser_sta_forward_heads", "laser_sta_forward_softmax", "laser_sta_forward_ragged",
@@ -33,6 +35,9 @@ EXPORTS = [
     "laser_gsta_backward_work_bytes",
     "laser_history_attention_forward", "laser_history_attention_backward", "laser_history_attention_backward_work_bytes",
     "laser_cache_append", "laser_cache_attention_forward", "laser_cache_attention_work_bytes", "laser_cache_weights", "laser_cache_evict",
+    "laser_rotary_frequencies", "laser_rotary_forward", "laser_rotary_backward",
+    "laser_cache8_append", "laser_cache8_attention_forward", "laser_cache8_attention_work_bytes",
+    "laser_pages_work_bytes", "laser_pages_grow", "laser_pages_fork", "laser_pages_free", "laser_pages_compact", "laser_pages_copy",
     "laser_status_string", "laser_version",
 ]
 
@@ -143,7 +148,26 @@ def load_library() -> ctypes.CDLL:
         getattr(lib, name).restype = i32
     lib.laser_history_attention_backward_work_bytes.argtypes = [i32] * 7
     lib.laser_cache_attention_work_bytes.argtypes = [i32] * 8
-    for name in ("laser_history_attention_backward_work_bytes", "laser_cache_attention_work_bytes"):
+    f64 = ctypes.c_double
+    lib.laser_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, vp]
+    lib.laser_rotary_forward.argtypes = [vp, i64, vp, i64, ip, vp] + [i32] * 6 + [f32, i32, vp, i64, vp, i64, vp]
+    lib.laser_rotary_backward.argtypes = lib.laser_rotary_forward.argtypes
+    lib.laser_cache8_append.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, ip, ip, ip] + [i32] * 11 + [vp]
+    lib.laser_cache8_attention_forward.argtypes = ([vp, i64, vp, vp, vp, vp, ip, ip, ip] + [i32] * 11 +
+                                                   [f32, i32, i32, vp, vp, vp, sz, vp])
+    lib.laser_pages_copy.argtypes = [vp, vp, i32, ip, ip, i32, i32, vp]
+    lib.laser_pages_grow.argtypes = [ip, ip, ip, ip, i32, i32, i32, i32, ip, vp, sz, vp]
+    lib.laser_pages_fork.argtypes = [vp, vp, i32, ip, ip, ip, ip] + [i32] * 6 + [ip, ip, ip, vp, sz, vp]
+    lib.laser_pages_free.argtypes = [ip, ip, ip, ip, i32, i32, i32, i32, vp]
+    lib.laser_pages_compact.argtypes = [vp, vp, i32, ip, ip, ip, i32, i32, i32, i32, ip, ip, ip, vp, sz, vp]
+    for name in ("laser_rotary_frequencies", "laser_rotary_forward", "laser_rotary_backward", "laser_cache8_append",
+                 "laser_cache8_attention_forward", "laser_pages_copy", "laser_pages_grow", "laser_pages_fork", "laser_pages_free",
+                 "laser_pages_compact"):
+        getattr(lib, name).restype = i32
+    lib.laser_cache8_attention_work_bytes.argtypes = [i32] * 8
+    lib.laser_pages_work_bytes.argtypes = [i32] * 2
+    for name in ("laser_history_attention_backward_work_bytes", "laser_cache_attention_work_bytes",
+                 "laser_cache8_attention_work_bytes", "laser_pages_work_bytes"):
         getattr(lib, name).restype = sz
     lib.laser_sta_kernel_name.argtypes = [i32, i32, i32, i32, i32]
     lib.laser_sta_kernel_name.restype = ctypes.c_char_p
@@ -1079,3 +1103,265 @@ def laser_cache_evict(k_cache, v_cache, weight, pages, lens, pages_out, budget: 
         return left, kept
 
     return _there(index, stream, call)
+
+
+def laser_rotary_frequencies(R: int, base: float = 10000.0, scaling: int = ROTARY_NONE, factor: float = 1.0, length: float = 4096.0,
+                             low: float = 1.0, high: float = 32.0, freq_out=None, device=None, stream=None):
+    """Angles that a position adds to each of the R / 2 pairs, fp64 [R / 2]; scaling: for contexts `factor` times as long as those of
+    training (ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS, which looks at the turns within `length` between low and high)."""
+    torch = _torch()
+    if freq_out is None:
+        device = torch.device("cuda" if device is None else device)
+        index = torch.cuda.current_device() if device.index is None else device.index
+    else:
+        index = _one_device("freq_out", freq_out)
+
+    def call():
+        freq = torch.empty(max(int(R) // 2, 1), dtype=torch.float64, device=f"cuda:{index}") if freq_out is None else freq_out
+        _check(load_library().laser_rotary_frequencies(int(R), float(base), int(scaling), float(factor), float(length), float(low),
+                                                       float(high), _flat(freq, "freq_out", (int(R) // 2,), torch.float64),
+                                                       _stream(stream)), "laser_rotary_frequencies")
+        return freq
+
+    return _there(index, stream, call)
+
+
+def _rotary(name: str, q, k, pos, freq, layout, scale, q_out, k_out, stream, names):
+    torch = _torch()
+    index = _one_device(names, q, k, pos, freq, q_out, k_out)
+    words = names.split()
+    shape, dtype = _heads_of(q, words[0]), q.dtype
+    T, H, D = shape
+    kv = None if k is None else (T, _heads_of(k, words[1])[1], D)
+    if any(x is not None and x.dtype != dtype for x in (k, q_out, k_out)):
+        raise TypeError(f"{words[0]}, {words[1]} and the outputs must share a dtype")
+    if k is None and k_out is not None:
+        raise ValueError(f"{words[5]} without {words[1]}")
+    if freq.dim() != 1:
+        raise ValueError("freq must be [R / 2]")
+
+    def call():
+        y = torch.empty(shape, dtype=dtype, device=q.device) if q_out is None else q_out
+        z = k_out if k is None or k_out is not None else torch.empty(kv, dtype=dtype, device=q.device)
+        keys = (None, 0) if k is None else (k.data_ptr(), _pitch(k, words[1], kv))
+        _check(getattr(load_library(), name)(
+            q.data_ptr(), _pitch(q, words[0], shape), *keys, _flat(pos, "pos", (T,), torch.int32),
+            _flat(freq, "freq", freq.shape, torch.float64), T, H, 0 if k is None else kv[1], D, 2 * freq.shape[0], int(layout),
+            float(scale), _dt(q), y.data_ptr(), _pitch(y, words[4], shape), None if k is None else z.data_ptr(),
+            0 if k is None else _pitch(z, words[5], kv), _stream(stream)), name)
+        return y, z
+
+    return _there(index, stream, call)
+
+
+def laser_rotary_forward(q, k, pos, freq, layout: int = ROTARY_HALF, scale: float = 1.0, q_out=None, k_out=None, stream=None):
+    """Queries [T,H,D] and keys [T,H_kv,D] (or None) turned by their positions int32 [T] (negative: the row is left out), pair i by pos *
+    freq[i], fp64 [R / 2] -> (q, k). The outputs may be the inputs, or column blocks of one tensor."""
+    return _rotary("laser_rotary_forward", q, k, pos, freq, layout, scale, q_out, k_out, stream, "q k pos freq q_out k_out")
+
+
+def laser_rotary_backward(d_q, d_k, pos, freq, layout: int = ROTARY_HALF, scale: float = 1.0, dq_out=None, dk_out=None, stream=None):
+    """Gradients of laser_rotary_forward: of its results -> of its queries and keys."""
+    return _rotary("laser_rotary_backward", d_q, d_k, pos, freq, layout, scale, dq_out, dk_out, stream,
+                   "d_q d_k pos freq dq_out dk_out")
+
+
+def _cache8_of(k_cache, v_cache, k_scale, v_scale, pages, lens):
+    """(P, H_kv, page, D, U, max_pages), block, and the pointers of all six."""
+    torch = _torch()
+    if k_cache.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise TypeError(f"k_cache must be {torch.float8_e4m3fn}, got {k_cache.dtype}")
+    sizes, kc, vc, table, held = _cache_of(k_cache, v_cache, pages, lens)
+    P, Hkv, page = sizes[:3]
+    if k_scale.dim() != 3 or k_scale.shape[:2] != (P, Hkv) or k_scale.shape[2] < 1 or page % k_scale.shape[2]:
+        raise ValueError(f"k_scale must be [{P}, {Hkv}, {page} / block], got {list(k_scale.shape)}")
+    scales = [_flat(x, name, k_scale.shape, torch.float32) for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+    return sizes, page // k_scale.shape[2], (kc, vc, *scales), table, held
+
+
+def laser_cache8_append(k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max: int, L_max: int, stream=None):
+    """As laser_cache_append into a cache of 8-bit blocks: k_cache, v_cache float8_e4m3fn [P,H_kv,page,D], whose items are their numbers
+    times k_scale, v_scale fp32 [P,H_kv,page/block], powers of two that grow where new items ask for it."""
+    torch = _torch()
+    index = _one_device("k v k_cache v_cache k_scale v_scale off pages lens", k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens)
+    (P, Hkv, page, D, U, max_pages), block, held, table, n = _cache8_of(k_cache, v_cache, k_scale, v_scale, pages, lens)
+    shape = (_heads_of(k, "k")[0], Hkv, D)
+    if v.dtype != k.dtype:
+        raise TypeError("k, v must share a dtype")
+
+    def call():
+        _check(load_library().laser_cache8_append(
+            k.data_ptr(), _pitch(k, "k", shape), v.data_ptr(), _pitch(v, "v", shape), *held, _flat(off, "off", (U + 1,), torch.int32),
+            table, n, U, shape[0], int(C_max), P, page, block, max_pages, int(L_max), Hkv, D, _dt(k), _stream(stream)),
+            "laser_cache8_append")
+
+    _there(index, stream, call)
+
+
+def laser_cache8_attention_work_bytes(U: int, T: int, C_max: int, L_max: int, H: int, H_kv: int, D: int, dt: int) -> int:
+    return load_library().laser_cache8_attention_work_bytes(U, T, C_max, L_max, H, H_kv, D, dt)
+
+
+def laser_cache8_attention_forward(q, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max: int, L_max: int, gamma: float,
+                                   causal: bool = True, o_out=None, lse_out=None, work=None, stream=None):
+    """As laser_cache_attention_forward over a cache of 8-bit blocks (laser_cache8_append); queries in fp32 or bf16."""
+    torch = _torch()
+    index = _one_device("q k_cache v_cache k_scale v_scale off pages lens o_out lse_out work", q, k_cache, v_cache, k_scale, v_scale, off,
+                        pages, lens, o_out, lse_out, work)
+    (P, Hkv, page, D, U, max_pages), block, held, table, n = _cache8_of(k_cache, v_cache, k_scale, v_scale, pages, lens)
+    T, H, _ = _heads_of(q, "q")
+    shape, dtype = (T, H, D), q.dtype
+
+    def call():
+        lib = load_library()
+        o = torch.empty(shape, dtype=dtype, device=q.device) if o_out is None else o_out
+        lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if lse_out is None else lse_out
+        room = work
+        if room is None:
+            need = lib.laser_cache8_attention_work_bytes(U, T, int(C_max), int(L_max), H, Hkv, D, _dt(q))
+            room = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        _check(lib.laser_cache8_attention_forward(
+            q.data_ptr(), _pitch(q, "q", shape), *held, _flat(off, "off", (U + 1,), torch.int32), table, n, U, T, int(C_max), P, page,
+            block, max_pages, int(L_max), H, Hkv, D, float(gamma), 1 if causal else 0, _dt(q), _flat(o, "o_out", shape, dtype),
+            _flat(lse, "lse_out", (T, H), torch.float32), _ptr(room, "work"), room.numel() * room.element_size(), _stream(stream)),
+            "laser_cache8_attention_forward")
+        return o, lse
+
+    return _there(index, stream, call)
+
+
+def laser_pages_work_bytes(U: int, P: int) -> int:
+    """Scratch of the calls below for U users (of the larger side) and a pool of P pages."""
+    return load_library().laser_pages_work_bytes(U, P)
+
+
+def _parts_of_page(parts, P: int):
+    """(host array of pointers, host array of bytes a page, how many) of tensors [P, ...]."""
+    n = len(parts)
+    at, size = (ctypes.c_void_p * max(n, 1))(), (ctypes.c_int64 * max(n, 1))()
+    for i, t in enumerate(parts):
+        if t.dim() < 1 or t.shape[0] != P:
+            raise ValueError(f"parts[{i}] must be [{P}, ...], got {list(t.shape)}")
+        at[i], size[i] = _ptr(t, f"parts[{i}]"), t.numel() // P * t.element_size()
+    return at, size, n
+
+
+def _page_tables(pages, lens, refs, device_of):
+    """(index of the device, U, max_pages, P, pointers of pages, lens and refs)"""
+    i32 = _torch().int32
+    if pages.dim() != 2 or refs.dim() != 1:
+        raise ValueError("pages must be [U, max_pages], refs [P]")
+    index = _one_device(*device_of)
+    U, max_pages = pages.shape
+    return (index, U, max_pages, refs.shape[0], _flat(pages, "pages", pages.shape, i32), _flat(lens, "lens", (U,), i32),
+            _flat(refs, "refs", refs.shape, i32))
+
+
+def _page_work(work, U: int, P: int, like):
+    torch = _torch()
+    if work is None:
+        work = torch.empty(max(load_library().laser_pages_work_bytes(U, P), 16), dtype=torch.uint8, device=like.device)
+    return _ptr(work, "work"), work.numel() * work.element_size(), work
+
+
+def _names(parts) -> str:
+    return " ".join(f"parts[{i}]" for i in range(len(parts)))
+
+
+def laser_pages_grow(pages, lens, off, refs, page: int, missing_out=None, work=None, stream=None):
+    """lens int32 [U] grow by the rows that off int32 [U+1] packs, and the tables pages int32 [U,max_pages] get fresh pages of `page` items for
+    them, the lowest free ones of the pool (refs int32 [P]: how many tables name a page). Returns missing [1], the pages that there were none for."""
+    torch = _torch()
+    index, U, max_pages, P, table, n, counts = _page_tables(
+        pages, lens, refs, ("pages lens off refs missing_out work", pages, lens, off, refs, missing_out, work))
+
+    def call():
+        missing = torch.empty(1, dtype=torch.int32, device=pages.device) if missing_out is None else missing_out
+        room, size, keep = _page_work(work, U, P, pages)
+        _check(load_library().laser_pages_grow(table, n, _flat(off, "off", (U + 1,), torch.int32), counts, U, P, int(page), max_pages,
+                                               _flat(missing, "missing_out", (1,), torch.int32), room, size, _stream(stream)),
+               "laser_pages_grow")
+        return missing
+
+    return _there(index, stream, call)
+
+
+def laser_pages_fork(parts, pages, lens, source, refs, page: int, max_pages_out: Optional[int] = None, pages_out=None, lens_out=None,
+                     missing_out=None, work=None, stream=None):
+    """New tables whose history v is that of user source[v], int32 [V]: whole pages are shared, a partly filled last one is copied, in
+    every one of the parts [P, ...], into a fresh page -> (pages_out [V,max_pages_out], lens_out [V])."""
+    torch = _torch()
+    index, U, max_pages, P, table, n, counts = _page_tables(
+        pages, lens, refs, ("pages lens source refs pages_out lens_out missing_out work " + _names(parts), pages, lens, source, refs, pages_out,
+                            lens_out, missing_out, work, *parts))
+    if source.dim() != 1 or source.shape[0] < 1:
+        raise ValueError("source must be [V]")
+    if pages_out is not None and pages_out.dim() != 2:
+        raise ValueError("pages_out must be [V, max_pages_out]")
+    V, i32 = source.shape[0], torch.int32
+    most = int(max_pages_out) if max_pages_out is not None else max_pages if pages_out is None else pages_out.shape[1]
+
+    def call():
+        to = torch.empty((V, most), dtype=i32, device=pages.device) if pages_out is None else pages_out
+        left = torch.empty((V,), dtype=i32, device=pages.device) if lens_out is None else lens_out
+        missing = torch.empty(1, dtype=i32, device=pages.device) if missing_out is None else missing_out
+        room, size, keep = _page_work(work, max(U, V), P, pages)
+        _check(load_library().laser_pages_fork(
+            *_parts_of_page(parts, P), table, n, _flat(source, "source", (V,), i32), counts, U, V, P, int(page), max_pages, most,
+            _flat(to, "pages_out", (V, most), i32), _flat(left, "lens_out", (V,), i32), _flat(missing, "missing_out", (1,), i32), room,
+            size, _stream(stream)), "laser_pages_fork")
+        return to, left
+
+    return _there(index, stream, call)
+
+
+def laser_pages_free(pages, lens, gone, refs, page: int, stream=None):
+    """Users with gone int32 [U] != 0 (None: all) give their pages back and have no items any more."""
+    torch = _torch()
+    index, U, max_pages, P, table, n, counts = _page_tables(pages, lens, refs, ("pages lens gone refs", pages, lens, gone, refs))
+
+    def call():
+        _check(load_library().laser_pages_free(table, n, None if gone is None else _flat(gone, "gone", (U,), torch.int32), counts, U, P,
+                                               int(page), max_pages, _stream(stream)), "laser_pages_free")
+
+    _there(index, stream, call)
+
+
+def laser_pages_compact(parts, pages, lens, refs, page: int, pages_out=None, refs_out=None, in_use_out=None, work=None, stream=None):
+    """The pages in use become the first ones of the pool, in every one of the parts [P, ...] -> (pages [U,max_pages] and refs [P] with the
+    new numbers, in_use [1])."""
+    torch = _torch()
+    index, U, max_pages, P, table, n, counts = _page_tables(
+        pages, lens, refs, ("pages lens refs pages_out refs_out in_use_out work " + _names(parts), pages, lens, refs, pages_out, refs_out,
+                            in_use_out, work, *parts))
+    i32 = torch.int32
+
+    def call():
+        to = torch.empty_like(pages) if pages_out is None else pages_out
+        counts_to = torch.empty_like(refs) if refs_out is None else refs_out
+        used = torch.empty(1, dtype=i32, device=pages.device) if in_use_out is None else in_use_out
+        room, size, keep = _page_work(work, U, P, pages)
+        _check(load_library().laser_pages_compact(
+            *_parts_of_page(parts, P), table, n, counts, U, P, int(page), max_pages, _flat(to, "pages_out", (U, max_pages), i32),
+            _flat(counts_to, "refs_out", (P,), i32), _flat(used, "in_use_out", (1,), i32), room, size, _stream(stream)),
+            "laser_pages_compact")
+        return to, counts_to, used
+
+    return _there(index, stream, call)
+
+
+def laser_pages_copy(parts, source, target, stream=None):
+    """Page target[i] becomes a copy of page source[i], int32 [n], in every one of the parts [P, ...]."""
+    torch = _torch()
+    if len(parts) == 0:
+        raise ValueError("there must be parts to copy")
+    index = _one_device("source target " + _names(parts), source, target, *parts)
+    if source.dim() != 1 or source.shape[0] < 1:
+        raise ValueError("source must be [n]")
+
+    def call():
+        n, P, i32 = source.shape[0], parts[0].shape[0], torch.int32
+        _check(load_library().laser_pages_copy(*_parts_of_page(parts, P), _flat(source, "source", (n,), i32),
+                                               _flat(target, "target", (n,), i32), n, P, _stream(stream)), "laser_pages_copy")
+
+    _there(index, stream, call)

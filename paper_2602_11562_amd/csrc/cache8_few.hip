@@ -1,0 +1,229 @@
+// A few rows per key-value head over a cache of 8-bit blocks: one new item or a handful of candidates a user. Bound by memory, as
+// cache_few.hip, whose split it has: a workgroup owns (user, key-value head, run of items), its four waves take tiles of 32 items in turn,
+// each with two tiles of its own in LDS and no barrier while it streams; at the end the waves' maxima, sums and outputs are joined in
+// LDS, and the runs of a long history by a second launch.
+//
+// Tiles stand in LDS as the bytes that they are. Keys are read by rows, values by the transpose load of bytes, and both become bf16 operands times
+// their block's scale in registers, exactly, so that scores and P V need no factors. Rows in bf16: P is rounded to bf16 ahead of its product.
+// Rows in fp32: the query and P are sums of three bf16 numbers each, whose products with the operands are exact.
+#include "cache8_tile.h"
+
+namespace laser {
+
+template <int DP>
+struct Few8Shape {
+  static constexpr int TILE = 32 * DP, STAGE = 2 * TILE, NST = 2, WAVE = NST * STAGE;
+  static constexpr int JOIN = DP * 32 * 4;   // [column][32 rows] of fp32, row r at r ^ column % 32
+  static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
+};
+
+template <int DP, int NP, typename T>
+__global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
+  using Sh = Few8Shape<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * Sh::WAVE];
+  __shared__ __attribute__((aligned(16))) float scales[4][Sh::NST][8];
+  __shared__ float join_m[4][32], join_l[4][32];
+  const CacheArgs& a = a8.c;
+  const int per = a.U * a.Hkv;
+  // (turned by one from run to run: a user's runs are not all one die's)
+  const int split = blockIdx.x / per, uh = (blockIdx.x + split) % per, u = uh / a.Hkv, hk = uh % a.Hkv;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int rows = cr.count * G;
+  if (rows == 0) return;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
+  const int lo = split * chunk, hi = n < lo + chunk ? n : lo + chunk;
+  if (lo >= n && split > 0) return;   // (the first run of an empty history still writes)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem) + wave * Sh::WAVE;
+  const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[wave][0][0]);
+  const int32_t* table = a.pages + (size_t)u * a.max_pages;
+
+  Tiles8<DP, 32> tiles;
+  tiles.init(a.D, a.page_log2, 0, lane);
+  const int step_items = 4 * 32, requests = tiles.requests();
+  int ask = lo + wave * 32, mine = ask;
+  int pending = 0, slot_in = 0, slot_out = 0;
+  tiles.look_up(table, ask, hi, a.page_log2);
+  auto request = [&]() __attribute__((always_inline)) {
+    const unsigned at = lds + slot_in * Sh::STAGE;
+    tiles.fetch(a8, hk, ask, hi, at, at + Sh::TILE, lds_s + slot_in * 32, lane);
+    slot_in = slot_in + 1 == Sh::NST ? 0 : slot_in + 1;
+    ask += step_items;
+    ++pending;
+    tiles.look_up(table, ask, hi, a.page_log2);
+  };
+
+  bf16x8 qreg[NP][KS];
+  int last;
+  {
+    const int r = l32 < rows ? l32 : rows - 1, i = (int)by_group.div(r), g = r - i * G;
+    last = a.causal ? n - cr.count + i : n - 1;
+    load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(cr.first + i) * a.qp + (size_t)(hk * G + g) * a.D, a.D, h, qreg);
+  }
+  const int first_seen = __builtin_amdgcn_readlane(last, 0);
+  bool whole_pages;
+  {
+    bool bad = false;
+    for (int x = (lo >> a.page_log2) + lane; x <= (hi - 1) >> a.page_log2 && lo < hi; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    whole_pages = __ballot(bad) == 0;
+  }
+  for (int x = 0; x < Sh::NST && ask < hi; ++x) request();
+
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero;
+  float m = -INFINITY, l = 0.0f;
+  const TileReader8<DP> read(lane);
+
+  for (; mine < hi; mine += step_items) {
+    // loads return in order: with a second tile asked for, the first is there when the second's requests are all that is left
+    wait_requests(pending > 1 ? requests : 0);
+    asm volatile("" ::: "memory");
+    const unsigned at = lds + slot_out * Sh::STAGE, at_s = lds_s + slot_out * 32;
+    const bool whole = whole_pages && mine + 31 <= first_seen && mine + 32 <= hi;
+    f32x16 sc = zero;
+    const float ks = read.key_scale(at_s);
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) {
+      const u32x4 w = read.rows(at, i);
+      const bf16x8 k0 = wide8(w[0], w[1], ks, ks), k1 = wide8(w[2], w[3], ks, ks);
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) {
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qreg[p][2 * i], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qreg[p][2 * i + 1], sc, 0, 0, 0);
+      }
+    }
+    unsigned items = ~0u;
+    if (!whole) {
+      const int left = hi - mine;
+      bool in = l32 < left;
+      if (!whole_pages) in = in && (unsigned)table[(mine + (in ? l32 : 0)) >> a.page_log2] < (unsigned)a.P;
+      items = (unsigned)__ballot(in);
+      const int seen = last - mine - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i0 = 8 * (r >> 2) + (r & 3);
+        if (i0 > seen || !((items >> (4 * h + i0)) & 1)) sc[r] = -INFINITY;
+      }
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = half_max(top) * scale;
+    if (__any(top > m)) {
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= c;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    bf16x8 p[NP][2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, -base));
+      l += p0;
+      __bf16 part[NP];
+      split_bf16<NP>(p0, part);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) p[i][r >> 3][r & 7] = part[i];
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const u32x2 vs = read.value_scales(at_s, s);
+      float v0 = __uint_as_float(vs[0]), v1 = __uint_as_float(vs[1]);
+      if (!whole) {   // (a block without items has no scale; its codes came as zeros)
+        v0 = (items >> (16 * s)) & 1 ? v0 : 1.0f;
+        v1 = (items >> (16 * s + 8)) & 1 ? v1 : 1.0f;
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x2 w = read.columns(at + Sh::TILE, s, db);
+        const bf16x8 v = wide8(w[0], w[1], v0, v1);
+#pragma unroll
+        for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i][s], acc[db], 0, 0, 0);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again
+    --pending;
+    slot_out = slot_out + 1 == Sh::NST ? 0 : slot_out + 1;
+    if (ask < hi) request();
+  }
+
+  // the waves' results, in the place of the tiles
+  float* out = reinterpret_cast<float*>(smem + wave * Sh::WAVE);
+  l = half_sum(l);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int d = 8 * (r >> 2) + 4 * h + (r & 3);
+      out[(db * 32 + d) * 32 + (l32 ^ d)] = acc[db][r];
+    }
+  if (h == 0) {
+    join_m[wave][l32] = m;
+    join_l[wave][l32] = l;
+  }
+  __syncthreads();
+  const bool final = n <= chunk;
+  for (int e = tid; e < rows * a.D; e += 256) {
+    const int r = e / a.D, d = e - r * a.D;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, join_m[w][r]);
+    float sum = 0.0f, x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = join_m[w][r], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
+      sum = fmaf(join_l[w][r], c, sum);
+      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 32 + (r ^ (d & 31))], c, x);
+    }
+    x = sum > 0.0f ? x / sum : 0.0f;
+    const float z = sum > 0.0f ? top + log2f(sum) : -INFINITY;
+    const int i = (int)by_group.div(r), g = r - i * G;
+    const size_t row = (size_t)(cr.first + i) * a.H + hk * G + g;
+    if (final) {
+      store_from_f32<T>(static_cast<T*>(a.o), row * a.D + d, x);
+      if (d == 0 && a.lse != nullptr) a.lse[row] = z * LN2;
+    } else {
+      const size_t all = (size_t)a.T * a.H;
+      a.work[(split * all + row) * a.D + d] = x;
+      if (d == 0) a.work[splits * all * a.D + split * all + row] = z;
+    }
+  }
+}
+
+template <int DP, int NP, typename T>
+static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
+  const CacheArgs& c = a.c;
+  const int G = c.H / c.Hkv;
+  const long long each = (long long)c.Hkv * r.runs;   // workgroups of a user
+  if (c.U * each > 0x7fffffffLL) return LASER_ERR_SHAPE;
+  const long long most = 0xffffffffLL / 256 / each;   // (a launch has fewer than 2^32 threads; a user has Hkv * runs <= 2^20 workgroups)
+  for (long long u = 0; u < c.U; u += most) {
+    Cache8Args part = a;
+    part.c.U = c.U - u < most ? (int)(c.U - u) : (int)most;
+    part.c.off = c.off + u;
+    part.c.pages = c.pages + u * c.max_pages;
+    part.c.lens = c.lens + u;
+    cache8_few_kernel<DP, NP, T><<<(unsigned)(part.c.U * each), 256, 0, c.stream>>>(part, G, mul_div(G), LOG2E / c.gamma, r.chunk, r.runs);
+    const laser_status s = launch_status();
+    if (s != LASER_OK) return s;
+  }
+  return r.runs > 1 ? cache_join_launch(c, r.chunk, r.runs) : LASER_OK;
+}
+template <int NP, typename T>
+static laser_status few8_width(const Cache8Args& a, const CacheRuns& r) {
+  if (a.c.D > 64) return few8_typed<128, NP, T>(a, r);
+  if (a.c.D > 32) return few8_typed<64, NP, T>(a, r);
+  return few8_typed<32, NP, T>(a, r);
+}
+laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r) {
+  return a.c.dt == LASER_F32 ? few8_width<3, float>(a, r) : few8_width<1, unsigned short>(a, r);
+}
+
+}  // namespace laser

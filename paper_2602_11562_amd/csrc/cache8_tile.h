@@ -1,0 +1,164 @@
+// Tiles of 8-bit keys and values for the matrix-core kernels over a cache of 8-bit blocks: how they come into LDS, and how they are read
+// as bf16 operands. Every e4m3 number times its block's power of two is a bf16 number, so nothing is rounded on the way.
+#pragma once
+
+#include "cache8.h"
+#include "history_tile.h"
+
+namespace laser {
+
+// A tile row of DP bytes is CH pieces of 16, piece c of row r at place c ^ swz8(r). The reads of 16 rows at one piece (keys), and the
+// transpose loads of rows {0..3, 8..11} or {4..7, 12..15} at two pieces (values), then find all banks.
+template <int CH> __device__ __forceinline__ int swz8(int r) {
+  return CH == 8 ? ((r >> 1) & 1) * 2 + ((r >> 3) & 1) * 4 + ((r >> 2) & 1) : CH == 4 ? (r >> 2) & 3 : (r >> 3) & 1;
+}
+
+// 8 e4m3 numbers, the first four times a, the others times b (powers of two)
+__device__ __forceinline__ bf16x8 wide8(unsigned lo, unsigned hi, float a, float b) {
+  const bf16x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, a, false), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, a, true),
+               x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, b, false), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, b, true);
+  return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(unsigned, x0), __builtin_bit_cast(unsigned, x1),
+                                          __builtin_bit_cast(unsigned, x2), __builtin_bit_cast(unsigned, x3)});
+}
+
+// Scales of a tile: group g of 8 items has its key scale at 16 (g / 2) + 4 (g % 2) and its value scale 8 bytes behind it. Four bytes per
+// lane from the lane's address to LDS (uniform address + 4 * lane), outside the compiler's sight as buffer_to_lds16.
+__device__ __forceinline__ void global_to_lds4(const void* p, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n" ::"s"(lds_addr), "v"(p) : "memory");
+}
+
+// Waits until at most n of this wave's vector-memory operations are outstanding
+__device__ __forceinline__ void wait_requests(int n) {
+  switch (n) {
+#define LASER_VM_CASE(i) case i: __builtin_amdgcn_s_waitcnt(vmcnt_imm(i)); break;
+    LASER_VM_CASE(3) LASER_VM_CASE(5) LASER_VM_CASE(6) LASER_VM_CASE(9) LASER_VM_CASE(10) LASER_VM_CASE(15)
+#undef LASER_VM_CASE
+    default: __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  }
+}
+
+// What a wave brings of a tile: ROWS rows of keys and of values and their scales
+template <int DP, int ROWS>
+struct Tiles8 {
+  static constexpr int CH = DP / 16, RPI = 64 / CH < ROWS ? 64 / CH : ROWS, REQ = ROWS / RPI, IDS = ROWS / 8;
+  unsigned off[REQ];
+  int ids[IDS];            // pages of the next rows: of their items 0, 8, ..
+  int part;                // rows of a request that are on one page
+  __device__ __forceinline__ void init(int D, int page_log2, int row0, int lane) {
+    part = (1 << page_log2) < RPI ? 1 << page_log2 : RPI;
+#pragma unroll
+    for (int x = 0; x < REQ; ++x) {
+      const int in = lane / CH, c = (lane % CH) ^ swz8<CH>(row0 + x * RPI + in);
+      off[x] = c * 16 < D && in < RPI ? (unsigned)(in * D + c * 16) : NO_COLUMN;
+    }
+  }
+  __device__ __forceinline__ int requests() const { return 2 * REQ * (RPI / part) + 1; }
+  __device__ __forceinline__ void look_up(const int32_t* table, int j, int end, int page_log2) {
+#pragma unroll
+    for (int x = 0; x < IDS; ++x) ids[x] = j + x * 8 < end ? scalar_int(table, (j + x * 8) >> page_log2) : -1;
+  }
+  // items j and on (behind `end` there are none: zeros); keys to k_at, values to v_at, scales to s_at
+  __device__ __forceinline__ void fetch(const Cache8Args& a, int hk, int j, int end, unsigned k_at, unsigned v_at, unsigned s_at, int lane) const {
+    const CacheArgs& c = a.c;
+    const int mask = (1 << c.page_log2) - 1;
+#pragma unroll
+    for (int x = 0; x < REQ; ++x) {
+      auto rows = [&](int id, int skip, int count) __attribute__((always_inline)) {
+        const int at = j + x * RPI + skip, left = end - at < count ? end - at : count;
+        const bool ok = left > 0 && (unsigned)id < (unsigned)c.P;
+        const long long row = ok ? (((long long)id * c.Hkv + hk) << c.page_log2) + (at & mask) - skip : 0;
+        const unsigned bytes = ok ? (unsigned)((skip + left) * c.D) : 0u;
+        buffer_to_lds16(buffer_of(static_cast<const unsigned char*>(c.k) + row * c.D, bytes), off[x], k_at + x * 1024);
+        buffer_to_lds16(buffer_of(static_cast<const unsigned char*>(c.v) + row * c.D, bytes), off[x], v_at + x * 1024);
+      };
+      if constexpr (RPI == 8) {
+        rows(ids[x], 0, 8);
+      } else {
+        if (part == RPI) {
+          if (RPI * CH == 64 || lane < RPI * CH) rows(ids[x * RPI / 8], 0, RPI);
+        } else {   // several pages a request: the lanes of each from its own
+#pragma unroll
+          for (int p = 0; p < RPI / 8; ++p)
+            if (p * 8 % part == 0 && (lane / CH) / part == p * 8 / part) rows(ids[x * RPI / 8 + p], p * 8, part);
+        }
+      }
+    }
+    if (lane < 2 * IDS) {
+      const int g = (lane >> 2) * 2 + (lane & 1);
+      int id = ids[0];
+#pragma unroll
+      for (int x = 1; x < IDS; ++x) id = g == x ? ids[x] : id;
+      const bool ok = (unsigned)id < (unsigned)c.P;
+      const long long s = ok ? (((long long)id * c.Hkv + hk) << (c.page_log2 - a.block_log2)) + (((j + g * 8) & mask) >> a.block_log2) : 0;
+      global_to_lds4((lane & 2 ? a.v_scale : a.k_scale) + s, s_at);
+    }
+  }
+};
+
+// How a lane reads tiles as the A operand of its products
+template <int DP>
+struct TileReader8 {
+  static constexpr int CH = DP / 16, KS = DP / 16, DB = DP / 32;
+  unsigned row, cols, ks;
+  __device__ __forceinline__ explicit TileReader8(int lane) {
+    const int l32 = lane & 31, h = lane >> 5, k = (lane & 15) >> 1, r = k < 4 ? 4 * h + k : 4 + 4 * h + k;
+    row = l32 * DP + ((h ^ swz8<CH>(l32)) << 4);
+    cols = r * DP + (((l32 >> 4) ^ swz8<CH>(r)) << 4) + (lane & 1) * 8;
+    ks = (l32 >> 4) * 16 + ((l32 >> 3) & 1) * 4;
+  }
+  // a product over the width: row lane % 32, columns 32 i + 16 (lane / 32) and on; two operands of eight columns
+  __device__ __forceinline__ u32x4 rows(unsigned at, int i) const {
+    return __builtin_bit_cast(u32x4, lds_read16(lds_at((at + row) ^ (i << 5))));
+  }
+  __device__ __forceinline__ float key_scale(unsigned at) const {
+    return *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at + ks));
+  }
+  // a product over the rows, of the transpose: columns 32 db + lane % 32, rows 16 s + {4h .. 4h+3, 8+4h .. 8+4h+3}
+  __device__ __forceinline__ u32x2 columns(unsigned at, int s, int db) const {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (__attribute__((address_space(3))) i32x2*)(lds_at(((at + cols) ^ (db << 5)) + s * 16 * DP))));
+  }
+  __device__ __forceinline__ u32x2 value_scales(unsigned at, int s) const {   // of rows 16 s .. +7 and the next eight
+    return *reinterpret_cast<const __attribute__((address_space(3))) u32x2*>(lds_at(at + s * 16 + 8));
+  }
+};
+
+// A number of 24 bits as a sum of bf16 numbers, the largest first: products with them and with e4m3 numbers are exact
+template <int NP>
+__device__ __forceinline__ void split_bf16(float x, __bf16* part) {
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    part[i] = (__bf16)x;
+    x -= (float)part[i];
+  }
+}
+
+// The query of a lane's row as B operands in the order of TileReader8::rows; bf16 as it is, fp32 in three parts
+template <int DP, int NP, typename T>
+__device__ __forceinline__ void load_query(const T* qr, int D, int h, bf16x8 (*q)[DP / 16]) {
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    const int d = (2 * (s >> 1) + h) * 16 + (s & 1) * 8;
+    if constexpr (NP == 1) {
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (d < D) raw = *reinterpret_cast<const u32x4*>(qr + d);
+      q[0][s] = __builtin_bit_cast(bf16x8, raw);
+    } else {
+      u32x4 raw[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
+      if (d < D) {
+        raw[0] = *reinterpret_cast<const u32x4*>(qr + d);
+        raw[1] = *reinterpret_cast<const u32x4*>(qr + d + 4);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        __bf16 part[NP];
+        split_bf16<NP>(__uint_as_float(raw[j >> 2][j & 3]), part);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) q[i][s][j] = part[i];
+      }
+    }
+  }
+}
+
+}  // namespace laser

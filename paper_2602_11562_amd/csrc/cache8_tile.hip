@@ -1,0 +1,241 @@
+// Many rows over a cache of 8-bit blocks: chunks of new items, and candidates. The split of history_mfma.hip: a workgroup of four waves
+// owns 128 rows of a key-value head and walks the items that the last of them sees in tiles of 64, which come by direct loads to LDS as
+// the bytes that they are; a wave owns 32 rows and makes its operands of the bytes in registers.
+#include "cache8_tile.h"
+
+namespace laser {
+
+struct Tile8Args {
+  Cache8Args a;
+  const int32_t* off;
+  int N, Hkv;
+  MulDiv by_group;       // / G
+  int G, tiles;          // tiles of the longest sequence's rows
+  Deal deal;             // of (tile, run) to workgroups
+  float scale;           // log2(e) / gamma
+  int chunk, runs;       // items a workgroup walks, and into how many such runs the longest history is cut
+};
+
+template <int DP, int SLOTS, int NP, typename T>
+__global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) {
+  constexpr int KS = DP / 16, DB = DP / 32, NW = 4, ROWS = NW * 32, KB = TI * DP, SLOT = 2 * KB, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
+  constexpr bool PATCHED = sizeof(T) == 2;   // (fp32 rows leave from the registers)
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * SLOT > PATCH || !PATCHED ? SLOTS * SLOT : PATCH];
+  __shared__ __attribute__((aligned(16))) float scales[SLOTS][TI / 8 * 2];
+  const CacheArgs& a = t.a.c;
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[0][0]);
+  const Place place = place_of(t.deal, blockIdx.x);
+  if (place.rank >= t.deal.tiles) return;
+  int tile = place.rank, run = 0;
+  if (t.runs > 1) {
+    run = tile / t.tiles;
+    tile -= run * t.tiles;
+  }
+  tile = t.tiles - 1 - tile;   // (the longest first)
+  const int u_seq = place.pair / t.Hkv, hk = place.pair - u_seq * t.Hkv;
+  const CandRange cr = cand_range(t.off, u_seq, a.C, a.T);
+  const int rows = cr.count * t.G, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const int n = cache_len(a.lens, u_seq, a.L, a.max_pages, a.page_log2);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+
+  int end;   // one past the last item that a row of this workgroup sees
+  {
+    const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
+    end = a.causal ? n - cr.count + (int)t.by_group.div(r) + 1 : n;
+  }
+  const bool joined = t.runs > 1 && n > t.chunk;   // others write their part of the result too
+  int begin = 0;
+  if (t.runs > 1) {
+    begin = run * t.chunk;
+    if (run > 0 && begin >= end) return;
+    end = end < begin + t.chunk ? end : begin + t.chunk;
+  }
+  const int turns = end > begin ? (end - begin + TI - 1) / TI : 0;
+  const int32_t* table = a.pages + (size_t)u_seq * a.max_pages;
+
+  Tiles8<DP, 16> tiles;
+  tiles.init(a.D, a.page_log2, wave * 16, lane);
+  const int requests = tiles.requests();
+  int asked = 0, in = 0;
+  auto request = [&]() __attribute__((always_inline)) {
+    const unsigned at = lds + in * SLOT + wave * 16 * DP;
+    tiles.fetch(t.a, hk, begin + asked * TI + wave * 16, n, at, at + KB, lds_s + in * (TI / 8 * 8) + wave * 16, lane);
+    in = in + 1 == SLOTS ? 0 : in + 1;
+    ++asked;
+    tiles.look_up(table, begin + asked * TI + wave * 16, end, a.page_log2);
+  };
+  if (turns > 0) {
+    tiles.look_up(table, begin + wave * 16, end, a.page_log2);
+    for (int x = 0; x < SLOTS - 1 && x < turns; ++x) request();
+  }
+
+  // this lane's row and the last item it sees
+  const int first = row0 + wave * 32;
+  int last;
+  bf16x8 qreg[NP][KS];
+  {
+    int r = first + l32;
+    r = r < rows ? r : rows - 1;
+    const int i = (int)t.by_group.div(r), g = r - i * t.G;
+    last = a.causal ? n - cr.count + i : n - 1;
+    load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(cr.first + i) * a.qp + (size_t)(hk * t.G + g) * a.D, a.D, h, qreg);
+  }
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
+  bool whole_pages;
+  {
+    bool bad = false;
+    if (turns > 0)
+      for (int x = (begin >> a.page_log2) + lane; x <= (end - 1) >> a.page_log2; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    whole_pages = __ballot(bad) == 0;
+  }
+
+  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero;
+  float m = -INFINITY, l = 0.0f;
+  const TileReader8<DP> read(lane);
+
+  auto block = [&](int t0, unsigned at, unsigned at_s) __attribute__((always_inline)) {
+    f32x16 sc = zero;
+    const float ks = read.key_scale(at_s);
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) {
+      const u32x4 w = read.rows(at, i);
+      const bf16x8 k0 = wide8(w[0], w[1], ks, ks), k1 = wide8(w[2], w[3], ks, ks);
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) {
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qreg[p][2 * i], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qreg[p][2 * i + 1], sc, 0, 0, 0);
+      }
+    }
+    const bool whole = whole_pages && t0 + 31 <= wave_first && t0 + 32 <= end;
+    unsigned items = ~0u;
+    if (!whole) {   // places without an item, and items behind a row's own
+      bool in = l32 < end - t0;
+      if (!whole_pages) in = in && (unsigned)table[(t0 + (in ? l32 : 0)) >> a.page_log2] < (unsigned)a.P;
+      items = (unsigned)__ballot(in);
+      const int seen = last - t0 - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i0 = 8 * (r >> 2) + (r & 3);
+        if (i0 > seen || !((items >> (4 * h + i0)) & 1)) sc[r] = -INFINITY;
+      }
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = half_max(top) * t.scale;
+    if (__any(top > m)) {
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= c;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    bf16x8 p[NP][2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], t.scale, -base));
+      l += p0;
+      __bf16 part[NP];
+      split_bf16<NP>(p0, part);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) p[i][r >> 3][r & 7] = part[i];
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const u32x2 vs = read.value_scales(at_s, s);
+      float v0 = __uint_as_float(vs[0]), v1 = __uint_as_float(vs[1]);
+      if (!whole) {   // (a block without items has no scale; its codes came as zeros)
+        v0 = (items >> (16 * s)) & 1 ? v0 : 1.0f;
+        v1 = (items >> (16 * s + 8)) & 1 ? v1 : 1.0f;
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x2 w = read.columns(at + KB, s, db);
+        const bf16x8 v = wide8(w[0], w[1], v0, v1);
+#pragma unroll
+        for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i][s], acc[db], 0, 0, 0);
+      }
+    }
+  };
+  int out = 0;
+  for (int u = 0; u < turns; ++u) {
+    wait_requests((asked - u - 1) * requests);
+    barrier_lds();   // tile u is there, and every wave is through with the one before, whose slot is asked for again
+    if (asked < turns) request();
+    const unsigned at = lds + out * SLOT, at_s = lds_s + out * (TI / 8 * 8);
+    out = out + 1 == SLOTS ? 0 : out + 1;
+    const int t0 = begin + u * TI;
+    if (t0 <= wave_last) block(t0, at, at_s);
+    if (t0 + 32 <= wave_last) block(t0 + 32, at + 32 * DP, at_s + 32);
+  }
+  barrier_lds();
+
+  const float sum = half_sum(l), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const int r = first + l32;
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  if (joined || !PATCHED) {
+    if (r >= rows) return;
+    const int i = (int)t.by_group.div(r), g = r - i * t.G;
+    const size_t all = (size_t)a.T * a.H, row = (size_t)(cr.first + i) * a.H + hk * t.G + g;
+    float* to = joined ? a.work + (run * all + row) * a.D : static_cast<float*>(a.o) + row * a.D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int c = db * 32 + x * 8 + h * 4;
+        if (c < a.D) *reinterpret_cast<f32x4*>(to + c) = f32x4{acc[db][x * 4] * inv, acc[db][x * 4 + 1] * inv, acc[db][x * 4 + 2] * inv,
+                                                               acc[db][x * 4 + 3] * inv};
+      }
+    const float z = sum > 0.0f ? m + log2f(sum) : -INFINITY;
+    if (h == 0 && joined) a.work[t.runs * all * a.D + run * all + row] = z;
+    if (h == 0 && !joined && a.lse != nullptr) a.lse[row] = z * LN2;
+    return;
+  }
+  if (a.lse != nullptr && h == 0 && r < rows) {
+    const int i = (int)t.by_group.div(r), g = r - i * t.G;
+    a.lse[(size_t)(cr.first + i) * a.H + hk * t.G + g] = sum > 0.0f ? (m + log2f(sum)) * LN2 : -INFINITY;
+  }
+  store_block<DP>(acc, inv, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
+    const int i = (int)t.by_group.div(first + r), g = first + r - i * t.G;
+    return static_cast<unsigned short*>(a.o) + ((size_t)(cr.first + i) * a.H + hk * t.G + g) * a.D;
+  });
+}
+
+template <int DP, int SLOTS, int NP, typename T>
+static laser_status tile8_typed(Tile8Args t) {
+  const CacheArgs& c = t.a.c;
+  t.tiles = (int)(((long long)c.C * t.G + 127) / 128);
+  return launch_dealt(t, (long long)t.tiles * t.runs, 256, [&](Tile8Args& part, long long n) {
+    part.a.c.pages += n * c.max_pages;
+    part.a.c.lens += n;
+    cache8_tile_kernel<DP, SLOTS, NP, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
+  });
+}
+template <int NP, typename T>
+static laser_status tile8_width(const Tile8Args& t) {
+  if (t.a.c.D > 64) return tile8_typed<128, 3, NP, T>(t);
+  if (t.a.c.D > 32) return tile8_typed<64, 4, NP, T>(t);
+  return tile8_typed<32, 4, NP, T>(t);
+}
+
+laser_status cache8_tile_launch(const Cache8Args& a, const CacheRuns& r) {
+  Tile8Args t{};
+  t.a = a;
+  t.off = a.c.off, t.N = a.c.U, t.Hkv = a.c.Hkv;
+  t.G = a.c.H / a.c.Hkv;
+  t.by_group = mul_div(t.G);
+  t.scale = LOG2E / a.c.gamma;
+  t.chunk = r.chunk, t.runs = r.runs;
+  const laser_status s = a.c.dt == LASER_F32 ? tile8_width<3, float>(t) : tile8_width<1, unsigned short>(t);
+  return s == LASER_OK && r.runs > 1 ? cache_join_launch(a.c, r.chunk, r.runs) : s;
+}
+
+}  // namespace laser

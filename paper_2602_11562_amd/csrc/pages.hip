@@ -1,0 +1,375 @@
+// The pages of a cache. refs[p] counts the tables that hold page p; a page with refs <= 0 is free, and free pages are taken from the
+// lowest number up, users in order, so that the same calls give the same tables whatever the order of atomics.
+//
+// A plan is made by one workgroup that walks the counts (a page's number among the free ones is a sum over all before it) and leaves
+// lists in the work buffer; copies and tables are then written by as many workgroups as that takes. Copies go piece by piece of 16 bytes
+// over all parts of all listed pages, whatever a page's size. Bound by latency for small calls (two launches), by memory for large ones.
+#include "pages.h"
+
+namespace laser {
+
+constexpr int PLAN = 1024;   // threads of the plan
+
+struct Tables {
+  const int32_t* pages;
+  const int32_t* lens;
+  int32_t* refs;
+  int U, P, log2, max_pages;
+};
+
+__device__ __forceinline__ int held_items(const Tables& t, int u) {   // of user u, within what its table can hold
+  const int n = t.lens[u], room = t.max_pages << t.log2;
+  return n < 0 ? 0 : n < room ? n : room;
+}
+__device__ __forceinline__ int pages_of(int n, int log2) { return (int)(((long long)n + (1 << log2) - 1) >> log2); }
+
+// Sum of x over the threads before this one, and over all (every thread calls it)
+__device__ __forceinline__ int sum_before(int x, int* all) {
+  __shared__ int waves[PLAN / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int sum = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(sum, d);
+    if (lane >= d) sum += y;
+  }
+  __syncthreads();   // (the last call's sums have been read)
+  if (lane == 63) waves[wave] = sum;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN / 64; ++w) {
+    before += w < wave ? waves[w] : 0;
+    total += waves[w];
+  }
+  *all = total;
+  return before + sum - x;
+}
+
+// The first `want` free pages to fresh[], their counts set to 1; returns how many there were
+__device__ __forceinline__ int take_free(int32_t* refs, int P, int want, int32_t* fresh) {
+  constexpr int EACH = 8;   // counts a thread holds at a time
+  int got = 0;
+  for (int p0 = 0; p0 < P && got < want; p0 += PLAN * EACH) {
+    const int mine = p0 + threadIdx.x * EACH;
+    unsigned free = 0;
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) free |= (mine + x < P && refs[mine + x] <= 0 ? 1u : 0u) << x;
+    int all;
+    int rank = got + sum_before(__popc(free), &all);
+    for (; free != 0 && rank < want; free &= free - 1, ++rank) {
+      const int p = mine + __ffs(free) - 1;
+      fresh[rank] = p;
+      refs[p] = 1;
+    }
+    got += all;
+  }
+  return got < want ? got : want;
+}
+
+// Fork, the plan: history v of the new tables gets a fresh page where the history it comes from ends within a page. rank[v]: the fresh
+// page's number, or -1
+__device__ __forceinline__ int forked_items(const Tables& t, const int32_t* source, int v, int max_out) {
+  const int u = source[v];
+  if ((unsigned)u >= (unsigned)t.U) return 0;
+  const int n = held_items(t, u), room = max_out << t.log2;
+  return n < room ? n : room;
+}
+__global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
+                                                         int32_t* __restrict__ rank, int32_t* __restrict__ fresh,
+                                                         int32_t* __restrict__ missing) {
+  int want = 0;
+  for (int v0 = 0; v0 < V; v0 += PLAN) {
+    const int v = v0 + threadIdx.x;
+    int need = 0;
+    if (v < V) {
+      const int n = forked_items(t, source, v, max_out);
+      if (n & ((1 << t.log2) - 1)) need = (unsigned)t.pages[(size_t)source[v] * t.max_pages + (n >> t.log2)] < (unsigned)t.P;
+    }
+    int all;
+    const int before = sum_before(need, &all);
+    if (v < V) rank[v] = need ? want + before : -1;
+    want += all;
+  }
+  const int got = take_free(t.refs, t.P, want, fresh);
+  for (int v = threadIdx.x; v < V; v += PLAN)      // (a thread's own ranks)
+    if (rank[v] >= got) rank[v] = -2;              // no page is left for it
+  if (threadIdx.x == 0) *missing = want - got;
+}
+
+// Pieces of listed pages from src[] to dst[], every part of them. A thread goes from piece to piece by the grid's threads.
+struct Moves {
+  PageParts parts;
+  long long total;           // pieces in all (at most, where `count` says how many entries there are)
+  const int32_t* count;      // entries, or nullptr: all
+};
+template <typename T>
+__device__ __forceinline__ void move_piece(unsigned char* base, long long bytes, int src, int dst, unsigned piece) {
+  reinterpret_cast<T*>(base + dst * bytes)[piece] = reinterpret_cast<const T*>(base + src * bytes)[piece];
+}
+// entry(e, &src, &dst): false where the entry moves nothing
+template <typename Entry>
+__device__ __forceinline__ void move_pages(const Moves& m, long long entries, unsigned block, unsigned blocks, const Entry& entry) {
+  const long long all = entries * m.parts.all;
+  for (long long g = (long long)block * 256 + threadIdx.x; g < all; g += (long long)blocks * 256) {
+    const long long e = g / m.parts.all;
+    unsigned piece = (unsigned)(g - e * m.parts.all);
+    int src, dst;
+    if (!entry(e, &src, &dst)) continue;
+    for (int i = 0; i < m.parts.n; ++i) {
+      if (piece < m.parts.pieces[i]) {
+        if (m.parts.piece_log2[i] == 4) move_piece<stream16>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
+        else if (m.parts.piece_log2[i] == 2) move_piece<unsigned>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
+        else move_piece<unsigned char>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
+        break;
+      }
+      piece -= m.parts.pieces[i];
+    }
+  }
+}
+
+// Fork, the rest: the first `copies` workgroups copy pages, the others write a table each
+__global__ __launch_bounds__(256) void fork_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
+                                                   const int32_t* __restrict__ rank, const int32_t* __restrict__ fresh,
+                                                   int32_t* __restrict__ pages_out, int32_t* __restrict__ lens_out, unsigned copies,
+                                                   bool tables, const Moves m) {
+  if (blockIdx.x < copies) {
+    move_pages(m, V, blockIdx.x, copies, [&](long long v, int* src, int* dst) __attribute__((always_inline)) {
+      const int r = rank[v];
+      if (r < 0) return false;
+      const int n = forked_items(t, source, (int)v, max_out);
+      *src = t.pages[(size_t)source[v] * t.max_pages + (n >> t.log2)];
+      *dst = fresh[r];
+      return true;
+    });
+    return;
+  }
+  if (!tables) return;
+  for (int v = blockIdx.x - copies; v < V; v += gridDim.x - copies) {
+    const int n = forked_items(t, source, v, max_out), whole = n >> t.log2, used = pages_of(n, t.log2);
+    for (int j = threadIdx.x; j < max_out; j += 256) {
+      int p = -1;
+      if (j < used) {
+        p = t.pages[(size_t)source[v] * t.max_pages + j];
+        if (j >= whole) {
+          if ((unsigned)p < (unsigned)t.P) p = rank[v] >= 0 ? fresh[rank[v]] : -1;
+        } else if ((unsigned)p < (unsigned)t.P) {
+          atomicAdd(t.refs + p, 1);
+        }
+      }
+      pages_out[(size_t)v * max_out + j] = p;
+    }
+    if (threadIdx.x == 0) lens_out[v] = n;
+  }
+}
+
+// Grow: user u's table gets the pages that its next c items ask for
+__global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_t* __restrict__ off, int32_t* pages, int32_t* lens,
+                                                    int32_t* __restrict__ rank, int32_t* __restrict__ fresh, int32_t* __restrict__ missing) {
+  auto grown = [&](int u, int n) {
+    const long long c = (long long)off[u + 1] - off[u], room = (long long)t.max_pages << t.log2, m = n + (c > 0 ? c : 0);
+    return (int)(m < room ? m : room);
+  };
+  int want = 0;
+  for (int u0 = 0; u0 < t.U; u0 += PLAN) {
+    const int u = u0 + threadIdx.x;
+    int need = 0;
+    if (u < t.U) {
+      const int n = held_items(t, u);
+      need = pages_of(grown(u, n), t.log2) - pages_of(n, t.log2);
+    }
+    int all;
+    const int before = sum_before(need, &all);
+    if (u < t.U) rank[u] = want + before;
+    want += all;
+  }
+  const int got = take_free(t.refs, t.P, want, fresh);
+  __syncthreads();
+  for (int u = threadIdx.x; u < t.U; u += PLAN) {
+    const int n = held_items(t, u), m = grown(u, n), first = pages_of(n, t.log2), last = pages_of(m, t.log2);
+    int r = rank[u];
+    for (int j = first; j < last; ++j, ++r) pages[(size_t)u * t.max_pages + j] = r < got ? fresh[r] : -1;
+    lens[u] = m;
+  }
+  if (threadIdx.x == 0) *missing = want - got;
+}
+
+// Free: a workgroup gives back the pages of a user
+__global__ __launch_bounds__(256) void free_kernel(const Tables t, const int32_t* __restrict__ gone, int32_t* lens) {
+  for (int u = blockIdx.x; u < t.U; u += gridDim.x) {
+    if (gone != nullptr && gone[u] == 0) continue;
+    const int used = pages_of(held_items(t, u), t.log2);
+    for (int j = threadIdx.x; j < used; j += 256) {
+      const int p = t.pages[(size_t)u * t.max_pages + j];
+      // (never below 0, should a page be given back more often than it is held)
+      if ((unsigned)p < (unsigned)t.P && atomicSub(t.refs + p, 1) <= 0) atomicAdd(t.refs + p, 1);
+    }
+    __syncthreads();   // (every wave has the length)
+    if (threadIdx.x == 0) lens[u] = 0;
+  }
+}
+
+// Compact, the plan: of M pages in use, those numbered M and more go to the free ones below M, in order
+__global__ __launch_bounds__(PLAN) void compact_plan_kernel(const int32_t* __restrict__ refs, int P, int32_t* __restrict__ src,
+                                                            int32_t* __restrict__ dst, int32_t* __restrict__ place,
+                                                            int32_t* __restrict__ moved, int32_t* __restrict__ in_use) {
+  constexpr int EACH = 8;
+  auto used_of = [&](int mine) {
+    unsigned used = 0;
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) used |= (mine + x < P && refs[mine + x] > 0 ? 1u : 0u) << x;
+    return used;
+  };
+  int count = 0;
+  for (int p = threadIdx.x * EACH; p < P; p += PLAN * EACH) count += __popc(used_of(p));
+  int M;
+  sum_before(count, &M);
+  int sources = 0, targets = 0;
+  for (int p0 = 0; p0 < P; p0 += PLAN * EACH) {
+    const int mine = p0 + threadIdx.x * EACH;
+    const unsigned used = used_of(mine);
+    unsigned from = 0, to = 0;
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) {
+      const int p = mine + x;
+      if (p >= P) continue;
+      if (used >> x & 1) from |= (p >= M ? 1u : 0u) << x;
+      else to |= (p < M ? 1u : 0u) << x;
+      if (!(from >> x & 1)) place[p] = p;
+    }
+    int all;
+    int a = sources + sum_before(__popc(from), &all);
+    sources += all;
+    for (; from; from &= from - 1) src[a++] = mine + __ffs(from) - 1;
+    int b = targets + sum_before(__popc(to), &all);
+    targets += all;
+    for (; to; to &= to - 1) dst[b++] = mine + __ffs(to) - 1;
+  }
+  __syncthreads();   // (as many of the one as of the other)
+  for (int i = threadIdx.x; i < sources; i += PLAN) place[src[i]] = dst[i];
+  if (threadIdx.x == 0) {
+    *moved = sources;
+    *in_use = M;
+  }
+}
+// Compact, the rest: the first `copies` workgroups copy pages, the others write tables and counts
+__global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                      const int32_t* __restrict__ place, int32_t* __restrict__ pages_out,
+                                                      int32_t* __restrict__ refs_out, const int32_t* __restrict__ in_use,
+                                                      unsigned copies, bool tables, const Moves m) {
+  if (blockIdx.x < copies) {
+    move_pages(m, *m.count, blockIdx.x, copies, [&](long long i, int* from, int* to) __attribute__((always_inline)) {
+      *from = src[i];
+      *to = dst[i];
+      return true;
+    });
+    return;
+  }
+  if (!tables) return;
+  const unsigned first = blockIdx.x - copies, step = gridDim.x - copies;
+  for (int u = first; u < t.U; u += step) {
+    const int used = pages_of(held_items(t, u), t.log2);
+    for (int j = threadIdx.x; j < t.max_pages; j += 256) {
+      int p = -1;
+      if (j < used) {
+        p = t.pages[(size_t)u * t.max_pages + j];
+        if ((unsigned)p < (unsigned)t.P) p = place[p];
+      }
+      pages_out[(size_t)u * t.max_pages + j] = p;
+    }
+  }
+  // a page in use has its count where it goes to; what lies behind the last of them is free
+  const int M = *in_use;
+  for (long long p = (long long)first * 256 + threadIdx.x; p < t.P; p += (long long)step * 256) {
+    const int count = t.refs[p];
+    if (count > 0) refs_out[place[p]] = count;
+    if (p >= M) refs_out[p] = 0;
+  }
+}
+
+__global__ __launch_bounds__(256) void copy_kernel(const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n, int P,
+                                                   const Moves m) {
+  move_pages(m, n, blockIdx.x, gridDim.x, [&](long long i, int* from, int* to) __attribute__((always_inline)) {
+    *from = src[i];
+    *to = dst[i];
+    return (unsigned)*from < (unsigned)P && (unsigned)*to < (unsigned)P;
+  });
+}
+
+// ---------------------------------------------------------------- launchers
+size_t pages_work_ints(int U, int P) { return (size_t)U + 3 * (size_t)P + 16; }
+
+static Tables tables_of(const PagesArgs& a) { return Tables{a.pages, a.lens, a.refs, a.U, a.P, a.page_log2, a.max_pages}; }
+
+// The parts from `first` on that one launch moves, with their pieces
+static PageParts parts_of(const PagesArgs& a, int first) {
+  PageParts p{};
+  for (int i = first; i < a.n_parts && p.n < PARTS_A_LAUNCH; ++i, ++p.n) {
+    const unsigned long long x = reinterpret_cast<unsigned long long>(a.parts[i]) | (unsigned long long)a.part_bytes[i];
+    p.at[p.n] = static_cast<unsigned char*>(a.parts[i]);
+    p.bytes[p.n] = a.part_bytes[i];
+    p.piece_log2[p.n] = x % 16 == 0 ? 4 : x % 4 == 0 ? 2 : 0;
+    p.pieces[p.n] = (unsigned)(a.part_bytes[i] >> p.piece_log2[p.n]);
+    p.all += p.pieces[p.n];
+  }
+  return p;
+}
+// go(moves, workgroups that copy, first): a launch for every 16 parts
+template <typename Go>
+static laser_status over_parts(const PagesArgs& a, long long entries, const int32_t* count, Go&& go) {
+  for (int i = 0; i == 0 || i < a.n_parts; i += PARTS_A_LAUNCH) {
+    Moves m{};
+    m.parts = parts_of(a, i);
+    m.count = count;
+    m.total = entries * m.parts.all;
+    const long long groups = (m.total + 255) / 256;
+    go(m, (unsigned)(groups < 4096 ? groups : 4096), i == 0);
+    const laser_status s = launch_status();
+    if (s != LASER_OK) return s;
+  }
+  return LASER_OK;
+}
+
+laser_status pages_fork_launch(const PagesArgs& a) {
+  int32_t *rank = a.work, *fresh = a.work + a.V;
+  const Tables t = tables_of(a);
+  fork_plan_kernel<<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing);
+  laser_status s = launch_status();
+  if (s != LASER_OK) return s;
+  return over_parts(a, a.V, nullptr, [&](const Moves& m, unsigned copies, bool first) {
+    const unsigned more = first ? (a.V < 4096 ? a.V : 4096) : 0;
+    if (copies + more > 0)
+      fork_kernel<<<copies + more, 256, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.pages_out, a.lens_out, copies, first, m);
+  });
+}
+
+laser_status pages_grow_launch(const PagesArgs& a) {
+  grow_kernel<<<1, PLAN, 0, a.stream>>>(tables_of(a), a.off, const_cast<int32_t*>(a.pages), a.lens_out, a.work, a.work + a.U, a.missing);
+  return launch_status();
+}
+
+laser_status pages_free_launch(const PagesArgs& a) {
+  free_kernel<<<a.U < 65536 ? a.U : 65536, 256, 0, a.stream>>>(tables_of(a), a.gone, a.lens_out);
+  return launch_status();
+}
+
+laser_status pages_compact_launch(const PagesArgs& a) {
+  int32_t *src = a.work, *dst = src + a.P, *place = dst + a.P, *moved = place + a.P;
+  const Tables t = tables_of(a);
+  compact_plan_kernel<<<1, PLAN, 0, a.stream>>>(a.refs, a.P, src, dst, place, moved, a.in_use);
+  laser_status s = launch_status();
+  if (s != LASER_OK) return s;
+  return over_parts(a, a.P / 2, moved, [&](const Moves& m, unsigned copies, bool first) {
+    const unsigned more = first ? 1024 : 0;
+    if (copies + more > 0)
+      compact_kernel<<<copies + more, 256, 0, a.stream>>>(t, src, dst, place, a.pages_out, a.refs_out, a.in_use, copies, first, m);
+  });
+}
+
+laser_status pages_copy_launch(const PagesArgs& a, const int32_t* src, const int32_t* dst, int n) {
+  return over_parts(a, n, nullptr, [&](const Moves& m, unsigned copies, bool) {
+    if (copies > 0) copy_kernel<<<copies, 256, 0, a.stream>>>(src, dst, n, a.P, m);
+  });
+}
+
+}  // namespace laser
