@@ -17,6 +17,7 @@ struct Cache8Args {
 };
 laser_status cache8_append_launch(const Cache8Args& a);
 CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt);
+int cache8_waves(int U, int Hkv, const CacheRuns& r);    // of a workgroup of the kernel for few rows
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status cache8_attention_launch(const Cache8Args& a);
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r);    // at most 32 rows a key-value head

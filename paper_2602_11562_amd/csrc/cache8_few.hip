@@ -1,5 +1,5 @@
 // A few rows per key-value head over a cache of 8-bit blocks: one new item or a handful of candidates a user. Bound by memory, as
-// cache_few.hip, whose split it has: a workgroup owns (user, key-value head, run of items), its four waves take tiles of 32 items in turn,
+// cache_few.hip, whose split it has: a workgroup owns (user, key-value head, run of items), its four or eight waves take tiles of 32 items in turn,
 // each with two tiles of its own in LDS and no barrier while it streams; at the end the waves' maxima, sums and outputs are joined in
 // LDS, and the runs of a long history by a second launch.
 //
@@ -17,13 +17,13 @@ struct Few8Shape {
   static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
 };
 
-template <int DP, int NP, typename T>
-__global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
+template <int DP, int NP, int NW, typename T>
+__global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
   using Sh = Few8Shape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * Sh::WAVE];
-  __shared__ __attribute__((aligned(16))) float scales[4][Sh::NST][8];
-  __shared__ float join_m[4][32], join_l[4][32];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * Sh::WAVE];
+  __shared__ __attribute__((aligned(16))) float scales[NW][Sh::NST][8];
+  __shared__ float join_m[NW][32], join_l[NW][32];
   const CacheArgs& a = a8.c;
   const int per = a.U * a.Hkv;
   // (turned by one from run to run: a user's runs are not all one die's)
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8,
 
   Tiles8<DP, 32> tiles;
   tiles.init(a.D, a.page_log2, 0, lane);
-  const int step_items = 4 * 32, requests = tiles.requests();
+  const int step_items = NW * 32, requests = tiles.requests();
   int ask = lo + wave * 32, mine = ask;
   int pending = 0, slot_in = 0, slot_out = 0;
   tiles.look_up(table, ask, hi, a.page_log2);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8,
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
     top = half_max(top) * scale;
-    if (__any(top > m)) {
+    if (__any(top > m + MAX_SLACK)) {   // (the first tile: m is -inf)
       const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
       m = next;
       l *= c;
@@ -123,15 +123,14 @@ __global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8,
     }
     const float base = m == -INFINITY ? 0.0f : m;
     bf16x8 p[NP][2];
+    float sum = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, -base));
-      l += p0;
-      __bf16 part[NP];
-      split_bf16<NP>(p0, part);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) p[i][r >> 3][r & 7] = part[i];
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], scale, -base));
+      sum += p0 + p1;
+      split_pair<NP>(p0, p1, r, p);
     }
+    l += sum;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const u32x2 vs = read.value_scales(at_s, s);
@@ -170,14 +169,14 @@ __global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8,
   }
   __syncthreads();
   const bool final = n <= chunk;
-  for (int e = tid; e < rows * a.D; e += 256) {
+  for (int e = tid; e < rows * a.D; e += 64 * NW) {
     const int r = e / a.D, d = e - r * a.D;
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, join_m[w][r]);
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, join_m[w][r]);
     float sum = 0.0f, x = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float mw = join_m[w][r], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
       sum = fmaf(join_l[w][r], c, sum);
       x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 32 + (r ^ (d & 31))], c, x);
@@ -197,20 +196,20 @@ __global__ __launch_bounds__(256, 2) void cache8_few_kernel(const Cache8Args a8,
   }
 }
 
-template <int DP, int NP, typename T>
+template <int DP, int NP, int NW, typename T>
 static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
   const CacheArgs& c = a.c;
   const int G = c.H / c.Hkv;
   const long long each = (long long)c.Hkv * r.runs;   // workgroups of a user
   if (c.U * each > 0x7fffffffLL) return LASER_ERR_SHAPE;
-  const long long most = 0xffffffffLL / 256 / each;   // (a launch has fewer than 2^32 threads; a user has Hkv * runs <= 2^20 workgroups)
+  const long long most = 0xffffffffLL / (64 * NW) / each;   // (a launch has fewer than 2^32 threads; a user has Hkv * runs <= 2^20 workgroups)
   for (long long u = 0; u < c.U; u += most) {
     Cache8Args part = a;
     part.c.U = c.U - u < most ? (int)(c.U - u) : (int)most;
     part.c.off = c.off + u;
     part.c.pages = c.pages + u * c.max_pages;
     part.c.lens = c.lens + u;
-    cache8_few_kernel<DP, NP, T><<<(unsigned)(part.c.U * each), 256, 0, c.stream>>>(part, G, mul_div(G), LOG2E / c.gamma, r.chunk, r.runs);
+    cache8_few_kernel<DP, NP, NW, T><<<(unsigned)(part.c.U * each), 64 * NW, 0, c.stream>>>(part, G, mul_div(G), LOG2E / c.gamma, r.chunk, r.runs);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
@@ -218,9 +217,14 @@ static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
 }
 template <int NP, typename T>
 static laser_status few8_width(const Cache8Args& a, const CacheRuns& r) {
-  if (a.c.D > 64) return few8_typed<128, NP, T>(a, r);
-  if (a.c.D > 32) return few8_typed<64, NP, T>(a, r);
-  return few8_typed<32, NP, T>(a, r);
+  if (cache8_waves(a.c.U, a.c.Hkv, r) == 8) {
+    if (a.c.D > 64) return few8_typed<128, NP, 8, T>(a, r);
+    if (a.c.D > 32) return few8_typed<64, NP, 8, T>(a, r);
+    return few8_typed<32, NP, 8, T>(a, r);
+  }
+  if (a.c.D > 64) return few8_typed<128, NP, 4, T>(a, r);
+  if (a.c.D > 32) return few8_typed<64, NP, 4, T>(a, r);
+  return few8_typed<32, NP, 4, T>(a, r);
 }
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r) {
   return a.c.dt == LASER_F32 ? few8_width<3, float>(a, r) : few8_width<1, unsigned short>(a, r);

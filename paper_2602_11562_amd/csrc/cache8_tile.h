@@ -134,6 +134,22 @@ __device__ __forceinline__ void split_bf16(float x, __bf16* part) {
   }
 }
 
+// Probabilities r and r + 1 of a block, of the operands p
+template <int NP>
+__device__ __forceinline__ void split_pair(float a, float b, int r, bf16x8 (*p)[2]) {
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const bf16x2 c = {(__bf16)a, (__bf16)b};
+    p[i][r >> 3][r & 7] = c[0];
+    p[i][r >> 3][(r & 7) + 1] = c[1];
+    a -= (float)c[0];
+    b -= (float)c[1];
+  }
+}
+
+// Where the maximum of a row is raised: probabilities may stand up to 2^8 above it meanwhile, sums and outputs are in its units
+constexpr float MAX_SLACK = 8.0f;
+
 // The query of a lane's row as B operands in the order of TileReader8::rows; bf16 as it is, fp32 in three parts
 template <int DP, int NP, typename T>
 __device__ __forceinline__ void load_query(const T* qr, int D, int h, bf16x8 (*q)[DP / 16]) {

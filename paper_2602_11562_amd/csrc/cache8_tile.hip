@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
     top = half_max(top) * t.scale;
-    if (__any(top > m)) {
+    if (__any(top > m + MAX_SLACK)) {   // (the first tile: m is -inf)
       const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
       m = next;
       l *= c;
@@ -139,15 +139,14 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
     }
     const float base = m == -INFINITY ? 0.0f : m;
     bf16x8 p[NP][2];
+    float sum = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], t.scale, -base));
-      l += p0;
-      __bf16 part[NP];
-      split_bf16<NP>(p0, part);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) p[i][r >> 3][r & 7] = part[i];
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r], t.scale, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[r + 1], t.scale, -base));
+      sum += p0 + p1;
+      split_pair<NP>(p0, p1, r, p);
     }
+    l += sum;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const u32x2 vs = read.value_scales(at_s, s);

@@ -44,11 +44,23 @@ static laser_status validate_cache8(const void* k_cache, const void* v_cache, co
 
 // Rows of a key-value head that one column block holds: the streaming kernel
 static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <= 32; }
-// Into how many runs: as for a cache of bf16 items (history_api.hip)
+// Into how many runs. A cut costs a join, 4 to 6 us, and what its parts weigh. Many rows: as in history_api.hip. Few rows, us by one run a
+// history, runs of 1024 items and runs of 512 (heads of 128 over 2 key-value heads unless said otherwise):
+//   1 x 65000, 16 heads (2 pairs)  -, 20.0, 18.6;  8 x 20000 (16)  -, 20.5, 26.3;  40 x 3000 fp32 (80)  28, 23.6, 31.8;  5 x 777 fp32 (10)  14.5, -, 16.8;
+//   32 x 1000, 8 over 8 of 64 (256)  14.0, -, 18.5;  128 x 970 of up to 4096 (256)  35.6 (two of 2048), 27.0, 29.3;  200 x 5000, 4 over 1 of 64 (200)
+//   33.5 (two), 30.8, 34.0;  256 x 1200 of up to 2000, four rows (512)  38.0, 47.8, 55.7
+// Rules: none where the histories alone are two workgroups a compute unit, or short; else runs of 512 while they are one workgroup a
+// compute unit, and of 1024 beyond.
 CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, laser_dtype) {
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
-  return few8_rows(C, H, Hkv) ? cache_runs(pairs, L, 1024, 512, 128) : cache_runs((rows + 127) / 128 * pairs, L, 2048, 256, 64);
+  if (!few8_rows(C, H, Hkv)) return cache_runs((rows + 127) / 128 * pairs, L, 2048, 256, 64);
+  if (pairs >= 512 || L <= 1024) return CacheRuns{(L + 255) / 256 * 256, 1};
+  return cache_runs(pairs, L, 1024, pairs * ((L + 511) / 512) <= 256 ? 512 : 1024, 256);
 }
+// Eight waves where there is about one workgroup a compute unit, whose way is then half as long (us by four and eight: 1 x 65000 19.5 and
+// 18.6, 40 x 3000 fp32 26.0 and 23.6, 32 x 1000 14.7 and 14.0); four beyond, two workgroups of which share a compute unit (128 x 970
+// 27.0 and 31.9, 256 x 1200 38.0 and 42.6).
+int cache8_waves(int U, int Hkv, const CacheRuns& r) { return (long long)U * Hkv * r.runs <= 320 ? 8 : 4; }
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const CacheRuns r = cache8_runs_of(U, C, L, H, Hkv, dt);
   return r.runs > 1 ? (size_t)r.runs * T * H * (D + 1) * 4 : 16;
