@@ -833,8 +833,9 @@ def _native(name: str, *args):
     entry = _ADDRESS.get(name)
     if entry is None:
         fn = getattr(load_library(), "laser_" + {"history_forward": "history_attention_forward", "history_backward":
-                     "history_attention_backward", "cache_attention": "cache_attention_forward"}.get(name, name))
-        entry = _ADDRESS[name] = (getattr(fast, name), ctypes.cast(fn, ctypes.c_void_p).value)
+                     "history_attention_backward", "cache_attention": "cache_attention_forward", "cache8_attention":
+                     "cache8_attention_forward"}.get(name, name))
+        entry = _ADDRESS[name] = (getattr(fast, name.replace("rotary_backward", "rotary_forward")), ctypes.cast(fn, ctypes.c_void_p).value)
     core = _torch()._C
     return entry[0](entry[1], core._cuda_getDevice(), *args, _stream(None))
 
@@ -1127,6 +1128,11 @@ def laser_rotary_frequencies(R: int, base: float = 10000.0, scaling: int = ROTAR
 
 
 def _rotary(name: str, q, k, pos, freq, layout, scale, q_out, k_out, stream, names):
+    if stream is None and q_out is not None and (k is None) == (k_out is None) and q.is_cuda:
+        code = _native(name, q, k, pos, freq, layout, scale, q_out, k_out)
+        if code is not None:
+            _check(code, "laser_" + name)
+            return q_out, k_out
     torch = _torch()
     index = _one_device(names, q, k, pos, freq, q_out, k_out)
     words = names.split()
@@ -1144,11 +1150,11 @@ def _rotary(name: str, q, k, pos, freq, layout, scale, q_out, k_out, stream, nam
         y = torch.empty(shape, dtype=dtype, device=q.device) if q_out is None else q_out
         z = k_out if k is None or k_out is not None else torch.empty(kv, dtype=dtype, device=q.device)
         keys = (None, 0) if k is None else (k.data_ptr(), _pitch(k, words[1], kv))
-        _check(getattr(load_library(), name)(
+        _check(getattr(load_library(), "laser_" + name)(
             q.data_ptr(), _pitch(q, words[0], shape), *keys, _flat(pos, "pos", (T,), torch.int32),
             _flat(freq, "freq", freq.shape, torch.float64), T, H, 0 if k is None else kv[1], D, 2 * freq.shape[0], int(layout),
             float(scale), _dt(q), y.data_ptr(), _pitch(y, words[4], shape), None if k is None else z.data_ptr(),
-            0 if k is None else _pitch(z, words[5], kv), _stream(stream)), name)
+            0 if k is None else _pitch(z, words[5], kv), _stream(stream)), "laser_" + name)
         return y, z
 
     return _there(index, stream, call)
@@ -1157,12 +1163,12 @@ def _rotary(name: str, q, k, pos, freq, layout, scale, q_out, k_out, stream, nam
 def laser_rotary_forward(q, k, pos, freq, layout: int = ROTARY_HALF, scale: float = 1.0, q_out=None, k_out=None, stream=None):
     """Queries [T,H,D] and keys [T,H_kv,D] (or None) turned by their positions int32 [T] (negative: the row is left out), pair i by pos *
     freq[i], fp64 [R / 2] -> (q, k). The outputs may be the inputs, or column blocks of one tensor."""
-    return _rotary("laser_rotary_forward", q, k, pos, freq, layout, scale, q_out, k_out, stream, "q k pos freq q_out k_out")
+    return _rotary("rotary_forward", q, k, pos, freq, layout, scale, q_out, k_out, stream, "q k pos freq q_out k_out")
 
 
 def laser_rotary_backward(d_q, d_k, pos, freq, layout: int = ROTARY_HALF, scale: float = 1.0, dq_out=None, dk_out=None, stream=None):
     """Gradients of laser_rotary_forward: of its results -> of its queries and keys."""
-    return _rotary("laser_rotary_backward", d_q, d_k, pos, freq, layout, scale, dq_out, dk_out, stream,
+    return _rotary("rotary_backward", d_q, d_k, pos, freq, layout, scale, dq_out, dk_out, stream,
                    "d_q d_k pos freq dq_out dk_out")
 
 
@@ -1182,6 +1188,11 @@ def _cache8_of(k_cache, v_cache, k_scale, v_scale, pages, lens):
 def laser_cache8_append(k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max: int, L_max: int, stream=None):
     """As laser_cache_append into a cache of 8-bit blocks: k_cache, v_cache float8_e4m3fn [P,H_kv,page,D], whose items are their numbers
     times k_scale, v_scale fp32 [P,H_kv,page/block], powers of two that grow where new items ask for it."""
+    if stream is None and k.is_cuda:
+        code = _native("cache8_append", k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max, L_max)
+        if code is not None:
+            _check(code, "laser_cache8_append")
+            return
     torch = _torch()
     index = _one_device("k v k_cache v_cache k_scale v_scale off pages lens", k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens)
     (P, Hkv, page, D, U, max_pages), block, held, table, n = _cache8_of(k_cache, v_cache, k_scale, v_scale, pages, lens)
@@ -1205,6 +1216,12 @@ def laser_cache8_attention_work_bytes(U: int, T: int, C_max: int, L_max: int, H:
 def laser_cache8_attention_forward(q, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max: int, L_max: int, gamma: float,
                                    causal: bool = True, o_out=None, lse_out=None, work=None, stream=None):
     """As laser_cache_attention_forward over a cache of 8-bit blocks (laser_cache8_append); queries in fp32 or bf16."""
+    if stream is None and o_out is not None and lse_out is not None and work is not None and q.is_cuda:
+        code = _native("cache8_attention", q, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max, L_max, gamma, causal, o_out,
+                       lse_out, work)
+        if code is not None:
+            _check(code, "laser_cache8_attention_forward")
+            return o_out, lse_out
     torch = _torch()
     index = _one_device("q k_cache v_cache k_scale v_scale off pages lens o_out lse_out work", q, k_cache, v_cache, k_scale, v_scale, off,
                         pages, lens, o_out, lse_out, work)
@@ -1271,6 +1288,11 @@ def _names(parts) -> str:
 def laser_pages_grow(pages, lens, off, refs, page: int, missing_out=None, work=None, stream=None):
     """lens int32 [U] grow by the rows that off int32 [U+1] packs, and the tables pages int32 [U,max_pages] get fresh pages of `page` items for
     them, the lowest free ones of the pool (refs int32 [P]: how many tables name a page). Returns missing [1], the pages that there were none for."""
+    if stream is None and missing_out is not None and work is not None and pages.is_cuda:
+        code = _native("pages_grow", pages, lens, off, refs, page, missing_out, work)
+        if code is not None:
+            _check(code, "laser_pages_grow")
+            return missing_out
     torch = _torch()
     index, U, max_pages, P, table, n, counts = _page_tables(
         pages, lens, refs, ("pages lens off refs missing_out work", pages, lens, off, refs, missing_out, work))
@@ -1290,6 +1312,12 @@ def laser_pages_fork(parts, pages, lens, source, refs, page: int, max_pages_out:
                      missing_out=None, work=None, stream=None):
     """New tables whose history v is that of user source[v], int32 [V]: whole pages are shared, a partly filled last one is copied, in
     every one of the parts [P, ...], into a fresh page -> (pages_out [V,max_pages_out], lens_out [V])."""
+    if (stream is None and max_pages_out is None and pages_out is not None and lens_out is not None and missing_out is not None and
+            work is not None and pages.is_cuda):
+        code = _native("pages_fork", parts, pages, lens, source, refs, page, pages_out, lens_out, missing_out, work)
+        if code is not None:
+            _check(code, "laser_pages_fork")
+            return pages_out, lens_out
     torch = _torch()
     index, U, max_pages, P, table, n, counts = _page_tables(
         pages, lens, refs, ("pages lens source refs pages_out lens_out missing_out work " + _names(parts), pages, lens, source, refs, pages_out,
@@ -1317,6 +1345,11 @@ def laser_pages_fork(parts, pages, lens, source, refs, page: int, max_pages_out:
 
 def laser_pages_free(pages, lens, gone, refs, page: int, stream=None):
     """Users with gone int32 [U] != 0 (None: all) give their pages back and have no items any more."""
+    if stream is None and pages.is_cuda:
+        code = _native("pages_free", pages, lens, gone, refs, page)
+        if code is not None:
+            _check(code, "laser_pages_free")
+            return
     torch = _torch()
     index, U, max_pages, P, table, n, counts = _page_tables(pages, lens, refs, ("pages lens gone refs", pages, lens, gone, refs))
 
@@ -1330,6 +1363,11 @@ def laser_pages_free(pages, lens, gone, refs, page: int, stream=None):
 def laser_pages_compact(parts, pages, lens, refs, page: int, pages_out=None, refs_out=None, in_use_out=None, work=None, stream=None):
     """The pages in use become the first ones of the pool, in every one of the parts [P, ...] -> (pages [U,max_pages] and refs [P] with the
     new numbers, in_use [1])."""
+    if stream is None and pages_out is not None and refs_out is not None and in_use_out is not None and work is not None and pages.is_cuda:
+        code = _native("pages_compact", parts, pages, lens, refs, page, pages_out, refs_out, in_use_out, work)
+        if code is not None:
+            _check(code, "laser_pages_compact")
+            return pages_out, refs_out, in_use_out
     torch = _torch()
     index, U, max_pages, P, table, n, counts = _page_tables(
         pages, lens, refs, ("pages lens refs pages_out refs_out in_use_out work " + _names(parts), pages, lens, refs, pages_out, refs_out,

@@ -1,4 +1,4 @@
-// The marshalling of laser_forward and of attention among a history's items in native code, for calls of the ordinary form: plain device
+// The marshalling of laser_forward, of attention among a history's items and of what serves it in native code, for calls of the ordinary form: plain device
 // tensors, contiguous (rows of heads: apart by token), outputs given. Anything else returns None, and the caller (binding.py) goes its
 // own way, with its own checks and errors. A small request is 8 us of kernels; attribute by attribute in Python, with ctypes, its host
 // part took 10.5 us a call. Torch's accessors are inlined here, so the module names the torch that it was built against (`stamp`), and the
@@ -313,10 +313,212 @@ static PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------- positions, the cache in 8 bits, the pages of a cache
+// (address, device, q, k or None, pos, freq, layout, scale, q_out, k_out or None, stream)
+static PyObject* rotary_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 11, [](Args& x, int* code) {
+    typedef int (*Fn)(const void*, int64_t, const void*, int64_t, const void*, const void*, int, int, int, int, int, int, float, int, void*,
+                      int64_t, void*, int64_t, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    int64_t s[3], kv[3] = {0, 0, 0}, half, qp, qop, kp = 0, kop = 0;
+    at::ScalarType type, type_k;
+    if (!x.sizes3(2, s, &type)) return;
+    const bool keys = x.a[3] != Py_None;
+    if (keys != (x.a[9] != Py_None) || (keys && !x.sizes3(3, kv, &type_k))) return x.ok = false, void();
+    const void *q = x.rows(2, type, s[0], s[1], s[2], &qp), *k = keys ? x.rows(3, type, s[0], kv[1], s[2], &kp) : nullptr,
+               *pos = x.flat(4, at::kInt, {s[0]}), *freq = x.flat(5, at::kDouble, {-1}, &half);
+    const int layout = x.number(6);
+    const float scale = x.real(7);
+    void *qo = x.rows(8, type, s[0], s[1], s[2], &qop), *ko = keys ? x.rows(9, type, s[0], kv[1], s[2], &kop) : nullptr;
+    void* stream = x.stream(10);
+    if (!x.ok || half > 64) return x.ok = false, void();
+    LASER_UNLOCKED(fn(q, qp, k, kp, pos, freq, (int)s[0], (int)s[1], (int)kv[1], (int)s[2], 2 * (int)half, layout, scale, dtype_of(type), qo, qop,
+                      ko, kop, stream));
+  });
+}
+
+// k_cache, v_cache, k_scale, v_scale and on, pages, lens
+struct Cache8 {
+  void *k = nullptr, *v = nullptr, *ks = nullptr, *vs = nullptr, *pages = nullptr, *lens = nullptr;
+  int64_t P = 0, Hkv = 0, page = 0, D = 0, U = 0, most = 0, block = 0;
+  Cache8(Args& x, int k_at, int pages_at) {
+    int64_t s[4], t[2], blocks;
+    if (!x.ok || !THPVariable_CheckExact(x.a[k_at])) {
+      x.ok = false;
+      return;
+    }
+    const at::ScalarType type = THPVariable_Unpack(x.a[k_at]).scalar_type();
+    if (type != at::kByte && type != at::kFloat8_e4m3fn) x.ok = false;
+    k = x.flat(k_at, type, {-1, -1, -1, -1}, s);
+    pages = x.flat(pages_at, at::kInt, {-1, -1}, t);
+    if (!x.ok) return;
+    P = s[0], Hkv = s[1], page = s[2], D = s[3], U = t[0], most = t[1];
+    v = x.flat(k_at + 1, type, {P, Hkv, page, D});
+    ks = x.flat(k_at + 2, at::kFloat, {P, Hkv, -1}, &blocks);
+    if (!x.ok || blocks < 1 || page % blocks != 0) {
+      x.ok = false;
+      return;
+    }
+    block = page / blocks;
+    vs = x.flat(k_at + 3, at::kFloat, {P, Hkv, blocks});
+    lens = x.flat(pages_at + 1, at::kInt, {U});
+  }
+};
+
+// (address, device, k, v, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max, L_max, stream)
+static PyObject* cache8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 14, [](Args& x, int* code) {
+    typedef int (*Fn)(const void*, int64_t, const void*, int64_t, void*, void*, void*, void*, const void*, const void*, const void*, int, int, int,
+                      int, int, int, int, int, int, int, int, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Cache8 c(x, 4, 9);
+    int64_t s[3], kp, vp;
+    at::ScalarType type;
+    if (!x.sizes3(2, s, &type)) return;
+    const void *k = x.rows(2, type, s[0], c.Hkv, c.D, &kp), *v = x.rows(3, type, s[0], c.Hkv, c.D, &vp), *off = x.flat(8, at::kInt, {c.U + 1});
+    const int C = x.number(11), L = x.number(12);
+    void* stream = x.stream(13);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(k, kp, v, vp, c.k, c.v, c.ks, c.vs, off, c.pages, c.lens, (int)c.U, (int)s[0], C, (int)c.P, (int)c.page, (int)c.block,
+                      (int)c.most, L, (int)c.Hkv, (int)c.D, dtype_of(type), stream));
+  });
+}
+
+// (address, device, q, k_cache, v_cache, k_scale, v_scale, off, pages, lens, C_max, L_max, gamma, causal, o_out, lse_out, work, stream)
+static PyObject* cache8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 18, [](Args& x, int* code) {
+    typedef int (*Fn)(const void*, int64_t, const void*, const void*, const void*, const void*, const void*, const void*, const void*, int, int, int,
+                      int, int, int, int, int, int, int, int, float, int, int, void*, void*, void*, size_t, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Cache8 c(x, 3, 8);
+    int64_t s[3], qp, room;
+    at::ScalarType type;
+    if (!x.sizes3(2, s, &type)) return;
+    const void *q = x.rows(2, type, s[0], s[1], c.D, &qp), *off = x.flat(7, at::kInt, {c.U + 1});
+    const int C = x.number(10), L = x.number(11), causal = x.number(13);
+    const float gamma = x.real(12);
+    void *o = x.flat(14, type, {s[0], s[1], c.D}), *lse = x.flat(15, at::kFloat, {s[0], s[1]}), *work = x.flat(16, at::kByte, {-1}, &room);
+    void* stream = x.stream(17);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(q, qp, c.k, c.v, c.ks, c.vs, off, c.pages, c.lens, (int)c.U, (int)s[0], C, (int)c.P, (int)c.page, (int)c.block, (int)c.most, L,
+                      (int)s[1], (int)c.Hkv, (int)c.D, gamma, causal != 0, dtype_of(type), o, lse, work, (size_t)room, stream));
+  });
+}
+
+// pages, lens and refs of a pool, and the parts of a page (a list or tuple of contiguous tensors [P, ...])
+struct Pool {
+  static constexpr int MOST = 64;
+  void *pages = nullptr, *lens = nullptr, *refs = nullptr;
+  int64_t U = 0, most = 0, P = 0;
+  void* part[MOST];
+  int64_t bytes[MOST];
+  int parts = 0;
+  Pool(Args& x, int parts_at, int pages_at, int lens_at, int refs_at) {
+    int64_t t[2];
+    pages = x.flat(pages_at, at::kInt, {-1, -1}, t);
+    refs = x.flat(refs_at, at::kInt, {-1}, &P);
+    if (!x.ok) return;
+    U = t[0], most = t[1];
+    lens = x.flat(lens_at, at::kInt, {U});
+    if (parts_at < 0) return;
+    PyObject* list = x.a[parts_at];
+    if (!PyList_CheckExact(list) && !PyTuple_CheckExact(list)) {
+      x.ok = false;
+      return;
+    }
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    if (n > MOST || P < 1) x.ok = false;
+    for (Py_ssize_t i = 0; x.ok && i < n; ++i) {
+      PyObject* o = PySequence_Fast_GET_ITEM(list, i);
+      if (!THPVariable_CheckExact(o)) {
+        x.ok = false;
+        break;
+      }
+      const at::Tensor& p = THPVariable_Unpack(o);
+      if (!p.defined() || !p.is_cuda() || p.get_device() != x.device || p.layout() != at::kStrided || !p.has_storage() || !p.is_contiguous() ||
+          p.dim() < 1 || p.size(0) != P) {
+        x.ok = false;
+        break;
+      }
+      part[parts] = p.data_ptr();
+      bytes[parts++] = p.numel() / P * (int64_t)p.element_size();
+    }
+  }
+};
+
+// (address, device, pages, lens, off, refs, page, missing_out, work, stream)
+static PyObject* pages_grow(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 10, [](Args& x, int* code) {
+    typedef int (*Fn)(void*, void*, const void*, void*, int, int, int, int, void*, void*, size_t, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Pool p(x, -1, 2, 3, 5);
+    int64_t room;
+    const void* off = x.ok ? x.flat(4, at::kInt, {p.U + 1}) : nullptr;
+    const int page = x.number(6);
+    void *missing = x.flat(7, at::kInt, {1}), *work = x.flat(8, at::kByte, {-1}, &room), *stream = x.stream(9);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(p.pages, p.lens, off, p.refs, (int)p.U, (int)p.P, page, (int)p.most, missing, work, (size_t)room, stream));
+  });
+}
+
+// (address, device, parts, pages, lens, source, refs, page, pages_out, lens_out, missing_out, work, stream)
+static PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 13, [](Args& x, int* code) {
+    typedef int (*Fn)(void* const*, const int64_t*, int, const void*, const void*, const void*, void*, int, int, int, int, int, int, void*, void*, void*,
+                      void*, size_t, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Pool p(x, 2, 3, 4, 6);
+    int64_t V, out[2], room;
+    const void* source = x.flat(5, at::kInt, {-1}, &V);
+    const int page = x.number(7);
+    if (!x.ok) return;
+    void *pages_out = x.flat(8, at::kInt, {V, -1}, out), *lens_out = x.flat(9, at::kInt, {V}), *missing = x.flat(10, at::kInt, {1});
+    void *work = x.flat(11, at::kByte, {-1}, &room), *stream = x.stream(12);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(p.part, p.bytes, p.parts, p.pages, p.lens, source, p.refs, (int)p.U, (int)V, (int)p.P, page, (int)p.most, (int)out[0], pages_out,
+                      lens_out, missing, work, (size_t)room, stream));
+  });
+}
+
+// (address, device, pages, lens, gone or None, refs, page, stream)
+static PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 8, [](Args& x, int* code) {
+    typedef int (*Fn)(const void*, void*, const void*, void*, int, int, int, int, void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Pool p(x, -1, 2, 3, 5);
+    if (!x.ok) return;
+    const void* gone = x.a[4] == Py_None ? nullptr : x.flat(4, at::kInt, {p.U});
+    const int page = x.number(6);
+    void* stream = x.stream(7);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(p.pages, p.lens, gone, p.refs, (int)p.U, (int)p.P, page, (int)p.most, stream));
+  });
+}
+
+// (address, device, parts, pages, lens, refs, page, pages_out, refs_out, in_use_out, work, stream)
+static PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(a, n, 12, [](Args& x, int* code) {
+    typedef int (*Fn)(void* const*, const int64_t*, int, const void*, const void*, const void*, int, int, int, int, void*, void*, void*, void*, size_t,
+                      void*);
+    const auto fn = reinterpret_cast<Fn>(x.address(0));
+    const Pool p(x, 2, 3, 4, 5);
+    int64_t room;
+    const int page = x.number(6);
+    if (!x.ok) return;
+    void *pages_out = x.flat(7, at::kInt, {p.U, p.most}), *refs_out = x.flat(8, at::kInt, {p.P}), *in_use = x.flat(9, at::kInt, {1});
+    void *work = x.flat(10, at::kByte, {-1}, &room), *stream = x.stream(11);
+    if (!x.ok) return;
+    LASER_UNLOCKED(fn(p.part, p.bytes, p.parts, p.pages, p.lens, p.refs, (int)p.U, (int)p.P, page, (int)p.most, pages_out, refs_out, in_use, work,
+                      (size_t)room, stream));
+  });
+}
+
 #define LASER_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 static PyMethodDef methods[] = {LASER_METHOD(forward),      LASER_METHOD(history_forward), LASER_METHOD(history_backward),
                                 LASER_METHOD(cache_append), LASER_METHOD(cache_attention), LASER_METHOD(cache_weights),
-                                LASER_METHOD(cache_evict),  {nullptr, nullptr, 0, nullptr}};
+                                LASER_METHOD(cache_evict),  LASER_METHOD(rotary_forward),  LASER_METHOD(cache8_append),
+                                LASER_METHOD(cache8_attention), LASER_METHOD(pages_grow), LASER_METHOD(pages_fork), LASER_METHOD(pages_free),
+                                LASER_METHOD(pages_compact), {nullptr, nullptr, 0, nullptr}};
 static PyModuleDef module = {PyModuleDef_HEAD_INIT, "laser_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 PyMODINIT_FUNC PyInit_laser_fast() {
   PyObject* m = PyModule_Create(&module);

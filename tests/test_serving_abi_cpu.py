@@ -137,7 +137,7 @@ def test_binding_refuses_what_it_cannot_hand_over():
     class OnDevice:
         """A CPU tensor that claims a device."""
         def __init__(self, t, index=0):
-            self.t, self.index, self.is_cuda, self.device = t, index, True, torch.device("cpu")
+            self.t, self.index = t, index
 
         def get_device(self):
             return self.index
@@ -184,3 +184,31 @@ def test_binding_refuses_what_it_cannot_hand_over():
         laser.laser_pages_fork([cache], pages, lens, dev(2, 2, dtype=i32), refs, 16)
     with pytest.raises(ValueError, match="one device"):
         laser.laser_pages_compact([dev(5, 2, 16, 16, index=1)], pages, lens, refs, 16)
+
+
+def test_the_native_marshalling_leaves_every_other_form_alone():
+    """Host tensors, subclasses, no tensors, numbers of other types and other numbers of arguments: None, whatever the address."""
+    class Sub(torch.Tensor):
+        pass
+    fast = laser.binding._fast()
+    i32 = torch.int32
+    x, c, s = torch.zeros(3, 2, 16), torch.zeros(4, 2, 8, 16, dtype=torch.float8_e4m3fn), torch.zeros(4, 2, 1)
+    off, lens, pages, refs, one = (torch.zeros(*n, dtype=i32) for n in ((2,), (1,), (1, 4), (4,), (1,)))
+    pos, freq, lse, room = torch.zeros(3, dtype=i32), torch.zeros(8, dtype=torch.float64), torch.zeros(3, 2), torch.zeros(16, dtype=torch.uint8)
+    good = {"rotary_forward": [x, x, pos, freq, 0, 1.0, x, x, None],
+            "cache8_append": [x, x, c, c, s, s, off, pages, lens, 1, 3, None],
+            "cache8_attention": [x, c, c, s, s, off, pages, lens, 1, 3, 1.0, True, x, lse, room, None],
+            "pages_grow": [pages, lens, off, refs, 8, one, room, None],
+            "pages_fork": [[c, s], pages, lens, lens, refs, 8, pages, lens, one, room, None],
+            "pages_free": [pages, lens, lens, refs, 8, None],
+            "pages_compact": [(c, s), pages, lens, refs, 8, pages, refs, one, room, None]}
+    for name, args in good.items():
+        f = getattr(fast, name)
+        for device in (0, -1, 1 << 40, "0"):
+            assert f(1, device, *args) is None, name          # (host tensors)
+        for address in (0, 1 << 70, -(1 << 70), 1.0, None):
+            assert f(address, 0, *args) is None, name
+        for at in range(len(args)):
+            for other in (None, "k", 1 << 40, 2.0, -1, x.as_subclass(Sub), torch.zeros(2, 2), [None], [1, x], [x.as_subclass(Sub)], [x] * 100, ()):
+                assert f(1, 0, *args[:at], other, *args[at + 1:]) is None, (name, at)
+        assert f(1, 0, *args[:-1]) is None and f(1, 0, *args, None) is None and f() is None, name
