@@ -1,14 +1,17 @@
 // The pages of a cache. refs[p] counts the tables that hold page p; a page with refs <= 0 is free, and free pages are taken from the
 // lowest number up, users in order, so that the same calls give the same tables whatever the order of atomics.
 //
-// A plan is made by one workgroup that walks the counts (a page's number among the free ones is a sum over all before it) and leaves
-// lists in the work buffer; copies and tables are then written by as many workgroups as that takes. Copies go piece by piece of 16 bytes
-// over all parts of all listed pages, whatever a page's size. Bound by latency for small calls (two launches), by memory for large ones.
+// A plan is made by one workgroup that walks the counts (a page's number among the free ones is a sum over all before it), or for the
+// compaction of a large pool by one for each 8192 pages, and leaves lists in the work buffer; copies and tables are then written by as many
+// workgroups as that takes. Copies go piece by piece of 16 bytes over all parts of all listed pages, whatever a page's size. Bound by latency for small calls (two launches), by memory for large ones.
 #include "pages.h"
 
 namespace laser {
 
 constexpr int PLAN = 1024;   // threads of the plan
+// A wave looks at `runs` runs of 64 pages at a time, the workgroup at a chunk: many where one workgroup walks until it has enough, few where
+// every page has something written and workgroups share them (10248 pages, the plan: one workgroup 9.3 us; runs of 2 in two launches, 5 workgroups, 42.3 us the call instead of 47.0)
+constexpr int TAKE_RUNS = 8, COMPACT_RUNS = 2, CHUNK = PLAN * COMPACT_RUNS;
 
 struct Tables {
   const int32_t* pages;
@@ -45,22 +48,63 @@ __device__ __forceinline__ int sum_before(int x, int* all) {
   *all = total;
   return before + sum - x;
 }
-
-// The first `want` free pages to fresh[], their counts set to 1; returns how many there were
-__device__ __forceinline__ int take_free(int32_t* refs, int P, int want, int32_t* fresh) {
-  constexpr int EACH = 8;   // counts a thread holds at a time
-  int got = 0;
-  for (int p0 = 0; p0 < P && got < want; p0 += PLAN * EACH) {
-    const int mine = p0 + threadIdx.x * EACH;
-    unsigned free = 0;
+// The same of a number that each wave has (two of up to 16 bits in one, if wanted)
+__device__ __forceinline__ int waves_before(int x, int* all) {
+  __shared__ int waves[PLAN / 64];
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) waves[wave] = x;
+  __syncthreads();
+  int before = 0, total = 0;
 #pragma unroll
-    for (int x = 0; x < EACH; ++x) free |= (mine + x < P && refs[mine + x] <= 0 ? 1u : 0u) << x;
+  for (int w = 0; w < PLAN / 64; ++w) {
+    before += w < wave ? waves[w] : 0;
+    total += waves[w];
+  }
+  *all = total;
+  return before;
+}
+
+// The counts of a wave's pages of a chunk: lane l holds those of pages 64 x + l
+template <int RUNS> struct Counts { int c[RUNS]; };
+template <int RUNS>
+__device__ __forceinline__ Counts<RUNS> counts_of(const int32_t* refs, long long first, int P) {
+  Counts<RUNS> x;
+#pragma unroll
+  for (int r = 0; r < RUNS; ++r) {
+    const long long p = first + r * 64 + (threadIdx.x & 63);
+    x.c[r] = p < P ? refs[p] : 0;
+  }
+  return x;
+}
+__device__ __forceinline__ int lanes_before(unsigned long long mask) { return __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1)); }
+
+// The first `want` free pages to fresh[], their counts set to 1; returns how many there were. `next`: the counts of the first chunk
+__device__ __forceinline__ int take_free(int32_t* refs, int P, int want, int32_t* fresh, Counts<TAKE_RUNS> next) {
+  constexpr int RUNS = TAKE_RUNS, CHUNK = PLAN * RUNS;
+  const int mine = (int)(threadIdx.x >> 6) * 64 * RUNS, lane = threadIdx.x & 63;
+  int got = 0;
+  for (int p0 = 0; p0 < P && got < want; p0 += CHUNK) {
+    const Counts<RUNS> here = next;
+    next = counts_of<RUNS>(refs, (long long)p0 + CHUNK + mine, P);   // (asked for ahead of this chunk's sums)
+    unsigned long long free[RUNS];
+    int sum = 0;
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+      free[r] = __ballot(here.c[r] <= 0 && p0 + mine + r * 64 + lane < P);
+      sum += __popcll(free[r]);
+    }
     int all;
-    int rank = got + sum_before(__popc(free), &all);
-    for (; free != 0 && rank < want; free &= free - 1, ++rank) {
-      const int p = mine + __ffs(free) - 1;
-      fresh[rank] = p;
-      refs[p] = 1;
+    int rank = got + waves_before(sum, &all);
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+      const int at = rank + lanes_before(free[r]);
+      if ((free[r] >> lane & 1) && at < want) {
+        const int p = p0 + mine + r * 64 + lane;
+        fresh[at] = p;
+        refs[p] = 1;
+      }
+      rank += __popcll(free[r]);
     }
     got += all;
   }
@@ -78,6 +122,7 @@ __device__ __forceinline__ int forked_items(const Tables& t, const int32_t* sour
 __global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
                                                          int32_t* __restrict__ rank, int32_t* __restrict__ fresh,
                                                          int32_t* __restrict__ missing) {
+  const Counts<TAKE_RUNS> first = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
   for (int v0 = 0; v0 < V; v0 += PLAN) {
     const int v = v0 + threadIdx.x;
@@ -91,17 +136,17 @@ __global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const i
     if (v < V) rank[v] = need ? want + before : -1;
     want += all;
   }
-  const int got = take_free(t.refs, t.P, want, fresh);
+  const int got = take_free(t.refs, t.P, want, fresh, first);
   for (int v = threadIdx.x; v < V; v += PLAN)      // (a thread's own ranks)
     if (rank[v] >= got) rank[v] = -2;              // no page is left for it
   if (threadIdx.x == 0) *missing = want - got;
 }
 
-// Pieces of listed pages from src[] to dst[], every part of them. A thread goes from piece to piece by the grid's threads.
+// Pieces of listed pages from src[] to dst[], every part of them
 struct Moves {
   PageParts parts;
-  long long total;           // pieces in all (at most, where `count` says how many entries there are)
-  const int32_t* count;      // entries, or nullptr: all
+  const int32_t* count;      // entries, where the host does not know
+  MulDiv by_all;             // / parts.all
 };
 template <typename T>
 __device__ __forceinline__ void move_piece(unsigned char* base, long long bytes, int src, int dst, unsigned piece) {
@@ -110,21 +155,17 @@ __device__ __forceinline__ void move_piece(unsigned char* base, long long bytes,
 // entry(e, &src, &dst): false where the entry moves nothing
 template <typename Entry>
 __device__ __forceinline__ void move_pages(const Moves& m, long long entries, unsigned block, unsigned blocks, const Entry& entry) {
-  const long long all = entries * m.parts.all;
+  const PageParts& parts = m.parts;
+  const long long all = entries * parts.all;
   for (long long g = (long long)block * 256 + threadIdx.x; g < all; g += (long long)blocks * 256) {
-    const long long e = g / m.parts.all;
-    unsigned piece = (unsigned)(g - e * m.parts.all);
-    int src, dst;
+    const long long e = all <= 0x7fffffffLL ? (long long)m.by_all.div((unsigned)g) : g / parts.all;
+    unsigned piece = (unsigned)(g - e * parts.all);
+    int src, dst, i = 0;
     if (!entry(e, &src, &dst)) continue;
-    for (int i = 0; i < m.parts.n; ++i) {
-      if (piece < m.parts.pieces[i]) {
-        if (m.parts.piece_log2[i] == 4) move_piece<stream16>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
-        else if (m.parts.piece_log2[i] == 2) move_piece<unsigned>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
-        else move_piece<unsigned char>(m.parts.at[i], m.parts.bytes[i], src, dst, piece);
-        break;
-      }
-      piece -= m.parts.pieces[i];
-    }
+    while (piece >= parts.pieces[i]) piece -= parts.pieces[i++];
+    if (parts.piece_log2[i] == 4) move_piece<stream16>(parts.at[i], parts.bytes[i], src, dst, piece);
+    else if (parts.piece_log2[i] == 2) move_piece<unsigned>(parts.at[i], parts.bytes[i], src, dst, piece);
+    else move_piece<unsigned char>(parts.at[i], parts.bytes[i], src, dst, piece);
   }
 }
 
@@ -170,6 +211,7 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
     const long long c = (long long)off[u + 1] - off[u], room = (long long)t.max_pages << t.log2, m = n + (c > 0 ? c : 0);
     return (int)(m < room ? m : room);
   };
+  const Counts<TAKE_RUNS> ahead = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
   for (int u0 = 0; u0 < t.U; u0 += PLAN) {
     const int u = u0 + threadIdx.x;
@@ -183,7 +225,7 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
     if (u < t.U) rank[u] = want + before;
     want += all;
   }
-  const int got = take_free(t.refs, t.P, want, fresh);
+  const int got = take_free(t.refs, t.P, want, fresh, ahead);
   __syncthreads();
   for (int u = threadIdx.x; u < t.U; u += PLAN) {
     const int n = held_items(t, u), m = grown(u, n), first = pages_of(n, t.log2), last = pages_of(m, t.log2);
@@ -209,49 +251,109 @@ __global__ __launch_bounds__(256) void free_kernel(const Tables t, const int32_t
   }
 }
 
-// Compact, the plan: of M pages in use, those numbered M and more go to the free ones below M, in order
-__global__ __launch_bounds__(PLAN) void compact_plan_kernel(const int32_t* __restrict__ refs, int P, int32_t* __restrict__ src,
-                                                            int32_t* __restrict__ dst, int32_t* __restrict__ place,
-                                                            int32_t* __restrict__ moved, int32_t* __restrict__ in_use) {
-  constexpr int EACH = 8;
-  auto used_of = [&](int mine) {
-    unsigned used = 0;
+// Compact, the plan: of M pages in use, those numbered M and more go to the free ones below M, in order. With `sums`, pages in use of each
+// chunk, a workgroup a chunk; otherwise one workgroup for all of them, a few.
+constexpr int CHUNKS_AT_ONCE = 2, WAVE_PAGES = 64 * COMPACT_RUNS;
+__device__ __forceinline__ int used_in(const Counts<COMPACT_RUNS>& x, unsigned long long* used) {
+  int sum = 0;
 #pragma unroll
-    for (int x = 0; x < EACH; ++x) used |= (mine + x < P && refs[mine + x] > 0 ? 1u : 0u) << x;
-    return used;
-  };
-  int count = 0;
-  for (int p = threadIdx.x * EACH; p < P; p += PLAN * EACH) count += __popc(used_of(p));
-  int M;
-  sum_before(count, &M);
-  int sources = 0, targets = 0;
-  for (int p0 = 0; p0 < P; p0 += PLAN * EACH) {
-    const int mine = p0 + threadIdx.x * EACH;
-    const unsigned used = used_of(mine);
-    unsigned from = 0, to = 0;
-#pragma unroll
-    for (int x = 0; x < EACH; ++x) {
-      const int p = mine + x;
-      if (p >= P) continue;
-      if (used >> x & 1) from |= (p >= M ? 1u : 0u) << x;
-      else to |= (p < M ? 1u : 0u) << x;
-      if (!(from >> x & 1)) place[p] = p;
-    }
-    int all;
-    int a = sources + sum_before(__popc(from), &all);
-    sources += all;
-    for (; from; from &= from - 1) src[a++] = mine + __ffs(from) - 1;
-    int b = targets + sum_before(__popc(to), &all);
-    targets += all;
-    for (; to; to &= to - 1) dst[b++] = mine + __ffs(to) - 1;
+  for (int r = 0; r < COMPACT_RUNS; ++r) {
+    used[r] = __ballot(x.c[r] > 0);
+    sum += __popcll(used[r]);
   }
-  __syncthreads();   // (as many of the one as of the other)
-  for (int i = threadIdx.x; i < sources; i += PLAN) place[src[i]] = dst[i];
-  if (threadIdx.x == 0) {
-    *moved = sources;
-    *in_use = M;
+  return sum;
+}
+__global__ __launch_bounds__(PLAN) void used_kernel(const int32_t* __restrict__ refs, int P, int32_t* __restrict__ sums) {
+  unsigned long long used[COMPACT_RUNS];
+  int all;
+  waves_before(used_in(counts_of<COMPACT_RUNS>(refs, (long long)blockIdx.x * CHUNK + (threadIdx.x >> 6) * WAVE_PAGES, P), used), &all);
+  if (threadIdx.x == 0) sums[blockIdx.x] = all;
+}
+struct CompactPlan {
+  int32_t *src, *dst, *place, *moved, *in_use;
+};
+// A wave's pages of a chunk that begins with page p0; before: pages in use ahead of the wave's, below: those below M
+__device__ __forceinline__ void plan_wave(const CompactPlan& o, const unsigned long long* used, int p0, int P, int M, int before, int below) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r = 0; r < COMPACT_RUNS; ++r) {
+    const int p = p0 + (int)(threadIdx.x >> 6) * WAVE_PAGES + r * 64 + lane, rank = before + lanes_before(used[r]);
+    if (p < P) {
+      if (used[r] >> lane & 1) {
+        if (p >= M) o.src[rank - below] = p;
+        o.place[p] = p >= M ? below - rank - 1 : p;   // (below 0: where the list says, which may not be whole yet)
+      } else {
+        if (p < M) o.dst[p - rank] = p;
+        o.place[p] = p;
+      }
+    }
+    before += __popcll(used[r]);
   }
 }
+__global__ __launch_bounds__(PLAN) void compact_plan_kernel(const int32_t* __restrict__ refs, int P, const CompactPlan o) {
+  unsigned long long used[CHUNKS_AT_ONCE][COMPACT_RUNS];
+  int before[CHUNKS_AT_ONCE], M = 0;
+  const int wave = (int)(threadIdx.x >> 6);
+  Counts<COMPACT_RUNS> x[CHUNKS_AT_ONCE];
+#pragma unroll
+  for (int c = 0; c < CHUNKS_AT_ONCE; ++c) x[c] = counts_of<COMPACT_RUNS>(refs, (long long)c * CHUNK + wave * WAVE_PAGES, P);
+#pragma unroll
+  for (int c = 0; c < CHUNKS_AT_ONCE; ++c) {
+    int all;
+    before[c] = M + waves_before(used_in(x[c], used[c]), &all);
+    M += all;
+  }
+  int below = 0;   // pages in use below M
+#pragma unroll
+  for (int c = 0; c < CHUNKS_AT_ONCE; ++c)
+#pragma unroll
+    for (int r = 0; r < COMPACT_RUNS; ++r) {
+      const int left = M - (c * CHUNK + wave * WAVE_PAGES + r * 64);
+      below += left >= 64 ? __popcll(used[c][r]) : left > 0 ? __popcll(used[c][r] & ((1ull << left) - 1)) : 0;
+    }
+  int all;
+  waves_before(below, &all);
+  below = all;
+#pragma unroll
+  for (int c = 0; c < CHUNKS_AT_ONCE; ++c) plan_wave(o, used[c], c * CHUNK, P, M, before[c], below);
+  if (threadIdx.x == 0) {
+    *o.moved = M - below;
+    *o.in_use = M;
+  }
+}
+__global__ __launch_bounds__(PLAN) void compact_chunk_kernel(const int32_t* __restrict__ refs, int P, const int32_t* __restrict__ sums,
+                                                             int chunks, const CompactPlan o) {
+  const int chunk = blockIdx.x, wave = (int)(threadIdx.x >> 6);
+  const Counts<COMPACT_RUNS> x = counts_of<COMPACT_RUNS>(refs, (long long)chunk * CHUNK + wave * WAVE_PAGES, P);
+  int total = 0, ahead = 0, M, before;
+  for (int c = threadIdx.x; c < chunks; c += PLAN) {
+    const int y = sums[c];
+    total += y;
+    ahead += c < chunk ? y : 0;
+  }
+  sum_before(total, &M);
+  sum_before(ahead, &before);
+  // pages in use below M: of whole chunks, and of the one that M is in
+  const int last = M / CHUNK;
+  int below = 0, all;
+  for (int c = threadIdx.x; c < last; c += PLAN) below += sums[c];
+  for (int p = last * CHUNK + threadIdx.x; p < M; p += PLAN) below += refs[p] > 0;
+  sum_before(below, &all);
+  below = all;
+  unsigned long long used[COMPACT_RUNS];
+  before += waves_before(used_in(x, used), &all);
+  plan_wave(o, used, chunk * CHUNK, P, M, before, below);
+  if (chunk == 0 && threadIdx.x == 0) {
+    *o.moved = M - below;
+    *o.in_use = M;
+  }
+}
+// Where page p goes
+__device__ __forceinline__ int place_of_page(const int32_t* place, const int32_t* dst, int p) {
+  const int x = place[p];
+  return x < 0 ? dst[-1 - x] : x;
+}
+
 // Compact, the rest: the first `copies` workgroups copy pages, the others write tables and counts
 __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                       const int32_t* __restrict__ place, int32_t* __restrict__ pages_out,
@@ -273,7 +375,7 @@ __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int3
       int p = -1;
       if (j < used) {
         p = t.pages[(size_t)u * t.max_pages + j];
-        if ((unsigned)p < (unsigned)t.P) p = place[p];
+        if ((unsigned)p < (unsigned)t.P) p = place_of_page(place, dst, p);
       }
       pages_out[(size_t)u * t.max_pages + j] = p;
     }
@@ -282,7 +384,7 @@ __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int3
   const int M = *in_use;
   for (long long p = (long long)first * 256 + threadIdx.x; p < t.P; p += (long long)step * 256) {
     const int count = t.refs[p];
-    if (count > 0) refs_out[place[p]] = count;
+    if (count > 0) refs_out[place_of_page(place, dst, (int)p)] = count;
     if (p >= M) refs_out[p] = 0;
   }
 }
@@ -297,7 +399,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const int32_t* __restrict__ s
 }
 
 // ---------------------------------------------------------------- launchers
-size_t pages_work_ints(int U, int P) { return (size_t)U + 3 * (size_t)P + 16; }
+size_t pages_work_ints(int U, int P) { return (size_t)U + 3 * (size_t)P + (P + CHUNK - 1) / CHUNK + 16; }
 
 static Tables tables_of(const PagesArgs& a) { return Tables{a.pages, a.lens, a.refs, a.U, a.P, a.page_log2, a.max_pages}; }
 
@@ -321,9 +423,9 @@ static laser_status over_parts(const PagesArgs& a, long long entries, const int3
     Moves m{};
     m.parts = parts_of(a, i);
     m.count = count;
-    m.total = entries * m.parts.all;
-    const long long groups = (m.total + 255) / 256;
-    go(m, (unsigned)(groups < 4096 ? groups : 4096), i == 0);
+    m.by_all = mul_div(m.parts.all > 0 ? m.parts.all : 1);
+    const long long groups = (entries * m.parts.all + 255) / 256;
+    go(m, (unsigned)(groups < 16384 ? groups : 16384), i == 0);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
@@ -354,11 +456,19 @@ laser_status pages_free_launch(const PagesArgs& a) {
 }
 
 laser_status pages_compact_launch(const PagesArgs& a) {
-  int32_t *src = a.work, *dst = src + a.P, *place = dst + a.P, *moved = place + a.P;
+  int32_t *src = a.work, *dst = src + a.P, *place = dst + a.P, *moved = place + a.P, *sums = moved + 1;
+  const CompactPlan o{src, dst, place, moved, a.in_use};
   const Tables t = tables_of(a);
-  compact_plan_kernel<<<1, PLAN, 0, a.stream>>>(a.refs, a.P, src, dst, place, moved, a.in_use);
-  laser_status s = launch_status();
-  if (s != LASER_OK) return s;
+  const int chunks = (a.P + CHUNK - 1) / CHUNK;
+  laser_status s;
+  if (chunks <= CHUNKS_AT_ONCE) {
+    compact_plan_kernel<<<1, PLAN, 0, a.stream>>>(a.refs, a.P, o);
+  } else {
+    used_kernel<<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums);
+    if ((s = launch_status()) != LASER_OK) return s;
+    compact_chunk_kernel<<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums, chunks, o);
+  }
+  if ((s = launch_status()) != LASER_OK) return s;
   return over_parts(a, a.P / 2, moved, [&](const Moves& m, unsigned copies, bool first) {
     const unsigned more = first ? 1024 : 0;
     if (copies + more > 0)
