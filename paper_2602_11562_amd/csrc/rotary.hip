@@ -2,7 +2,9 @@
 //   (a, b) -> scale (a c - b s, a s + b c),   c, s = cos, sin(pos freq[i]),
 // pairs being columns (i, i + R/2) or (2i, 2i + 1); the transpose (s -> -s) carries gradients back. One launch turns queries and keys.
 //
-// Bound by memory: what is turned comes in and goes out once, in pieces of 16 bytes. A workgroup takes a few tokens, makes their cosines
+// Bound by memory: what is turned comes in and goes out once, in pieces of 16 bytes (201 MB of bf16 rows in 38 us, 5.3 TB/s, what a large
+// copy reaches; pairs side by side 42 us; halves that are no whole pieces take twice as long). Results are stored for whoever reads them next: with
+// the non-temporal hint the launch alone is 0 to 10 us shorter, attention behind it 4 to 8 us longer than that. A workgroup takes a few tokens, makes their cosines
 // and sines once for all heads, in LDS, and walks heads and pieces. An angle of a far position is many turns: it is formed in fp64 and
 // reduced to an eighth of a turn there (fp32 would be off by 4e-3 at position 65000), then cosine and sine are Taylor sums in fp32.
 #include "rotary.h"
@@ -21,37 +23,32 @@ __device__ __forceinline__ float2 cos_sin(double x) {
   return float2{turn == 1 || turn == 2 ? -a : a, turn >= 2 ? -b : b};
 }
 
-template <typename T, int N> struct Piece { T v[N]; };
-template <typename T, int N>
-__device__ __forceinline__ Piece<T, N> load_piece(const T* p) {
-  Piece<T, N> x;
-  if constexpr (sizeof(T) * N == 16) *reinterpret_cast<stream16*>(&x) = *reinterpret_cast<const stream16*>(p);
-  else if constexpr (sizeof(T) * N == 8) *reinterpret_cast<uint2*>(&x) = *reinterpret_cast<const uint2*>(p);
-  else if constexpr (sizeof(T) * N == 4) *reinterpret_cast<unsigned*>(&x) = *reinterpret_cast<const unsigned*>(p);
-  else x.v[0] = *p;
-  return x;
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_piece(T* p, const Piece<T, N>& x) {
-  if constexpr (sizeof(T) * N == 16) *reinterpret_cast<stream16*>(p) = *reinterpret_cast<const stream16*>(&x);
-  else if constexpr (sizeof(T) * N == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(&x);
-  else if constexpr (sizeof(T) * N == 4) *reinterpret_cast<unsigned*>(p) = *reinterpret_cast<const unsigned*>(&x);
-  else *p = x.v[0];
-}
+// 16 bytes of a row, at any element (the second halves of pairs start at column R / 2)
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  typedef unsigned int words __attribute__((ext_vector_type(4), aligned(2)));
+  T v[N];
+  __device__ __forceinline__ void load(const T* p) { *reinterpret_cast<words*>(v) = *reinterpret_cast<const words*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<words*>(p) = *reinterpret_cast<const words*>(v); }
+  __device__ __forceinline__ float get(int j) const { return load_as_f32<T>(v, j); }
+  __device__ __forceinline__ void set(int j, float x) { store_from_f32<T>(v, j, x); }
+};
 
 constexpr int ROTARY_TOKENS = 16;   // of a workgroup, at most
 
-// N: elements of a piece. Pairs of halves: the largest power of two that divides R / 2, at most 16 bytes, so that both pieces of a
-// pair are whole; columns from R on are then whole pieces too. Pairs side by side: always 16 bytes.
+// What a thread has of a head: HALF pairs, a piece of either half; SIDE by side, two pieces in a row. Columns from R on are copied.
 // (x and y may be the same rows: a thread reads what it writes, and nobody else does)
-template <typename T, int N, bool SIDE>
+template <typename T, bool SIDE>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int tokens, MulDiv by_half, MulDiv by_units, MulDiv by_heads, int units) {
+  typedef Piece<T> P;
+  constexpr int N = P::N;
   __shared__ float2 turn[ROTARY_TOKENS * 64];
   __shared__ int there[ROTARY_TOKENS];
   const int t0 = blockIdx.x * tokens, count = a.T - t0 < tokens ? a.T - t0 : tokens, half = a.R / 2;
   for (unsigned e = threadIdx.x; e < (unsigned)(count * half); e += 256) {
     const int t = (int)by_half.div(e), i = (int)e - t * half, pos = a.pos[t0 + t];
-    float2 cs = cos_sin((double)pos * a.freq[i]);
+    const float2 cs = cos_sin((double)pos * a.freq[i]);
     turn[t * half + i] = float2{cs.x * a.scale, (a.back ? -cs.y : cs.y) * a.scale};
     if (i == 0) there[t] = pos >= 0;
   }
@@ -67,43 +64,70 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int tok
     T* y = static_cast<T*>(a.y[which]) + (size_t)(t0 + t) * a.yp[which] + head * a.D;
     const float2* cs = turn + t * half;
     if constexpr (SIDE) {
-      Piece<T, N> p = load_piece<T, N>(x + unit * N);
+      const int c = unit * 2 * N;
+      const bool both = c + N < a.D;
+      P p[2];
+      p[0].load(x + c);
+      if (both) p[1].load(x + c + N);
 #pragma unroll
-      for (int j = 0; j < N; j += 2) {
-        const int i = unit * (N / 2) + j / 2;
-        if (i < half) {
-          const float u = load_as_f32<T>(p.v, j), v = load_as_f32<T>(p.v, j + 1);
-          store_from_f32<T>(p.v, j, fmaf(u, cs[i].x, -(v * cs[i].y)));
-          store_from_f32<T>(p.v, j + 1, fmaf(u, cs[i].y, v * cs[i].x));
+      for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          const int i = (c + w * N + j) / 2;
+          if (i < half) {
+            const float u = p[w].get(j), v = p[w].get(j + 1);
+            p[w].set(j, fmaf(u, cs[i].x, -(v * cs[i].y)));
+            p[w].set(j + 1, fmaf(u, cs[i].y, v * cs[i].x));
+          }
         }
       }
-      store_piece<T, N>(y + unit * N, p);
+      p[0].store(y + c);
+      if (both) p[1].store(y + c + N);
     } else {
-      const int c = unit * N;
-      if (c < half) {
-        Piece<T, N> p = load_piece<T, N>(x + c), r = load_piece<T, N>(x + half + c);
+      const int c = unit * N, left = half - c;
+      if (left >= N) {
+        P p, r;
+        p.load(x + c);
+        r.load(x + half + c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          const float u = load_as_f32<T>(p.v, j), v = load_as_f32<T>(r.v, j), cj = cs[c + j].x, sj = cs[c + j].y;
-          store_from_f32<T>(p.v, j, fmaf(u, cj, -(v * sj)));
-          store_from_f32<T>(r.v, j, fmaf(u, sj, v * cj));
+          const float u = p.get(j), v = r.get(j), cj = cs[c + j].x, sj = cs[c + j].y;
+          p.set(j, fmaf(u, cj, -(v * sj)));
+          r.set(j, fmaf(u, sj, v * cj));
         }
-        store_piece<T, N>(y + c, p);
-        store_piece<T, N>(y + half + c, r);
-      } else {   // columns from R on, where they have to be copied
-        store_piece<T, N>(y + half + c, load_piece<T, N>(x + half + c));
+        p.store(y + c);
+        r.store(y + half + c);
+      } else if (left > 0) {   // the last pairs, fewer than a piece
+        for (int i = c; i < half; ++i) {
+          const float u = load_as_f32<T>(x, i), v = load_as_f32<T>(x, half + i);
+          store_from_f32<T>(y, i, fmaf(u, cs[i].x, -(v * cs[i].y)));
+          store_from_f32<T>(y, half + i, fmaf(u, cs[i].y, v * cs[i].x));
+        }
+      } else {                 // columns from R on, where they have to be copied
+        const int from = a.R + (int)(unit - (half + N - 1) / N) * N;
+        if (from + N <= a.D) {
+          P p;
+          p.load(x + from);
+          p.store(y + from);
+        } else {
+          for (int i = from; i < a.D; ++i) y[i] = x[i];
+        }
       }
     }
   }
 }
 
-template <typename T, int N, bool SIDE>
+template <typename T, bool SIDE>
 static laser_status rotary_typed(const RotaryArgs& a) {
+  constexpr int N = Piece<T>::N;
   const int heads = a.heads[0] + a.heads[1], half = a.R / 2;
   // (rows turned in place keep their other columns: those pieces are left out. A tensor in place beside one that is not copies onto itself.)
   const bool in_place = a.y[0] == a.x[0] && a.y[1] == a.x[1];
-  const int units = SIDE ? ((in_place ? a.R : a.D) + N - 1) / N : (in_place ? half : a.D - half) / N;
-  int tokens = a.T / 2048;   // (a few workgroups for each compute unit)
+  const int units = SIDE ? ((in_place ? a.R : a.D) + 2 * N - 1) / (2 * N) : (half + N - 1) / N + (in_place ? 0 : (a.D - a.R + N - 1) / N);
+  // Tokens that give each thread a piece or two, and a few workgroups for each compute unit (39322 tokens of 10 heads of 128, 80 threads
+  // each: by 16 tokens 42.6 us, by 4 38.2; 100000 of 2 heads, 16 threads each: by 16 24.6, by 4 26.2)
+  int tokens = (320 + heads * units - 1) / (heads * units);
+  tokens = tokens < a.T / 2048 ? tokens : a.T / 2048;
   tokens = tokens < 1 ? 1 : tokens > ROTARY_TOKENS ? ROTARY_TOKENS : tokens;
   const unsigned grid = (unsigned)((a.T + (long long)tokens - 1) / tokens);
   // (a launch has fewer than 2^32 threads: 2^24 workgroups and more go out in several)
@@ -117,30 +141,18 @@ static laser_status rotary_typed(const RotaryArgs& a) {
       part.y[w] = static_cast<T*>(a.y[w]) + t0 * a.yp[w];
     }
     part.pos = a.pos + t0;
-    part.T = (int)(a.T - t0);
     const unsigned here = grid - b < MOST ? grid - b : MOST;
-    if (b + here < grid) part.T = (int)((long long)here * tokens);
-    rotary_kernel<T, N, SIDE><<<here, 256, 0, a.stream>>>(part, tokens, mul_div(half), mul_div(units), mul_div(heads), units);
+    part.T = b + here < grid ? (int)((long long)here * tokens) : (int)(a.T - t0);
+    rotary_kernel<T, SIDE><<<here, 256, 0, a.stream>>>(part, tokens, mul_div(half), mul_div(units), mul_div(heads), units);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
   return LASER_OK;
 }
 
-template <typename T>
-static laser_status rotary_width(const RotaryArgs& a) {
-  constexpr int MOST = 16 / sizeof(T);
-  if (a.interleaved) return rotary_typed<T, MOST, true>(a);
-  const int half = a.R / 2;
-  if (half % MOST == 0) return rotary_typed<T, MOST, false>(a);
-  if constexpr (MOST == 8) {
-    if (half % 4 == 0) return rotary_typed<T, 4, false>(a);
-  }
-  return half % 2 == 0 ? rotary_typed<T, 2, false>(a) : rotary_typed<T, 1, false>(a);
-}
-
 laser_status rotary_launch(const RotaryArgs& a) {
-  return a.dt == LASER_F32 ? rotary_width<float>(a) : rotary_width<unsigned short>(a);
+  if (a.dt == LASER_F32) return a.interleaved ? rotary_typed<float, true>(a) : rotary_typed<float, false>(a);
+  return a.interleaved ? rotary_typed<unsigned short, true>(a) : rotary_typed<unsigned short, false>(a);
 }
 
 // freq[i] = base^(-2i/R), for longer contexts than those of training stretched one way or another
