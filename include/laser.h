@@ -624,7 +624,7 @@ laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const voi
  *   written. A page must not be listed twice, by one user or two, where new rows go.
  * laser_cache8_attention_forward: as laser_cache_attention_forward over the items' values (number times scale). bf16 rows:
  *   probabilities are rounded to bf16 ahead of their product with the values, o is rounded once; fp32 rows: every product and sum is of
- *   fp32's precision. work: laser_cache8_attention_work_bytes() bytes.
+ *   fp32's precision. A row whose query is NaN is NaN. work: laser_cache8_attention_work_bytes() bytes.
  * Results are the same from run to run. Everything else, alignment (4 bytes for scales) and errors as for the cache above.
  */
 laser_status laser_cache8_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,

@@ -16,11 +16,12 @@ struct Cache8Args {
   long long kp, vp;
 };
 laser_status cache8_append_launch(const Cache8Args& a);
-CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, laser_dtype dt);
+CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 int cache8_waves(int U, int Hkv, const CacheRuns& r);    // of a workgroup of the kernel for few rows
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status cache8_attention_launch(const Cache8Args& a);
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r);    // at most 32 rows a key-value head
+constexpr int CACHE8_RANKED = 64;                        // so many users the tiles of rows come by their lengths, a lane for each
 laser_status cache8_tile_launch(const Cache8Args& a, const CacheRuns& r);
 
 constexpr float E4M3_MAX = 448.0f;                       // 1.75 * 2^8

@@ -181,8 +181,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
       sum = fmaf(join_l[w][r], c, sum);
       x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 32 + (r ^ (d & 31))], c, x);
     }
-    x = sum > 0.0f ? x / sum : 0.0f;
-    const float z = sum > 0.0f ? top + log2f(sum) : -INFINITY;
+    x = sum == 0.0f ? 0.0f : x / sum;
+    const float z = log_sum(top, sum, !final);
     const int i = (int)by_group.div(r), g = r - i * G;
     const size_t row = (size_t)(cr.first + i) * a.H + hk * G + g;
     if (final) {

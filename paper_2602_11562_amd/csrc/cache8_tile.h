@@ -147,6 +147,12 @@ __device__ __forceinline__ void split_pair(float a, float b, int r, bf16x8 (*p)[
   }
 }
 
+// A row's sum in units of 2^m, as the logarithm to 2: nothing seen -inf; a sum that is NaN stays that, and is +inf in a part of a row, of which
+// the join makes NaN whatever the other parts hold
+__device__ __forceinline__ float log_sum(float m, float sum, bool in_part) {
+  return sum == 0.0f ? -INFINITY : sum != sum && in_part ? INFINITY : m + log2f(sum);
+}
+
 // Where the maximum of a row is raised: probabilities may stand up to 2^8 above it meanwhile, sums and outputs are in its units
 constexpr float MAX_SLACK = 8.0f;
 

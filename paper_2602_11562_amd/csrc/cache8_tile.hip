@@ -1,6 +1,10 @@
 // Many rows over a cache of 8-bit blocks: chunks of new items, and candidates. The split of history_mfma.hip: a workgroup of four waves
 // owns 128 rows of a key-value head and walks the items that the last of them sees in tiles of 64, which come by direct loads to LDS as
-// the bytes that they are; a wave owns 32 rows and makes its operands of the bytes in registers.
+// the bytes that they are; a wave owns 32 rows and makes its operands of the bytes in registers. (Scores of bf16 queries, as two numbers of
+// 8 bits each, straight from the bytes by the products of 8-bit operands: 215 us would be 202 for 512 new items x up to 10000, but those products
+// sum in fewer than 32 bits: errors of lse 4e-6 against 4e-7.)
+// Bound by the vector units beside the products: an exponential, a product and a sum for a score of one, and the values' bytes. Ragged
+// histories leave a part of the chip without work behind the others' end, hence the order below.
 #include "cache8_tile.h"
 
 namespace laser {
@@ -14,7 +18,77 @@ struct Tile8Args {
   Deal deal;             // of (tile, run) to workgroups
   float scale;           // log2(e) / gamma
   int chunk, runs;       // items a workgroup walks, and into how many such runs the longest history is cut
+  bool ranked;           // workgroups by what they have to do, the most first
 };
+
+// Which tile of rows of which user and head, and which run of its items, a workgroup has
+struct Part8 { int user, head, tile, run, first, count, n; };   // (and the user's rows and items)
+__device__ __forceinline__ bool part_in_turn(const Tile8Args& t, Part8* p) {
+  const Place place = place_of(t.deal, blockIdx.x);
+  if (place.rank >= t.deal.tiles) return false;
+  p->run = t.runs > 1 ? place.rank / t.tiles : 0;
+  p->tile = t.tiles - 1 - (place.rank - p->run * t.tiles);   // (the longest first)
+  p->user = place.pair / t.Hkv;
+  p->head = place.pair - p->user * t.Hkv;
+  const CandRange cr = cand_range(t.off, p->user, t.a.c.C, t.a.c.T);
+  p->first = cr.first;
+  p->count = cr.count;
+  if (p->tile * 128 >= cr.count * t.G) return false;
+  p->n = cache_len(t.a.c.lens, p->user, t.a.c.L, t.a.c.max_pages, t.a.c.page_log2);
+  return true;
+}
+// At most 64 users, a lane for each: the whole runs of all of them come first, then what is left of each, the longest first, since workgroups
+// are started in the order of their numbers. Against the order of users (us, with the join): 512 new items x up to 10000, 16 users of 128 252
+// and 207; 256 rows x up to 4096, 32 of 64 79.9 and 67.7; 128 x up to 4096, 64 of 128 133 and 110; equal lengths 386 and 395; 1000 x up to
+// 1500, 50 of 128 (3200 workgroups, four or more for each place, which even out by themselves) 130 and 134.
+// Workgroups of whole runs go to the eighths of the chip, each with an L2 cache of its own, in even parts, so that the tiles of a run meet
+// there (against the plain order 208 and 207, 130 and 125 for 400 x 9000, 12 of 128).
+__device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Part8* p) {
+  const CacheArgs& a = t.a.c;
+  const int u = lane < t.N ? lane : t.N - 1;
+  const CandRange cr = cand_range(t.off, u, a.C, a.T);
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2), tiles = lane < t.N ? (cr.count * t.G + 127) / 128 : 0;
+  const int whole = t.runs > 1 ? n / t.chunk : 0, rest = n - whole * t.chunk;
+  int at = blockIdx.x, behind = whole * tiles * t.Hkv;   // the workgroups of whole runs up to this user's last
+  const int mine = behind;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int other = __shfl_up(behind, d);
+    behind += lane >= d ? other : 0;
+  }
+  const int all = __builtin_amdgcn_readlane(behind, 63);
+  int first, last_run = 0;
+  unsigned long long found;
+  if (at < all) {
+    const int eighth = all >> 3;
+    if (at < eighth * 8) at = (at & 7) * eighth + (at >> 3);
+    first = behind - mine;
+    found = __ballot(at >= first && at < behind);
+  } else {
+    at -= all;
+    const int w = rest > 0 || n == 0 ? tiles * t.Hkv : 0;
+    first = 0;
+    for (int v = 0; v < t.N; ++v) {
+      const int r = __builtin_amdgcn_readlane(rest, v), x = __builtin_amdgcn_readlane(w, v);
+      first += r > rest || (r == rest && v < lane) ? x : 0;
+    }
+    found = __ballot(at >= first && at < first + w);
+    last_run = 1;
+  }
+  if (found == 0) return false;
+  const int who = __builtin_ctzll(found), count = __builtin_amdgcn_readlane(tiles, who);
+  at -= __builtin_amdgcn_readlane(first, who);
+  p->user = who;
+  const int pair = at / count;
+  p->tile = count - 1 - (at - pair * count);   // (the longest first)
+  const int run = pair / t.Hkv;
+  p->head = pair - run * t.Hkv;
+  p->run = last_run ? __builtin_amdgcn_readlane(whole, who) : run;
+  p->first = __builtin_amdgcn_readlane(cr.first, who);
+  p->count = __builtin_amdgcn_readlane(cr.count, who);
+  p->n = __builtin_amdgcn_readlane(n, who);
+  return true;
+}
 
 template <int DP, int SLOTS, int NP, typename T>
 __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) {
@@ -25,25 +99,15 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   const CacheArgs& a = t.a.c;
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[0][0]);
-  const Place place = place_of(t.deal, blockIdx.x);
-  if (place.rank >= t.deal.tiles) return;
-  int tile = place.rank, run = 0;
-  if (t.runs > 1) {
-    run = tile / t.tiles;
-    tile -= run * t.tiles;
-  }
-  tile = t.tiles - 1 - tile;   // (the longest first)
-  const int u_seq = place.pair / t.Hkv, hk = place.pair - u_seq * t.Hkv;
-  const CandRange cr = cand_range(t.off, u_seq, a.C, a.T);
-  const int rows = cr.count * t.G, row0 = tile * ROWS;
-  if (row0 >= rows) return;
-  const int n = cache_len(a.lens, u_seq, a.L, a.max_pages, a.page_log2);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  Part8 part;
+  if (!(t.ranked ? part_by_length(t, lane, &part) : part_in_turn(t, &part))) return;
+  const int u_seq = part.user, hk = part.head, run = part.run, n = part.n, rows = part.count * t.G, row0 = part.tile * ROWS;
 
   int end;   // one past the last item that a row of this workgroup sees
   {
     const int r = row0 + ROWS < rows ? row0 + ROWS - 1 : rows - 1;
-    end = a.causal ? n - cr.count + (int)t.by_group.div(r) + 1 : n;
+    end = a.causal ? n - part.count + (int)t.by_group.div(r) + 1 : n;
   }
   const bool joined = t.runs > 1 && n > t.chunk;   // others write their part of the result too
   int begin = 0;
@@ -79,8 +143,8 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
     int r = first + l32;
     r = r < rows ? r : rows - 1;
     const int i = (int)t.by_group.div(r), g = r - i * t.G;
-    last = a.causal ? n - cr.count + i : n - 1;
-    load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(cr.first + i) * a.qp + (size_t)(hk * t.G + g) * a.D, a.D, h, qreg);
+    last = a.causal ? n - part.count + i : n - 1;
+    load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(part.first + i) * a.qp + (size_t)(hk * t.G + g) * a.D, a.D, h, qreg);
   }
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
   bool whole_pages;
@@ -177,13 +241,13 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   }
   barrier_lds();
 
-  const float sum = half_sum(l), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const float sum = half_sum(l), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int r = first + l32;
   typedef float f32x4 __attribute__((ext_vector_type(4)));
   if (joined || !PATCHED) {
     if (r >= rows) return;
     const int i = (int)t.by_group.div(r), g = r - i * t.G;
-    const size_t all = (size_t)a.T * a.H, row = (size_t)(cr.first + i) * a.H + hk * t.G + g;
+    const size_t all = (size_t)a.T * a.H, row = (size_t)(part.first + i) * a.H + hk * t.G + g;
     float* to = joined ? a.work + (run * all + row) * a.D : static_cast<float*>(a.o) + row * a.D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -193,18 +257,18 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
         if (c < a.D) *reinterpret_cast<f32x4*>(to + c) = f32x4{acc[db][x * 4] * inv, acc[db][x * 4 + 1] * inv, acc[db][x * 4 + 2] * inv,
                                                                acc[db][x * 4 + 3] * inv};
       }
-    const float z = sum > 0.0f ? m + log2f(sum) : -INFINITY;
+    const float z = log_sum(m, sum, joined);
     if (h == 0 && joined) a.work[t.runs * all * a.D + run * all + row] = z;
     if (h == 0 && !joined && a.lse != nullptr) a.lse[row] = z * LN2;
     return;
   }
   if (a.lse != nullptr && h == 0 && r < rows) {
     const int i = (int)t.by_group.div(r), g = r - i * t.G;
-    a.lse[(size_t)(cr.first + i) * a.H + hk * t.G + g] = sum > 0.0f ? (m + log2f(sum)) * LN2 : -INFINITY;
+    a.lse[(size_t)(part.first + i) * a.H + hk * t.G + g] = log_sum(m, sum, false) * LN2;
   }
   store_block<DP>(acc, inv, smem + wave * 32 * OP, rows - first, a.D, lane, [&](int r) {
     const int i = (int)t.by_group.div(first + r), g = first + r - i * t.G;
-    return static_cast<unsigned short*>(a.o) + ((size_t)(cr.first + i) * a.H + hk * t.G + g) * a.D;
+    return static_cast<unsigned short*>(a.o) + ((size_t)(part.first + i) * a.H + hk * t.G + g) * a.D;
   });
 }
 
@@ -212,6 +276,12 @@ template <int DP, int SLOTS, int NP, typename T>
 static laser_status tile8_typed(Tile8Args t) {
   const CacheArgs& c = t.a.c;
   t.tiles = (int)(((long long)c.C * t.G + 127) / 128);
+  const long long most = (long long)t.N * t.Hkv * t.tiles * t.runs;
+  t.ranked = t.N <= CACHE8_RANKED && most <= 2560;   // (ten a compute unit)
+  if (t.ranked) {
+    cache8_tile_kernel<DP, SLOTS, NP, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
+    return launch_status();
+  }
   return launch_dealt(t, (long long)t.tiles * t.runs, 256, [&](Tile8Args& part, long long n) {
     part.a.c.pages += n * c.max_pages;
     part.a.c.lens += n;

@@ -288,13 +288,13 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a, int 
       *reinterpret_cast<f32x4*>(part + (group * pieces + piece) * 4) = o;
     }
     __syncthreads();
-    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
     for (int d = tid; d < a.D; d += NT) {
       float y = 0.0f;
       for (int g = 0; g < groups; ++g) y += part[g * a.D + d];
       store_from_f32<T>(static_cast<T*>(a.o), row * a.D + d, y * by);
     }
-    if (tid == 0 && a.lse != nullptr) a.lse[row] = sum > 0.0f ? (top + log2f(sum)) * LN2 : -INFINITY;
+    if (tid == 0 && a.lse != nullptr) a.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
     __syncthreads();
   }
 }
@@ -343,13 +343,13 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(const CacheArgs a, 
       for (int d = 0; d < 4; ++d) o[d] = fmaf(c, y[s][d], o[d]);
     }
   }
-  const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + row * a.D + piece * 4) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
   } else {
     *reinterpret_cast<u32x2*>(static_cast<unsigned short*>(a.o) + row * a.D + piece * 4) = u32x2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
   }
-  if (piece == 0 && a.lse != nullptr) a.lse[row] = sum > 0.0f ? (top + log2f(sum)) * LN2 : -INFINITY;
+  if (piece == 0 && a.lse != nullptr) a.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
 laser_status cache_join_launch(const CacheArgs& a, int chunk, int splits) {

@@ -44,16 +44,22 @@ static laser_status validate_cache8(const void* k_cache, const void* v_cache, co
 
 // Rows of a key-value head that one column block holds: the streaming kernel
 static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <= 32; }
-// Into how many runs. A cut costs a join, 4 to 6 us, and what its parts weigh. Many rows: as in history_api.hip. Few rows, us by one run a
-// history, runs of 1024 items and runs of 512 (heads of 128 over 2 key-value heads unless said otherwise):
+// Into how many runs. A cut costs a join, 4 to 6 us, and what its parts weigh.
+// Many rows: two workgroups for each place that the chip has for them (three a compute unit of heads of 128, four of 64), which come by their
+// lengths (us by 1024, 1536 and 2048 wanted; 8 heads over 2, rows x longest history, users: 512 x 10000, 16 of 128 211, 191, 200; 400 x 9000, 12
+// of 128 112, 118, 123; 200 x 20000, 8 of 128 98, 96, 112; 256 x 4096, 32 of 64 71.5, 70.8, 67.7; more users, in their own order: 64 x 4096, 100
+// of 128 -, 116, 111), of 512 items or more, of 256 where the longest history has few runs anyway and for fp32 (us by 256 and 512: 100 x
+// 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1).
+// Few rows, us by one run a history, runs of 1024 items and runs of 512 (heads of 128 over 2 key-value heads unless said otherwise):
 //   1 x 65000, 16 heads (2 pairs)  -, 20.0, 18.6;  8 x 20000 (16)  -, 20.5, 26.3;  40 x 3000 fp32 (80)  28, 23.6, 31.8;  5 x 777 fp32 (10)  14.5, -, 16.8;
 //   32 x 1000, 8 over 8 of 64 (256)  14.0, -, 18.5;  128 x 970 of up to 4096 (256)  35.6 (two of 2048), 27.0, 29.3;  200 x 5000, 4 over 1 of 64 (200)
 //   33.5 (two), 30.8, 34.0;  256 x 1200 of up to 2000, four rows (512)  38.0, 47.8, 55.7
 // Rules: none where the histories alone are two workgroups a compute unit, or short; else runs of 512 while they are one workgroup a
 // compute unit, and of 1024 beyond.
-CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, laser_dtype) {
+CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
-  if (!few8_rows(C, H, Hkv)) return cache_runs((rows + 127) / 128 * pairs, L, 2048, 256, 64);
+  if (!few8_rows(C, H, Hkv))
+    return cache_runs((rows + 127) / 128 * pairs, L, D > 64 && U <= CACHE8_RANKED ? 1536 : 2048, L > 2048 && dt != LASER_F32 ? 512 : 256, 64);
   if (pairs >= 512 || L <= 1024) return CacheRuns{(L + 255) / 256 * 256, 1};
   return cache_runs(pairs, L, 1024, pairs * ((L + 511) / 512) <= 256 ? 512 : 1024, 256);
 }
@@ -62,11 +68,11 @@ CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, laser_dtype) {
 // 27.0 and 31.9, 256 x 1200 38.0 and 42.6).
 int cache8_waves(int U, int Hkv, const CacheRuns& r) { return (long long)U * Hkv * r.runs <= 320 ? 8 : 4; }
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
-  const CacheRuns r = cache8_runs_of(U, C, L, H, Hkv, dt);
+  const CacheRuns r = cache8_runs_of(U, C, L, H, Hkv, D, dt);
   return r.runs > 1 ? (size_t)r.runs * T * H * (D + 1) * 4 : 16;
 }
 laser_status cache8_attention_launch(const Cache8Args& a) {
-  const CacheRuns r = cache8_runs_of(a.c.U, a.c.C, a.c.L, a.c.H, a.c.Hkv, a.c.dt);
+  const CacheRuns r = cache8_runs_of(a.c.U, a.c.C, a.c.L, a.c.H, a.c.Hkv, a.c.D, a.c.dt);
   return few8_rows(a.c.C, a.c.H, a.c.Hkv) ? cache8_few_launch(a, r) : cache8_tile_launch(a, r);
 }
 
