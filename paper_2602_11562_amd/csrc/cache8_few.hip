@@ -17,7 +17,7 @@ struct Few8Shape {
   static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
 };
 
-template <int DP, int NP, int NW, typename T>
+template <int DP, int NP, int NW, int PART, typename T>
 __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
   using Sh = Few8Shape<DP>;
   constexpr int KS = DP / 16, DB = DP / 32;
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
   const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[wave][0][0]);
   const int32_t* table = a.pages + (size_t)u * a.max_pages;
 
-  Tiles8<DP, 32> tiles;
+  Tiles8<DP, 32, PART> tiles;
   tiles.init(a.D, a.page_log2, 0, lane);
   const int step_items = NW * 32, requests = tiles.requests();
   int ask = lo + wave * 32, mine = ask;
@@ -209,7 +209,10 @@ static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
     part.c.off = c.off + u;
     part.c.pages = c.pages + u * c.max_pages;
     part.c.lens = c.lens + u;
-    cache8_few_kernel<DP, NP, NW, T><<<(unsigned)(part.c.U * each), 64 * NW, 0, c.stream>>>(part, G, mul_div(G), LOG2E / c.gamma, r.chunk, r.runs);
+    const unsigned grid = (unsigned)(part.c.U * each);
+    const MulDiv by_group = mul_div(G);
+    if (c.page_log2 >= 4) cache8_few_kernel<DP, NP, NW, 16, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
+    else cache8_few_kernel<DP, NP, NW, 8, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }

@@ -37,57 +37,72 @@ __device__ __forceinline__ void wait_requests(int n) {
   }
 }
 
-// What a wave brings of a tile: ROWS rows of keys and of values and their scales
-template <int DP, int ROWS>
+// What a wave brings of a tile: ROWS rows of keys and of values and their scales. Pages hold PART items or more each (8 or 16), which then
+// share where they come from: a lone wave issues an instruction every 5 to 9 cycles, and those for the addresses of 32 rows were as many
+// as for their products.
+template <int DP, int ROWS, int PART>
 struct Tiles8 {
-  static constexpr int CH = DP / 16, RPI = 64 / CH < ROWS ? 64 / CH : ROWS, REQ = ROWS / RPI, IDS = ROWS / 8;
+  static constexpr int CH = DP / 16, RPI = 64 / CH < ROWS ? 64 / CH : ROWS, REQ = ROWS / RPI, IDS = ROWS / PART, EACH = PART / RPI;
   unsigned off[REQ];
-  int ids[IDS];            // pages of the next rows: of their items 0, 8, ..
+  int ids[IDS];            // pages of the next rows: of their items 0, PART, ..
   int part;                // rows of a request that are on one page
   __device__ __forceinline__ void init(int D, int page_log2, int row0, int lane) {
     part = (1 << page_log2) < RPI ? 1 << page_log2 : RPI;
 #pragma unroll
     for (int x = 0; x < REQ; ++x) {
       const int in = lane / CH, c = (lane % CH) ^ swz8<CH>(row0 + x * RPI + in);
-      off[x] = c * 16 < D && in < RPI ? (unsigned)(in * D + c * 16) : NO_COLUMN;
+      off[x] = c * 16 < D && in < RPI ? (unsigned)(((EACH > 1 ? x % EACH * RPI : 0) + in) * D + c * 16) : NO_COLUMN;
     }
   }
   __device__ __forceinline__ int requests() const { return 2 * REQ * (RPI / part) + 1; }
   __device__ __forceinline__ void look_up(const int32_t* table, int j, int end, int page_log2) {
 #pragma unroll
-    for (int x = 0; x < IDS; ++x) ids[x] = j + x * 8 < end ? scalar_int(table, (j + x * 8) >> page_log2) : -1;
+    for (int x = 0; x < IDS; ++x) ids[x] = j + x * PART < end ? scalar_int(table, (j + x * PART) >> page_log2) : -1;
   }
   // items j and on (behind `end` there are none: zeros); keys to k_at, values to v_at, scales to s_at
   __device__ __forceinline__ void fetch(const Cache8Args& a, int hk, int j, int end, unsigned k_at, unsigned v_at, unsigned s_at, int lane) const {
     const CacheArgs& c = a.c;
     const int mask = (1 << c.page_log2) - 1;
-#pragma unroll
-    for (int x = 0; x < REQ; ++x) {
-      auto rows = [&](int id, int skip, int count) __attribute__((always_inline)) {
-        const int at = j + x * RPI + skip, left = end - at < count ? end - at : count;
-        const bool ok = left > 0 && (unsigned)id < (unsigned)c.P;
-        const long long row = ok ? (((long long)id * c.Hkv + hk) << c.page_log2) + (at & mask) - skip : 0;
-        const unsigned bytes = ok ? (unsigned)((skip + left) * c.D) : 0u;
-        buffer_to_lds16(buffer_of(static_cast<const unsigned char*>(c.k) + row * c.D, bytes), off[x], k_at + x * 1024);
-        buffer_to_lds16(buffer_of(static_cast<const unsigned char*>(c.v) + row * c.D, bytes), off[x], v_at + x * 1024);
+    // items at .. at + count - 1, on page id, for a request's rows skip and on
+    auto rows = [&](int id, int at, int skip, int count, auto&& to) __attribute__((always_inline)) {
+      const int left = end - at < count ? end - at : count;
+      const bool ok = left > 0 && (unsigned)id < (unsigned)c.P;
+      const long long row = ok ? (((long long)id * c.Hkv + hk) << c.page_log2) + (at & mask) - skip : 0;
+      const unsigned bytes = ok ? (unsigned)((skip + left) * c.D) : 0u;
+      to(buffer_of(static_cast<const unsigned char*>(c.k) + row * c.D, bytes), buffer_of(static_cast<const unsigned char*>(c.v) + row * c.D, bytes));
+    };
+    auto ask = [&](int x) __attribute__((always_inline)) {
+      return [&, x](u32x4 k, u32x4 v) __attribute__((always_inline)) {
+        buffer_to_lds16(k, off[x], k_at + x * 1024);
+        buffer_to_lds16(v, off[x], v_at + x * 1024);
       };
-      if constexpr (RPI == 8) {
-        rows(ids[x], 0, 8);
-      } else {
+    };
+    if constexpr (EACH >= 1) {
+#pragma unroll
+      for (int p = 0; p < IDS; ++p)
+        rows(ids[p], j + p * PART, 0, PART, [&](u32x4 k, u32x4 v) __attribute__((always_inline)) {
+#pragma unroll
+          for (int x = p * EACH; x < (p + 1) * EACH; ++x)
+            if (RPI * CH == 64 || lane < RPI * CH) ask(x)(k, v);
+        });
+    } else {
+#pragma unroll
+      for (int x = 0; x < REQ; ++x) {
         if (part == RPI) {
-          if (RPI * CH == 64 || lane < RPI * CH) rows(ids[x * RPI / 8], 0, RPI);
+          if (RPI * CH == 64 || lane < RPI * CH) rows(ids[x * RPI / PART], j + x * RPI, 0, RPI, ask(x));
         } else {   // several pages a request: the lanes of each from its own
 #pragma unroll
-          for (int p = 0; p < RPI / 8; ++p)
-            if (p * 8 % part == 0 && (lane / CH) / part == p * 8 / part) rows(ids[x * RPI / 8 + p], p * 8, part);
+          for (int p = 0; p < RPI / PART; ++p)
+            if (p * PART % part == 0 && (lane / CH) / part == p * PART / part)
+              rows(ids[x * RPI / PART + p], j + x * RPI + p * PART, p * PART, part, ask(x));
         }
       }
     }
-    if (lane < 2 * IDS) {
+    if (lane < ROWS / 4) {
       const int g = (lane >> 2) * 2 + (lane & 1);
       int id = ids[0];
 #pragma unroll
-      for (int x = 1; x < IDS; ++x) id = g == x ? ids[x] : id;
+      for (int x = 1; x < IDS; ++x) id = g >= x * PART / 8 ? ids[x] : id;
       const bool ok = (unsigned)id < (unsigned)c.P;
       const long long s = ok ? (((long long)id * c.Hkv + hk) << (c.page_log2 - a.block_log2)) + (((j + g * 8) & mask) >> a.block_log2) : 0;
       global_to_lds4((lane & 2 ? a.v_scale : a.k_scale) + s, s_at);

@@ -90,7 +90,7 @@ __device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Par
   return true;
 }
 
-template <int DP, int SLOTS, int NP, typename T>
+template <int DP, int SLOTS, int NP, int PART, typename T>
 __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) {
   constexpr int KS = DP / 16, DB = DP / 32, NW = 4, ROWS = NW * 32, KB = TI * DP, SLOT = 2 * KB, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
   constexpr bool PATCHED = sizeof(T) == 2;   // (fp32 rows leave from the registers)
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   const int turns = end > begin ? (end - begin + TI - 1) / TI : 0;
   const int32_t* table = a.pages + (size_t)u_seq * a.max_pages;
 
-  Tiles8<DP, 16> tiles;
+  Tiles8<DP, 16, PART> tiles;
   tiles.init(a.D, a.page_log2, wave * 16, lane);
   const int requests = tiles.requests();
   int asked = 0, in = 0;
@@ -279,13 +279,15 @@ static laser_status tile8_typed(Tile8Args t) {
   const long long most = (long long)t.N * t.Hkv * t.tiles * t.runs;
   t.ranked = t.N <= CACHE8_RANKED && most <= 2560;   // (ten a compute unit)
   if (t.ranked) {
-    cache8_tile_kernel<DP, SLOTS, NP, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
+    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
+    else cache8_tile_kernel<DP, SLOTS, NP, 8, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
     return launch_status();
   }
   return launch_dealt(t, (long long)t.tiles * t.runs, 256, [&](Tile8Args& part, long long n) {
     part.a.c.pages += n * c.max_pages;
     part.a.c.lens += n;
-    cache8_tile_kernel<DP, SLOTS, NP, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
+    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
+    else cache8_tile_kernel<DP, SLOTS, NP, 8, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
   });
 }
 template <int NP, typename T>
