@@ -10,98 +10,40 @@
 
 namespace laser {
 
-template <int DP>
-struct Few8Shape {
-  static constexpr int TILE = 32 * DP, STAGE = 2 * TILE, NST = 2, WAVE = NST * STAGE;
-  static constexpr int JOIN = DP * 32 * 4;   // [column][32 rows] of fp32, row r at r ^ column % 32
-  static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
-};
-
-template <int DP, int NP, int NW, int PART, typename T>
-__global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
-  using Sh = Few8Shape<DP>;
-  constexpr int KS = DP / 16, DB = DP / 32;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * Sh::WAVE];
-  __shared__ __attribute__((aligned(16))) float scales[NW][Sh::NST][8];
-  __shared__ float join_m[NW][32], join_l[NW][32];
-  const CacheArgs& a = a8.c;
-  const int per = a.U * a.Hkv;
-  // (turned by one from run to run: a user's runs are not all one die's)
-  const int split = blockIdx.x / per, uh = (blockIdx.x + split) % per, u = uh / a.Hkv, hk = uh % a.Hkv;
-  const CandRange cr = cand_range(a.off, u, a.C, a.T);
-  const int rows = cr.count * G;
-  if (rows == 0) return;
-  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
-  const int lo = split * chunk, hi = n < lo + chunk ? n : lo + chunk;
-  if (lo >= n && split > 0) return;   // (the first run of an empty history still writes)
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
-  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem) + wave * Sh::WAVE;
-  const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[wave][0][0]);
-  const int32_t* table = a.pages + (size_t)u * a.max_pages;
-
-  Tiles8<DP, 32, PART> tiles;
-  tiles.init(a.D, a.page_log2, 0, lane);
-  const int step_items = NW * 32, requests = tiles.requests();
-  int ask = lo + wave * 32, mine = ask;
-  int pending = 0, slot_in = 0, slot_out = 0;
-  tiles.look_up(table, ask, hi, a.page_log2);
-  auto request = [&]() __attribute__((always_inline)) {
-    const unsigned at = lds + slot_in * Sh::STAGE;
-    tiles.fetch(a8, hk, ask, hi, at, at + Sh::TILE, lds_s + slot_in * 32, lane);
-    slot_in = slot_in + 1 == Sh::NST ? 0 : slot_in + 1;
-    ask += step_items;
-    ++pending;
-    tiles.look_up(table, ask, hi, a.page_log2);
-  };
-
-  bf16x8 qreg[NP][KS];
-  int last;
-  {
-    const int r = l32 < rows ? l32 : rows - 1, i = (int)by_group.div(r), g = r - i * G;
-    last = a.causal ? n - cr.count + i : n - 1;
-    load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(cr.first + i) * a.qp + (size_t)(hk * G + g) * a.D, a.D, h, qreg);
-  }
-  const int first_seen = __builtin_amdgcn_readlane(last, 0);
-  bool whole_pages;
-  {
-    bool bad = false;
-    for (int x = (lo >> a.page_log2) + lane; x <= (hi - 1) >> a.page_log2 && lo < hi; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
-    whole_pages = __ballot(bad) == 0;
-  }
-  for (int x = 0; x < Sh::NST && ask < hi; ++x) request();
-
-  const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+// A tile's products, and the state of a wave's rows: a lane holds a row's scores of 16 of the tile's items.
+template <int DP, int NP>
+struct Rows32 {
+  static constexpr int ROWS = 32, KS = DP / 16, DB = DP / 32;
+  static constexpr bool OCTETS = false;
+  const TileReader8<DP> read;
+  bf16x8 q[NP][KS];
   f32x16 acc[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) acc[db] = zero;
   float m = -INFINITY, l = 0.0f;
-  const TileReader8<DP> read(lane);
-
-  for (; mine < hi; mine += step_items) {
-    // loads return in order: with a second tile asked for, the first is there when the second's requests are all that is left
-    wait_requests(pending > 1 ? requests : 0);
-    asm volatile("" ::: "memory");
-    const unsigned at = lds + slot_out * Sh::STAGE, at_s = lds_s + slot_out * 32;
-    const bool whole = whole_pages && mine + 31 <= first_seen && mine + 32 <= hi;
-    f32x16 sc = zero;
+  __device__ __forceinline__ explicit Rows32(int lane) : read(lane) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[db][r] = 0.0f;
+  }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* qr, int D, int lane) { load_query<DP, NP>(qr, D, lane >> 5, q); }
+  // `items` and `last`, where not all rows see all of the tile: the tile's items that are there, and the place of the last that the row sees
+  __device__ __forceinline__ void tile(unsigned at_k, unsigned at_v, unsigned at_s, float scale, bool whole, unsigned items, int last, int lane) {
+    const int h = lane >> 5;
+    f32x16 sc = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     const float ks = read.key_scale(at_s);
 #pragma unroll
     for (int i = 0; i < KS / 2; ++i) {
-      const u32x4 w = read.rows(at, i);
+      const u32x4 w = read.rows(at_k, i);
       const bf16x8 k0 = wide8(w[0], w[1], ks, ks), k1 = wide8(w[2], w[3], ks, ks);
 #pragma unroll
       for (int p = NP - 1; p >= 0; --p) {
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qreg[p][2 * i], sc, 0, 0, 0);
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qreg[p][2 * i + 1], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, q[p][2 * i], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, q[p][2 * i + 1], sc, 0, 0, 0);
       }
     }
-    unsigned items = ~0u;
     if (!whole) {
-      const int left = hi - mine;
-      bool in = l32 < left;
-      if (!whole_pages) in = in && (unsigned)table[(mine + (in ? l32 : 0)) >> a.page_log2] < (unsigned)a.P;
-      items = (unsigned)__ballot(in);
-      const int seen = last - mine - 4 * h;
+      const int seen = last - 4 * h;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int i0 = 8 * (r >> 2) + (r & 3);
@@ -141,12 +83,236 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const u32x2 w = read.columns(at + Sh::TILE, s, db);
+        const u32x2 w = read.columns(at_v, s, db);
         const bf16x8 v = wide8(w[0], w[1], v0, v1);
 #pragma unroll
         for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i][s], acc[db], 0, 0, 0);
       }
     }
+  }
+  // to [column][32 rows], row r at r ^ column % 32
+  __device__ __forceinline__ void leave(float* out, float* to_m, float* to_l, int lane) {
+    const int l32 = lane & 31, h = lane >> 5;
+    l = half_sum(l);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = 8 * (r >> 2) + 4 * h + (r & 3);
+        out[(db * 32 + d) * 32 + (l32 ^ d)] = acc[db][r];
+      }
+    if (h == 0) {
+      to_m[l32] = m;
+      to_l[l32] = l;
+    }
+  }
+};
+
+// At most 16 rows: a lane holds a row's scores of 8 of the items, half the exponentials and half the time of the products. Product x of a
+// tile's two has the items 8 (i / 4) + 4 x + i % 4 as its rows i, so that a lane of the scores, items 8 g + 4 x .. + 3 for g = lane / 16,
+// has the octet 8 g .. 8 g + 7 that it is to have of the other factor.
+template <int DP, int NP>
+struct Rows16 {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  static constexpr int ROWS = 16, CH = DP / 16, KC = DP / 64, DB = DP / 16;
+  static constexpr bool OCTETS = true;
+  unsigned row, cols, ks, vs;
+  bf16x8 q[NP][KC][2];
+  f32x4 acc[DB];
+  float m = -INFINITY, l = 0.0f;
+  __device__ __forceinline__ explicit Rows16(int lane) {
+    const int i = lane & 15, g = lane >> 4, r = 8 * (i >> 2) + (i & 3), k = 8 * g + (i >> 1);
+    row = r * DP + ((g ^ swz8_octets<CH>(r)) << 4);
+    cols = k * DP + (swz8_octets<CH>(k) << 4) + (i & 1) * 8;
+    ks = (i >> 3) * 16 + ((i >> 2) & 1) * 4;
+    vs = (g >> 1) * 16 + (g & 1) * 4 + 8;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // columns 64 c + 16 (lane / 16) and on
+  template <typename T>
+  __device__ __forceinline__ void load(const T* qr, int D, int lane) {
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int d = c * 64 + (lane >> 4) * 16 + s * 8;
+        float x[8];
+        bf16x8 part[NP];
+        if constexpr (NP == 1) {
+          u32x4 raw = {0u, 0u, 0u, 0u};
+          if (d < D) raw = *reinterpret_cast<const u32x4*>(qr + d);
+          part[0] = __builtin_bit_cast(bf16x8, raw);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; j += 4) {
+            f32x4 raw = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (d < D) raw = *reinterpret_cast<const f32x4*>(qr + d + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j + e] = raw[e];
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            __bf16 b[NP];
+            split_bf16<NP>(x[j], b);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) part[i][j] = b[i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) q[i][c][s] = part[i];
+      }
+  }
+  __device__ __forceinline__ void tile(unsigned at_k, unsigned at_v, unsigned at_s, float scale, bool whole, unsigned items, int last, int lane) {
+    const int g = lane >> 4;
+    f32x4 sc[2];
+    const float k_scale = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at_s + ks));
+    float v_scale = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at_s + vs));
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      sc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
+        const u32x4 w = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 2 : 1) << 4)) + x * 4 * DP)));
+        const bf16x8 k0 = wide8(w[0], w[1], k_scale, k_scale), k1 = wide8(w[2], w[3], k_scale, k_scale);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) {
+          sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[p][c][0], sc[x], 0, 0, 0);
+          sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[p][c][1], sc[x], 0, 0, 0);
+        }
+      }
+    }
+    if (!whole) {
+      const int seen = last - 8 * g;
+      const unsigned mine = items >> (8 * g);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (4 * x + r > seen || !((mine >> (4 * x + r)) & 1)) sc[x][r] = -INFINITY;
+      v_scale = mine & 1 ? v_scale : 1.0f;   // (a block without items has no scale; its codes came as zeros)
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) top = fmaxf(top, sc[r >> 2][r & 3]);
+    top = quarter_max(top) * scale;
+    if (__any(top > m + MAX_SLACK)) {   // (the first tile: m is -inf)
+      const float next = fmaxf(m, top), c = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= c;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[db][r] *= c;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    bf16x8 p[NP][2];
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[r >> 2][r & 3], scale, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[r >> 2][(r & 3) + 1], scale, -base));
+      sum += p0 + p1;
+      split_pair<NP>(p0, p1, r, p);
+    }
+    l += sum;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_at((at_v + cols) ^ (db << 4)))));
+      const bf16x8 v = wide8(w[0], w[1], v_scale, v_scale);
+#pragma unroll
+      for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][0], acc[db], 0, 0, 0);
+    }
+  }
+  // to [column][16 rows], row r at r ^ column % 16
+  __device__ __forceinline__ void leave(float* out, float* to_m, float* to_l, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    l = quarter_sum(l);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[(db * 16 + 4 * g + r) * 16 + (i ^ (4 * g + r))] = acc[db][r];
+    if (g == 0) {
+      to_m[i] = m;
+      to_l[i] = l;
+    }
+  }
+};
+
+template <int DP>
+struct Few8Shape {
+  static constexpr int TILE = 32 * DP, STAGE = 2 * TILE, NST = 2, WAVE = NST * STAGE;
+  static constexpr int JOIN = DP * 32 * 4;   // [column][32 rows] of fp32, row r at r ^ column % 32
+  static_assert(JOIN <= WAVE, "the outputs take the tiles' place");
+};
+
+template <int DP, int NW, int PART, typename Rows, typename T>
+__global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args a8, int G, MulDiv by_group, float scale, int chunk, int splits) {
+  using Sh = Few8Shape<DP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * Sh::WAVE];
+  __shared__ __attribute__((aligned(16))) float scales[NW][Sh::NST][8];
+  __shared__ float join_m[NW][Rows::ROWS], join_l[NW][Rows::ROWS];
+  const CacheArgs& a = a8.c;
+  const int per = a.U * a.Hkv;
+  // (turned by one from run to run: a user's runs are not all one die's)
+  const int split = blockIdx.x / per, uh = (blockIdx.x + split) % per, u = uh / a.Hkv, hk = uh % a.Hkv;
+  const CandRange cr = cand_range(a.off, u, a.C, a.T);
+  const int rows = cr.count * G;
+  if (rows == 0) return;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2);
+  const int lo = split * chunk, hi = n < lo + chunk ? n : lo + chunk;
+  if (lo >= n && split > 0) return;   // (the first run of an empty history still writes)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem) + wave * Sh::WAVE;
+  const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[wave][0][0]);
+  const int32_t* table = a.pages + (size_t)u * a.max_pages;
+
+  Tiles8<DP, 32, PART, Rows::OCTETS> tiles;
+  tiles.init(a.D, a.page_log2, 0, lane);
+  const int step_items = NW * 32, requests = tiles.requests();
+  int ask = lo + wave * 32, mine = ask;
+  int pending = 0, slot_in = 0, slot_out = 0;
+  tiles.look_up(table, ask, hi, a.page_log2);
+  auto request = [&]() __attribute__((always_inline)) {
+    const unsigned at = lds + slot_in * Sh::STAGE;
+    tiles.fetch(a8, hk, ask, hi, at, at + Sh::TILE, lds_s + slot_in * 32, lane);
+    slot_in = slot_in + 1 == Sh::NST ? 0 : slot_in + 1;
+    ask += step_items;
+    ++pending;
+    tiles.look_up(table, ask, hi, a.page_log2);
+  };
+
+  Rows mine_rows(lane);
+  int last;
+  {
+    const int at = lane & (Rows::ROWS - 1), r = at < rows ? at : rows - 1, i = (int)by_group.div(r), g = r - i * G;
+    last = a.causal ? n - cr.count + i : n - 1;
+    mine_rows.load(static_cast<const T*>(a.q) + (size_t)(cr.first + i) * a.qp + (size_t)(hk * G + g) * a.D, a.D, lane);
+  }
+  const int first_seen = __builtin_amdgcn_readlane(last, 0);
+  bool whole_pages;
+  {
+    bool bad = false;
+    for (int x = (lo >> a.page_log2) + lane; x <= (hi - 1) >> a.page_log2 && lo < hi; x += 64) bad |= (unsigned)table[x] >= (unsigned)a.P;
+    whole_pages = __ballot(bad) == 0;
+  }
+  for (int x = 0; x < Sh::NST && ask < hi; ++x) request();
+
+  for (; mine < hi; mine += step_items) {
+    // loads return in order: with a second tile asked for, the first is there when the second's requests are all that is left
+    wait_requests(pending > 1 ? requests : 0);
+    asm volatile("" ::: "memory");
+    const unsigned at = lds + slot_out * Sh::STAGE, at_s = lds_s + slot_out * 32;
+    const bool whole = whole_pages && mine + 31 <= first_seen && mine + 32 <= hi;
+    unsigned items = ~0u;
+    if (!whole) {
+      const int at = lane & 31;
+      bool in = at < hi - mine;
+      if (!whole_pages) in = in && (unsigned)table[(mine + (in ? at : 0)) >> a.page_log2] < (unsigned)a.P;
+      items = (unsigned)__ballot(in);
+    }
+    mine_rows.tile(at, at + Sh::TILE, at_s, scale, whole, items, last - mine, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again
     --pending;
     slot_out = slot_out + 1 == Sh::NST ? 0 : slot_out + 1;
@@ -154,19 +320,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
   }
 
   // the waves' results, in the place of the tiles
-  float* out = reinterpret_cast<float*>(smem + wave * Sh::WAVE);
-  l = half_sum(l);
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int d = 8 * (r >> 2) + 4 * h + (r & 3);
-      out[(db * 32 + d) * 32 + (l32 ^ d)] = acc[db][r];
-    }
-  if (h == 0) {
-    join_m[wave][l32] = m;
-    join_l[wave][l32] = l;
-  }
+  mine_rows.leave(reinterpret_cast<float*>(smem + wave * Sh::WAVE), join_m[wave], join_l[wave], lane);
   __syncthreads();
   const bool final = n <= chunk;
   for (int e = tid; e < rows * a.D; e += 64 * NW) {
@@ -179,7 +333,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
     for (int w = 0; w < NW; ++w) {
       const float mw = join_m[w][r], c = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - top);
       sum = fmaf(join_l[w][r], c, sum);
-      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * 32 + (r ^ (d & 31))], c, x);
+      x = fmaf(reinterpret_cast<const float*>(smem + w * Sh::WAVE)[d * Rows::ROWS + (r ^ (d & (Rows::ROWS - 1)))], c, x);
     }
     x = sum == 0.0f ? 0.0f : x / sum;
     const float z = log_sum(top, sum, !final);
@@ -196,7 +350,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
   }
 }
 
-template <int DP, int NP, int NW, typename T>
+template <int DP, int NW, typename Rows, typename T>
 static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
   const CacheArgs& c = a.c;
   const int G = c.H / c.Hkv;
@@ -211,26 +365,23 @@ static laser_status few8_typed(const Cache8Args& a, const CacheRuns& r) {
     part.c.lens = c.lens + u;
     const unsigned grid = (unsigned)(part.c.U * each);
     const MulDiv by_group = mul_div(G);
-    if (c.page_log2 >= 4) cache8_few_kernel<DP, NP, NW, 16, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
-    else cache8_few_kernel<DP, NP, NW, 8, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
+    if (c.page_log2 >= 4) cache8_few_kernel<DP, NW, 16, Rows, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
+    else cache8_few_kernel<DP, NW, 8, Rows, T><<<grid, 64 * NW, 0, c.stream>>>(part, G, by_group, LOG2E / c.gamma, r.chunk, r.runs);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
   return r.runs > 1 ? cache_join_launch(c, r.chunk, r.runs) : LASER_OK;
 }
-template <int NP, typename T>
+template <int NP, int NW, typename T>
 static laser_status few8_width(const Cache8Args& a, const CacheRuns& r) {
-  if (cache8_waves(a.c.U, a.c.Hkv, r) == 8) {
-    if (a.c.D > 64) return few8_typed<128, NP, 8, T>(a, r);
-    if (a.c.D > 32) return few8_typed<64, NP, 8, T>(a, r);
-    return few8_typed<32, NP, 8, T>(a, r);
-  }
-  if (a.c.D > 64) return few8_typed<128, NP, 4, T>(a, r);
-  if (a.c.D > 32) return few8_typed<64, NP, 4, T>(a, r);
-  return few8_typed<32, NP, 4, T>(a, r);
+  const bool sixteen = a.c.C * (a.c.H / a.c.Hkv) <= 16;
+  if (a.c.D > 64) return sixteen ? few8_typed<128, NW, Rows16<128, NP>, T>(a, r) : few8_typed<128, NW, Rows32<128, NP>, T>(a, r);
+  if (a.c.D > 32) return sixteen ? few8_typed<64, NW, Rows16<64, NP>, T>(a, r) : few8_typed<64, NW, Rows32<64, NP>, T>(a, r);
+  return few8_typed<32, NW, Rows32<32, NP>, T>(a, r);
 }
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r) {
-  return a.c.dt == LASER_F32 ? few8_width<3, float>(a, r) : few8_width<1, unsigned short>(a, r);
+  if (cache8_waves(a.c.U, a.c.Hkv, r) == 8) return a.c.dt == LASER_F32 ? few8_width<3, 8, float>(a, r) : few8_width<1, 8, unsigned short>(a, r);
+  return a.c.dt == LASER_F32 ? few8_width<3, 4, float>(a, r) : few8_width<1, 4, unsigned short>(a, r);
 }
 
 }  // namespace laser

@@ -12,6 +12,11 @@ namespace laser {
 template <int CH> __device__ __forceinline__ int swz8(int r) {
   return CH == 8 ? ((r >> 1) & 1) * 2 + ((r >> 3) & 1) * 4 + ((r >> 2) & 1) : CH == 4 ? (r >> 2) & 3 : (r >> 3) & 1;
 }
+// The same for reads of rows {0..3, 8..11, 16..19, 24..27} (+ 4) at one piece, and transpose loads of rows 8 g .. 8 g + 7 at one
+template <int CH> __device__ __forceinline__ int swz8_octets(int r) {
+  const int b2 = (r >> 2) & 1, b3 = (r >> 3) & 1, b4 = (r >> 4) & 1;
+  return CH == 8 ? ((r >> 1) & 1) + (b3 ^ b2) * 2 + b4 * 4 : (b3 ^ b2) + b4 * 2;
+}
 
 // 8 e4m3 numbers, the first four times a, the others times b (powers of two)
 __device__ __forceinline__ bf16x8 wide8(unsigned lo, unsigned hi, float a, float b) {
@@ -40,7 +45,7 @@ __device__ __forceinline__ void wait_requests(int n) {
 // What a wave brings of a tile: ROWS rows of keys and of values and their scales. Pages hold PART items or more each (8 or 16), which then
 // share where they come from: a lone wave issues an instruction every 5 to 9 cycles, and those for the addresses of 32 rows were as many
 // as for their products.
-template <int DP, int ROWS, int PART>
+template <int DP, int ROWS, int PART, bool OCTETS = false>
 struct Tiles8 {
   static constexpr int CH = DP / 16, RPI = 64 / CH < ROWS ? 64 / CH : ROWS, REQ = ROWS / RPI, IDS = ROWS / PART, EACH = PART / RPI;
   unsigned off[REQ];
@@ -50,7 +55,7 @@ struct Tiles8 {
     part = (1 << page_log2) < RPI ? 1 << page_log2 : RPI;
 #pragma unroll
     for (int x = 0; x < REQ; ++x) {
-      const int in = lane / CH, c = (lane % CH) ^ swz8<CH>(row0 + x * RPI + in);
+      const int in = lane / CH, r = row0 + x * RPI + in, c = (lane % CH) ^ (OCTETS ? swz8_octets<CH>(r) : swz8<CH>(r));
       off[x] = c * 16 < D && in < RPI ? (unsigned)(((EACH > 1 ? x % EACH * RPI : 0) + in) * D + c * 16) : NO_COLUMN;
     }
   }
@@ -138,6 +143,16 @@ struct TileReader8 {
     return *reinterpret_cast<const __attribute__((address_space(3))) u32x2*>(lds_at(at + s * 16 + 8));
   }
 };
+
+// max and sum over the four lanes that share a row of 16
+__device__ __forceinline__ float quarter_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quarter_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
 
 // A number of 24 bits as a sum of bf16 numbers, the largest first: products with them and with e4m3 numbers are exact
 template <int NP>
