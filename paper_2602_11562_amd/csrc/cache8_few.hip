@@ -168,13 +168,24 @@ struct Rows16 {
     f32x4 sc[2];
     const float k_scale = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at_s + ks));
     float v_scale = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds_at(at_s + vs));
+    u32x4 kw[2][KC];
+    u32x2 vw[DB];   // (read ahead of the scores, so that no product waits for LDS)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int c = 0; c < KC; ++c)   // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
+        kw[x][c] = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 2 : 1) << 4)) + x * 4 * DP)));
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      vw[db] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_at((at_v + cols) ^ (db << 4)))));
+    }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       sc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
-        const u32x4 w = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 2 : 1) << 4)) + x * 4 * DP)));
+        const u32x4 w = kw[x][c];
         const bf16x8 k0 = wide8(w[0], w[1], k_scale, k_scale), k1 = wide8(w[2], w[3], k_scale, k_scale);
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p) {
@@ -218,9 +229,7 @@ struct Rows16 {
     l += sum;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      typedef int i32x2 __attribute__((ext_vector_type(2)));
-      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_at((at_v + cols) ^ (db << 4)))));
-      const bf16x8 v = wide8(w[0], w[1], v_scale, v_scale);
+      const bf16x8 v = wide8(vw[db][0], vw[db][1], v_scale, v_scale);
 #pragma unroll
       for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][0], acc[db], 0, 0, 0);
     }
