@@ -50,22 +50,22 @@ static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <
 // of 128 112, 118, 123; 200 x 20000, 8 of 128 98, 96, 112; 256 x 4096, 32 of 64 71.5, 70.8, 67.7; more users, in their own order: 64 x 4096, 100
 // of 128 -, 116, 111), of 512 items or more, of 256 where the longest history has few runs anyway and for fp32 (us by 256 and 512: 100 x
 // 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1).
-// Few rows, us by one run a history, runs of 1024 items and runs of 512 (heads of 128 over 2 key-value heads unless said otherwise):
-//   1 x 65000, 16 heads (2 pairs)  -, 20.0, 18.6;  8 x 20000 (16)  -, 20.5, 26.3;  40 x 3000 fp32 (80)  28, 23.6, 31.8;  5 x 777 fp32 (10)  14.5, -, 16.8;
-//   32 x 1000, 8 over 8 of 64 (256)  14.0, -, 18.5;  128 x 970 of up to 4096 (256)  35.6 (two of 2048), 27.0, 29.3;  200 x 5000, 4 over 1 of 64 (200)
-//   33.5 (two), 30.8, 34.0;  256 x 1200 of up to 2000, four rows (512)  38.0, 47.8, 55.7
-// Rules: none where the histories alone are two workgroups a compute unit, or short; else runs of 512 while they are one workgroup a
-// compute unit, and of 1024 beyond.
+// Few rows, us by one run a history and runs of 1024 and 512 items (heads of 128 over 2 key-value heads unless said otherwise):
+//   1 x 65000, 16 heads (2 pairs)  307, 15.8, 15.2;  30 x 2000 (60)  13.1, 11.9, 9.8;  8 x 20000 (16)  88, 17.3, 17.9;  40 x 3000 fp32 (80)  25.7, 16.9, 17.7;
+//   5 x 777 fp32 (10)  7.7, -, 9.2;  32 x 1000, 8 over 8 of 64 (256)  7.8, -, 10.4;  100 x 2000 (200)  16.9, 19.2, 22.1;  100 x 3000 (200)  21.8,
+//   23.4, 26.8, most of them short 18.0, 18.5, 16.6;  128 x 4096 (256)  31.2, 37.9, 39.9, most short 24.6, 21.1, 24.0;  256 x 2000, four rows (512)  33.6, 42.9, 48.8
+// Rules: none where the histories alone are two workgroups a compute unit, or short, or one for every other unit and of medium length; else
+// runs of 512 while they are one workgroup a compute unit, and of 1024 beyond.
 CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
   if (!few8_rows(C, H, Hkv))
     return cache_runs((rows + 127) / 128 * pairs, L, D > 64 && U <= CACHE8_RANKED ? 1536 : 2048, L > 2048 && dt != LASER_F32 ? 512 : 256, 64);
-  if (pairs >= 512 || L <= 1024) return CacheRuns{(L + 255) / 256 * 256, 1};
+  if (pairs >= 512 || L <= (pairs > 128 ? 3200 : 1024)) return CacheRuns{(L + 255) / 256 * 256, 1};
   return cache_runs(pairs, L, 1024, pairs * ((L + 511) / 512) <= 256 ? 512 : 1024, 256);
 }
-// Eight waves where there is about one workgroup a compute unit, whose way is then half as long (us by four and eight: 1 x 65000 19.5 and
-// 18.6, 40 x 3000 fp32 26.0 and 23.6, 32 x 1000 14.7 and 14.0); four beyond, two workgroups of which share a compute unit (128 x 970
-// 27.0 and 31.9, 256 x 1200 38.0 and 42.6).
+// Eight waves where there is about one workgroup a compute unit, whose way is then half as long (us by four and eight: 1 x 65000 15.5 and
+// 14.8, 40 x 3000 fp32 18.7 and 17.0, 32 x 1000 9.4 and 7.8); four beyond, two workgroups of which share a compute unit (128 x 4096, most
+// of them short, 21.5 and 25.0, 256 x 2000, four rows, 34.2 and 36.2).
 int cache8_waves(int U, int Hkv, const CacheRuns& r) { return (long long)U * Hkv * r.runs <= 320 ? 8 : 4; }
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const CacheRuns r = cache8_runs_of(U, C, L, H, Hkv, D, dt);

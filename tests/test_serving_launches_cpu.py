@@ -48,7 +48,7 @@ def test_appends_cover_every_user(recorder, U, C, Hkv, block, dt):
 
 #       U  Hkv H    L   C   waves  runs
 FORMS = [(1, 2, 16, 65000, 1, 8, 127), (8, 2, 8, 20000, 1, 8, 20), (40, 2, 8, 3000, 1, 8, 3), (128, 2, 8, 4096, 1, 4, 4), (256, 2, 8, 2000, 4, 4, 1),
-         (5, 2, 4, 777, 1, 8, 1), (200, 1, 4, 5000, 1, 4, 5), (600, 1, 4, 100000, 2, 4, 1)]
+         (5, 2, 4, 777, 1, 8, 1), (200, 1, 4, 5000, 1, 4, 5), (600, 1, 4, 100000, 2, 4, 1), (100, 2, 8, 3000, 1, 8, 1), (65, 2, 8, 3201, 8, 4, 4)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
