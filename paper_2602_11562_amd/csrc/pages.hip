@@ -119,9 +119,8 @@ __device__ __forceinline__ int forked_items(const Tables& t, const int32_t* sour
   const int n = held_items(t, u), room = max_out << t.log2;
   return n < room ? n : room;
 }
-__global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
-                                                         int32_t* __restrict__ rank, int32_t* __restrict__ fresh,
-                                                         int32_t* __restrict__ missing) {
+__device__ __forceinline__ void fork_plan(const Tables& t, const int32_t* source, int V, int max_out, int32_t* rank, int32_t* fresh,
+                                          int32_t* missing) {
   const Counts<TAKE_RUNS> first = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
   for (int v0 = 0; v0 < V; v0 += PLAN) {
@@ -141,6 +140,10 @@ __global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const i
     if (rank[v] >= got) rank[v] = -2;              // no page is left for it
   if (threadIdx.x == 0) *missing = want - got;
 }
+__global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
+                                                         int32_t* rank, int32_t* fresh, int32_t* missing) {
+  fork_plan(t, source, V, max_out, rank, fresh, missing);
+}
 
 // Pieces of listed pages from src[] to dst[], every part of them
 struct Moves {
@@ -153,11 +156,11 @@ __device__ __forceinline__ void move_piece(unsigned char* base, long long bytes,
   reinterpret_cast<T*>(base + dst * bytes)[piece] = reinterpret_cast<const T*>(base + src * bytes)[piece];
 }
 // entry(e, &src, &dst): false where the entry moves nothing
-template <typename Entry>
+template <int THREADS = 256, typename Entry>
 __device__ __forceinline__ void move_pages(const Moves& m, long long entries, unsigned block, unsigned blocks, const Entry& entry) {
   const PageParts& parts = m.parts;
   const long long all = entries * parts.all;
-  for (long long g = (long long)block * 256 + threadIdx.x; g < all; g += (long long)blocks * 256) {
+  for (long long g = (long long)block * THREADS + threadIdx.x; g < all; g += (long long)blocks * THREADS) {
     const long long e = all <= 0x7fffffffLL ? (long long)m.by_all.div((unsigned)g) : g / parts.all;
     unsigned piece = (unsigned)(g - e * parts.all);
     int src, dst, i = 0;
@@ -169,38 +172,54 @@ __device__ __forceinline__ void move_pages(const Moves& m, long long entries, un
   }
 }
 
-// Fork, the rest: the first `copies` workgroups copy pages, the others write a table each
-__global__ __launch_bounds__(256) void fork_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
-                                                   const int32_t* __restrict__ rank, const int32_t* __restrict__ fresh,
-                                                   int32_t* __restrict__ pages_out, int32_t* __restrict__ lens_out, unsigned copies,
-                                                   bool tables, const Moves m) {
+// Fork, the rest: where a page that is copied comes from and goes to, and entry j of table v
+struct Fork {
+  const int32_t *source, *rank, *fresh;
+  int32_t *pages_out, *lens_out;
+  int V, max_out;
+};
+__device__ __forceinline__ bool forked_page(const Tables& t, const Fork& f, int v, int* src, int* dst) {
+  const int r = f.rank[v];
+  if (r < 0) return false;
+  const int n = forked_items(t, f.source, v, f.max_out);
+  *src = t.pages[(size_t)f.source[v] * t.max_pages + (n >> t.log2)];
+  *dst = f.fresh[r];
+  return true;
+}
+__device__ __forceinline__ void forked_entry(const Tables& t, const Fork& f, int v, int j, int n) {
+  int p = -1;
+  if (j < pages_of(n, t.log2)) {
+    p = t.pages[(size_t)f.source[v] * t.max_pages + j];
+    if (j >= n >> t.log2) {
+      if ((unsigned)p < (unsigned)t.P) p = f.rank[v] >= 0 ? f.fresh[f.rank[v]] : -1;
+    } else if ((unsigned)p < (unsigned)t.P) {
+      atomicAdd(t.refs + p, 1);
+    }
+  }
+  f.pages_out[(size_t)v * f.max_out + j] = p;
+  if (j == 0) f.lens_out[v] = n;
+}
+// The first `copies` workgroups copy pages, the others write a table each
+__global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f, unsigned copies, bool tables, const Moves m) {
   if (blockIdx.x < copies) {
-    move_pages(m, V, blockIdx.x, copies, [&](long long v, int* src, int* dst) __attribute__((always_inline)) {
-      const int r = rank[v];
-      if (r < 0) return false;
-      const int n = forked_items(t, source, (int)v, max_out);
-      *src = t.pages[(size_t)source[v] * t.max_pages + (n >> t.log2)];
-      *dst = fresh[r];
-      return true;
-    });
+    move_pages(m, f.V, blockIdx.x, copies, [&](long long v, int* src, int* dst) __attribute__((always_inline)) { return forked_page(t, f, (int)v, src, dst); });
     return;
   }
   if (!tables) return;
-  for (int v = blockIdx.x - copies; v < V; v += gridDim.x - copies) {
-    const int n = forked_items(t, source, v, max_out), whole = n >> t.log2, used = pages_of(n, t.log2);
-    for (int j = threadIdx.x; j < max_out; j += 256) {
-      int p = -1;
-      if (j < used) {
-        p = t.pages[(size_t)source[v] * t.max_pages + j];
-        if (j >= whole) {
-          if ((unsigned)p < (unsigned)t.P) p = rank[v] >= 0 ? fresh[rank[v]] : -1;
-        } else if ((unsigned)p < (unsigned)t.P) {
-          atomicAdd(t.refs + p, 1);
-        }
-      }
-      pages_out[(size_t)v * max_out + j] = p;
-    }
-    if (threadIdx.x == 0) lens_out[v] = n;
+  for (int v = blockIdx.x - copies; v < f.V; v += gridDim.x - copies) {
+    const int n = forked_items(t, f.source, v, f.max_out);
+    for (int j = threadIdx.x; j < f.max_out; j += 256) forked_entry(t, f, v, j, n);
+  }
+}
+// A small fork, plan and rest in one launch
+__global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const Fork f, int32_t* rank, int32_t* fresh, int32_t* missing,
+                                                          MulDiv by_out, const Moves m) {
+  fork_plan(t, f.source, f.V, f.max_out, rank, fresh, missing);
+  __syncthreads();   // ranks, fresh pages and their counts are written
+  move_pages<PLAN>(m, f.V, 0, 1, [&](long long v, int* src, int* dst) __attribute__((always_inline)) { return forked_page(t, f, (int)v, src, dst); });
+  for (int x = threadIdx.x; x < f.V * f.max_out; x += PLAN) {
+    const int v = (int)by_out.div((unsigned)x);
+    forked_entry(t, f, v, x - v * f.max_out, forked_items(t, f.source, v, f.max_out));
   }
 }
 
@@ -432,16 +451,28 @@ static laser_status over_parts(const PagesArgs& a, long long entries, const int3
   return LASER_OK;
 }
 
+// Of so many pieces and entries a fork is one workgroup's, plan and all: the GPU takes as long (three histories of 63 pages, two parts of
+// 4096 bytes: 9.3 us by two launches and 9.5 by one, with the release of the forks), the host less (a fork, a growth and a release: 17.1 and 15.7)
+constexpr int SMALL_FORK = 2 * PLAN;
 laser_status pages_fork_launch(const PagesArgs& a) {
   int32_t *rank = a.work, *fresh = a.work + a.V;
   const Tables t = tables_of(a);
+  const Fork f{a.source, rank, fresh, a.pages_out, a.lens_out, a.V, a.max_out};
+  if (a.n_parts <= PARTS_A_LAUNCH && (long long)a.V * a.max_out <= SMALL_FORK) {
+    Moves m{};
+    m.parts = parts_of(a, 0);
+    m.by_all = mul_div(m.parts.all > 0 ? m.parts.all : 1);
+    if ((long long)a.V * m.parts.all <= SMALL_FORK) {
+      fork_small_kernel<<<1, PLAN, 0, a.stream>>>(t, f, rank, fresh, a.missing, mul_div(a.max_out), m);
+      return launch_status();
+    }
+  }
   fork_plan_kernel<<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing);
   laser_status s = launch_status();
   if (s != LASER_OK) return s;
   return over_parts(a, a.V, nullptr, [&](const Moves& m, unsigned copies, bool first) {
     const unsigned more = first ? (a.V < 4096 ? a.V : 4096) : 0;
-    if (copies + more > 0)
-      fork_kernel<<<copies + more, 256, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.pages_out, a.lens_out, copies, first, m);
+    if (copies + more > 0) fork_kernel<<<copies + more, 256, 0, a.stream>>>(t, f, copies, first, m);
   });
 }
 
