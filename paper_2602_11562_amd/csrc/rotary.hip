@@ -3,11 +3,13 @@
 // pairs being columns (i, i + R/2) or (2i, 2i + 1); the transpose (s -> -s) carries gradients back. One launch turns queries and keys.
 //
 // Bound by memory: what is turned comes in and goes out once, in pieces of 16 bytes (201 MB of bf16 rows in 38 us, 5.3 TB/s, what a large
-// copy reaches; pairs side by side 42 us; halves that are no whole pieces take twice as long). Results are stored for whoever reads them next: with
+// copy reaches; pairs side by side 42 us; halves that are no whole pieces take up to twice as long). Results are stored for whoever reads them next: with
 // the non-temporal hint the launch alone is 0 to 10 us shorter, attention behind it 4 to 8 us longer than that. A workgroup takes a few tokens, makes their cosines
 // and sines once for all heads, in LDS, and walks heads and pieces. An angle of a far position is many turns: it is formed in fp64 and
 // reduced to an eighth of a turn there (fp32 would be off by 4e-3 at position 65000), then cosine and sine are Taylor sums in fp32.
 #include "rotary.h"
+
+#include <type_traits>
 
 namespace laser {
 
@@ -35,7 +37,34 @@ struct Piece {
   __device__ __forceinline__ void set(int j, float x) { store_from_f32<T>(v, j, x); }
 };
 
+// The last elements of a row, fewer than a piece: by halves of one, quarters, .., of which `left` has each once or not at all, M elements from
+// the element on that the larger ones end at; they stand in a Piece from N - 2 M on
+template <typename T, int M, typename Go>
+__device__ __forceinline__ void over_rest(int left, const Go& go) {
+  if constexpr (M > 0) {
+    if (left & M) go(std::integral_constant<int, M>(), left & ~(2 * M - 1));
+    over_rest<T, M / 2>(left, go);
+  }
+}
+template <typename T, int M>
+struct Some {
+  typedef T type __attribute__((ext_vector_type(M), aligned(sizeof(T) < 2 ? 1 : 2)));
+  static __device__ __forceinline__ void copy(T* to, const T* from) { *reinterpret_cast<type*>(to) = *reinterpret_cast<const type*>(from); }
+};
+
 constexpr int ROTARY_TOKENS = 16;   // of a workgroup, at most
+
+// Cosines and sines of a workgroup's tokens, and which of them have a position
+__device__ __forceinline__ void make_turns(const RotaryArgs& a, int t0, int count, const MulDiv& by_half, float2* turn, int* there) {
+  const int half = a.R / 2;
+  for (unsigned e = threadIdx.x; e < (unsigned)(count * half); e += 256) {
+    const int t = (int)by_half.div(e), i = (int)e - t * half, pos = a.pos[t0 + t];
+    const float2 cs = cos_sin((double)pos * a.freq[i]);
+    turn[t * half + i] = float2{cs.x * a.scale, (a.back ? -cs.y : cs.y) * a.scale};
+    if (i == 0) there[t] = pos >= 0;
+  }
+  __syncthreads();
+}
 
 // What a thread has of a head: HALF pairs, a piece of either half; SIDE by side, two pieces in a row. Columns from R on are copied.
 // (x and y may be the same rows: a thread reads what it writes, and nobody else does)
@@ -46,13 +75,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int tok
   __shared__ float2 turn[ROTARY_TOKENS * 64];
   __shared__ int there[ROTARY_TOKENS];
   const int t0 = blockIdx.x * tokens, count = a.T - t0 < tokens ? a.T - t0 : tokens, half = a.R / 2;
-  for (unsigned e = threadIdx.x; e < (unsigned)(count * half); e += 256) {
-    const int t = (int)by_half.div(e), i = (int)e - t * half, pos = a.pos[t0 + t];
-    const float2 cs = cos_sin((double)pos * a.freq[i]);
-    turn[t * half + i] = float2{cs.x * a.scale, (a.back ? -cs.y : cs.y) * a.scale};
-    if (i == 0) there[t] = pos >= 0;
-  }
-  __syncthreads();
+  make_turns(a, t0, count, by_half, turn, there);
   const int heads = a.heads[0] + a.heads[1];
   for (unsigned e = threadIdx.x; e < (unsigned)(count * heads * units); e += 256) {
     const unsigned row = by_units.div(e), unit = e - row * units, t = by_heads.div(row);
@@ -98,11 +121,24 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int tok
         p.store(y + c);
         r.store(y + half + c);
       } else if (left > 0) {   // the last pairs, fewer than a piece
-        for (int i = c; i < half; ++i) {
-          const float u = load_as_f32<T>(x, i), v = load_as_f32<T>(x, half + i);
-          store_from_f32<T>(y, i, fmaf(u, cs[i].x, -(v * cs[i].y)));
-          store_from_f32<T>(y, half + i, fmaf(u, cs[i].y, v * cs[i].x));
-        }
+        P p, r;
+        over_rest<T, N / 2>(left, [&](auto m, int o) __attribute__((always_inline)) {
+          constexpr int M = decltype(m)::value;
+          Some<T, M>::copy(p.v + N - 2 * M, x + c + o);
+          Some<T, M>::copy(r.v + N - 2 * M, x + half + c + o);
+        });
+        over_rest<T, N / 2>(left, [&](auto m, int o) __attribute__((always_inline)) {
+          constexpr int M = decltype(m)::value;
+#pragma unroll
+          for (int j = N - 2 * M; j < N - M; ++j) {
+            const float2 f = cs[c + o + j - (N - 2 * M)];
+            const float u = p.get(j), v = r.get(j);
+            p.set(j, fmaf(u, f.x, -(v * f.y)));
+            r.set(j, fmaf(u, f.y, v * f.x));
+          }
+          Some<T, M>::copy(y + c + o, p.v + N - 2 * M);
+          Some<T, M>::copy(y + half + c + o, r.v + N - 2 * M);
+        });
       } else {                 // columns from R on, where they have to be copied
         const int from = a.R + (int)(unit - (half + N - 1) / N) * N;
         if (from + N <= a.D) {
@@ -110,10 +146,60 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int tok
           p.load(x + from);
           p.store(y + from);
         } else {
-          for (int i = from; i < a.D; ++i) y[i] = x[i];
+          P p;
+          over_rest<T, N / 2>(a.D - from, [&](auto m, int o) __attribute__((always_inline)) {
+            Some<T, decltype(m)::value>::copy(p.v + N - 2 * decltype(m)::value, x + from + o);
+          });
+          over_rest<T, N / 2>(a.D - from, [&](auto m, int o) __attribute__((always_inline)) {
+            Some<T, decltype(m)::value>::copy(y + from + o, p.v + N - 2 * decltype(m)::value);
+          });
         }
       }
     }
+  }
+}
+
+// Halves that are no whole pieces, to other rows than they come from: a thread has a piece of the result, whole and aligned, and reads the
+// piece's own columns and the other halves of its pairs, wherever they start. (Bound by requests: 20000 tokens, 10 heads of 128, 100 columns
+// turned, 37 us against 39.5 by the kernel above, which is left with rows in place; fp32, 38 of 80, 36 against 49. Whole halves 21.)
+template <typename T>
+__global__ __launch_bounds__(256) void rotary_apart_kernel(const RotaryArgs a, int tokens, MulDiv by_half, MulDiv by_units, MulDiv by_heads, int units) {
+  typedef Piece<T> P;
+  constexpr int N = P::N;
+  __shared__ float2 turn[ROTARY_TOKENS * 64];
+  __shared__ int there[ROTARY_TOKENS];
+  const int t0 = blockIdx.x * tokens, count = a.T - t0 < tokens ? a.T - t0 : tokens, half = a.R / 2;
+  make_turns(a, t0, count, by_half, turn, there);
+  const int heads = a.heads[0] + a.heads[1];
+  for (unsigned e = threadIdx.x; e < (unsigned)(count * heads * units); e += 256) {
+    const unsigned row = by_units.div(e), unit = e - row * units, t = by_heads.div(row);
+    if (!there[t]) continue;
+    unsigned head = row - t * heads;
+    const int which = head >= (unsigned)a.heads[0], c = unit * N;
+    head -= which ? a.heads[0] : 0;
+    const T* x = static_cast<const T*>(a.x[which]) + (size_t)(t0 + t) * a.xp[which] + head * a.D;
+    T* y = static_cast<T*>(a.y[which]) + (size_t)(t0 + t) * a.yp[which] + head * a.D;
+    const float2* cs = turn + t * half;
+    P p, r;
+    p.load(x + c);
+    if (c < a.R) {
+      if (c + N <= half) r.load(x + c + half);
+      else if (c >= half) r.load(x + c - half);
+      else {   // on both sides of the middle
+#pragma unroll
+        for (int j = 0; j < N; ++j) r.v[j] = x[c + j < half ? c + j + half : c + j < a.R ? c + j - half : c + j];
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int i = c + j;
+        if (i < a.R) {
+          const float2 f = cs[i < half ? i : i - half];
+          const float u = p.get(j), v = r.get(j);
+          p.set(j, i < half ? fmaf(u, f.x, -(v * f.y)) : fmaf(v, f.y, u * f.x));
+        }
+      }
+    }
+    p.store(y + c);
   }
 }
 
@@ -123,7 +209,8 @@ static laser_status rotary_typed(const RotaryArgs& a) {
   const int heads = a.heads[0] + a.heads[1], half = a.R / 2;
   // (rows turned in place keep their other columns: those pieces are left out. A tensor in place beside one that is not copies onto itself.)
   const bool in_place = a.y[0] == a.x[0] && a.y[1] == a.x[1];
-  const int units = SIDE ? ((in_place ? a.R : a.D) + 2 * N - 1) / (2 * N) : (half + N - 1) / N + (in_place ? 0 : (a.D - a.R + N - 1) / N);
+  const bool apart = !SIDE && half % N != 0 && (a.x[0] == nullptr || a.y[0] != a.x[0]) && (a.x[1] == nullptr || a.y[1] != a.x[1]);
+  const int units = apart ? a.D / N : SIDE ? ((in_place ? a.R : a.D) + 2 * N - 1) / (2 * N) : (half + N - 1) / N + (in_place ? 0 : (a.D - a.R + N - 1) / N);
   // Tokens that give each thread a piece or two, and a few workgroups for each compute unit (39322 tokens of 10 heads of 128, 80 threads
   // each: by 16 tokens 42.6 us, by 4 38.2; 100000 of 2 heads, 16 threads each: by 16 24.6, by 4 26.2)
   int tokens = (320 + heads * units - 1) / (heads * units);
@@ -143,7 +230,8 @@ static laser_status rotary_typed(const RotaryArgs& a) {
     part.pos = a.pos + t0;
     const unsigned here = grid - b < MOST ? grid - b : MOST;
     part.T = b + here < grid ? (int)((long long)here * tokens) : (int)(a.T - t0);
-    rotary_kernel<T, SIDE><<<here, 256, 0, a.stream>>>(part, tokens, mul_div(half), mul_div(units), mul_div(heads), units);
+    if (apart) rotary_apart_kernel<T><<<here, 256, 0, a.stream>>>(part, tokens, mul_div(half), mul_div(units), mul_div(heads), units);
+    else rotary_kernel<T, SIDE><<<here, 256, 0, a.stream>>>(part, tokens, mul_div(half), mul_div(units), mul_div(heads), units);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
