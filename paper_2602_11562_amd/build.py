@@ -135,8 +135,17 @@ def build_history_host_check(out: str) -> str:
     """Build tests/history_host_check.cpp with the host halves of the sources for attention among a history's items, validation and
     launchers, instrumented with AddressSanitizer and UndefinedBehaviorSanitizer; launches are recorded (tests/launch_recorder.cpp), no
     device code is there. No GPU needed to build or run it."""
+    return _recorded_host_check(out, "history_host_check.cpp", ("history_", "cache_"))
+
+
+def build_serving_host_check(out: str) -> str:
+    """The same of tests/serving_host_check.cpp: rotary positions, the cache in 8 bits and the pages of a cache."""
+    return _recorded_host_check(out, "serving_host_check.cpp", ("serving_", "rotary", "cache8_", "pages", "cache_few"))
+
+
+def _recorded_host_check(out: str, main: str, sources: tuple) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
-    no_kernels = os.path.join(OBJDIR, "no_kernels_host_check.bin")
+    no_kernels = os.path.join(OBJDIR, "no_kernels_" + main.replace(".cpp", ".bin"))
     with open(no_kernels, "wb") as f:
         f.write(b"none")
     san = ["-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined"]
@@ -145,20 +154,20 @@ def build_history_host_check(out: str) -> str:
         "-O1", "-g", "-Xclang", "-fcuda-include-gpubinary", "-Xclang", no_kernels]
 
     def compile_one(src: str) -> str:
-        obj = os.path.join(OBJDIR, "san_" + os.path.basename(src).rsplit(".", 1)[0] + ".o")
+        obj = os.path.join(OBJDIR, f"san_{main[:7]}_" + os.path.basename(src).rsplit(".", 1)[0] + ".o")
         cmd = [_hipcc(), "-x", "hip", "--offload-host-only", *flags, *arch_host, "-c", src, "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"host half of {src}:\n" + r.stderr[-4000:])
         return obj
 
-    srcs = [os.path.join(CSRC, s) for s in SOURCES if s.startswith(("history_", "cache_"))]
-    srcs += [os.path.join(ROOT, "tests", s) for s in ("launch_recorder.cpp", "history_host_check.cpp")]
+    srcs = [os.path.join(CSRC, s) for s in SOURCES if s.startswith(sources)]
+    srcs += [os.path.join(ROOT, "tests", s) for s in ("launch_recorder.cpp", main)]
     with ThreadPoolExecutor(max_workers=6) as ex:
         objs = list(ex.map(compile_one, srcs))
     r = subprocess.run(["/opt/rocm/lib/llvm/bin/clang++", *san, "-o", out, *objs, "-ldl"], capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("history host check link failed:\n" + r.stderr[-4000:])
+        raise RuntimeError("host check link failed:\n" + r.stderr[-4000:])
     return out
 
 
