@@ -108,7 +108,10 @@ struct Rows32 {
   }
 };
 
-// At most 16 rows: a lane holds a row's scores of 8 of the items, half the exponentials and half the time of the products. Product x of a
+// At most 16 rows: a lane holds a row's scores of 8 of the items, half the exponentials and half the time of the products, and the values are
+// read ahead of the scores, for which there are registers (us by 32 rows and by 16: one token for 128 users x up to 4096 24.6 and 21.6, fp32 for
+// 5 x up to 777 10.3 and 7.8, 64 x 1000 11.8 and 10.1; keys and values at once, with the tile's place asked for again ahead of the products: 22.5, 7.7, 10.3;
+// four tiles a wave instead of two, with 32 rows of 64: 25.2 and 30.9 us for 64 x up to 8192). Product x of a
 // tile's two has the items 8 (i / 4) + 4 x + i % 4 as its rows i, so that a lane of the scores, items 8 g + 4 x .. + 3 for g = lane / 16,
 // has the octet 8 g .. 8 g + 7 that it is to have of the other factor.
 template <int DP, int NP>
@@ -174,7 +177,7 @@ struct Rows16 {
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int c = 0; c < KC; ++c)   // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
-        kw[x][c] = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 2 : 1) << 4)) + x * 4 * DP)));
+        kw[x][c] = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 4 : 1) << 4)) + x * 4 * DP)));
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       typedef int i32x2 __attribute__((ext_vector_type(2)));

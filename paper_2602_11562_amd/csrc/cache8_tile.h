@@ -12,10 +12,11 @@ namespace laser {
 template <int CH> __device__ __forceinline__ int swz8(int r) {
   return CH == 8 ? ((r >> 1) & 1) * 2 + ((r >> 3) & 1) * 4 + ((r >> 2) & 1) : CH == 4 ? (r >> 2) & 3 : (r >> 3) & 1;
 }
-// The same for reads of rows {0..3, 8..11, 16..19, 24..27} (+ 4) at one piece, and transpose loads of rows 8 g .. 8 g + 7 at one
+// The same for reads of rows {0..3, 8..11, 16..19, 24..27} (+ 4), the lanes of 16 at one piece and those of the next 16 at the next, and transpose
+// loads of rows 0..15 or 16..31 at one
 template <int CH> __device__ __forceinline__ int swz8_octets(int r) {
-  const int b2 = (r >> 2) & 1, b3 = (r >> 3) & 1, b4 = (r >> 4) & 1;
-  return CH == 8 ? ((r >> 1) & 1) + (b3 ^ b2) * 2 + b4 * 4 : (b3 ^ b2) + b4 * 2;
+  const int b1 = (r >> 1) & 1, b2 = (r >> 2) & 1, b3 = (r >> 3) & 1, b4 = (r >> 4) & 1;
+  return CH == 8 ? b1 + b3 * 2 + (b2 ^ b4) * 4 : (b2 ^ b4) + (b3 ^ b4) * 2;
 }
 
 // 8 e4m3 numbers, the first four times a, the others times b (powers of two)
@@ -44,7 +45,7 @@ __device__ __forceinline__ void wait_requests(int n) {
 
 // What a wave brings of a tile: ROWS rows of keys and of values and their scales. Pages hold PART items or more each (8 or 16), which then
 // share where they come from: a lone wave issues an instruction every 5 to 9 cycles, and those for the addresses of 32 rows were as many
-// as for their products.
+// as for their products (one token for 128 users x up to 4096 by parts of 8 and of 16: 26.0 and 24.4 us).
 template <int DP, int ROWS, int PART, bool OCTETS = false>
 struct Tiles8 {
   static constexpr int CH = DP / 16, RPI = 64 / CH < ROWS ? 64 / CH : ROWS, REQ = ROWS / RPI, IDS = ROWS / PART, EACH = PART / RPI;
