@@ -223,6 +223,7 @@ __global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const 
   }
 }
 
+constexpr int OWN_ENTRIES = 16;
 // Grow: user u's table gets the pages that its next c items ask for
 __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_t* __restrict__ off, int32_t* pages, int32_t* lens,
                                                     int32_t* __restrict__ rank, int32_t* __restrict__ fresh, int32_t* __restrict__ missing) {
@@ -246,11 +247,24 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
   }
   const int got = take_free(t.refs, t.P, want, fresh, ahead);
   __syncthreads();
-  for (int u = threadIdx.x; u < t.U; u += PLAN) {
-    const int n = held_items(t, u), m = grown(u, n), first = pages_of(n, t.log2), last = pages_of(m, t.log2);
-    int r = rank[u];
-    for (int j = first; j < last; ++j, ++r) pages[(size_t)u * t.max_pages + j] = r < got ? fresh[r] : -1;
-    lens[u] = m;
+  // A user's first entries by a thread, the others by its wave, where few users are dealt to all waves (65000 items of one user in pages of
+  // 8: 822 us by the thread alone and 27 so, 16 users' 5000 in pages of 16 49 and 14, 128 users' 1000 23 and 16).
+  const bool deal = t.U <= PLAN / 4;
+  for (int u0 = 0; u0 < t.U; u0 += PLAN) {
+    const int lane = threadIdx.x & 63, u = u0 + (deal ? lane * (PLAN / 64) + (int)(threadIdx.x >> 6) : (int)threadIdx.x);
+    int first = 0, last = 0, r = 0;
+    if (u < t.U) {
+      const int n = held_items(t, u), m = grown(u, n);
+      first = pages_of(n, t.log2), last = pages_of(m, t.log2), r = rank[u] - first;
+      lens[u] = m;
+    }
+    auto entry = [&](int u, int r, int j) { pages[(size_t)u * t.max_pages + j] = r + j < got ? fresh[r + j] : -1; };
+    for (int j = first; j < last && j < first + OWN_ENTRIES; ++j) entry(u, r, j);
+    for (unsigned long long more = __ballot(last - first > OWN_ENTRIES); more != 0; more &= more - 1) {
+      const int l = __builtin_ctzll(more), end = __builtin_amdgcn_readlane(last, l), their_u = __builtin_amdgcn_readlane(u, l),
+                their_r = __builtin_amdgcn_readlane(r, l);
+      for (int j = __builtin_amdgcn_readlane(first, l) + OWN_ENTRIES + lane; j < end; j += 64) entry(their_u, their_r, j);
+    }
   }
   if (threadIdx.x == 0) *missing = want - got;
 }

@@ -269,3 +269,36 @@ def test_another_stream():
     laser.laser_pages_free(out, out_n, None, refs, 16, stream=side)
     side.synchronize()
     assert refs.tolist() == pool.refs and out_n.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("needs,P", [([9000], 9500), ([0, 700, 1, 0, 17, 16, 3000, 15], 4000), ([5, 2000, 40], 900), ([1] * 300 + [2500] + [20] * 60, 5000)])
+def test_growth_by_many_pages(needs, P):
+    """Users that get thousands of pages beside others that get one or none, with enough of them and without."""
+    r = random.Random(P)
+    held = [r.randint(0, 3) for _ in needs]
+    start, page = sum(held), 8
+    deal = list(range(P))
+    r.shuffle(deal)
+    refs, width = [0] * P, max(needs) + 4
+    rows = []
+    for n in held:
+        rows.append([deal.pop() for _ in range(n)])
+        for p in rows[-1]:
+            refs[p] = 1
+    pages, lens = ints([t + [-7] * (width - len(t)) for t in rows]), ints([n * page for n in held])
+    off = [0]
+    for n in needs:
+        off.append(off[-1] + (n * page - r.randint(0, page - 1) if n else 0))
+    free, device_refs = [p for p in range(P) if refs[p] == 0], ints(refs)
+    missing = laser.laser_pages_grow(pages, lens, ints(off), device_refs, page)
+    got = [free.pop(0) if free else -1 for _ in range(sum(needs))]
+    assert missing.item() == max(0, sum(needs) - (P - start)) == got.count(-1)
+    at, want = 0, []
+    for t, n in zip(rows, needs):
+        want.append(t + got[at:at + n] + [-7] * (width - len(t) - n))
+        at += n
+    for p in got:
+        if p >= 0:
+            refs[p] = 1
+    assert torch.equal(pages, ints(want)) and torch.equal(device_refs, ints(refs))
+    assert lens.tolist() == [n * page + b - a for n, a, b in zip(held, off, off[1:])]
