@@ -1,8 +1,8 @@
 // The pages of a cache. refs[p] counts the tables that hold page p; a page with refs <= 0 is free, and free pages are taken from the
 // lowest number up, users in order, so that the same calls give the same tables whatever the order of atomics.
 //
-// A plan is made by one workgroup that walks the counts (a page's number among the free ones is a sum over all before it), or for the
-// compaction of a large pool by one for each 8192 pages, and leaves lists in the work buffer; copies and tables are then written by as many
+// A plan is made by one workgroup that walks the counts (a page's number among the free ones is a sum over all before it), for the
+// compaction of more than 4096 pages by one for each 2048, and leaves lists in the work buffer; copies and tables are then written by as many
 // workgroups as that takes. Copies go piece by piece of 16 bytes over all parts of all listed pages, whatever a page's size. Bound by latency for small calls (two launches), by memory for large ones.
 #include "pages.h"
 
@@ -79,36 +79,86 @@ __device__ __forceinline__ Counts<RUNS> counts_of(const int32_t* refs, long long
 }
 __device__ __forceinline__ int lanes_before(unsigned long long mask) { return __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1)); }
 
-// The first `want` free pages to fresh[], their counts set to 1; returns how many there were. `next`: the counts of the first chunk
-__device__ __forceinline__ int take_free(int32_t* refs, int P, int want, int32_t* fresh, Counts<TAKE_RUNS> next) {
-  constexpr int RUNS = TAKE_RUNS, CHUNK = PLAN * RUNS;
-  const int mine = (int)(threadIdx.x >> 6) * 64 * RUNS, lane = threadIdx.x & 63;
-  int got = 0;
-  for (int p0 = 0; p0 < P && got < want; p0 += CHUNK) {
-    const Counts<RUNS> here = next;
-    next = counts_of<RUNS>(refs, (long long)p0 + CHUNK + mine, P);   // (asked for ahead of this chunk's sums)
-    unsigned long long free[RUNS];
-    int sum = 0;
+template <int RUNS>
+__device__ __forceinline__ int used_in(const Counts<RUNS>& x, unsigned long long* used) {
+  int sum = 0;
 #pragma unroll
-    for (int r = 0; r < RUNS; ++r) {
-      free[r] = __ballot(here.c[r] <= 0 && p0 + mine + r * 64 + lane < P);
-      sum += __popcll(free[r]);
-    }
-    int all;
-    int rank = got + waves_before(sum, &all);
-#pragma unroll
-    for (int r = 0; r < RUNS; ++r) {
-      const int at = rank + lanes_before(free[r]);
-      if ((free[r] >> lane & 1) && at < want) {
-        const int p = p0 + mine + r * 64 + lane;
-        fresh[at] = p;
-        refs[p] = 1;
-      }
-      rank += __popcll(free[r]);
-    }
-    got += all;
+  for (int r = 0; r < RUNS; ++r) {
+    used[r] = __ballot(x.c[r] > 0);
+    sum += __popcll(used[r]);
   }
-  return got < want ? got : want;
+  return sum;
+}
+// Pages in use of each chunk
+template <int RUNS>
+__global__ __launch_bounds__(PLAN) void used_kernel(const int32_t* __restrict__ refs, int P, int32_t* __restrict__ sums) {
+  unsigned long long used[RUNS];
+  int all;
+  waves_before(used_in(counts_of<RUNS>(refs, (long long)blockIdx.x * PLAN * RUNS + (threadIdx.x >> 6) * 64 * RUNS, P), used), &all);
+  if (threadIdx.x == 0) sums[blockIdx.x] = all;
+}
+
+// The first `want` free pages to fresh[], their counts set to 1; returns how many there were. One workgroup walks the pool by chunks of 8192
+// pages; of a large pool (FULL) `used` says which chunks are full, and those are left out: 128 users that grow by a page each, the free
+// ones last of 100000 pages 29 us without and 13 with, of 500000 117 and 14, of 10000 9 without. next: the counts of the first chunk, where it is not.
+constexpr int TAKE_CHUNK = PLAN * TAKE_RUNS, FULL_POOL = 4 * TAKE_CHUNK;
+struct Taken {
+  int32_t *refs, *fresh;
+  int P, want, got;
+};
+__device__ __forceinline__ void take_chunk(Taken& t, int p0, const Counts<TAKE_RUNS>& here) {
+  const int mine = (int)(threadIdx.x >> 6) * 64 * TAKE_RUNS, lane = threadIdx.x & 63;
+  unsigned long long free[TAKE_RUNS];
+  int sum = 0;
+#pragma unroll
+  for (int r = 0; r < TAKE_RUNS; ++r) {
+    free[r] = __ballot(here.c[r] <= 0 && (long long)p0 + mine + r * 64 + lane < t.P);
+    sum += __popcll(free[r]);
+  }
+  int all;
+  int rank = t.got + waves_before(sum, &all);
+#pragma unroll
+  for (int r = 0; r < TAKE_RUNS; ++r) {
+    const int at = rank + lanes_before(free[r]);
+    if ((free[r] >> lane & 1) && at < t.want) {
+      const int p = p0 + mine + r * 64 + lane;
+      t.fresh[at] = p;
+      t.refs[p] = 1;
+    }
+    rank += __popcll(free[r]);
+  }
+  t.got += all;
+}
+template <bool FULL>
+__device__ __forceinline__ int take_free(int32_t* refs, int P, int want, int32_t* fresh, Counts<TAKE_RUNS> next, const int32_t* used) {
+  const int mine = (int)(threadIdx.x >> 6) * 64 * TAKE_RUNS;
+  Taken t{refs, fresh, P, want, 0};
+  if constexpr (FULL) {
+    __shared__ int list[PLAN];
+    const int chunks = (P + TAKE_CHUNK - 1) / TAKE_CHUNK;
+    for (int c0 = 0; c0 < chunks && t.got < want; c0 += PLAN) {
+      const int c = c0 + (int)threadIdx.x, size = c < chunks ? (P - c * TAKE_CHUNK < TAKE_CHUNK ? P - c * TAKE_CHUNK : TAKE_CHUNK) : 0;
+      const bool has = size > 0 && used[c] < size;
+      int count;
+      const int at = sum_before(has, &count);
+      if (has) list[at] = c;
+      __syncthreads();
+      if (count > 0) next = counts_of<TAKE_RUNS>(refs, (long long)list[0] * TAKE_CHUNK + mine, P);
+      for (int k = 0; k < count && t.got < want; ++k) {
+        const Counts<TAKE_RUNS> here = next;
+        if (k + 1 < count) next = counts_of<TAKE_RUNS>(refs, (long long)list[k + 1] * TAKE_CHUNK + mine, P);
+        take_chunk(t, list[k] * TAKE_CHUNK, here);
+      }
+      __syncthreads();   // (the list has been read)
+    }
+  } else {
+    for (int p0 = 0; p0 < P && t.got < want; p0 += TAKE_CHUNK) {
+      const Counts<TAKE_RUNS> here = next;
+      next = counts_of<TAKE_RUNS>(refs, (long long)p0 + TAKE_CHUNK + mine, P);   // (asked for ahead of this chunk's sums)
+      take_chunk(t, p0, here);
+    }
+  }
+  return t.got < want ? t.got : want;
 }
 
 // Fork, the plan: history v of the new tables gets a fresh page where the history it comes from ends within a page. rank[v]: the fresh
@@ -119,9 +169,11 @@ __device__ __forceinline__ int forked_items(const Tables& t, const int32_t* sour
   const int n = held_items(t, u), room = max_out << t.log2;
   return n < room ? n : room;
 }
+template <bool FULL>
 __device__ __forceinline__ void fork_plan(const Tables& t, const int32_t* source, int V, int max_out, int32_t* rank, int32_t* fresh,
-                                          int32_t* missing) {
-  const Counts<TAKE_RUNS> first = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
+                                          int32_t* missing, const int32_t* used) {
+  Counts<TAKE_RUNS> first = {};
+  if (!FULL) first = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
   for (int v0 = 0; v0 < V; v0 += PLAN) {
     const int v = v0 + threadIdx.x;
@@ -135,14 +187,15 @@ __device__ __forceinline__ void fork_plan(const Tables& t, const int32_t* source
     if (v < V) rank[v] = need ? want + before : -1;
     want += all;
   }
-  const int got = take_free(t.refs, t.P, want, fresh, first);
+  const int got = take_free<FULL>(t.refs, t.P, want, fresh, first, used);
   for (int v = threadIdx.x; v < V; v += PLAN)      // (a thread's own ranks)
     if (rank[v] >= got) rank[v] = -2;              // no page is left for it
   if (threadIdx.x == 0) *missing = want - got;
 }
+template <bool FULL>
 __global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const int32_t* __restrict__ source, int V, int max_out,
-                                                         int32_t* rank, int32_t* fresh, int32_t* missing) {
-  fork_plan(t, source, V, max_out, rank, fresh, missing);
+                                                         int32_t* rank, int32_t* fresh, int32_t* missing, const int32_t* __restrict__ used) {
+  fork_plan<FULL>(t, source, V, max_out, rank, fresh, missing, used);
 }
 
 // Pieces of listed pages from src[] to dst[], every part of them
@@ -214,7 +267,7 @@ __global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f,
 // A small fork, plan and rest in one launch
 __global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const Fork f, int32_t* rank, int32_t* fresh, int32_t* missing,
                                                           MulDiv by_out, const Moves m) {
-  fork_plan(t, f.source, f.V, f.max_out, rank, fresh, missing);
+  fork_plan<false>(t, f.source, f.V, f.max_out, rank, fresh, missing, nullptr);
   __syncthreads();   // ranks, fresh pages and their counts are written
   move_pages<PLAN>(m, f.V, 0, 1, [&](long long v, int* src, int* dst) __attribute__((always_inline)) { return forked_page(t, f, (int)v, src, dst); });
   for (int x = threadIdx.x; x < f.V * f.max_out; x += PLAN) {
@@ -225,13 +278,16 @@ __global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const 
 
 constexpr int OWN_ENTRIES = 16;
 // Grow: user u's table gets the pages that its next c items ask for
+template <bool FULL>
 __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_t* __restrict__ off, int32_t* pages, int32_t* lens,
-                                                    int32_t* __restrict__ rank, int32_t* __restrict__ fresh, int32_t* __restrict__ missing) {
+                                                    int32_t* __restrict__ rank, int32_t* __restrict__ fresh, int32_t* __restrict__ missing,
+                                                    const int32_t* __restrict__ used) {
   auto grown = [&](int u, int n) {
     const long long c = (long long)off[u + 1] - off[u], room = (long long)t.max_pages << t.log2, m = n + (c > 0 ? c : 0);
     return (int)(m < room ? m : room);
   };
-  const Counts<TAKE_RUNS> ahead = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
+  Counts<TAKE_RUNS> ahead = {};
+  if (!FULL) ahead = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
   for (int u0 = 0; u0 < t.U; u0 += PLAN) {
     const int u = u0 + threadIdx.x;
@@ -245,7 +301,7 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
     if (u < t.U) rank[u] = want + before;
     want += all;
   }
-  const int got = take_free(t.refs, t.P, want, fresh, ahead);
+  const int got = take_free<FULL>(t.refs, t.P, want, fresh, ahead, used);
   __syncthreads();
   // A user's first entries by a thread, the others by its wave, where few users are dealt to all waves (65000 items of one user in pages of
   // 8: 822 us by the thread alone and 27 so, 16 users' 5000 in pages of 16 49 and 14, 128 users' 1000 23 and 16).
@@ -287,21 +343,6 @@ __global__ __launch_bounds__(256) void free_kernel(const Tables t, const int32_t
 // Compact, the plan: of M pages in use, those numbered M and more go to the free ones below M, in order. With `sums`, pages in use of each
 // chunk, a workgroup a chunk; otherwise one workgroup for all of them, a few.
 constexpr int CHUNKS_AT_ONCE = 2, WAVE_PAGES = 64 * COMPACT_RUNS;
-__device__ __forceinline__ int used_in(const Counts<COMPACT_RUNS>& x, unsigned long long* used) {
-  int sum = 0;
-#pragma unroll
-  for (int r = 0; r < COMPACT_RUNS; ++r) {
-    used[r] = __ballot(x.c[r] > 0);
-    sum += __popcll(used[r]);
-  }
-  return sum;
-}
-__global__ __launch_bounds__(PLAN) void used_kernel(const int32_t* __restrict__ refs, int P, int32_t* __restrict__ sums) {
-  unsigned long long used[COMPACT_RUNS];
-  int all;
-  waves_before(used_in(counts_of<COMPACT_RUNS>(refs, (long long)blockIdx.x * CHUNK + (threadIdx.x >> 6) * WAVE_PAGES, P), used), &all);
-  if (threadIdx.x == 0) sums[blockIdx.x] = all;
-}
 struct CompactPlan {
   int32_t *src, *dst, *place, *moved, *in_use;
 };
@@ -465,6 +506,15 @@ static laser_status over_parts(const PagesArgs& a, long long entries, const int3
   return LASER_OK;
 }
 
+// Of a large pool, pages in use of each chunk that pages are taken from
+static laser_status full_chunks(const PagesArgs& a, int32_t* sums, const int32_t** used) {
+  *used = nullptr;
+  if (a.P <= FULL_POOL) return LASER_OK;
+  used_kernel<TAKE_RUNS><<<(a.P + TAKE_CHUNK - 1) / TAKE_CHUNK, PLAN, 0, a.stream>>>(a.refs, a.P, sums);
+  *used = sums;
+  return launch_status();
+}
+
 // Of so many pieces and entries a fork is one workgroup's, plan and all: the GPU takes as long (three histories of 63 pages, two parts of
 // 4096 bytes: 9.3 us by two launches and 9.5 by one, with the release of the forks), the host less (a fork, a growth and a release: 17.1 and 15.7)
 constexpr int SMALL_FORK = 2 * PLAN;
@@ -472,7 +522,7 @@ laser_status pages_fork_launch(const PagesArgs& a) {
   int32_t *rank = a.work, *fresh = a.work + a.V;
   const Tables t = tables_of(a);
   const Fork f{a.source, rank, fresh, a.pages_out, a.lens_out, a.V, a.max_out};
-  if (a.n_parts <= PARTS_A_LAUNCH && (long long)a.V * a.max_out <= SMALL_FORK) {
+  if (a.P <= FULL_POOL && a.n_parts <= PARTS_A_LAUNCH && (long long)a.V * a.max_out <= SMALL_FORK) {
     Moves m{};
     m.parts = parts_of(a, 0);
     m.by_all = mul_div(m.parts.all > 0 ? m.parts.all : 1);
@@ -481,9 +531,12 @@ laser_status pages_fork_launch(const PagesArgs& a) {
       return launch_status();
     }
   }
-  fork_plan_kernel<<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing);
-  laser_status s = launch_status();
-  if (s != LASER_OK) return s;
+  laser_status s;
+  const int32_t* used;
+  if ((s = full_chunks(a, fresh + a.P, &used)) != LASER_OK) return s;
+  if (used != nullptr) fork_plan_kernel<true><<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing, used);
+  else fork_plan_kernel<false><<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing, nullptr);
+  if ((s = launch_status()) != LASER_OK) return s;
   return over_parts(a, a.V, nullptr, [&](const Moves& m, unsigned copies, bool first) {
     const unsigned more = first ? (a.V < 4096 ? a.V : 4096) : 0;
     if (copies + more > 0) fork_kernel<<<copies + more, 256, 0, a.stream>>>(t, f, copies, first, m);
@@ -491,7 +544,13 @@ laser_status pages_fork_launch(const PagesArgs& a) {
 }
 
 laser_status pages_grow_launch(const PagesArgs& a) {
-  grow_kernel<<<1, PLAN, 0, a.stream>>>(tables_of(a), a.off, const_cast<int32_t*>(a.pages), a.lens_out, a.work, a.work + a.U, a.missing);
+  const Tables t = tables_of(a);
+  int32_t *rank = a.work, *fresh = a.work + a.U, *pages = const_cast<int32_t*>(a.pages);
+  const int32_t* used;
+  const laser_status s = full_chunks(a, fresh + a.P, &used);
+  if (s != LASER_OK) return s;
+  if (used != nullptr) grow_kernel<true><<<1, PLAN, 0, a.stream>>>(t, a.off, pages, a.lens_out, rank, fresh, a.missing, used);
+  else grow_kernel<false><<<1, PLAN, 0, a.stream>>>(t, a.off, pages, a.lens_out, rank, fresh, a.missing, nullptr);
   return launch_status();
 }
 
@@ -509,7 +568,7 @@ laser_status pages_compact_launch(const PagesArgs& a) {
   if (chunks <= CHUNKS_AT_ONCE) {
     compact_plan_kernel<<<1, PLAN, 0, a.stream>>>(a.refs, a.P, o);
   } else {
-    used_kernel<<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums);
+    used_kernel<COMPACT_RUNS><<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums);
     if ((s = launch_status()) != LASER_OK) return s;
     compact_chunk_kernel<<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums, chunks, o);
   }

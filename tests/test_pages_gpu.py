@@ -302,3 +302,40 @@ def test_growth_by_many_pages(needs, P):
             refs[p] = 1
     assert torch.equal(pages, ints(want)) and torch.equal(device_refs, ints(refs))
     assert lens.tolist() == [n * page + b - a for n, a, b in zip(held, off, off[1:])]
+
+
+@pytest.mark.parametrize("P,free", [(32769, 500), (9_000_000, 3000), (9_000_000, 700)])
+def test_a_large_pool(P, free):
+    """Free pages far apart, whole chunks of the pool in use, more chunks than a workgroup has threads; too few pages for everyone at last."""
+    g = torch.Generator().manual_seed(P + free)
+    refs = torch.ones(P, dtype=torch.int32)
+    at = torch.randperm(P, generator=g)[:free]
+    at[0], at[1] = P - 1, P // 2
+    refs[at] = torch.randint(-1, 1, (free,), generator=g, dtype=torch.int32)      # (0 or less: free)
+    order = torch.nonzero(refs <= 0)[:, 0]
+    U, page, width = 300, 8, 4
+    pages, lens, device_refs = ints([[-1] * width] * U), ints([0] * U), refs.cuda()
+    needs = torch.randint(0, 4, (U,), generator=g)
+    off = torch.cat((torch.zeros(1, dtype=torch.int64), torch.cumsum(needs * page - (needs > 0).long(), 0))).int().cuda()      # (the last page not whole)
+    total = int(needs.sum())
+    assert total < free and laser.laser_pages_grow(pages, lens, off, device_refs, page).item() == 0
+    there = torch.arange(width)[None, :] < needs[:, None]
+    want = torch.full((U, width), -1, dtype=torch.int64)
+    want[there] = order[:total]
+    refs[order[:total]] = 1
+    assert torch.equal(pages.cpu().long(), want) and torch.equal(device_refs.cpu(), refs)
+    part = torch.arange(P, dtype=torch.int64, device="cuda").view(P, 1)
+    forks, fork_lens, missing = torch.empty_like(pages), torch.empty_like(lens), ints([7])
+    laser.laser_pages_fork([part], pages, lens, torch.arange(U, dtype=torch.int32, device="cuda"), device_refs, page, pages_out=forks,
+                           lens_out=fork_lens, missing_out=missing)
+    cut = torch.nonzero(needs > 0)[:, 0]
+    fresh = order[total:total + len(cut)]
+    assert missing.item() == max(0, len(cut) - (free - total))
+    last = needs[cut] - 1
+    old = want[cut, last]
+    whole = torch.arange(width)[None, :] < needs[:, None] - 1
+    refs += torch.bincount(want[whole], minlength=P).int()
+    refs[fresh] = 1
+    want[cut, last] = torch.cat((fresh, torch.full((len(cut) - len(fresh),), -1)))
+    assert torch.equal(forks.cpu().long(), want) and torch.equal(device_refs.cpu(), refs) and torch.equal(fork_lens, lens)
+    assert torch.equal(part[fresh.cuda(), 0].cpu(), old[:len(fresh)])

@@ -102,6 +102,16 @@ def test_compaction_without_parts(recorder, P, plans):
     assert len(records) == plans + 1 and all(r.grid * r.block < 1 << 32 for r in records)
 
 
+@pytest.mark.parametrize("P,counts", [(32768, 0), (32769, 1), (1 << 26, 1)])
+def test_taking_pages_of_a_large_pool(recorder, P, counts):
+    """Chunks that are full are counted ahead, and a fork is then never one workgroup's."""
+    grow = launches(recorder, lambda lib: lib.laser_pages_grow(A, A, A, A, 2, P, 16, 4, A, A, 1 << 40, None))
+    assert len(grow) == 1 + counts and all(r.grid * r.block < 1 << 32 for r in grow)
+    part = (ctypes.c_void_p * 1)(A), (ctypes.c_int64 * 1)(4096)
+    fork = launches(recorder, lambda lib: lib.laser_pages_fork(*part, 1, A, A, A, A, 2, 3, P, 16, 4, 4, A, A, A, A, 1 << 40, None))
+    assert len(fork) == (1 if not counts else 3)
+
+
 def test_no_kernel_uses_scratch(scratch):
     kernels = {k: n for k, n in scratch.items() if "5laser" in k and any(name in k for name in (
         "cache8_", "rotary_", "fork_", "grow_kernel", "free_kernel", "used_kernel", "compact_", "copy_kernel"))}
