@@ -1,4 +1,5 @@
-"""Many rows over the cache of 8-bit blocks: users in the order of what they have to do, and queries of all sizes."""
+"""Attention over the cache of 8-bit blocks: many users' rows in the order of what they have to do, queries of all sizes, every number of
+rows and every width of the streaming form."""
 import math
 
 import pytest
@@ -36,7 +37,9 @@ def test_ragged_users(U, C, H, Hkv, D, L, causal, dtype):
     q, off, host = queries(new, H, D, dtype)
     o, lse = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:2], 7.0, device="cuda")
     gamma = math.sqrt(D)
-    laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, L, gamma, causal=causal, o_out=o, lse_out=lse)
+    need = laser.load_library().laser_cache8_attention_work_bytes(U, q.shape[0], C, L, H, Hkv, D, 0 if dtype == "f32" else 1)
+    work = torch.full((need,), 255, dtype=torch.uint8, device="cuda")      # (NaN: no part that was not written is joined)
+    laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, L, gamma, causal=causal, o_out=o, lse_out=lse, work=work)
     check(o, lse, q, cache, host, gamma, causal, dtype)
     assert (o[:1] == 7.0).all() and (o[host[-1]:] == 7.0).all() and (lse[host[-1]:] == 7.0).all()
     again, _ = laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, L, gamma, causal=causal)
@@ -91,3 +94,18 @@ def test_keys_of_the_least_and_the_largest_scale():
     gamma = 2.0 ** 104
     o, lse = laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, 40, 96, gamma, causal=False)
     check(o, lse, q, cache, host, gamma, False, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page,block", [(8, 8), (16, 8), (64, 32)])
+@pytest.mark.parametrize("D", [16, 48, 64, 80, 112, 128])
+@pytest.mark.parametrize("C,H,Hkv", [(1, 1, 1), (1, 3, 1), (2, 8, 2), (15, 1, 1), (2, 16, 2), (17, 1, 1), (4, 16, 2)])
+def test_few_rows_of_every_width(C, H, Hkv, D, page, block, dtype):
+    """1 to 32 rows of a key-value head, by products of 16 rows and of 32, histories around the tiles' edges."""
+    lens = [1, 31, 32, 33, 0, 257, 2100 if C == 2 else 100]
+    new = [min(n, C) for n in lens]
+    cache = Cache8(lens, Hkv, D, page, block, DT[dtype])
+    q, off, host = queries(new, H, D, dtype)
+    for causal in (True, False):
+        o, lse = laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, max(lens), math.sqrt(D), causal=causal)
+        check(o, lse, q, cache, host, math.sqrt(D), causal, dtype)
