@@ -21,6 +21,7 @@ int cache8_waves(int U, int Hkv, const CacheRuns& r);    // of a workgroup of th
 size_t cache8_attention_work_bytes(int U, int T, int C, int L, int H, int Hkv, int D, laser_dtype dt);
 laser_status cache8_attention_launch(const Cache8Args& a);
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r);    // at most 32 rows a key-value head
+laser_status cache8_join_launch(const CacheArgs& a, const CacheRuns& r);
 constexpr int CACHE8_RANKED = 64;                        // so many users the tiles of rows come by their lengths, a lane for each
 laser_status cache8_tile_launch(const Cache8Args& a, const CacheRuns& r);
 

@@ -306,7 +306,7 @@ laser_status cache8_tile_launch(const Cache8Args& a, const CacheRuns& r) {
   t.scale = LOG2E / a.c.gamma;
   t.chunk = r.chunk, t.runs = r.runs;
   const laser_status s = a.c.dt == LASER_F32 ? tile8_width<3, float>(t) : tile8_width<1, unsigned short>(t);
-  return s == LASER_OK && r.runs > 1 ? cache_join_launch(a.c, r.chunk, r.runs) : s;
+  return s == LASER_OK && r.runs > 1 ? cache8_join_launch(a.c, r) : s;
 }
 
 }  // namespace laser

@@ -109,3 +109,20 @@ def test_few_rows_of_every_width(C, H, Hkv, D, page, block, dtype):
     for causal in (True, False):
         o, lse = laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, max(lens), math.sqrt(D), causal=causal)
         check(o, lse, q, cache, host, math.sqrt(D), causal, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [16, 48, 80, 112, 128])
+def test_many_parts(D, dtype):
+    """A history in more than 16 parts beside short ones and an empty one."""
+    lens, new, H, Hkv, C, L = [9300, 600, 0, 40, 8704, 512], [2, 2, 0, 1, 1, 2], 4, 2, 2, 9300
+    cache = Cache8(lens, Hkv, D, 64, 32, DT[dtype])
+    q, off, host = queries(new, H, D, dtype)
+    need = laser.load_library().laser_cache8_attention_work_bytes(6, q.shape[0], C, L, H, Hkv, D, 0 if dtype == "f32" else 1)
+    assert need == 19 * q.shape[0] * H * (D + 1) * 4
+    for causal in (True, False):
+        work = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        o, lse = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:2], 7.0, device="cuda")
+        laser.laser_cache8_attention_forward(q, *cache.tensors(), off, cache.pages, cache.lens, C, L, math.sqrt(D), causal=causal, o_out=o, lse_out=lse, work=work)
+        check(o, lse, q, cache, host, math.sqrt(D), causal, dtype)
+        assert (o[:1] == 7.0).all() and (o[host[-1]:] == 7.0).all() and (lse[host[-1]:] == 7.0).all()

@@ -78,6 +78,15 @@ def test_forms_of_many_rows(recorder, U, Hkv, H, L, C, D, runs):
         assert recorder.laser_cache8_attention_work_bytes(U, U * C, C, L, H, Hkv, D, dt) == (runs * U * C * H * (D + 1) * 4 if runs > 1 else 16)
 
 
+@pytest.mark.parametrize("U,H,L,C,D,kernel", [(1, 16, 65000, 1, 128, "cache8_join_kernel"), (1, 8, 8000, 1, 128, "cache_join_few_kernel"),
+                                              (8, 8, 20000, 1, 128, "cache8_join_kernel"), (1, 8, 30000, 100, 128, "cache_join_kernel")])
+def test_joins(recorder, U, H, L, C, D, kernel):
+    """More than 16 parts of few rows, of many, and few parts."""
+    for dt in (F32, BF16):
+        records = launches(recorder, attend(U, U * C, C, L, H, 2, D, dt))
+        assert len(records) == 2 and kernel in records[1].kernel.decode()
+
+
 def test_positions_of_many_rows(recorder):
     T = (1 << 31) // 8 - 1
     for D, layout in ((8, 0), (128, 1)):
