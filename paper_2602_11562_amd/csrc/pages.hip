@@ -395,22 +395,37 @@ __global__ __launch_bounds__(PLAN) void compact_plan_kernel(const int32_t* __res
     *o.in_use = M;
   }
 }
+// ALONE: without sums, every workgroup counts all pages, where they are few (the call without contents, captured, us by sums of a launch ahead
+// and alone: 4097 pages 8.7 and 7.8, 10248 9.5 and 9.0, 16384 9.3 and 8.5, 32768 9.3 and 9.7, 131072 11.2 and 18.8)
+constexpr int CHUNKS_ALONE = 8;
+template <bool ALONE>
 __global__ __launch_bounds__(PLAN) void compact_chunk_kernel(const int32_t* __restrict__ refs, int P, const int32_t* __restrict__ sums,
                                                              int chunks, const CompactPlan o) {
   const int chunk = blockIdx.x, wave = (int)(threadIdx.x >> 6);
   const Counts<COMPACT_RUNS> x = counts_of<COMPACT_RUNS>(refs, (long long)chunk * CHUNK + wave * WAVE_PAGES, P);
   int total = 0, ahead = 0, M, before;
-  for (int c = threadIdx.x; c < chunks; c += PLAN) {
-    const int y = sums[c];
-    total += y;
-    ahead += c < chunk ? y : 0;
+  if constexpr (ALONE) {
+#pragma unroll 8
+    for (int p = threadIdx.x; p < P; p += PLAN) {
+      const int y = refs[p] > 0;
+      total += y;
+      ahead += p < chunk * CHUNK ? y : 0;
+    }
+  } else {
+    for (int c = threadIdx.x; c < chunks; c += PLAN) {
+      const int y = sums[c];
+      total += y;
+      ahead += c < chunk ? y : 0;
+    }
   }
   sum_before(total, &M);
   sum_before(ahead, &before);
   // pages in use below M: of whole chunks, and of the one that M is in
-  const int last = M / CHUNK;
+  const int last = ALONE ? 0 : M / CHUNK;
   int below = 0, all;
-  for (int c = threadIdx.x; c < last; c += PLAN) below += sums[c];
+  if constexpr (!ALONE)
+    for (int c = threadIdx.x; c < last; c += PLAN) below += sums[c];
+#pragma unroll 8
   for (int p = last * CHUNK + threadIdx.x; p < M; p += PLAN) below += refs[p] > 0;
   sum_before(below, &all);
   below = all;
@@ -567,10 +582,12 @@ laser_status pages_compact_launch(const PagesArgs& a) {
   laser_status s;
   if (chunks <= CHUNKS_AT_ONCE) {
     compact_plan_kernel<<<1, PLAN, 0, a.stream>>>(a.refs, a.P, o);
+  } else if (chunks <= CHUNKS_ALONE) {
+    compact_chunk_kernel<true><<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, nullptr, chunks, o);
   } else {
     used_kernel<COMPACT_RUNS><<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums);
     if ((s = launch_status()) != LASER_OK) return s;
-    compact_chunk_kernel<<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums, chunks, o);
+    compact_chunk_kernel<false><<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums, chunks, o);
   }
   if ((s = launch_status()) != LASER_OK) return s;
   return over_parts(a, a.P / 2, moved, [&](const Moves& m, unsigned copies, bool first) {

@@ -104,7 +104,7 @@ def test_parts_of_a_page_by_sixteen(recorder, n):
     assert len(fork) == (1 if n == 1 else 1 + -(-n // 16))      # (a small one is one workgroup's, plan and all)
 
 
-@pytest.mark.parametrize("P,plans", [(1, 1), (4096, 1), (4097, 2), (1 << 26, 2)])
+@pytest.mark.parametrize("P,plans", [(1, 1), (4096, 1), (4097, 1), (16384, 1), (16385, 2), (1 << 26, 2)])
 def test_compaction_without_parts(recorder, P, plans):
     """Tables and counts alone: the plan and one launch, for pools of any size."""
     records = launches(recorder, lambda lib: lib.laser_pages_compact(None, None, 0, A, A, A, 2, P, 16, 4, A, A, A, A, 1 << 40, None))
