@@ -5,12 +5,13 @@
 
 namespace laser {
 
-constexpr int PARTS_A_LAUNCH = 16;
-struct PageParts {           // arrays [P, page bytes] that a page is made of
-  unsigned char* at[PARTS_A_LAUNCH];
-  long long bytes[PARTS_A_LAUNCH];   // of a page
-  unsigned pieces[PARTS_A_LAUNCH];   // of a page
-  int piece_log2[PARTS_A_LAUNCH];    // bytes of a piece: 4 (16 bytes), 2 or 0
+// Arrays [P, page bytes] that a page is made of, at most N a launch. (4 or 16: 100 bytes of arguments cost a launch 0.2 us)
+constexpr int FEW_PARTS = 4, PARTS_A_LAUNCH = 16;
+template <int N>
+struct PageParts {
+  unsigned char* at[N];
+  unsigned bytes[N];         // of a page
+  unsigned char piece_log2[N];   // bytes of a piece: 4 (16 bytes), 2 or 0
   int n;
   unsigned all;              // pieces of a page in all parts
 };

@@ -199,26 +199,29 @@ __global__ __launch_bounds__(PLAN) void fork_plan_kernel(const Tables t, const i
 }
 
 // Pieces of listed pages from src[] to dst[], every part of them
+template <int N>
 struct Moves {
-  PageParts parts;
+  static constexpr int PARTS = N;
+  PageParts<N> parts;
   const int32_t* count;      // entries, where the host does not know
   MulDiv by_all;             // / parts.all
 };
 template <typename T>
-__device__ __forceinline__ void move_piece(unsigned char* base, long long bytes, int src, int dst, unsigned piece) {
+__device__ __forceinline__ void move_piece(unsigned char* base, unsigned page_bytes, int src, int dst, unsigned piece) {
+  const long long bytes = page_bytes;
   reinterpret_cast<T*>(base + dst * bytes)[piece] = reinterpret_cast<const T*>(base + src * bytes)[piece];
 }
 // entry(e, &src, &dst): false where the entry moves nothing
-template <int THREADS = 256, typename Entry>
-__device__ __forceinline__ void move_pages(const Moves& m, long long entries, unsigned block, unsigned blocks, const Entry& entry) {
-  const PageParts& parts = m.parts;
+template <int THREADS = 256, int N, typename Entry>
+__device__ __forceinline__ void move_pages(const Moves<N>& m, long long entries, unsigned block, unsigned blocks, const Entry& entry) {
+  const PageParts<N>& parts = m.parts;
   const long long all = entries * parts.all;
   for (long long g = (long long)block * THREADS + threadIdx.x; g < all; g += (long long)blocks * THREADS) {
     const long long e = all <= 0x7fffffffLL ? (long long)m.by_all.div((unsigned)g) : g / parts.all;
     unsigned piece = (unsigned)(g - e * parts.all);
     int src, dst, i = 0;
     if (!entry(e, &src, &dst)) continue;
-    while (piece >= parts.pieces[i]) piece -= parts.pieces[i++];
+    for (unsigned here; piece >= (here = parts.bytes[i] >> parts.piece_log2[i]); ++i) piece -= here;
     if (parts.piece_log2[i] == 4) move_piece<stream16>(parts.at[i], parts.bytes[i], src, dst, piece);
     else if (parts.piece_log2[i] == 2) move_piece<unsigned>(parts.at[i], parts.bytes[i], src, dst, piece);
     else move_piece<unsigned char>(parts.at[i], parts.bytes[i], src, dst, piece);
@@ -253,7 +256,8 @@ __device__ __forceinline__ void forked_entry(const Tables& t, const Fork& f, int
   if (j == 0) f.lens_out[v] = n;
 }
 // The first `copies` workgroups copy pages, the others write a table each
-__global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f, unsigned copies, bool tables, const Moves m) {
+template <int N>
+__global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f, unsigned copies, bool tables, const Moves<N> m) {
   if (blockIdx.x < copies) {
     move_pages(m, f.V, blockIdx.x, copies, [&](long long v, int* src, int* dst) __attribute__((always_inline)) { return forked_page(t, f, (int)v, src, dst); });
     return;
@@ -266,7 +270,7 @@ __global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f,
 }
 // A small fork, plan and rest in one launch
 __global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const Fork f, int32_t* rank, int32_t* fresh, int32_t* missing,
-                                                          MulDiv by_out, const Moves m) {
+                                                          MulDiv by_out, const Moves<FEW_PARTS> m) {
   fork_plan<false>(t, f.source, f.V, f.max_out, rank, fresh, missing, nullptr);
   __syncthreads();   // ranks, fresh pages and their counts are written
   move_pages<PLAN>(m, f.V, 0, 1, [&](long long v, int* src, int* dst) __attribute__((always_inline)) { return forked_page(t, f, (int)v, src, dst); });
@@ -444,10 +448,11 @@ __device__ __forceinline__ int place_of_page(const int32_t* place, const int32_t
 }
 
 // Compact, the rest: the first `copies` workgroups copy pages, the others write tables and counts
+template <int N>
 __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                       const int32_t* __restrict__ place, int32_t* __restrict__ pages_out,
                                                       int32_t* __restrict__ refs_out, const int32_t* __restrict__ in_use,
-                                                      unsigned copies, bool tables, const Moves m) {
+                                                      unsigned copies, bool tables, const Moves<N> m) {
   if (blockIdx.x < copies) {
     move_pages(m, *m.count, blockIdx.x, copies, [&](long long i, int* from, int* to) __attribute__((always_inline)) {
       *from = src[i];
@@ -478,8 +483,9 @@ __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int3
   }
 }
 
+template <int N>
 __global__ __launch_bounds__(256) void copy_kernel(const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n, int P,
-                                                   const Moves m) {
+                                                   const Moves<N> m) {
   move_pages(m, n, blockIdx.x, gridDim.x, [&](long long i, int* from, int* to) __attribute__((always_inline)) {
     *from = src[i];
     *to = dst[i];
@@ -493,32 +499,36 @@ size_t pages_work_ints(int U, int P) { return (size_t)U + 3 * (size_t)P + (P + C
 static Tables tables_of(const PagesArgs& a) { return Tables{a.pages, a.lens, a.refs, a.U, a.P, a.page_log2, a.max_pages}; }
 
 // The parts from `first` on that one launch moves, with their pieces
-static PageParts parts_of(const PagesArgs& a, int first) {
-  PageParts p{};
-  for (int i = first; i < a.n_parts && p.n < PARTS_A_LAUNCH; ++i, ++p.n) {
+template <int N>
+static Moves<N> moves_of(const PagesArgs& a, int first, const int32_t* count) {
+  Moves<N> m{};
+  PageParts<N>& p = m.parts;
+  for (int i = first; i < a.n_parts && p.n < N; ++i, ++p.n) {
     const unsigned long long x = reinterpret_cast<unsigned long long>(a.parts[i]) | (unsigned long long)a.part_bytes[i];
     p.at[p.n] = static_cast<unsigned char*>(a.parts[i]);
-    p.bytes[p.n] = a.part_bytes[i];
+    p.bytes[p.n] = (unsigned)a.part_bytes[i];
     p.piece_log2[p.n] = x % 16 == 0 ? 4 : x % 4 == 0 ? 2 : 0;
-    p.pieces[p.n] = (unsigned)(a.part_bytes[i] >> p.piece_log2[p.n]);
-    p.all += p.pieces[p.n];
+    p.all += p.bytes[p.n] >> p.piece_log2[p.n];
   }
-  return p;
+  m.count = count;
+  m.by_all = mul_div(p.all > 0 ? p.all : 1);
+  return m;
 }
-// go(moves, workgroups that copy, first): a launch for every 16 parts
-template <typename Go>
-static laser_status over_parts(const PagesArgs& a, long long entries, const int32_t* count, Go&& go) {
-  for (int i = 0; i == 0 || i < a.n_parts; i += PARTS_A_LAUNCH) {
-    Moves m{};
-    m.parts = parts_of(a, i);
-    m.count = count;
-    m.by_all = mul_div(m.parts.all > 0 ? m.parts.all : 1);
+// go(moves, workgroups that copy, first): a launch for every N parts
+template <int N, typename Go>
+static laser_status over_parts_by(const PagesArgs& a, long long entries, const int32_t* count, Go&& go) {
+  for (int i = 0; i == 0 || i < a.n_parts; i += N) {
+    const Moves<N> m = moves_of<N>(a, i, count);
     const long long groups = (entries * m.parts.all + 255) / 256;
     go(m, (unsigned)(groups < 16384 ? groups : 16384), i == 0);
     const laser_status s = launch_status();
     if (s != LASER_OK) return s;
   }
   return LASER_OK;
+}
+template <typename Go>
+static laser_status over_parts(const PagesArgs& a, long long entries, const int32_t* count, Go&& go) {
+  return a.n_parts <= FEW_PARTS ? over_parts_by<FEW_PARTS>(a, entries, count, go) : over_parts_by<PARTS_A_LAUNCH>(a, entries, count, go);
 }
 
 // Of a large pool, pages in use of each chunk that pages are taken from
@@ -537,10 +547,8 @@ laser_status pages_fork_launch(const PagesArgs& a) {
   int32_t *rank = a.work, *fresh = a.work + a.V;
   const Tables t = tables_of(a);
   const Fork f{a.source, rank, fresh, a.pages_out, a.lens_out, a.V, a.max_out};
-  if (a.P <= FULL_POOL && a.n_parts <= PARTS_A_LAUNCH && (long long)a.V * a.max_out <= SMALL_FORK) {
-    Moves m{};
-    m.parts = parts_of(a, 0);
-    m.by_all = mul_div(m.parts.all > 0 ? m.parts.all : 1);
+  if (a.P <= FULL_POOL && a.n_parts <= FEW_PARTS && (long long)a.V * a.max_out <= SMALL_FORK) {
+    const Moves<FEW_PARTS> m = moves_of<FEW_PARTS>(a, 0, nullptr);
     if ((long long)a.V * m.parts.all <= SMALL_FORK) {
       fork_small_kernel<<<1, PLAN, 0, a.stream>>>(t, f, rank, fresh, a.missing, mul_div(a.max_out), m);
       return launch_status();
@@ -552,7 +560,7 @@ laser_status pages_fork_launch(const PagesArgs& a) {
   if (used != nullptr) fork_plan_kernel<true><<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing, used);
   else fork_plan_kernel<false><<<1, PLAN, 0, a.stream>>>(t, a.source, a.V, a.max_out, rank, fresh, a.missing, nullptr);
   if ((s = launch_status()) != LASER_OK) return s;
-  return over_parts(a, a.V, nullptr, [&](const Moves& m, unsigned copies, bool first) {
+  return over_parts(a, a.V, nullptr, [&](const auto& m, unsigned copies, bool first) {
     const unsigned more = first ? (a.V < 4096 ? a.V : 4096) : 0;
     if (copies + more > 0) fork_kernel<<<copies + more, 256, 0, a.stream>>>(t, f, copies, first, m);
   });
@@ -590,7 +598,7 @@ laser_status pages_compact_launch(const PagesArgs& a) {
     compact_chunk_kernel<false><<<chunks, PLAN, 0, a.stream>>>(a.refs, a.P, sums, chunks, o);
   }
   if ((s = launch_status()) != LASER_OK) return s;
-  return over_parts(a, a.P / 2, moved, [&](const Moves& m, unsigned copies, bool first) {
+  return over_parts(a, a.P / 2, moved, [&](const auto& m, unsigned copies, bool first) {
     const unsigned more = first ? 1024 : 0;
     if (copies + more > 0)
       compact_kernel<<<copies + more, 256, 0, a.stream>>>(t, src, dst, place, a.pages_out, a.refs_out, a.in_use, copies, first, m);
@@ -598,7 +606,7 @@ laser_status pages_compact_launch(const PagesArgs& a) {
 }
 
 laser_status pages_copy_launch(const PagesArgs& a, const int32_t* src, const int32_t* dst, int n) {
-  return over_parts(a, n, nullptr, [&](const Moves& m, unsigned copies, bool) {
+  return over_parts(a, n, nullptr, [&](const auto& m, unsigned copies, bool) {
     if (copies > 0) copy_kernel<<<copies, 256, 0, a.stream>>>(src, dst, n, a.P, m);
   });
 }
