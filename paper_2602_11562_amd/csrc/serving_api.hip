@@ -49,7 +49,9 @@ static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <
 // lengths (us by 1024, 1536 and 2048 wanted; 8 heads over 2, rows x longest history, users: 512 x 10000, 16 of 128 211, 191, 200; 400 x 9000, 12
 // of 128 112, 118, 123; 200 x 20000, 8 of 128 98, 96, 112; 256 x 4096, 32 of 64 71.5, 70.8, 67.7; more users, in their own order: 64 x 4096, 100
 // of 128 -, 116, 111), of 512 items or more, of 256 where the longest history has few runs anyway and for fp32 (us by 256 and 512: 100 x
-// 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1).
+// 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1). None where the histories are short and two tiles of rows a compute
+// unit (512) without a cut: 32 x 1000, 256 of 128, in four runs and whole: all of that length 117, 54, of lengths up to it 63, 50, most short 40, 43; 128 x 1000, 32
+// of 128 (256 tiles) 33, 44.
 // Few rows, us by one run a history and runs of 1024 and 512 items (heads of 128 over 2 key-value heads unless said otherwise):
 //   1 x 65000, 16 heads (2 pairs)  307, 15.8, 15.2;  30 x 2000 (60)  13.1, 11.9, 9.8;  8 x 20000 (16)  88, 17.3, 17.9;  40 x 3000 fp32 (80)  25.7, 16.9, 17.7;
 //   5 x 777 fp32 (10)  7.7, -, 9.2;  32 x 1000, 8 over 8 of 64 (256)  7.8, -, 10.4;  100 x 2000 (200)  16.9, 19.2, 22.1;  100 x 3000 (200)  21.8,
@@ -58,8 +60,11 @@ static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <
 // runs of 512 while they are one workgroup a compute unit, and of 1024 beyond.
 CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
-  if (!few8_rows(C, H, Hkv))
-    return cache_runs((rows + 127) / 128 * pairs, L, D > 64 && U <= CACHE8_RANKED ? 1536 : 2048, L > 2048 && dt != LASER_F32 ? 512 : 256, 64);
+  const long long tiles = (rows + 127) / 128 * pairs;
+  if (!few8_rows(C, H, Hkv)) {
+    if (tiles >= 512 && L <= 1024) return CacheRuns{(L + 63) / 64 * 64, 1};
+    return cache_runs(tiles, L, D > 64 && U <= CACHE8_RANKED ? 1536 : 2048, L > 2048 && dt != LASER_F32 ? 512 : 256, 64);
+  }
   if (pairs >= 512 || L <= (pairs > 128 ? 3200 : 1024)) return CacheRuns{(L + 255) / 256 * 256, 1};
   return cache_runs(pairs, L, 1024, pairs * ((L + 511) / 512) <= 256 ? 512 : 1024, 256);
 }
