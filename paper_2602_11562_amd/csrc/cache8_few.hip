@@ -110,36 +110,37 @@ struct Rows32 {
 
 // At most 16 rows: a lane holds a row's scores of 8 of the items, half the exponentials and half the time of the products, and the values are
 // read ahead of the scores, for which there are registers (us by 32 rows and by 16: one token for 128 users x up to 4096 24.6 and 21.6, fp32 for
-// 5 x up to 777 10.3 and 7.8, 64 x 1000 11.8 and 10.1; keys and values at once, with the tile's place asked for again ahead of the products: 22.5, 7.7, 10.3;
+// 5 x up to 777 10.3 and 7.8, 64 x 1000 11.8 and 10.1, 100 x up to 3000 of width 32
+// 18.0 and 15.5; keys and values at once, with the tile's place asked for again ahead of the products: 22.5, 7.7, 10.3;
 // four tiles a wave instead of two, with 32 rows of 64: 25.2 and 30.9 us for 64 x up to 8192). Product x of a
 // tile's two has the items 8 (i / 4) + 4 x + i % 4 as its rows i, so that a lane of the scores, items 8 g + 4 x .. + 3 for g = lane / 16,
 // has the octet 8 g .. 8 g + 7 that it is to have of the other factor.
 template <int DP, int NP>
 struct Rows16 {
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  static constexpr int ROWS = 16, CH = DP / 16, KC = DP / 64, DB = DP / 16;
+  static constexpr int ROWS = 16, CH = DP / 16, KC = DP > 32 ? DP / 64 : 1, KS = DP > 32 ? 2 : 1, DB = DP / 16;   // (width 32: one product of 32 columns)
   static constexpr bool OCTETS = true;
   unsigned row, cols, ks, vs;
-  bf16x8 q[NP][KC][2];
+  bf16x8 q[NP][KC][KS];
   f32x4 acc[DB];
   float m = -INFINITY, l = 0.0f;
   __device__ __forceinline__ explicit Rows16(int lane) {
     const int i = lane & 15, g = lane >> 4, r = 8 * (i >> 2) + (i & 3), k = 8 * g + (i >> 1);
-    row = r * DP + ((g ^ swz8_octets<CH>(r)) << 4);
+    row = r * DP + (KS == 2 ? (g ^ swz8_octets<CH>(r)) << 4 : (((g >> 1) ^ swz8_octets<CH>(r)) << 4) + (g & 1) * 8);
     cols = k * DP + (swz8_octets<CH>(k) << 4) + (i & 1) * 8;
     ks = (i >> 3) * 16 + ((i >> 2) & 1) * 4;
     vs = (g >> 1) * 16 + (g & 1) * 4 + 8;
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  // columns 64 c + 16 (lane / 16) and on
+  // columns 64 c + 16 (lane / 16) and on; of width 32 8 (lane / 16) and on
   template <typename T>
   __device__ __forceinline__ void load(const T* qr, int D, int lane) {
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int d = c * 64 + (lane >> 4) * 16 + s * 8;
+      for (int s = 0; s < KS; ++s) {
+        const int d = c * 64 + (lane >> 4) * 8 * KS + s * 8;
         float x[8];
         bf16x8 part[NP];
         if constexpr (NP == 1) {
@@ -176,8 +177,14 @@ struct Rows16 {
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int c = 0; c < KC; ++c)   // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
-        kw[x][c] = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 4 : 1) << 4)) + x * 4 * DP)));
+      for (int c = 0; c < KC; ++c) {   // (row + 4 x: its piece moves by the swizzle of bit 2 alone)
+        if constexpr (KS == 2) {
+          kw[x][c] = __builtin_bit_cast(u32x4, lds_read16(lds_at(((at_k + row) ^ (c << 6) ^ (x * (CH == 8 ? 4 : 1) << 4)) + x * 4 * DP)));
+        } else {
+          const u32x2 w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2*>(lds_at(at_k + row + x * 4 * DP));
+          kw[x][c] = u32x4{w[0], w[1], 0u, 0u};
+        }
+      }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -193,7 +200,7 @@ struct Rows16 {
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p) {
           sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[p][c][0], sc[x], 0, 0, 0);
-          sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[p][c][1], sc[x], 0, 0, 0);
+          if constexpr (KS == 2) sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[p][c][1], sc[x], 0, 0, 0);
         }
       }
     }
@@ -480,7 +487,7 @@ static laser_status few8_width(const Cache8Args& a, const CacheRuns& r) {
   const bool sixteen = a.c.C * (a.c.H / a.c.Hkv) <= 16;
   if (a.c.D > 64) return sixteen ? few8_typed<128, NW, Rows16<128, NP>, T>(a, r) : few8_typed<128, NW, Rows32<128, NP>, T>(a, r);
   if (a.c.D > 32) return sixteen ? few8_typed<64, NW, Rows16<64, NP>, T>(a, r) : few8_typed<64, NW, Rows32<64, NP>, T>(a, r);
-  return few8_typed<32, NW, Rows32<32, NP>, T>(a, r);
+  return sixteen ? few8_typed<32, NW, Rows16<32, NP>, T>(a, r) : few8_typed<32, NW, Rows32<32, NP>, T>(a, r);
 }
 laser_status cache8_few_launch(const Cache8Args& a, const CacheRuns& r) {
   if (cache8_waves(a.c.U, a.c.Hkv, r) == 8) return a.c.dt == LASER_F32 ? few8_width<3, 8, float>(a, r) : few8_width<1, 8, unsigned short>(a, r);

@@ -16,7 +16,7 @@ template <int CH> __device__ __forceinline__ int swz8(int r) {
 // loads of rows 0..15 or 16..31 at one
 template <int CH> __device__ __forceinline__ int swz8_octets(int r) {
   const int b1 = (r >> 1) & 1, b2 = (r >> 2) & 1, b3 = (r >> 3) & 1, b4 = (r >> 4) & 1;
-  return CH == 8 ? b1 + b3 * 2 + (b2 ^ b4) * 4 : (b2 ^ b4) + (b3 ^ b4) * 2;
+  return CH == 8 ? b1 + b3 * 2 + (b2 ^ b4) * 4 : CH == 4 ? (b2 ^ b4) + (b3 ^ b4) * 2 : b3;
 }
 
 // 8 e4m3 numbers, the first four times a, the others times b (powers of two)
