@@ -1,6 +1,6 @@
 // Many rows over a cache of 8-bit blocks: chunks of new items, and candidates. The split of history_mfma.hip: a workgroup of four waves
 // owns 128 rows of a key-value head and walks the items that the last of them sees in tiles of 64, which come by direct loads to LDS as
-// the bytes that they are; a wave owns 32 rows and makes its operands of the bytes in registers. (Scores of bf16 queries, as two numbers of
+// the bytes that they are; a wave owns 32 rows (SPLIT: of half of the items) and makes its operands of the bytes in registers. (Scores of bf16 queries, as two numbers of
 // 8 bits each, straight from the bytes by the products of 8-bit operands: 215 us would be 202 for 512 new items x up to 10000, but those products
 // sum in fewer than 32 bits: errors of lse 4e-6 against 4e-7.)
 // Bound by the vector units beside the products: an exponential, a product and a sum for a score of one, and the values' bytes. Ragged
@@ -90,9 +90,9 @@ __device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Par
   return true;
 }
 
-template <int DP, int SLOTS, int NP, int PART, typename T>
+template <int DP, int SLOTS, int NP, int PART, int SPLIT, typename T>
 __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) {
-  constexpr int KS = DP / 16, DB = DP / 32, NW = 4, ROWS = NW * 32, KB = TI * DP, SLOT = 2 * KB, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
+  constexpr int KS = DP / 16, DB = DP / 32, NW = 4, BLOCKS = NW / SPLIT, ROWS = BLOCKS * 32, KB = TI * DP, SLOT = 2 * KB, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
   constexpr bool PATCHED = sizeof(T) == 2;   // (fp32 rows leave from the registers)
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * SLOT > PATCH || !PATCHED ? SLOTS * SLOT : PATCH];
   __shared__ __attribute__((aligned(16))) float scales[SLOTS][TI / 8 * 2];
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   }
 
   // this lane's row and the last item it sees
-  const int first = row0 + wave * 32;
+  const int first = row0 + wave % BLOCKS * 32;
   int last;
   bf16x8 qreg[NP][KS];
   {
@@ -236,10 +236,41 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
     const unsigned at = lds + out * SLOT, at_s = lds_s + out * (TI / 8 * 8);
     out = out + 1 == SLOTS ? 0 : out + 1;
     const int t0 = begin + u * TI;
-    if (t0 <= wave_last) block(t0, at, at_s);
-    if (t0 + 32 <= wave_last) block(t0 + 32, at + 32 * DP, at_s + 32);
+    if constexpr (SPLIT == 1) {
+      if (t0 <= wave_last) block(t0, at, at_s);
+      if (t0 + 32 <= wave_last) block(t0 + 32, at + 32 * DP, at_s + 32);
+    } else {
+      const int half = wave / BLOCKS * 32;
+      if (t0 + half <= wave_last) block(t0 + half, at + half * DP, at_s + half);
+    }
   }
   barrier_lds();
+  if constexpr (SPLIT == 2) {   // the second halves' results to the waves of the first
+    constexpr int BOX = DP * 32 + 128;
+    static_assert(BLOCKS * BOX * 4 <= SLOTS * SLOT, "they take the tiles' place");
+    float* box = reinterpret_cast<float*>(smem) + wave % BLOCKS * BOX + lane;
+    if (wave >= BLOCKS) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) box[(db * 16 + r) * 64] = acc[db][r];
+      box[DP * 32] = m;
+      box[DP * 32 + 64] = l;
+    }
+    barrier_lds();
+    if (wave < BLOCKS) {
+      const float other = box[DP * 32], next = fmaxf(m, other);
+      const float c = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - next), c2 = other == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(other - next);
+      m = next;
+      l = fmaf(box[DP * 32 + 64], c2, l * c);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = fmaf(box[(db * 16 + r) * 64], c2, acc[db][r] * c);
+    }
+    barrier_lds();
+    if (wave >= BLOCKS) return;
+  }
 
   const float sum = half_sum(l), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int r = first + l32;
@@ -272,23 +303,29 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   });
 }
 
-template <int DP, int SLOTS, int NP, typename T>
-static laser_status tile8_typed(Tile8Args t) {
+template <int DP, int SLOTS, int NP, int SPLIT, typename T>
+static laser_status tile8_split(Tile8Args t) {
   const CacheArgs& c = t.a.c;
   t.tiles = (int)(((long long)c.C * t.G + 127) / 128);
   const long long most = (long long)t.N * t.Hkv * t.tiles * t.runs;
   t.ranked = t.N <= CACHE8_RANKED && most <= 2560;   // (ten a compute unit)
   if (t.ranked) {
-    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
-    else cache8_tile_kernel<DP, SLOTS, NP, 8, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
+    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, SPLIT, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
+    else cache8_tile_kernel<DP, SLOTS, NP, 8, SPLIT, T><<<(unsigned)most, 256, 0, c.stream>>>(t);
     return launch_status();
   }
   return launch_dealt(t, (long long)t.tiles * t.runs, 256, [&](Tile8Args& part, long long n) {
     part.a.c.pages += n * c.max_pages;
     part.a.c.lens += n;
-    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
-    else cache8_tile_kernel<DP, SLOTS, NP, 8, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
+    if (c.page_log2 >= 4) cache8_tile_kernel<DP, SLOTS, NP, 16, SPLIT, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
+    else cache8_tile_kernel<DP, SLOTS, NP, 8, SPLIT, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
   });
+}
+// Heads of at most 64 rows: two waves have the same rows, and a half of each tile's items (us by four waves of rows and so: 64 rows x up to 4096, 32
+// users of 128 33.7 and 26.8, of 64 26.3 and 22.2; 40 x up to 3000, 64 of 64 28.5 and 24.8; fp32, 64 x up to 3000, 16 of 128 24.8 and 21.6)
+template <int DP, int SLOTS, int NP, typename T>
+static laser_status tile8_typed(const Tile8Args& t) {
+  return (long long)t.a.c.C * t.G <= 64 ? tile8_split<DP, SLOTS, NP, 2, T>(t) : tile8_split<DP, SLOTS, NP, 1, T>(t);
 }
 template <int NP, typename T>
 static laser_status tile8_width(const Tile8Args& t) {

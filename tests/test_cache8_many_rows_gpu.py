@@ -28,7 +28,8 @@ def ragged(U, C, L, seed, chunk=256):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("U,C,H,Hkv,D,L", [(1, 70, 2, 1, 64, 1500), (9, 90, 6, 2, 128, 1500), (63, 40, 2, 2, 64, 1100), (64, 33, 2, 1, 128, 1100),
-                                           (65, 33, 2, 1, 64, 1100), (64, 100, 3, 3, 32, 800), (12, 150, 4, 2, 80, 2100)])
+                                           (65, 33, 2, 1, 64, 1100), (64, 100, 3, 3, 32, 800), (12, 150, 4, 2, 80, 2100), (10, 16, 8, 2, 128, 1500), (30, 11, 3, 1, 112, 900),
+                                           (70, 50, 1, 1, 64, 700), (6, 64, 2, 2, 32, 1200)])
 def test_ragged_users(U, C, H, Hkv, D, L, causal, dtype):
     lens, new = ragged(U, C, L, U)
     if not causal:      # (as candidates: users without a history have rows too)
@@ -70,7 +71,7 @@ def test_queries_of_many_sizes(D, spread, size):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-@pytest.mark.parametrize("C,D,L", [(64, 64, 200), (64, 128, 700), (64, 32, 700), (1, 64, 700), (3, 128, 30000)])    # (one run, some, and many)
+@pytest.mark.parametrize("C,D,L", [(64, 64, 200), (64, 128, 700), (64, 32, 700), (30, 128, 700), (1, 64, 700), (3, 128, 30000)])    # (one run, some, and many)
 def test_a_query_that_is_no_number(C, D, L, bad, dtype):
     """It is NaN, and the rows beside it are what they were."""
     cache = Cache8([L], 1, D, 32, 16, DT[dtype])
