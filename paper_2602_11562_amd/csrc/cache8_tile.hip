@@ -14,7 +14,7 @@ struct Tile8Args {
   const int32_t* off;
   int N, Hkv;
   MulDiv by_group;       // / G
-  int G, tiles;          // tiles of the longest sequence's rows
+  int G, tiles, rows_log2;   // tiles of the longest sequence's rows, of 128 or 64
   Deal deal;             // of (tile, run) to workgroups
   float scale;           // log2(e) / gamma
   int chunk, runs;       // items a workgroup walks, and into how many such runs the longest history is cut
@@ -33,7 +33,7 @@ __device__ __forceinline__ bool part_in_turn(const Tile8Args& t, Part8* p) {
   const CandRange cr = cand_range(t.off, p->user, t.a.c.C, t.a.c.T);
   p->first = cr.first;
   p->count = cr.count;
-  if (p->tile * 128 >= cr.count * t.G) return false;
+  if (p->tile << t.rows_log2 >= cr.count * t.G) return false;
   p->n = cache_len(t.a.c.lens, p->user, t.a.c.L, t.a.c.max_pages, t.a.c.page_log2);
   return true;
 }
@@ -47,7 +47,7 @@ __device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Par
   const CacheArgs& a = t.a.c;
   const int u = lane < t.N ? lane : t.N - 1;
   const CandRange cr = cand_range(t.off, u, a.C, a.T);
-  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2), tiles = lane < t.N ? (cr.count * t.G + 127) / 128 : 0;
+  const int n = cache_len(a.lens, u, a.L, a.max_pages, a.page_log2), tiles = lane < t.N ? (cr.count * t.G + (1 << t.rows_log2) - 1) >> t.rows_log2 : 0;
   const int whole = t.runs > 1 ? n / t.chunk : 0, rest = n - whole * t.chunk;
   int at = blockIdx.x, behind = whole * tiles * t.Hkv;   // the workgroups of whole runs up to this user's last
   const int mine = behind;
@@ -306,7 +306,8 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
 template <int DP, int SLOTS, int NP, int SPLIT, typename T>
 static laser_status tile8_split(Tile8Args t) {
   const CacheArgs& c = t.a.c;
-  t.tiles = (int)(((long long)c.C * t.G + 127) / 128);
+  t.rows_log2 = SPLIT == 2 ? 6 : 7;
+  t.tiles = (int)(((long long)c.C * t.G + 128 / SPLIT - 1) / (128 / SPLIT));
   const long long most = (long long)t.N * t.Hkv * t.tiles * t.runs;
   t.ranked = t.N <= CACHE8_RANKED && most <= 2560;   // (ten a compute unit)
   if (t.ranked) {
@@ -321,11 +322,15 @@ static laser_status tile8_split(Tile8Args t) {
     else cache8_tile_kernel<DP, SLOTS, NP, 8, SPLIT, T><<<part.deal.grid, 256, 0, c.stream>>>(part);
   });
 }
-// Heads of at most 64 rows: two waves have the same rows, and a half of each tile's items (us by four waves of rows and so: 64 rows x up to 4096, 32
-// users of 128 33.7 and 26.8, of 64 26.3 and 22.2; 40 x up to 3000, 64 of 64 28.5 and 24.8; fp32, 64 x up to 3000, 16 of 128 24.8 and 21.6)
+// Two waves have the same 32 rows, and a half of each tile's items, where a head has at most 64 rows (us by four waves of rows and so: 64 rows x up
+// to 4096, 32 users of 128 33.7 and 26.8, of 64 26.3 and 22.2; 40 x up to 3000, 64 of 64 28.5 and 24.8; fp32, 64 x up to 3000, 16 of 128 24.8 and
+// 21.6), and where the tiles of 128 rows are one a compute unit or fewer: the way of each is then half as long, of twice as many (400 rows x 1000,
+// 1 of 64 13.6 and 11.6; 800 x 3000, 2 of 128 30.9 and 25.9; 1200 x up to 600, 3 of 128 18.8 and 15.3; of 480 tiles 400 x 30000, 1 of 128 40.0 and
+// 42.7, 100 x up to 3000, 20 of 64 24.8 and 22.4).
 template <int DP, int SLOTS, int NP, typename T>
 static laser_status tile8_typed(const Tile8Args& t) {
-  return (long long)t.a.c.C * t.G <= 64 ? tile8_split<DP, SLOTS, NP, 2, T>(t) : tile8_split<DP, SLOTS, NP, 1, T>(t);
+  const long long rows = (long long)t.a.c.C * t.G, workgroups = (rows + 127) / 128 * t.N * t.Hkv * t.runs;
+  return rows <= 64 || workgroups <= 256 ? tile8_split<DP, SLOTS, NP, 2, T>(t) : tile8_split<DP, SLOTS, NP, 1, T>(t);
 }
 template <int NP, typename T>
 static laser_status tile8_width(const Tile8Args& t) {

@@ -72,9 +72,11 @@ def test_forms_of_many_rows(recorder, U, Hkv, H, L, C, D, runs):
     so do very many workgroups, of rows enough."""
     for dt, runs in zip((BF16, F32), runs if isinstance(runs, tuple) else (runs, runs)):
         records = launches(recorder, attend(U, U * C, C, L, H, Hkv, D, dt))
-        workgroups = U * Hkv * -(-C * (H // Hkv) // 128) * runs
+        rows = C * (H // Hkv)
+        split = 2 if rows <= 64 or U * Hkv * -(-rows // 128) * runs <= 256 else 1      # (waves that have the same rows)
+        workgroups = U * Hkv * -(-rows * split // 128) * runs
         assert "cache8_tile_kernel" in records[0].kernel.decode() and records[0].block == 256
-        assert f"ELi{2 if C * (H // Hkv) <= 64 else 1}E{'f' if dt == F32 else 't'}E" in records[0].kernel.decode()      # (64 rows: two waves have them)
+        assert f"ELi{split}E{'f' if dt == F32 else 't'}E" in records[0].kernel.decode()
         assert records[0].grid == workgroups if U <= 64 and workgroups <= 2560 else workgroups <= records[0].grid < workgroups * 1.1 + 64
         assert len(records) == (2 if runs > 1 else 1) and all("join" in r.kernel.decode() for r in records[1:])
         assert recorder.laser_cache8_attention_work_bytes(U, U * C, C, L, H, Hkv, D, dt) == (runs * U * C * H * (D + 1) * 4 if runs > 1 else 16)
