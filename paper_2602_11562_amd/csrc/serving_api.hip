@@ -51,7 +51,7 @@ static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <
 // of 128 -, 116, 111), of 512 items or more, of 256 where the longest history has few runs anyway and for fp32 (us by 256 and 512: 100 x
 // 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1). None where the histories are short and two tiles of rows a compute
 // unit (512) without a cut: 32 x 1000, 256 of 128, in four runs and whole: all of that length 117, 54, of lengths up to it 63, 50, most short 40, 43; 128 x 1000, 32
-// of 128 (256 tiles) 33, 44.
+// of 128 (256 tiles) 33, 44. Nor where they are very short (two runs and whole: 50 x up to 300, 20 of 64 12.5, 11.0; 40 x 500, 4 of 64 11.8, 12.5).
 // Few rows, us by one run a history and runs of 1024 and 512 items (heads of 128 over 2 key-value heads unless said otherwise):
 //   1 x 65000, 16 heads (2 pairs)  307, 15.8, 15.2;  30 x 2000 (60)  13.1, 11.9, 9.8;  8 x 20000 (16)  88, 17.3, 17.9;  40 x 3000 fp32 (80)  25.7, 16.9, 17.7;
 //   5 x 777 fp32 (10)  7.7, -, 9.2;  32 x 1000, 8 over 8 of 64 (256)  7.8, -, 10.4;  100 x 2000 (200)  16.9, 19.2, 22.1;  100 x 3000 (200)  21.8,
@@ -62,7 +62,7 @@ CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
   const long long tiles = (rows + 127) / 128 * pairs;
   if (!few8_rows(C, H, Hkv)) {
-    if (tiles >= 512 && L <= 1024) return CacheRuns{(L + 63) / 64 * 64, 1};
+    if (L <= (tiles >= 512 ? 1024 : 384)) return CacheRuns{(L + 63) / 64 * 64, 1};
     return cache_runs(tiles, L, D > 64 && U <= CACHE8_RANKED ? 1536 : 2048, L > 2048 && dt != LASER_F32 ? 512 : 256, 64);
   }
   if (pairs >= 512 || L <= (pairs > 128 ? 3200 : 1024)) return CacheRuns{(L + 255) / 256 * 256, 1};

@@ -66,7 +66,7 @@ def test_forms_of_few_rows(recorder, U, Hkv, H, L, C, waves, runs, dt):
 
 @pytest.mark.parametrize("U,Hkv,H,L,C,D,runs", [(16, 2, 8, 10000, 512, 128, 3), (64, 2, 8, 4096, 256, 64, 2), (65, 2, 8, 4096, 256, 64, 2), (1, 2, 8, 30000, 100, 128, (59, 118)),
                                                 (1, 2, 8, 1000, 100, 64, 4), (200, 1, 8, 100, 500, 32, 1), (50, 2, 8, 1500, 1000, 128, 1), (256, 2, 8, 1000, 32, 128, 1), (255, 2, 8, 1000, 32, 128, 4), (256, 2, 8, 1025, 32, 128, 4), (1, 1, 1, 5000, 128, 128, (10, 20)), (32, 2, 8, 4096, 16, 128, (8, 16)),
-                                                (3, 1, 1, 300, 33, 64, 2), (2, 1, 1, 300, 65, 32, 2)])
+                                                (3, 1, 1, 384, 33, 64, 1), (2, 1, 1, 385, 65, 32, 2)])
 def test_forms_of_many_rows(recorder, U, Hkv, H, L, C, D, runs):
     """Runs by the rules beside cache8_runs_of. Up to 64 users a workgroup for each tile and run; more in the dealt order, a multiple of eight;
     so do very many workgroups, of rows enough."""
