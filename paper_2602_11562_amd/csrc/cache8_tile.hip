@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
     last = a.causal ? n - part.count + i : n - 1;
     load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(part.first + i) * a.qp + (size_t)(hk * t.G + g) * a.D, a.D, h, qreg);
   }
-  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = __builtin_amdgcn_readlane(last, 31);
+  const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = first < rows ? __builtin_amdgcn_readlane(last, 31) : -1;   // (without rows: none)
   bool whole_pages;
   {
     bool bad = false;
