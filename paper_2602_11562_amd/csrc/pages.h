@@ -5,6 +5,13 @@
 
 namespace laser {
 
+// go(u) for users first, first + step, .. below U, which may be 2^31 - 1 of tables of one page: the step behind the last (of 2^16 at most) does
+// not fit an int, which would go on below 0 and still be less than U
+template <typename Go>
+__host__ __device__ __forceinline__ void for_users(unsigned first, unsigned step, int U, Go&& go) {
+  for (unsigned u = first; u < (unsigned)U; u += step) go((int)u);
+}
+
 // Arrays [P, page bytes] that a page is made of, at most N a launch. (4 or 16: 100 bytes of arguments cost a launch 0.2 us)
 constexpr int FEW_PARTS = 4, PARTS_A_LAUNCH = 16;
 template <int N>

@@ -175,21 +175,22 @@ __device__ __forceinline__ void fork_plan(const Tables& t, const int32_t* source
   Counts<TAKE_RUNS> first = {};
   if (!FULL) first = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
-  for (int v0 = 0; v0 < V; v0 += PLAN) {
-    const int v = v0 + threadIdx.x;
+  for_users(0, PLAN, V, [&](int v0) __attribute__((always_inline)) {
+    const unsigned v = v0 + threadIdx.x;
     int need = 0;
-    if (v < V) {
-      const int n = forked_items(t, source, v, max_out);
+    if (v < (unsigned)V) {
+      const int n = forked_items(t, source, (int)v, max_out);
       if (n & ((1 << t.log2) - 1)) need = (unsigned)t.pages[(size_t)source[v] * t.max_pages + (n >> t.log2)] < (unsigned)t.P;
     }
     int all;
     const int before = sum_before(need, &all);
-    if (v < V) rank[v] = need ? want + before : -1;
+    if (v < (unsigned)V) rank[v] = need ? want + before : -1;
     want += all;
-  }
+  });
   const int got = take_free<FULL>(t.refs, t.P, want, fresh, first, used);
-  for (int v = threadIdx.x; v < V; v += PLAN)      // (a thread's own ranks)
-    if (rank[v] >= got) rank[v] = -2;              // no page is left for it
+  for_users(threadIdx.x, PLAN, V, [&](int v) __attribute__((always_inline)) {   // (a thread's own ranks)
+    if (rank[v] >= got) rank[v] = -2;                                           // no page is left for it
+  });
   if (threadIdx.x == 0) *missing = want - got;
 }
 template <bool FULL>
@@ -263,10 +264,10 @@ __global__ __launch_bounds__(256) void fork_kernel(const Tables t, const Fork f,
     return;
   }
   if (!tables) return;
-  for (int v = blockIdx.x - copies; v < f.V; v += gridDim.x - copies) {
+  for_users(blockIdx.x - copies, gridDim.x - copies, f.V, [&](int v) __attribute__((always_inline)) {
     const int n = forked_items(t, f.source, v, f.max_out);
     for (int j = threadIdx.x; j < f.max_out; j += 256) forked_entry(t, f, v, j, n);
-  }
+  });
 }
 // A small fork, plan and rest in one launch
 __global__ __launch_bounds__(PLAN) void fork_small_kernel(const Tables t, const Fork f, int32_t* rank, int32_t* fresh, int32_t* missing,
@@ -293,27 +294,28 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
   Counts<TAKE_RUNS> ahead = {};
   if (!FULL) ahead = counts_of<TAKE_RUNS>(t.refs, (threadIdx.x >> 6) * 64 * TAKE_RUNS, t.P);
   int want = 0;
-  for (int u0 = 0; u0 < t.U; u0 += PLAN) {
-    const int u = u0 + threadIdx.x;
+  for_users(0, PLAN, t.U, [&](int u0) __attribute__((always_inline)) {
+    const unsigned u = u0 + threadIdx.x;
     int need = 0;
-    if (u < t.U) {
-      const int n = held_items(t, u);
-      need = pages_of(grown(u, n), t.log2) - pages_of(n, t.log2);
+    if (u < (unsigned)t.U) {
+      const int n = held_items(t, (int)u);
+      need = pages_of(grown((int)u, n), t.log2) - pages_of(n, t.log2);
     }
     int all;
     const int before = sum_before(need, &all);
-    if (u < t.U) rank[u] = want + before;
+    if (u < (unsigned)t.U) rank[u] = want + before;
     want += all;
-  }
+  });
   const int got = take_free<FULL>(t.refs, t.P, want, fresh, ahead, used);
   __syncthreads();
   // A user's first entries by a thread, the others by its wave, where few users are dealt to all waves (65000 items of one user in pages of
   // 8: 822 us by the thread alone and 27 so, 16 users' 5000 in pages of 16 49 and 14, 128 users' 1000 23 and 16).
   const bool deal = t.U <= PLAN / 4;
-  for (int u0 = 0; u0 < t.U; u0 += PLAN) {
-    const int lane = threadIdx.x & 63, u = u0 + (deal ? lane * (PLAN / 64) + (int)(threadIdx.x >> 6) : (int)threadIdx.x);
+  for_users(0, PLAN, t.U, [&](int u0) __attribute__((always_inline)) {
+    const unsigned lane = threadIdx.x & 63, at = u0 + (deal ? lane * (PLAN / 64) + (threadIdx.x >> 6) : threadIdx.x);
+    const int u = (int)at;
     int first = 0, last = 0, r = 0;
-    if (u < t.U) {
+    if (at < (unsigned)t.U) {
       const int n = held_items(t, u), m = grown(u, n);
       first = pages_of(n, t.log2), last = pages_of(m, t.log2), r = rank[u] - first;
       lens[u] = m;
@@ -325,14 +327,14 @@ __global__ __launch_bounds__(PLAN) void grow_kernel(const Tables t, const int32_
                 their_r = __builtin_amdgcn_readlane(r, l);
       for (int j = __builtin_amdgcn_readlane(first, l) + OWN_ENTRIES + lane; j < end; j += 64) entry(their_u, their_r, j);
     }
-  }
+  });
   if (threadIdx.x == 0) *missing = want - got;
 }
 
 // Free: a workgroup gives back the pages of a user
 __global__ __launch_bounds__(256) void free_kernel(const Tables t, const int32_t* __restrict__ gone, int32_t* lens) {
-  for (int u = blockIdx.x; u < t.U; u += gridDim.x) {
-    if (gone != nullptr && gone[u] == 0) continue;
+  for_users(blockIdx.x, gridDim.x, t.U, [&](int u) __attribute__((always_inline)) {
+    if (gone != nullptr && gone[u] == 0) return;
     const int used = pages_of(held_items(t, u), t.log2);
     for (int j = threadIdx.x; j < used; j += 256) {
       const int p = t.pages[(size_t)u * t.max_pages + j];
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(256) void free_kernel(const Tables t, const int32_t
     }
     __syncthreads();   // (every wave has the length)
     if (threadIdx.x == 0) lens[u] = 0;
-  }
+  });
 }
 
 // Compact, the plan: of M pages in use, those numbered M and more go to the free ones below M, in order. With `sums`, pages in use of each
@@ -463,7 +465,7 @@ __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int3
   }
   if (!tables) return;
   const unsigned first = blockIdx.x - copies, step = gridDim.x - copies;
-  for (int u = first; u < t.U; u += step) {
+  for_users(first, step, t.U, [&](int u) __attribute__((always_inline)) {
     const int used = pages_of(held_items(t, u), t.log2);
     for (int j = threadIdx.x; j < t.max_pages; j += 256) {
       int p = -1;
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(256) void compact_kernel(const Tables t, const int3
       }
       pages_out[(size_t)u * t.max_pages + j] = p;
     }
-  }
+  });
   // a page in use has its count where it goes to; what lies behind the last of them is free
   const int M = *in_use;
   for (long long p = (long long)first * 256 + threadIdx.x; p < t.P; p += (long long)step * 256) {
