@@ -531,7 +531,8 @@ laser_status laser_history_attention_backward(const void* q, int64_t q_pitch, co
  *   places are set to 0. A page must not be listed twice, by one user or two, where new rows go.
  * laser_cache_attention_forward: o_out [T,H,D] dt, lse_out [T,H] fp32 (NULL: not wanted). causal != 0: the rows are the last
  *   c items of the cache (laser_cache_append has run), row i sees items 0 .. lens[u] - c + i. causal = 0: the rows are
- *   not in the cache (a request's candidates) and see all of it. A row that sees nothing gets zeros and lse = -inf.
+ *   not in the cache (a request's candidates) and see all of it. A row that sees nothing gets zeros and lse = -inf. Items are
+ *   taken to be finite, as above: an infinite or NaN value can reach rows of the same call that do not see it.
  *   work: laser_cache_attention_work_bytes() bytes of caller-owned scratch, contents unspecified before and after; calls that
  *   overlap need one each.
  * laser_cache_weights: what each item received, weight[its place] = sum of exp(s - lse) over the rows that see it and
@@ -624,7 +625,8 @@ laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const voi
  *   written. A page must not be listed twice, by one user or two, where new rows go.
  * laser_cache8_attention_forward: as laser_cache_attention_forward over the items' values (number times scale). bf16 rows:
  *   probabilities are rounded to bf16 ahead of their product with the values, o is rounded once; fp32 rows: every product and sum is of
- *   fp32's precision. A row whose query is NaN is NaN. work: laser_cache8_attention_work_bytes() bytes.
+ *   fp32's precision. A row whose query is NaN is NaN; so is one that sees a key that is NaN, and, in its columns, one that sees a value
+ *   that is; rows that do not see such an item have nothing of it. work: laser_cache8_attention_work_bytes() bytes.
  * Results are the same from run to run. Everything else, alignment (4 bytes for scales) and errors as for the cache above.
  */
 laser_status laser_cache8_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,

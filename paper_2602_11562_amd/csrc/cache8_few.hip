@@ -44,10 +44,11 @@ struct Rows32 {
     }
     if (!whole) {
       const int seen = last - 4 * h;
+      const unsigned mine = items >> (4 * h);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int i0 = 8 * (r >> 2) + (r & 3);
-        if (i0 > seen || !((items >> (4 * h + i0)) & 1)) sc[r] = -INFINITY;
+        if (i0 > seen || !((mine >> i0) & 1)) sc[r] = -INFINITY;
       }
     }
     float top = sc[0];
@@ -90,6 +91,7 @@ struct Rows32 {
       }
     }
   }
+  __device__ __forceinline__ void see_nan(unsigned at_v, int last, int lane) { nan_seen32<DP>(read, at_v, last - 4 * (lane >> 5), acc); }
   // to [column][32 rows], row r at r ^ column % 32
   __device__ __forceinline__ void leave(float* out, float* to_m, float* to_l, int lane) {
     const int l32 = lane & 31, h = lane >> 5;
@@ -167,6 +169,10 @@ struct Rows16 {
         for (int i = 0; i < NP; ++i) q[i][c][s] = part[i];
       }
   }
+  __device__ __forceinline__ u32x2 columns(unsigned at_v, int db) const {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_at((at_v + cols) ^ (db << 4)))));
+  }
   __device__ __forceinline__ void tile(unsigned at_k, unsigned at_v, unsigned at_s, float scale, bool whole, unsigned items, int last, int lane) {
     const int g = lane >> 4;
     f32x4 sc[2];
@@ -186,10 +192,7 @@ struct Rows16 {
         }
       }
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      typedef int i32x2 __attribute__((ext_vector_type(2)));
-      vw[db] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_at((at_v + cols) ^ (db << 4)))));
-    }
+    for (int db = 0; db < DB; ++db) vw[db] = columns(at_v, db);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       sc[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -242,6 +245,18 @@ struct Rows16 {
       const bf16x8 v = wide8(vw[db][0], vw[db][1], v_scale, v_scale);
 #pragma unroll
       for (int i = NP - 1; i >= 0; --i) acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][0], acc[db], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void see_nan(unsigned at_v, int last, int lane) {
+    bf16x8 sees;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sees[r] = (__bf16)(r <= last - 8 * (lane >> 4) ? 1.0f : 0.0f);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones_at(nan_codes(columns(at_v, db))), sees, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[db][r] = count[r] > 0.0f ? __builtin_nanf("") : acc[db][r];
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // to [column][16 rows], row r at r ^ column % 16
@@ -330,6 +345,10 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
       bool in = at < hi - mine;
       if (!whole_pages) in = in && (unsigned)table[(mine + (in ? at : 0)) >> a.page_log2] < (unsigned)a.P;
       items = (unsigned)__ballot(in);
+    }
+    if ((mine + 32 < hi ? mine + 32 : hi) - 1 > first_seen && any_nan<Sh::TILE>(at + Sh::TILE, lane)) {   // (items that not every row sees)
+      mine_rows.see_nan(at + Sh::TILE, last - mine, lane);
+      clear_nan<Sh::TILE>(at + Sh::TILE, lane);
     }
     mine_rows.tile(at, at + Sh::TILE, at_s, scale, whole, items, last - mine, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read: its place may be asked for again

@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   constexpr bool PATCHED = sizeof(T) == 2;   // (fp32 rows leave from the registers)
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * SLOT > PATCH || !PATCHED ? SLOTS * SLOT : PATCH];
   __shared__ __attribute__((aligned(16))) float scales[SLOTS][TI / 8 * 2];
+  __shared__ int odd[2][NW];
   const CacheArgs& a = t.a.c;
   const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem);
   const unsigned lds_s = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) float*)&scales[0][0]);
@@ -146,6 +147,7 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
     last = a.causal ? n - part.count + i : n - 1;
     load_query<DP, NP>(static_cast<const T*>(a.q) + (size_t)(part.first + i) * a.qp + (size_t)(hk * t.G + g) * a.D, a.D, h, qreg);
   }
+  const int all_see = a.causal ? n - part.count + (int)t.by_group.div(row0) : 0x7fffffff;   // up to this item all rows see all that is there
   const int wave_first = __builtin_amdgcn_readlane(last, 0), wave_last = first < rows ? __builtin_amdgcn_readlane(last, 31) : -1;   // (without rows: none)
   bool whole_pages;
   {
@@ -182,10 +184,11 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
       if (!whole_pages) in = in && (unsigned)table[(t0 + (in ? l32 : 0)) >> a.page_log2] < (unsigned)a.P;
       items = (unsigned)__ballot(in);
       const int seen = last - t0 - 4 * h;
+      const unsigned mine = items >> (4 * h);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int i0 = 8 * (r >> 2) + (r & 3);
-        if (i0 > seen || !((items >> (4 * h + i0)) & 1)) sc[r] = -INFINITY;
+        if (i0 > seen || !((mine >> i0) & 1)) sc[r] = -INFINITY;
       }
     }
     float top = sc[0];
@@ -231,11 +234,25 @@ __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) 
   int out = 0;
   for (int u = 0; u < turns; ++u) {
     wait_requests((asked - u - 1) * requests);
+    const unsigned at = lds + out * SLOT, at_s = lds_s + out * (TI / 8 * 8);
+    const int t0 = begin + u * TI;
+    const bool hidden = t0 + TI - 1 > all_see;
+    if (hidden) {
+      asm volatile("" ::: "memory");
+      const bool any = any_nan<16 * DP>(at + KB + wave * 16 * DP, lane);
+      if (lane == 0) odd[u & 1][wave] = any;
+    }
     barrier_lds();   // tile u is there, and every wave is through with the one before, whose slot is asked for again
     if (asked < turns) request();
-    const unsigned at = lds + out * SLOT, at_s = lds_s + out * (TI / 8 * 8);
     out = out + 1 == SLOTS ? 0 : out + 1;
-    const int t0 = begin + u * TI;
+    if (hidden && __builtin_amdgcn_readfirstlane(odd[u & 1][0] | odd[u & 1][1] | odd[u & 1][2] | odd[u & 1][3])) {
+      const int half = SPLIT == 1 ? 0 : wave / BLOCKS * 32;
+#pragma unroll 1
+      for (int x = half; x < (SPLIT == 1 ? TI : half + 32); x += 32) nan_seen32<DP>(read, at + KB + x * DP, last - t0 - x - 4 * h, acc);
+      barrier_lds();   // every wave has seen the codes
+      clear_nan<16 * DP>(at + KB + wave * 16 * DP, lane);
+      barrier_lds();
+    }
     if constexpr (SPLIT == 1) {
       if (t0 <= wave_last) block(t0, at, at_s);
       if (t0 + 32 <= wave_last) block(t0 + 32, at + 32 * DP, at_s + 32);
