@@ -622,7 +622,8 @@ laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const voi
  *   smallest power of two 2^x, -100 <= x <= 119, with |y| <= 448 2^x for all finite elements y of the new ones); each new element becomes
  *   the e4m3 number nearest to y / scale (of two equally near the even one), at most 448 in magnitude, infinities too; NaN stays
  *   NaN. Where the scale grows, the older items' numbers are rounded again to the new one. Places behind a user's items are not
- *   written. A page must not be listed twice, by one user or two, where new rows go.
+ *   written. A page must not be listed twice, by one user or two, where new rows go. The blocks that min(C_max, L_max, T) rows touch
+ *   are, times H_kv, at most 2^23 - 1.
  * laser_cache8_attention_forward: as laser_cache_attention_forward over the items' values (number times scale). bf16 rows:
  *   probabilities are rounded to bf16 ahead of their product with the values, o is rounded once; fp32 rows: every product and sum is of
  *   fp32's precision. A row whose query is NaN is NaN; so is one that sees a key that is NaN, and, in its columns, one that sees a value

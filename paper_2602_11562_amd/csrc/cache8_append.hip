@@ -104,7 +104,8 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(const Cache8Args a, 
 
 laser_status cache8_append_launch(const Cache8Args& a) {
   const CacheArgs& c = a.c;
-  const long long rows = c.C < c.L ? c.C : c.L, blocks = (rows + 2 * (1 << a.block_log2) - 2) >> a.block_log2;   // that a user's rows touch
+  const int least = c.C < c.L ? c.C : c.L;
+  const long long rows = least < c.T ? least : c.T, blocks = (rows + 2 * (1 << a.block_log2) - 2) >> a.block_log2;   // that a user's rows touch
   // (a launch has fewer than 2^32 threads, and 65535 of a grid's second and third sides)
   const long long most = 0xffffffffLL / 256 / (blocks * c.Hkv * 2);
   if (most <= 0) return LASER_ERR_SHAPE;
