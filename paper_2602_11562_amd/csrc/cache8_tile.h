@@ -33,11 +33,11 @@ __device__ __forceinline__ void global_to_lds4(const void* p, unsigned lds_addr)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n" ::"s"(lds_addr), "v"(p) : "memory");
 }
 
-// Waits until at most n of this wave's vector-memory operations are outstanding
+// Waits until at most n of this wave's vector-memory operations are outstanding: the requests of a tile ahead (3, 5 or 9), or of two of 16 rows (6 or 10)
 __device__ __forceinline__ void wait_requests(int n) {
   switch (n) {
 #define LASER_VM_CASE(i) case i: __builtin_amdgcn_s_waitcnt(vmcnt_imm(i)); break;
-    LASER_VM_CASE(3) LASER_VM_CASE(5) LASER_VM_CASE(6) LASER_VM_CASE(9) LASER_VM_CASE(10) LASER_VM_CASE(15)
+    LASER_VM_CASE(3) LASER_VM_CASE(5) LASER_VM_CASE(6) LASER_VM_CASE(9) LASER_VM_CASE(10)
 #undef LASER_VM_CASE
     default: __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   }

@@ -93,6 +93,7 @@ __device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Par
 template <int DP, int SLOTS, int NP, int PART, int SPLIT, typename T>
 __global__ __launch_bounds__(256, 2) void cache8_tile_kernel(const Tile8Args t) {
   constexpr int KS = DP / 16, DB = DP / 32, NW = 4, BLOCKS = NW / SPLIT, ROWS = BLOCKS * 32, KB = TI * DP, SLOT = 2 * KB, OP = DP * 2 + 16, PATCH = NW * 32 * OP;
+  static_assert(SLOTS <= 4, "wait_requests knows the requests of two tiles ahead at most");
   constexpr bool PATCHED = sizeof(T) == 2;   // (fp32 rows leave from the registers)
   __shared__ __attribute__((aligned(1024))) unsigned char smem[SLOTS * SLOT > PATCH || !PATCHED ? SLOTS * SLOT : PATCH];
   __shared__ __attribute__((aligned(16))) float scales[SLOTS][TI / 8 * 2];

@@ -48,7 +48,7 @@ __device__ __forceinline__ int sum_before(int x, int* all) {
   *all = total;
   return before + sum - x;
 }
-// The same of a number that each wave has (two of up to 16 bits in one, if wanted)
+// The same of a number that each wave has
 __device__ __forceinline__ int waves_before(int x, int* all) {
   __shared__ int waves[PLAN / 64];
   const int wave = threadIdx.x >> 6;
