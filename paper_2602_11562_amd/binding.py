@@ -1259,7 +1259,7 @@ def _parts_of_page(parts, P: int):
     for i, t in enumerate(parts):
         if t.dim() < 1 or t.shape[0] != P:
             raise ValueError(f"parts[{i}] must be [{P}, ...], got {list(t.shape)}")
-        at[i], size[i] = _ptr(t, f"parts[{i}]"), t.numel() // P * t.element_size()
+        at[i], size[i] = _ptr(t, f"parts[{i}]"), t.numel() // max(P, 1) * t.element_size()
     return at, size, n
 
 
