@@ -611,7 +611,8 @@ laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const voi
                                    laser_dtype dt, void* dq_out, int64_t dq_pitch, void* dk_out, int64_t dk_pitch, void* stream);
 
 /*
- * The paged cache with its items in 8 bits, half the bytes of the bf16 one and what bounds few rows over long histories.
+ * The paged cache with its items in 8 bits, half the bytes of the bf16 one and what bounds few rows over long histories. It is appended to and
+ * attended over; received weights and eviction (laser_cache_weights, laser_cache_evict) are of the fp32 and bf16 caches alone.
  *   k_cache, v_cache [P,H_kv,page,D] e4m3 (4 bits of exponent, 3 of mantissa, largest 448, no infinities); D a multiple of 16, at most 128.
  *   k_scale, v_scale [P,H_kv,page/block] fp32: what the numbers of each block of `block` items (a power of two, 8 to page) of a head are
  *   times; a power of two from 2^-100 to 2^119 (of any other value, what comes of the block's items is unspecified).
@@ -627,7 +628,8 @@ laser_status laser_rotary_backward(const void* d_q, int64_t d_q_pitch, const voi
  * laser_cache8_attention_forward: as laser_cache_attention_forward over the items' values (number times scale). bf16 rows:
  *   probabilities are rounded to bf16 ahead of their product with the values, o is rounded once; fp32 rows: every product and sum is of
  *   fp32's precision. A row whose query is NaN is NaN; so is one that sees a key that is NaN, and, in its columns, one that sees a value
- *   that is; rows that do not see such an item have nothing of it. work: laser_cache8_attention_work_bytes() bytes.
+ *   that is; rows that do not see such an item have nothing of it. Values are summed in fp32 ahead of the division, with probabilities of up to
+ *   2^8: of values beyond 2^119 / lens the sum may overflow. work: laser_cache8_attention_work_bytes() bytes.
  * Results are the same from run to run. Everything else, alignment (4 bytes for scales) and errors as for the cache above.
  */
 laser_status laser_cache8_append(const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* k_cache, void* v_cache,
@@ -651,7 +653,8 @@ laser_status laser_cache8_attention_forward(const void* q, int64_t q_pitch, cons
  * Entries outside [0, P) are pages without items: they pass on as they are, are counted and copied nowhere. lens are clamped to
  * [0, max_pages * page].
  * laser_pages_grow: lens[u] += off[u+1] - off[u] (nothing where that is negative; to max_pages * page at most), and the table gets
- *   fresh pages, counts 1, for the entries that the new length asks for. Ahead of an append of the rows that off packs.
+ *   fresh pages, counts 1, for the entries that the new length asks for. Ahead of an append of the rows that off packs. (Where a table is
+ *   full the length stays, and the append puts the last rows in the place of items that were there: max_pages is to allow for them.)
  * laser_pages_fork: history v of the new tables pages_out [V,max_pages_out], lens_out [V] is the one of user source[v] (int32; outside
  *   [0, U): an empty one; a longer one than max_pages_out pages hold is cut there). Whole pages are shared, their counts go up; a partly filled last
  *   one is copied into a fresh page, all of it, so that either history can be appended to. Entries behind a history's pages become -1. The old tables
@@ -661,7 +664,8 @@ laser_status laser_cache8_attention_forward(const void* q, int64_t q_pitch, cons
  *   entries are left alone.
  * laser_pages_compact: the M pages in use move so that they are pages 0 .. M-1: those numbered M and more, in order, into the free ones
  *   below M, in order. pages_out [U,max_pages]: the tables with the new numbers (-1 behind a user's pages), refs_out [P] the counts,
- *   in_use_out [1] M. Tables must name no page whose count is 0.
+ *   in_use_out [1] M. Tables must name no page whose count is 0, and all tables are one call's (those of forks side by side with the
+ *   others): one that is not given keeps numbers that are no longer its pages'.
  * laser_pages_copy: page to[i] becomes a copy of page from[i] (int32 [n]; a pair with one outside [0, P) is left out). No page may be
  *   in `to` twice or in both.
  * page: items of one, a power of two, 8 to 4096. P <= 2^26; U * max_pages, V * max_pages_out, and items of a table below 2^31. work:

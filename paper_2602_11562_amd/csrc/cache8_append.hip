@@ -4,7 +4,8 @@
 // smallest ones, whose last bits fall off.
 //
 // A workgroup owns a block that new items come into (the first of a user's may hold older ones), for a head's keys or values: largest
-// new item, scale, codes. Bound by latency for single items, by memory for chunks.
+// new item, scale, codes. Bound by loads behind one another: offset, length and page, then the rows twice, for the largest and for the codes (the second
+// time from the L2 cache): 2.5 us for one item of 5 users, 4.3 of 128, 7.5 for 512 items of 16 (8 MB in and out, 1.6 us at a copy's rate).
 #include "cache8.h"
 
 namespace laser {

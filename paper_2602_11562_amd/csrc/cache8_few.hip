@@ -389,9 +389,9 @@ __global__ __launch_bounds__(64 * NW, 2) void cache8_few_kernel(const Cache8Args
 }
 
 // Joins the parts of a row that are more than 16: a workgroup a row and 32 of its columns, eight lanes a part, 128 parts at a time, whose columns are
-// asked for ahead of the parts' shares, so that a row is two loads behind one another and not three. For few rows: the call with it, us, by
-// cache_join_kernel and by this one: 16 rows of 128 columns in 127 parts 15.1 and 13.7, 64 rows in 59 15.2 and 14.6, 800 rows in 59 39.7 and 41.0,
-// 7200 rows of 64 in 34 110 and 118.
+// asked for ahead of the parts' shares, so that a row is two loads behind one another and not three. For few rows: the call with it, captured, us, by
+// cache_join_kernel and by this one: 16 rows of 128 columns in 127 parts 15.1 and 13.9 (fp32 17.8 and 16.2; calls in a row from Python are 15.7 by either,
+// the host's part), 64 rows in 59 18.3 and 17.6, 64 rows of 8 users in 20 27.5 and 26.8; 800 rows in 59 39.7 and 41.0, 7200 rows of 64 in 34 110 and 118.
 constexpr int JOIN_PARTS = 1024, JOIN_COLUMNS = 32;
 template <typename T>
 __global__ __launch_bounds__(256) void cache8_join_kernel(const CacheArgs a, int chunk, int splits, MulDiv by_slices, int slices) {

@@ -38,11 +38,11 @@ __device__ __forceinline__ bool part_in_turn(const Tile8Args& t, Part8* p) {
   return true;
 }
 // At most 64 users, a lane for each: the whole runs of all of them come first, then what is left of each, the longest first, since workgroups
-// are started in the order of their numbers. Against the order of users (us, with the join): 512 new items x up to 10000, 16 users of 128 252
-// and 207; 256 rows x up to 4096, 32 of 64 79.9 and 67.7; 128 x up to 4096, 64 of 128 133 and 110; equal lengths 386 and 395; 1000 x up to
+// are started in the order of their numbers. Against the order of users (us, with the join): 512 new items x up to 10000, 16 users of 128 229
+// and 191; 256 rows x up to 4096, 32 of 64 80.3 and 65.1; 128 x up to 4096, 64 of 128 122 and 100; equal lengths 360 and 365; 1000 x up to
 // 1500, 50 of 128 (3200 workgroups, four or more for each place, which even out by themselves) 130 and 134.
 // Workgroups of whole runs go to the eighths of the chip, each with an L2 cache of its own, in even parts, so that the tiles of a run meet
-// there (against the plain order 208 and 207, 130 and 125 for 400 x 9000, 12 of 128).
+// there (against the plain order 193 and 191, 119 and 116 for 400 x up to 9000, 12 of 128).
 __device__ __forceinline__ bool part_by_length(const Tile8Args& t, int lane, Part8* p) {
   const CacheArgs& a = t.a.c;
   const int u = lane < t.N ? lane : t.N - 1;
@@ -341,9 +341,9 @@ static laser_status tile8_split(Tile8Args t) {
   });
 }
 // Two waves have the same 32 rows, and a half of each tile's items, where a head has at most 64 rows (us by four waves of rows and so: 64 rows x up
-// to 4096, 32 users of 128 33.7 and 26.8, of 64 26.3 and 22.2; 40 x up to 3000, 64 of 64 28.5 and 24.8; fp32, 64 x up to 3000, 16 of 128 24.8 and
+// to 4096, 32 users of 128 32.0 and 27.5, of 64 26.2 and 22.6; 40 x up to 3000, 64 of 64 28.5 and 24.7; fp32, 64 x up to 3000, 16 of 128 24.7 and
 // 21.6), and where the tiles of 128 rows are one a compute unit or fewer: the way of each is then half as long, of twice as many (400 rows x 1000,
-// 1 of 64 13.6 and 11.6; 800 x 3000, 2 of 128 30.9 and 25.9; 1200 x up to 600, 3 of 128 18.8 and 15.3; of 480 tiles 400 x 30000, 1 of 128 40.0 and
+// 1 of 64 14.0 and 12.4; 800 x 3000, 2 of 128 29.1 and 26.7; 1200 x up to 600, 3 of 128 18.8 and 15.8; of 480 tiles 400 x 30000, 1 of 128 40.0 and
 // 42.7, 100 x up to 3000, 20 of 64 24.8 and 22.4).
 template <int DP, int SLOTS, int NP, typename T>
 static laser_status tile8_typed(const Tile8Args& t) {

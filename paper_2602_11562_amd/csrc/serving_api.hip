@@ -44,20 +44,34 @@ static laser_status validate_cache8(const void* k_cache, const void* v_cache, co
 
 // Rows of a key-value head that one column block holds: the streaming kernel
 static bool few8_rows(int C, int H, int Hkv) { return (long long)C * (H / Hkv) <= 32; }
-// Into how many runs. A cut costs a join, 4 to 6 us, and what its parts weigh.
+// Into how many runs the longest history is cut. A cut costs a join, 4 to 6 us, and what its parts weigh; sizes alone decide, which whoever
+// provides the work buffer knows too. Figures: us of captured calls; users x history, bf16 over 2 key-value heads of 128 unless said
+// otherwise; "full": all histories that long, "up to": of all lengths up to it, "spread": over decades of lengths.
+//
 // Many rows: two workgroups for each place that the chip has for them (three a compute unit of heads of 128, four of 64), which come by their
-// lengths (us by 1024, 1536 and 2048 wanted; 8 heads over 2, rows x longest history, users: 512 x 10000, 16 of 128 211, 191, 200; 400 x 9000, 12
-// of 128 112, 118, 123; 200 x 20000, 8 of 128 98, 96, 112; 256 x 4096, 32 of 64 71.5, 70.8, 67.7; more users, in their own order: 64 x 4096, 100
-// of 128 -, 116, 111), of 512 items or more, of 256 where the longest history has few runs anyway and for fp32 (us by 256 and 512: 100 x
-// 30000, 1 of 128 49.1, 41.6; 300 x 5000, 4 of 128 45.1, 41.3; 100 x 1000, 1 of 64 17.4, 21.3; fp32, 100 x 3000, 4 of 128 30.6, 38.1). None where the histories are short and two tiles of rows a compute
-// unit (512) without a cut: 32 x 1000, 256 of 128, in four runs and whole: all of that length 117, 54, of lengths up to it 63, 50, most short 40, 43; 128 x 1000, 32
-// of 128 (256 tiles) 33, 44. Nor where they are very short (two runs and whole: 50 x up to 300, 20 of 64 12.5, 11.0; 40 x 500, 4 of 64 11.8, 12.5).
-// Few rows, us by one run a history and runs of 1024 and 512 items (heads of 128 over 2 key-value heads unless said otherwise):
-//   1 x 65000, 16 heads (2 pairs)  307, 15.8, 15.2;  30 x 2000 (60)  13.1, 11.9, 9.8;  8 x 20000 (16)  88, 17.3, 17.9;  40 x 3000 fp32 (80)  25.7, 16.9, 17.7;
-//   5 x 777 fp32 (10)  7.7, -, 9.2;  32 x 1000, 8 over 8 of 64 (256)  7.8, -, 10.4;  100 x 2000 (200)  16.9, 19.2, 22.1;  100 x 3000 (200)  21.8,
-//   23.4, 26.8, most of them short 18.0, 18.5, 16.6;  128 x 4096 (256)  31.2, 37.9, 39.9, most short 24.6, 21.1, 24.0;  256 x 2000, four rows (512)  33.6, 42.9, 48.8
-// Rules: none where the histories alone are two workgroups a compute unit, or short, or one for every other unit and of medium length; else
-// runs of 512 while they are one workgroup a compute unit, and of 1024 beyond.
+// lengths; more users, in their own order, a few more. By 1024, 1536 and 2048 wanted, 8 heads, new rows a user ahead:
+//   512, 16 x up to 10000       210, 192, 196      256, 32 x up to 4096 of 64    76.1, 68.7, 65.5
+//   400, 12 x up to 9000        112, 117, 120      64, 100 x up to 4096          108, 105, 104
+//   200, 8 x up to 20000        95.8, 93.9, 109
+// Runs of 512 items or more, of 256 where the longest history has few runs anyway (100, 1 x 30000 by 256 and 512: 44.7, 40.2; 300, 4 x up to
+// 5000: 42.0, 39.7; 100, 1 x 1000 of 64: 12.1, 15.5) and for fp32 (100, 4 x 3000: 40.0, 37.5, spread 24.6, 24.7; 300, 8 x up to 3000 64.2,
+// 57.4: since two waves may share their rows, 512 would do there too). None where the histories are short and the tiles of rows two a compute unit (512)
+// without a cut (in four runs and whole: 32, 256 x 1000 109, 51.5, up to 1000 59.3, 45.9, spread 37.8, 39.2; 256 tiles, 128, 32 x up to 1000, 30.4,
+// 31.8). Nor where they are very short (in two runs and whole: 50, 20 x up to 300 of 64 13.2, 11.8; 40, 4 x 500 of 64 12.4, 13.1).
+//
+// Few rows, by one run a history, runs of 1024 and of 512 items (pairs of a user and a key-value head in brackets):
+//   1 x 65000, 16 heads (2)     296, 15.7, 13.7    32 x 1000, 8 of 64 (256)      9.0, -, 11.8
+//   30 x 2000 (60)              14.6, 13.5, 11.1   100 x 2000 (200)              20.6, 24.0, 27.6
+//   8 x 20000 (16)              96, 26.8, 25.3     100 x 3000 (200)              27.3, 36.4, 35.9, spread 18.6, 19.4, 16.6
+//   40 x 3000 fp32 (80)         26.1, 19.8, 20.8   256 x 2000, four rows (512)   46.7, 56.6, 65.1, spread 25.6, 28.6, 29.4
+//   5 x 777 of 64 fp32 (10)     8.6, -, 9.6
+// None where the histories alone are two workgroups a compute unit, or short, or one for every other unit and of medium length; else runs of 512
+// while they are one workgroup a compute unit, and of 1024 beyond. Between 129 and 511 pairs sizes do not tell full histories, for which a cut costs
+// up to a quarter, from spread ones, which wait for their longest: whole and cut, full, up to and spread
+//   128 x 4096 (256)   43.3, 49.4   31.6, 37.8   25.4, 21.5      80 x 8000 (160)    59.9, 64.6   43.6, 44.0   40.3, 23.8
+//   100 x 4096 (200)   34.8, 41.2   27.4, 34.0   24.5, 19.6      200 x 8000 (400)   143, 160     112, 105     72.7, 43.5
+//   200 x 3500 (400)   66.3, 79.5   42.9, 43.7   36.1, 25.6      250 x 4096 (500)   94.8, 103    62.7, 66.7   40.1, 35.2
+// so beyond 3200 items the rule goes by the spread ones, where the wait is up to two fifths.
 CacheRuns cache8_runs_of(int U, int C, int L, int H, int Hkv, int D, laser_dtype dt) {
   const long long pairs = (long long)U * Hkv, rows = (long long)C * (H / Hkv);
   const long long tiles = (rows + 127) / 128 * pairs;
